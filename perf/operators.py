@@ -1,0 +1,360 @@
+"""The output head of a Sparse-BitNet model as its user runs it, for timing and comparing: what the dense matrix behind the last
+block is trained on, distilled with and served in.
+
+A case is a dict of plain values.  Its "kind" says what one pass does:
+
+kind      one pass
+ce        softmax cross entropy of T tokens over a vocabulary, straight from the hidden states and the head's weights; with "grad" the
+          gradients of both as well
+distill   the same against a teacher's top logits at a temperature, with "hard" the cross entropy in the same pass; "grad" as above
+quantize  weights or activations to microscaled 4-bit floating point and back to the values that it stands for
+linear    activations through a head (or another layer) whose weights are held in that form
+
+The sizes are those of the repository's benchmark (hidden 2560, FFN 6912, 4096 and 16384 tokens) and generic vocabularies.
+"""
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda"
+
+
+def listed():
+    return [
+        # the smallest training step there is: launches and latency only
+        {"name": "ce_16_tokens_small", "kind": "ce", "tokens": 16, "d_in": 256, "vocab": 1000, "ignored": 0.0, "grad": True},
+        # serving: how likely one token was, the head streamed from memory once
+        {"name": "ce_score_1_token", "kind": "ce", "tokens": 1, "d_in": 2560, "vocab": 131072, "ignored": 0.0, "grad": False},
+        # evaluation of one sequence, no gradients
+        {"name": "ce_eval_2048", "kind": "ce", "tokens": 2048, "d_in": 2560, "vocab": 32000, "ignored": 0.0, "grad": False},
+        # fine-tuning on answers only: sizes that fit no tile, a third of the targets left out
+        {"name": "ce_ragged", "kind": "ce", "tokens": 1531, "d_in": 1000, "vocab": 50001, "ignored": 0.3, "grad": True},
+        # the training step of the benchmark, 8 sequences of 2048
+        {"name": "ce_train_16384", "kind": "ce", "tokens": 16384, "d_in": 2560, "vocab": 131072, "ignored": 0.02, "grad": True},
+        # a short odd sequence against a few teacher logits, some of them missing
+        {"name": "distill_ragged", "kind": "distill", "tokens": 37, "d_in": 1000, "vocab": 32001, "top": 7, "tau": 1.0, "hard": False, "dtype": "fp32", "empty": 0.2, "grad": True},
+        # a distillation step with the hard loss beside it
+        {"name": "distill_train_4096", "kind": "distill", "tokens": 4096, "d_in": 2560, "vocab": 131072, "top": 64, "tau": 2.0, "hard": True, "dtype": "bf16", "empty": 0.02, "grad": True},
+        # a few odd activation rows, latency only
+        {"name": "quantize_rows", "kind": "quantize", "rows": 77, "cols": 1000, "dtype": "fp32"},
+        # the head's weights, once per checkpoint
+        {"name": "quantize_head", "kind": "quantize", "rows": 131072, "cols": 2560, "dtype": "bf16"},
+        # decode: one token through the head
+        {"name": "linear_1_token", "kind": "linear", "tokens": 1, "d_in": 2560, "d_out": 131072, "bias": False},
+        # a decode batch through a layer as wide as the benchmark's, with a bias
+        {"name": "linear_32_tokens", "kind": "linear", "tokens": 32, "d_in": 2560, "d_out": 6912, "bias": True},
+        # the benchmark's prefill
+        {"name": "linear_4096_tokens", "kind": "linear", "tokens": 4096, "d_in": 2560, "d_out": 6912, "bias": False},
+    ]
+
+
+def _log(rng, lo, hi, step=1):
+    """A multiple of `step` between lo and hi, spread over its logarithm."""
+    v = math.exp(rng.uniform(math.log(lo), math.log(hi)))
+    return max(-(-lo // step) * step, min(hi // step * step, int(round(v / step)) * step))
+
+
+def draw(rng):
+    kind = rng.choice(["ce", "ce", "distill", "distill", "quantize", "linear", "linear"])
+    if kind == "quantize":
+        return {"kind": kind, "rows": _log(rng, 1, 131072), "cols": _log(rng, 64, 4096, 8), "dtype": rng.choice(["bf16", "fp32"])}
+    d_in = _log(rng, 64, 4096, 8)
+    if kind == "linear":
+        tokens, d_out = _log(rng, 1, 8192), _log(rng, 64, 131072)
+        while tokens * d_out > 1 << 28:
+            tokens, d_out = _log(rng, 1, 8192), _log(rng, 64, 131072)
+        return {"kind": kind, "tokens": tokens, "d_in": d_in, "d_out": d_out, "bias": rng.random() < 0.5}
+    tokens, vocab = _log(rng, 1, 16384), _log(rng, 500, 131072)
+    while tokens * vocab * d_in > 16384 * 131072 * 2560 // 4:
+        tokens, vocab = _log(rng, 1, 16384), _log(rng, 500, 131072)
+    case = {"kind": kind, "tokens": tokens, "d_in": d_in, "vocab": vocab, "grad": rng.random() < 0.7}
+    if kind == "ce":
+        return {**case, "ignored": rng.choice([0.0, 0.05, 0.5])}
+    return {**case, "top": _log(rng, 1, 128), "tau": rng.choice([1.0, 2.0, 4.0, rng.uniform(0.5, 8.0)]), "hard": rng.random() < 0.5,
+            "dtype": rng.choice(["bf16", "fp32"]), "empty": rng.choice([0.0, 0.1])}
+
+
+# ---- inputs ------------------------------------------------------------------------------------------------------------------------
+def _gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def _randn(g, *shape, scale=1.0, dtype=torch.bfloat16):
+    return torch.randn(*shape, generator=g, device=DEV, dtype=torch.float32).mul_(scale).to(dtype)
+
+
+def _head(case, g):
+    """Normalised hidden states and head weights whose logits have a deviation of about 3, targets towards the frequent tokens."""
+    T, d, V = case["tokens"], case["d_in"], case["vocab"]
+    H, W = _randn(g, T, d), _randn(g, V, d, scale=3.0 / math.sqrt(d))
+    targets = (torch.rand(T, generator=g, device=DEV) ** 3 * V).long().clamp_(max=V - 1)
+    return H, W, targets
+
+
+def prepare(case, seed):
+    g = _gen(seed)
+    kind = case["kind"]
+    if kind == "ce":
+        H, W, targets = _head(case, g)
+        targets[torch.rand(case["tokens"], generator=g, device=DEV) < case["ignored"]] = -100
+        kept = targets >= 0
+        return {"kind": kind, "grad": case["grad"], "H": H, "W": W, "targets": targets, "d_ce": kept.float() / kept.sum().clamp(min=1)}
+    if kind == "distill":
+        H, W, targets = _head(case, g)
+        T, V, K = case["tokens"], case["vocab"], case["top"]
+        # distinct tokens for each row, logits that fall off; the end of some lists and some whole lists are missing
+        first = torch.randint(0, V, (T, 1), generator=g, device=DEV)
+        step = torch.randint(1, max(2, V // K), (T, 1), generator=g, device=DEV)
+        top_idx = (first + step * torch.arange(K, device=DEV)) % V
+        fall = -torch.log(torch.rand(T, K, generator=g, device=DEV).clamp_(min=1e-6)).cumsum(1)
+        top_logits = (12.0 - fall * (8.0 / K) ** 0.5).to(torch.bfloat16 if case["dtype"] == "bf16" else torch.float32)
+        some = torch.rand(T, 1, generator=g, device=DEV)
+        length = torch.where(some < case["empty"], torch.zeros_like(first), torch.where(some < 2 * case["empty"], torch.full_like(first, K - K // 3), torch.full_like(first, K)))
+        top_idx = torch.where(torch.arange(K, device=DEV) < length, top_idx, torch.full_like(top_idx, -1))
+        state = {"kind": kind, "grad": case["grad"], "H": H, "W": W, "targets": None, "d_ce": None, "top_idx": top_idx, "top_logits": top_logits,
+                 "tau": case["tau"], "d_kd": torch.full((T,), 0.7 / T, device=DEV)}
+        if case["hard"]:
+            state.update(targets=targets, d_ce=torch.full((T,), 0.3 / T, device=DEV))
+        return state
+    if kind == "quantize":
+        dtype = torch.bfloat16 if case["dtype"] == "bf16" else torch.float32
+        X = _randn(g, case["rows"], case["cols"], scale=0.06, dtype=dtype)
+        X *= torch.exp2(torch.randint(-6, 7, (case["rows"], 1), generator=g, device=DEV)).to(dtype)
+        return {"kind": kind, "X": X}
+    X = _randn(g, case["tokens"], case["d_in"])
+    X[torch.rand(X.shape, generator=g, device=DEV) < 0.002] *= 20   # activations have outliers
+    codes, scales = _plain_quantize(_randn(g, case["d_out"], case["d_in"], scale=1.0 / math.sqrt(case["d_in"])))
+    bias = torch.randn(case["d_out"], generator=g, device=DEV) if case["bias"] else None
+    return {"kind": kind, "X": X, "codes": codes, "scales": scales, "bias": bias, "d_out": case["d_out"]}
+
+
+# ---- plain forms -------------------------------------------------------------------------------------------------------------------
+def _plain_head(s):
+    H, W = s["H"].float(), s["W"].float()
+    distill = s["kind"] == "distill"
+    z = H @ W.t()
+    m = z.amax(1, keepdim=True)
+    out = {}
+    g = z_top = None
+    if distill:
+        V, tau = z.shape[1], s["tau"]
+        valid = (s["top_idx"] >= 0) & (s["top_idx"] < V) & (s["top_logits"] > -math.inf)
+        at = torch.where(valid, s["top_idx"], 0)
+        a = torch.where(valid, s["top_logits"].float() / tau, -math.inf)
+        some = valid.any(1, keepdim=True)
+        a = a - torch.where(some, a.amax(1, keepdim=True), 0.0)
+        e = torch.exp(a)
+        total = torch.where(some, e.sum(1, keepdim=True), 1.0)
+        q, log_q = e / total, a - torch.log(total)
+        z_top = z.gather(1, at)
+    if s["targets"] is not None:
+        kept = s["targets"] >= 0
+        target = torch.where(kept, s["targets"], 0)[:, None]
+        z_target = z.gather(1, target)[:, 0]
+        e1 = torch.exp(z - m)
+        sum1 = e1.sum(1, keepdim=True)
+        out["ce"] = torch.where(kept, m[:, 0] + torch.log(sum1[:, 0]) - z_target, 0.0)
+        if s["grad"]:
+            d = torch.where(kept, s["d_ce"], 0.0)[:, None]
+            g = e1.mul_(d / sum1)
+            g.scatter_add_(1, target, -d)
+        del e1
+    if distill:
+        e2 = z.sub_(m).div_(tau).exp_()
+        sum2 = e2.sum(1, keepdim=True)
+        lse = m / tau + torch.log(sum2)
+        out["kd"] = torch.where(some[:, 0], tau * tau * torch.where(valid & (q > 0), q * (log_q - z_top / tau + lse), 0.0).sum(1), 0.0)
+        if s["grad"]:
+            d = torch.where(some, s["d_kd"][:, None] * tau, 0.0)
+            e2.mul_(d / sum2)
+            e2.scatter_add_(1, at, -d * q)
+            g = e2 if g is None else g.add_(e2)
+    del z
+    if s["grad"]:
+        out["dH"] = (g @ W).to(torch.bfloat16)
+        out["dW"] = (g.t() @ H).to(torch.bfloat16)
+    return out
+
+
+def _plain_quantize(X):
+    """Codes (two to a byte, the even column in the low half) and scales of rows padded with zeros to whole 128 columns."""
+    rows, cols = X.shape
+    wide = -(-cols // 128) * 128
+    x = torch.zeros(rows, wide, device=X.device)
+    x[:, :cols] = X
+    x = x.view(rows, wide // 32, 32)
+    field = (x.abs().amax(2).view(torch.int32) >> 23) - 2
+    scales = field.clamp(min=0)
+    x = x * torch.exp2((127 - scales).float())[:, :, None]
+    v = x.abs()
+    step = torch.where(v < 2, 0.5, torch.where(v < 4, 1.0, 2.0))
+    v = (torch.round(v / step) * step).clamp(max=6.0)
+    code = torch.where(v < 2, 2 * v, torch.where(v < 4, v + 2, v / 2 + 4)).to(torch.uint8) | ((x.view(torch.int32) < 0).to(torch.uint8) << 3)
+    code = code.view(rows, wide)
+    return code[:, 0::2] | (code[:, 1::2] << 4), scales.to(torch.uint8)
+
+
+def _plain_values(codes, scales, cols):
+    rows = codes.shape[0]
+    code = torch.stack((codes & 15, codes >> 4), 2).view(rows, -1).int()
+    m = code & 7
+    v = torch.where(m < 4, m * 0.5, torch.where(m < 6, m - 2.0, m * 2.0 - 8.0))
+    v = torch.where(code > 7, -v, v).view(rows, -1, 32) * torch.exp2(scales.float() - 127)[:, :, None]
+    return v.view(rows, -1)[:, :cols]
+
+
+def run(state):
+    s = state
+    if own:
+        return _own(s)
+    if s["kind"] in ("ce", "distill"):
+        return _plain_head(s)
+    X = s["X"]
+    values = _plain_values(*_plain_quantize(X), X.shape[1])
+    if s["kind"] == "quantize":
+        return values.to(X.dtype)
+    y = values @ _plain_values(s["codes"], s["scales"], X.shape[1]).t()
+    return y if s["bias"] is None else y + s["bias"]
+
+
+# ---- the framework's calls ---------------------------------------------------------------------------------------------------------
+_kept = {}
+
+
+def _workspace(sbn, nbytes):
+    """One scratch buffer for the program, grown where a call needs more."""
+    if "ws" not in _kept or _kept["ws"].numel() < nbytes:
+        _kept["ws"] = None
+        _kept["ws"] = sbn.new_workspace(nbytes, DEV)
+    return _kept["ws"]
+
+
+def _own(s):
+    import paper_2603_05168_amd as sbn
+    f32 = {"dtype": torch.float32, "device": DEV}
+    X = s["X"] if "X" in s else s["H"]
+    T, d = X.shape
+    if s["kind"] == "quantize":
+        code_bytes, scale_bytes = sbn.sbn_mxfp4_bytes(T, d)
+        codes = torch.empty(code_bytes, dtype=torch.uint8, device=DEV)
+        scales = torch.empty(scale_bytes, dtype=torch.uint8, device=DEV)
+        Y = torch.empty_like(X)
+        sbn.sbn_mxfp4_quantize(X, codes, scales)
+        sbn.sbn_mxfp4_dequantize(codes, scales, Y)
+        return Y
+    if s["kind"] == "linear":
+        Y = torch.empty(T, s["d_out"], **f32)
+        sbn.sbn_mxfp4_linear(X, s["codes"], s["scales"], Y, _workspace(sbn, sbn.sbn_mxfp4_workspace_bytes(T, d)), bias=s["bias"])
+        return Y
+    W = s["W"]
+    out, grads = {}, {}
+    if s["grad"]:
+        grads = {"dH": torch.empty_like(s["H"]), "dW": torch.empty_like(W)}
+    if s["kind"] == "ce":
+        ws = _workspace(sbn, sbn.sbn_head_workspace_bytes(T, d, W.shape[0], backward=s["grad"]))
+        ce, lse = torch.empty(T, **f32), torch.empty(T, **f32)
+        sbn.sbn_head_cross_entropy(X, W, s["targets"], ce, lse, ws)
+        if s["grad"]:
+            sbn.sbn_head_cross_entropy_backward(X, W, s["targets"], lse, s["d_ce"], ws, **grads)
+        return {"ce": ce, **grads}
+    K = s["top_idx"].shape[1]
+    ws = _workspace(sbn, sbn.sbn_head_workspace_bytes(T, d, W.shape[0], top_k=K, backward=s["grad"]))
+    kd, lse, z_top = torch.empty(T, **f32), torch.empty(2, T, **f32), torch.empty(T, K, **f32)
+    if s["targets"] is not None:
+        out["ce"] = torch.empty(T, **f32)
+    sbn.sbn_head_distill(X, W, s["top_idx"], s["top_logits"], s["tau"], kd, lse, z_top, ws, targets=s["targets"], ce=out.get("ce"))
+    if s["grad"]:
+        sbn.sbn_head_distill_backward(X, W, s["top_idx"], s["top_logits"], s["tau"], lse, z_top, s["d_kd"], ws, targets=s["targets"], d_ce=s["d_ce"], **grads)
+    return {**out, "kd": kd, **grads}
+
+
+# ---- what a pass cannot do without, and its values in 64 bits ------------------------------------------------------------------------
+def work(case):
+    if case["kind"] == "quantize":
+        n, size = case["rows"] * case["cols"], 2 if case["dtype"] == "bf16" else 4
+        return {"bytes": n * (2 * size + 17 / 32), "flops": 0}
+    T, d = case["tokens"], case["d_in"]
+    if case["kind"] == "linear":
+        V = case["d_out"]
+        return {"bytes": 2 * T * d + V * d * 17 / 32 + 4 * T * V + (4 * V if case["bias"] else 0), "flops": 2 * T * V * d}
+    V = case["vocab"]
+    nbytes = 2 * (T + V) * d + 4 * T
+    if case["kind"] == "ce" or case["hard"]:
+        nbytes += 8 * T
+    if case["kind"] == "distill":
+        nbytes += T * case["top"] * (8 + (2 if case["dtype"] == "bf16" else 4))
+    # the gradient's products are two, and without the logits kept they are made once more
+    return {"bytes": nbytes + (2 * (T + V) * d + 4 * T if case["grad"] else 0), "flops": (8 if case["grad"] else 2) * T * V * d}
+
+
+def _exact_values(X):
+    """What 4-bit microscaled values X stands for, in 64 bits: every magnitude as the count of the rounding borders below it."""
+    rows, cols = X.shape
+    out = torch.zeros(rows, cols, dtype=torch.float64, device=X.device)
+    grid = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float64, device=X.device)
+    for first in range(0, cols, 32):
+        x = X[:, first:first + 32].double()
+        most = x.abs().amax(1, keepdim=True)
+        _, exponent = torch.frexp(most)
+        e = torch.where(most > 0, exponent - 3, -127).clamp(-127, 127).double()
+        v = x.abs() * torch.exp2(-e)
+        n = torch.zeros(v.shape, dtype=torch.long, device=X.device)
+        for border, up in ((0.25, False), (0.75, True), (1.25, False), (1.75, True), (2.5, False), (3.5, True), (5.0, False)):   # ties to the even code
+            n += (v >= border) if up else (v > border)
+        out[:, first:first + 32] = grid[n] * torch.exp2(e) * torch.sign(x)
+    return out
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["kind"] == "quantize":
+        return _exact_values(s["X"])
+    if case["kind"] == "linear":
+        table = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, -0.0, -0.5, -1, -1.5, -2, -3, -4, -6], dtype=torch.float64, device=DEV)
+        pair = s["codes"].long()
+        w = torch.empty(pair.shape[0], 2 * pair.shape[1], dtype=torch.float64, device=DEV)
+        w[:, 0::2], w[:, 1::2] = table[pair % 16], table[pair // 16]
+        w *= torch.repeat_interleave(torch.exp2(s["scales"].double() - 127), 32, dim=1)
+        y = _exact_values(s["X"]) @ w[:, :case["d_in"]].t()
+        return y if s["bias"] is None else y + s["bias"].double()
+    W = s["W"].double()
+    T, V = case["tokens"], case["vocab"]
+    parts = {"ce": [], "kd": [], "dH": []}
+    dW = torch.zeros(V, case["d_in"], dtype=torch.float64, device=DEV)
+    for t in range(0, T, 2048):
+        rows = slice(t, min(T, t + 2048))
+        H = s["H"][rows].double()
+        z = H @ W.t()
+        G = torch.zeros_like(z)
+        here = torch.arange(z.shape[0], device=DEV)
+        if s["targets"] is not None:
+            y = s["targets"][rows]
+            logp = torch.log_softmax(z, 1)
+            on = y >= 0
+            parts["ce"].append(torch.where(on, -logp[here, y.clamp(min=0)], 0.0))
+            if case["grad"]:
+                d = s["d_ce"][rows].double() * on
+                p = torch.exp(logp)
+                p[here, y.clamp(min=0)] -= 1.0
+                G += p * d[:, None]
+        if case["kind"] == "distill":
+            tau, idx, a = s["tau"], s["top_idx"][rows], s["top_logits"][rows].double()
+            q = torch.zeros(z.shape[0], V + 1, dtype=torch.float64, device=DEV)   # column V takes what is missing
+            w = torch.exp((a - a.max()) / tau) * (idx >= 0)
+            w = w / w.sum(1, keepdim=True).clamp(min=1e-300)
+            q.scatter_add_(1, torch.where(idx >= 0, idx, V), w)
+            q = q[:, :V]
+            logp = torch.log_softmax(z / tau, 1)
+            parts["kd"].append(tau ** 2 * (torch.xlogy(q, q) - q * logp).sum(1))
+            if case["grad"]:
+                any_ = (idx >= 0).any(1, keepdim=True).double()
+                G += s["d_kd"][rows].double()[:, None] * tau * (torch.exp(logp) * any_ - q)
+        if case["grad"]:
+            parts["dH"].append(G @ W)
+            dW += G.t() @ H
+    out = {k: torch.cat(v) for k, v in parts.items() if v}
+    if case["grad"]:
+        out["dW"] = dW
+    return out
