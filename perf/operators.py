@@ -261,12 +261,12 @@ def _own(s):
         return {"ce": ce, **grads}
     K = s["top_idx"].shape[1]
     ws = _workspace(sbn, sbn.sbn_head_workspace_bytes(T, d, W.shape[0], top_k=K, backward=s["grad"]))
-    kd, lse, z_top = torch.empty(T, **f32), torch.empty(2, T, **f32), torch.empty(T, K, **f32)
+    kd, lse = torch.empty(T, **f32), torch.empty(2, T, **f32)
     if s["targets"] is not None:
         out["ce"] = torch.empty(T, **f32)
-    sbn.sbn_head_distill(X, W, s["top_idx"], s["top_logits"], s["tau"], kd, lse, z_top, ws, targets=s["targets"], ce=out.get("ce"))
+    sbn.sbn_head_distill(X, W, s["top_idx"], s["top_logits"], s["tau"], kd, lse, ws, targets=s["targets"], ce=out.get("ce"))
     if s["grad"]:
-        sbn.sbn_head_distill_backward(X, W, s["top_idx"], s["top_logits"], s["tau"], lse, z_top, s["d_kd"], ws, targets=s["targets"], d_ce=s["d_ce"], **grads)
+        sbn.sbn_head_distill_backward(X, W, s["top_idx"], s["top_logits"], s["tau"], lse, s["d_kd"], ws, targets=s["targets"], d_ce=s["d_ce"], **grads)
     return {**out, "kd": kd, **grads}
 
 
