@@ -385,6 +385,68 @@ sbn_status sbn_test_chosen_kernels(int count, const int64_t *tokens, const int64
 sbn_status sbn_test_takes_blocks(int count, const int64_t *tokens, const int64_t *d_in, const int64_t *d_out, int N, int M,
                                  int *blocks);
 
+/*
+ * The output head: the dense matrix behind the last block, trained against tokens or a teacher.  With z = H W^T (never stored)
+ * and lse(x)[t] = log sum_v exp x[t,v]
+ *   ce[t]  = lse(z)[t] - z[t, y_t]
+ *   kd[t]  = tau^2 sum_v q[t,v] (log q[t,v] - z[t,v] / tau + lse(z / tau)[t]),   q[t,:] = softmax(top_logits[t,:] / tau) at top_idx[t,:]
+ * and for given gradients d_ce, d_kd of the two losses
+ *   G[t,v] = d_ce[t] (softmax(z)[t,v] - (v == y_t)) + d_kd[t] tau (softmax(z / tau)[t,v] - q[t,v]),   dH = G W,   dW = G^T H
+ * (the factor tau^2 of kd keeps its gradient in step with that of ce at any temperature).
+ *   H          device, bf16 [tokens, d_in];  W  device, bf16 [vocab, d_in]: 16-byte aligned, d_in % 8 == 0
+ *   targets    device, int64 [tokens]; a target outside [0, vocab) leaves its token out: ce 0, no share in the gradients
+ *   top_idx    device, int64 [tokens, top_k];  top_logits  device, fp32 or bf16 [tokens, top_k].  An entry whose index is outside
+ *              [0, vocab) or whose logit is -inf is missing; a token with no entry has kd 0 and no share in the gradients; an
+ *              index that a token's list holds more than once counts with the sum of its probabilities
+ *   ce, kd     device, fp32 [tokens]; written
+ *   lse        device, fp32 [tokens] (cross_entropy: lse(z)) or [2, tokens] (distill: lse(z), written where targets are given, then
+ *              lse(z / tau)); written by the forward, read by the backward
+ *   dH, dW     device, bf16 [tokens, d_in] / [vocab, d_in], 16-byte aligned, overwritten; either may be NULL
+ *   targets, ce, d_ce of the distillation calls: all given (both losses from one pass over W) or all NULL
+ *   workspace  device, 256-byte aligned, >= sbn_head_workspace_bytes(tokens, d_in, vocab, top_k, backward); top_k 0 for cross entropy
+ * Arithmetic: products on bf16 operands with fp32 accumulation, maxima, sums and losses in fp32; G is rounded to bf16 once as the operand
+ * of its products, whose sums are fp32 until they are rounded to dH and dW.  No atomics: a call repeated gives the same bits.
+ * H and W must be finite, also in tokens that are left out.
+ * Errors: SBN_EINVAL (null, non-positive size, tau not positive and finite), SBN_EALIGN, SBN_ESIZE, SBN_EUNSUPPORTED (d_in % 8 != 0, d_in >
+ * 2^16, tokens or vocab > 2^24, tokens * vocab > 2^38, either times d_in > 2^34, top_k > 1024, vocab > 2^21 with a teacher), SBN_EHIP.
+ */
+sbn_status sbn_head_workspace_bytes(int64_t tokens, int64_t d_in, int64_t vocab, int64_t top_k, int backward, size_t *bytes);
+sbn_status sbn_head_cross_entropy(const void *H, const void *W, const int64_t *targets, int64_t tokens, int64_t d_in, int64_t vocab,
+                                  float *ce, float *lse, void *workspace, size_t ws_bytes, void *stream);
+sbn_status sbn_head_cross_entropy_backward(const void *H, const void *W, const int64_t *targets, const float *lse, const float *d_ce,
+                                           int64_t tokens, int64_t d_in, int64_t vocab, void *dH, void *dW, void *workspace,
+                                           size_t ws_bytes, void *stream);
+sbn_status sbn_head_distill(const void *H, const void *W, const int64_t *top_idx, const void *top_logits, sbn_dtype top_dtype, int64_t top_k,
+                            float tau, const int64_t *targets, int64_t tokens, int64_t d_in, int64_t vocab, float *kd, float *ce,
+                            float *lse, void *workspace, size_t ws_bytes, void *stream);
+sbn_status sbn_head_distill_backward(const void *H, const void *W, const int64_t *top_idx, const void *top_logits, sbn_dtype top_dtype,
+                                     int64_t top_k, float tau, const int64_t *targets, const float *lse, const float *d_kd, const float *d_ce,
+                                     int64_t tokens, int64_t d_in, int64_t vocab, void *dH, void *dW, void *workspace, size_t ws_bytes,
+                                     void *stream);
+
+/*
+ * Microscaled 4-bit floating point, in which the output head (or another dense layer) is served: blocks of 32 consecutive values
+ * of a row share a scale, a value is a sign (bit 3) and a code of {0, 0.5, 1, 1.5, 2, 3, 4, 6} (bits 0 .. 2).
+ *   codes   rows of ceil(cols / 128) * 64 bytes: column 2 i in the low half of byte i, 2 i + 1 in the high half
+ *   scales  rows of ceil(cols / 128) * 4 bytes, one per block: s stands for 2^(s - 127)
+ * Columns that pad a row are zeros, a block of zeros has s = 0.  quantize takes s = max(e - 2, 0), e the exponent field (as of fp32) of the
+ * block's largest magnitude, and of every value / 2^(s - 127) the nearest code, ties to the even one, magnitudes above 6 to 6.
+ *   X, Y    device, fp32 or bf16 [rows, cols], 16-byte aligned; dequantize is exact in both types
+ *   codes   device, 16-byte aligned;  scales  device, 4-byte aligned: sbn_mxfp4_bytes() bytes each, no scale of 255
+ * linear: Y[t,o] = sum_k q(X)[t,k] W[o,k] (+ bias[o]), q(X) the values that quantize makes of X, products exact, sums in fp32
+ *   X       device, bf16 [tokens, d_in], 16-byte aligned;  codes, scales  of W [d_out, d_in]
+ *   bias    device, fp32 [d_out], or NULL;  Y  device, fp32 [tokens, d_out], 16-byte aligned; written
+ *   workspace  device, 256-byte aligned, >= sbn_mxfp4_workspace_bytes(tokens, d_in)
+ * Errors: SBN_EINVAL, SBN_EALIGN, SBN_ESIZE, SBN_EUNSUPPORTED (cols or d_in % 8 != 0 or above 2^20, more than 2^34 values with those that
+ * pad the rows, 2^38 outputs or more), SBN_EHIP.
+ */
+sbn_status sbn_mxfp4_bytes(int64_t rows, int64_t cols, size_t *code_bytes, size_t *scale_bytes);
+sbn_status sbn_mxfp4_quantize(const void *X, sbn_dtype dtype, int64_t rows, int64_t cols, void *codes, void *scales, void *stream);
+sbn_status sbn_mxfp4_dequantize(const void *codes, const void *scales, int64_t rows, int64_t cols, void *Y, sbn_dtype dtype, void *stream);
+sbn_status sbn_mxfp4_workspace_bytes(int64_t tokens, int64_t d_in, size_t *bytes);
+sbn_status sbn_mxfp4_linear(const void *X, int64_t tokens, int64_t d_in, int64_t d_out, const void *codes, const void *scales,
+                            const float *bias, float *Y, void *workspace, size_t ws_bytes, void *stream);
+
 /* Text of the last HIP error seen by this thread ("" if none). */
 const char *sbn_last_error(void);
 

@@ -83,6 +83,26 @@ def _load():
     lib.sbn_test_forward_kernels.argtypes = [cint, pp, pi64, pi64, pi64, cint, cint, pp, ctypes.POINTER(cint)]
     lib.sbn_test_chosen_kernels.restype = cint
     lib.sbn_test_chosen_kernels.argtypes = [cint, pi64, pi64, pi64, cint, cint, ctypes.POINTER(cint)]
+    lib.sbn_head_workspace_bytes.restype = cint
+    lib.sbn_head_workspace_bytes.argtypes = [i64, i64, i64, i64, cint, ctypes.POINTER(sz)]
+    lib.sbn_head_cross_entropy.restype = cint
+    lib.sbn_head_cross_entropy.argtypes = [vp, vp, vp, i64, i64, i64, vp, vp, vp, sz, vp]
+    lib.sbn_head_cross_entropy_backward.restype = cint
+    lib.sbn_head_cross_entropy_backward.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, vp, vp, vp, sz, vp]
+    lib.sbn_head_distill.restype = cint
+    lib.sbn_head_distill.argtypes = [vp, vp, vp, vp, cint, i64, ctypes.c_float, vp, i64, i64, i64, vp, vp, vp, vp, sz, vp]
+    lib.sbn_head_distill_backward.restype = cint
+    lib.sbn_head_distill_backward.argtypes = [vp, vp, vp, vp, cint, i64, ctypes.c_float, vp, vp, vp, vp, i64, i64, i64, vp, vp, vp, sz, vp]
+    lib.sbn_mxfp4_bytes.restype = cint
+    lib.sbn_mxfp4_bytes.argtypes = [i64, i64, ctypes.POINTER(sz), ctypes.POINTER(sz)]
+    lib.sbn_mxfp4_quantize.restype = cint
+    lib.sbn_mxfp4_quantize.argtypes = [vp, cint, i64, i64, vp, vp, vp]
+    lib.sbn_mxfp4_dequantize.restype = cint
+    lib.sbn_mxfp4_dequantize.argtypes = [vp, vp, i64, i64, vp, cint, vp]
+    lib.sbn_mxfp4_workspace_bytes.restype = cint
+    lib.sbn_mxfp4_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(sz)]
+    lib.sbn_mxfp4_linear.restype = cint
+    lib.sbn_mxfp4_linear.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, vp, sz, vp]
     lib.sbn_mask_flips.restype = cint
     lib.sbn_mask_flips.argtypes = [vp, vp, i64, i64, cint, cint, vp, vp, sz, vp]
     return lib
@@ -436,6 +456,134 @@ def sbn_mask_flips(packed_a, packed_b, d_out: int, d_in: int, N: int, M: int, fl
     """flips_out: int64 device tensor of one element (the count is non-negative and below 2**63)."""
     _check(_lib.sbn_mask_flips(_ptr(packed_a), _ptr(packed_b), d_out, d_in, N, M, _ptr(flips_out), _ptr(workspace),
                                workspace.numel() * workspace.element_size(), _stream()), "sbn_mask_flips")
+
+
+def _expect(name, t, shape, *dtypes):
+    """t, where it is a contiguous tensor of this shape and one of these types (or None)."""
+    if t is not None:
+        if t.dtype not in dtypes:
+            raise TypeError(f"{name} must be {' or '.join(str(d).removeprefix('torch.') for d in dtypes)}")
+        if t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous {list(shape)}, not {list(t.shape)} with strides {list(t.stride())}")
+    return t
+
+
+def _bytes_of(ws):
+    return ws.numel() * ws.element_size()
+
+
+def sbn_head_workspace_bytes(tokens: int, d_in: int, vocab: int, top_k: int = 0, backward: bool = True) -> int:
+    """Workspace of the forward calls of the output head, and of their backward calls where `backward` is set."""
+    out = ctypes.c_size_t(0)
+    _check(_lib.sbn_head_workspace_bytes(tokens, d_in, vocab, top_k, int(backward), ctypes.byref(out)), "sbn_head_workspace_bytes")
+    return out.value
+
+
+def _head_sizes(H, W, targets, ce, dH=None, dW=None):
+    bf16, f32 = torch.bfloat16, torch.float32
+    (tokens, d_in), vocab = H.shape, W.shape[0]
+    _expect("H", H, (tokens, d_in), bf16)
+    _expect("W", W, (vocab, d_in), bf16)
+    _expect("targets", targets, (tokens,), torch.int64)
+    _expect("ce", ce, (tokens,), f32)
+    _expect("dH", dH, (tokens, d_in), bf16)
+    _expect("dW", dW, (vocab, d_in), bf16)
+    return tokens, d_in, vocab
+
+
+def sbn_head_cross_entropy(H, W, targets, ce, lse, workspace):
+    """ce, lse (fp32 [tokens]) of z = H W^T against targets (int64; outside the vocabulary: left out), the logits never stored."""
+    tokens, d_in, vocab = _head_sizes(H, W, targets, ce)
+    _expect("lse", lse, (tokens,), torch.float32)
+    _check(_lib.sbn_head_cross_entropy(_ptr(H), _ptr(W), _ptr(targets), tokens, d_in, vocab, _ptr(ce), _ptr(lse), _ptr(workspace),
+                                       _bytes_of(workspace), _stream()), "sbn_head_cross_entropy")
+
+
+def sbn_head_cross_entropy_backward(H, W, targets, lse, d_ce, workspace, dH=None, dW=None):
+    """dH, dW (bf16, overwritten; None: not wanted) for the gradient d_ce (fp32 [tokens]) of ce."""
+    tokens, d_in, vocab = _head_sizes(H, W, targets, d_ce, dH, dW)
+    _expect("lse", lse, (tokens,), torch.float32)
+    _check(_lib.sbn_head_cross_entropy_backward(_ptr(H), _ptr(W), _ptr(targets), _ptr(lse), _ptr(d_ce), tokens, d_in, vocab, _ptr(dH), _ptr(dW),
+                                                _ptr(workspace), _bytes_of(workspace), _stream()), "sbn_head_cross_entropy_backward")
+
+
+def _teacher(top_idx, top_logits, tokens):
+    top_k = top_idx.shape[1]
+    _expect("top_idx", top_idx, (tokens, top_k), torch.int64)
+    _expect("top_logits", top_logits, (tokens, top_k), torch.float32, torch.bfloat16)
+    return SBN_BF16 if top_logits.dtype == torch.bfloat16 else SBN_F32, top_k
+
+
+def sbn_head_distill(H, W, top_idx, top_logits, tau: float, kd, lse, workspace, targets=None, ce=None):
+    """kd (fp32 [tokens]) against the teacher's entries top_idx (int64) and top_logits (fp32 or bf16), both [tokens, k], at temperature
+    tau; lse fp32 [2, tokens]; with targets and ce the cross entropy from the same pass."""
+    tokens, d_in, vocab = _head_sizes(H, W, targets, ce)
+    dtype, top_k = _teacher(top_idx, top_logits, tokens)
+    _expect("kd", kd, (tokens,), torch.float32)
+    _expect("lse", lse, (2, tokens), torch.float32)
+    _check(_lib.sbn_head_distill(_ptr(H), _ptr(W), _ptr(top_idx), _ptr(top_logits), dtype, top_k, tau, _ptr(targets), tokens, d_in, vocab,
+                                 _ptr(kd), _ptr(ce), _ptr(lse), _ptr(workspace), _bytes_of(workspace), _stream()), "sbn_head_distill")
+
+
+def sbn_head_distill_backward(H, W, top_idx, top_logits, tau: float, lse, d_kd, workspace, targets=None, d_ce=None, dH=None, dW=None):
+    """dH, dW (bf16, overwritten; None: not wanted) for the gradients d_kd and, with targets, d_ce of the two losses."""
+    tokens, d_in, vocab = _head_sizes(H, W, targets, d_ce, dH, dW)
+    dtype, top_k = _teacher(top_idx, top_logits, tokens)
+    _expect("d_kd", d_kd, (tokens,), torch.float32)
+    _expect("lse", lse, (2, tokens), torch.float32)
+    _check(_lib.sbn_head_distill_backward(_ptr(H), _ptr(W), _ptr(top_idx), _ptr(top_logits), dtype, top_k, tau, _ptr(targets), _ptr(lse),
+                                          _ptr(d_kd), _ptr(d_ce), tokens, d_in, vocab, _ptr(dH), _ptr(dW), _ptr(workspace),
+                                          _bytes_of(workspace), _stream()), "sbn_head_distill_backward")
+
+
+def sbn_mxfp4_bytes(rows: int, cols: int):
+    """Bytes of the codes and of the scales of a [rows, cols] matrix."""
+    codes, scales = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(_lib.sbn_mxfp4_bytes(rows, cols, ctypes.byref(codes), ctypes.byref(scales)), "sbn_mxfp4_bytes")
+    return codes.value, scales.value
+
+
+def _mxfp4(codes, scales, rows, cols):
+    """Codes and scales as uint8 buffers of any shape that hold a [rows, cols] matrix."""
+    wide = -(-cols // 128) * 128
+    for name, t, nbytes in (("codes", codes, rows * wide // 2), ("scales", scales, rows * wide // 32)):
+        if t.dtype != torch.uint8:
+            raise TypeError(f"{name} must be uint8")
+        if t.numel() != nbytes or not t.is_contiguous():
+            raise ValueError(f"{name} must be {nbytes} contiguous bytes for [{rows}, {cols}], not {t.numel()}")
+
+
+def sbn_mxfp4_quantize(X, codes, scales):
+    """X (fp32 or bf16 [rows, cols]) to microscaled 4-bit codes and block scales (uint8)."""
+    rows, cols = X.shape
+    _expect("X", X, (rows, cols), torch.float32, torch.bfloat16)
+    _mxfp4(codes, scales, rows, cols)
+    _check(_lib.sbn_mxfp4_quantize(_ptr(X), _dtype_code(X), rows, cols, _ptr(codes), _ptr(scales), _stream()), "sbn_mxfp4_quantize")
+
+
+def sbn_mxfp4_dequantize(codes, scales, Y):
+    """The values that codes and scales stand for, exactly, into Y (fp32 or bf16 [rows, cols])."""
+    rows, cols = Y.shape
+    _expect("Y", Y, (rows, cols), torch.float32, torch.bfloat16)
+    _mxfp4(codes, scales, rows, cols)
+    _check(_lib.sbn_mxfp4_dequantize(_ptr(codes), _ptr(scales), rows, cols, _ptr(Y), _dtype_code(Y), _stream()), "sbn_mxfp4_dequantize")
+
+
+def sbn_mxfp4_workspace_bytes(tokens: int, d_in: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.sbn_mxfp4_workspace_bytes(tokens, d_in, ctypes.byref(out)), "sbn_mxfp4_workspace_bytes")
+    return out.value
+
+
+def sbn_mxfp4_linear(X, codes, scales, Y, workspace, bias=None):
+    """Y (fp32 [tokens, d_out]) = q(X) W^T (+ bias): X bf16, quantized on the way; W as codes and scales."""
+    (tokens, d_in), d_out = X.shape, Y.shape[1]
+    _expect("X", X, (tokens, d_in), torch.bfloat16)
+    _expect("Y", Y, (tokens, d_out), torch.float32)
+    _expect("bias", bias, (d_out,), torch.float32)
+    _mxfp4(codes, scales, d_out, d_in)
+    _check(_lib.sbn_mxfp4_linear(_ptr(X), tokens, d_in, d_out, _ptr(codes), _ptr(scales), _ptr(bias), _ptr(Y), _ptr(workspace),
+                                 _bytes_of(workspace), _stream()), "sbn_mxfp4_linear")
 
 
 def new_workspace(nbytes: int, device="cuda") -> torch.Tensor:

@@ -1,0 +1,1026 @@
+// The output head in training: softmax cross entropy and distillation from a teacher's top logits over a vocabulary, without keeping
+// the logits.  H [tokens, d] and W [vocab, d] are bf16, z = H W^T, and per token t
+//   ce = lse(z) - z_y,                                         lse(x) = log sum_v exp x_v
+//   kd = tau^2 sum_v q_v (log q_v - (z_v / tau - lse(z / tau))),   q = softmax(a / tau) over the teacher's entries
+//   G  = d_ce (softmax(z) - onehot(y)) + d_kd tau (softmax(z / tau) - q),   dH = G W,   dW = G^T H
+// Forward: one product whose tiles leave a maximum and sums of exponentials per token and 128 (64) words of the vocabulary; they are joined
+// in a fixed order.  Backward: the vocabulary is cut into pieces; the logits of a piece are made once more, turned into G (bf16) on their
+// way out, and both gradients' products read G.  All products run on the bf16 matrix cores (v_mfma_f32_32x32x16_bf16, fp32
+// accumulation).  Nothing is added atomically: results do not depend on the order of blocks.
+#include <algorithm>
+
+#include "sbn_internal.hpp"
+#include "sbn_mfma.hpp"
+
+namespace sbn {
+
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f;
+
+// two values rounded to bf16 (to nearest, ties to even), lo in the low half: v_cvt_pk_bf16_f32
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{lo, hi}, v2bf));
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp
+
+// ---- block tile product -------------------------------------------------------------------------------------------------------------
+// acc[n, m] = sum_k P[n, k] Q[m, k] for a block tile of 256 x 256 (eight wavefronts of 128 x 64) or 128 x 128 (four of 64 x 64, two blocks
+// per multiprocessor).  Either operand lies with k contiguous ([rows, ld]) or the other way round ([k, ld], "transposed": read from LDS by
+// ds_read_b64_tr_b16).  Stages of 64 k come by LDS-DMA into a ring of five slots that the operands take in turns, so that P lies in LDS two
+// stages ahead and Q one; a stage is consumed in quarters of 16 k, the fragments of the next quarter are read and the requests for later
+// stages issued between the matrix instructions of the current one.
+constexpr int STAGE_K = 64;
+template <bool BIG> struct HeadTile {
+    static constexpr int N = BIG ? 256 : 128, M = N;
+    static constexpr int WAVES = BIG ? 8 : 4, WN = 2, WM = WAVES / WN;       // wavefronts along n and m
+    static constexpr int WP = N / WN / 32, WQ = M / WM / 32;                 // 32 x 32 tiles of a wavefront: 4 x 2 or 2 x 2
+    static constexpr int SLOT = N * STAGE_K * 2, SLOTS = 5;                  // one operand's share of a stage
+    static constexpr int LDS = SLOTS * SLOT, STAGING = 4 * SLOT / WAVES;     // the last: of a wavefront, for its result
+    static constexpr int ROW = WP * 128;                                     // bytes of a staged row of fp32 results
+};
+
+struct Operand {
+    const uint16_t *base;   // row 0, k 0
+    int64_t ld;
+    int rows, k;            // what the matrix has (k: from the product's first k on)
+};
+
+// The requests of one operand: four instructions of 1 KB per wavefront and stage.  Rows and k past the matrix read as zeros or as what
+// zero_tail overwrites; stages past the last fetch nothing.  A buffer's size has 32 bits and ends with the rows of the tile.
+template <bool BIG, bool TRANSPOSED> struct Requests {
+    using S = HeadTile<BIG>;
+    v4i buffer;
+    uint32_t off[4], bytes, bytes_last;
+    uint64_t step;
+    int nk, kleft, wave, lane;
+
+    __device__ __forceinline__ Requests(const Operand &op, int row0, int nk_, int wave_, int lane_) : nk(nk_), wave(wave_), lane(lane_)
+    {
+        const uint32_t pitch = 2u * (uint32_t)op.ld;
+        kleft = op.k - (nk - 1) * STAGE_K;
+        kleft = kleft < STAGE_K ? kleft : STAGE_K;
+        if constexpr (TRANSPOSED) {
+            // a stage is 64 k rows of S::N values, one instruction fills 1024 bytes of them; slot s of row k holds granule s ^ f(k),
+            // f = 4 (k & 3) | 2 ((k >> 2) & 1): the four k rows that a transposing read of 16 lanes takes lie in different banks
+            auto up_to_end = [&](const int k) { return (uint32_t)std::min((uint64_t)k * pitch - 2u * (uint32_t)row0, (uint64_t)0xfffffff0u); };
+            bytes = up_to_end(STAGE_K);
+            bytes_last = up_to_end(kleft);
+            step = (uint64_t)op.ld * (STAGE_K * 2);
+            asm volatile("" : "+s"(step));
+            buffer = buffer_of(op.base + row0, nk > 1 ? bytes : bytes_last);
+            constexpr int GPR = S::N / 8, RPI = 64 / GPR;   // granules of a k row, k rows per instruction
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int k = RPI * (4 * wave + i) + lane / GPR;
+                const int gran = (lane % GPR) ^ (4 * (k & 3) | 2 * ((k >> 2) & 1));
+                off[i] = (uint32_t)k * pitch + 16u * gran;
+            }
+        } else {
+            // one instruction fills 8 rows x 128 bytes: lane l row l / 8, slot l % 8 holding granule slot ^ ((row >> 1) & 7)
+            const int rows = op.rows - row0 < S::N ? op.rows - row0 : S::N;
+            bytes = (uint32_t)(rows - 1) * pitch + 2 * STAGE_K;
+            bytes_last = (uint32_t)(rows - 1) * pitch + 2 * kleft;
+            step = 2 * STAGE_K;
+            buffer = buffer_of(op.base + (int64_t)row0 * op.ld, nk > 1 ? bytes : bytes_last);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = 32 * wave + 8 * i + (lane >> 3);
+                off[i] = (uint32_t)row * pitch + 16u * ((lane & 7) ^ ((row >> 1) & 7));
+            }
+        }
+    }
+    // instruction i of stage kt; the fourth moves on to the next stage
+    __device__ __forceinline__ void issue(const int kt, const uint32_t slot, const int i)
+    {
+        lds_dma16_buffer(buffer, off[i], 0, slot + wave * 4096 + i * 1024);
+        if (i < 3) return;
+        const uint64_t base = ((uint64_t)(uint32_t)buffer[1] << 32 | (uint32_t)buffer[0]) + step;
+        buffer[0] = (int)(uint32_t)base;
+        buffer[1] = (int)(uint32_t)(base >> 32);
+        buffer[2] = kt + 2 < nk ? (int)bytes : kt + 2 == nk ? (int)bytes_last : 0;
+    }
+    // k of the last stage past a row's end: the next row was fetched in their place.  A lane overwrites what it asked for itself, behind
+    // its own wait and in front of the barrier that publishes the stage.
+    __device__ __forceinline__ void zero_tail(const uint32_t slot) const
+    {
+        if constexpr (TRANSPOSED) return;
+        typedef __attribute__((address_space(3))) v4i *lds_v4i;
+        asm volatile("" ::: "memory");   // not in front of the wait
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int k = 8 * ((lane & 7) ^ (((32 * wave + 8 * i + (lane >> 3)) >> 1) & 7));
+            if (k >= kleft) *(lds_v4i)(uintptr_t)(slot + wave * 4096 + i * 1024 + 16 * lane) = v4i{0, 0, 0, 0};
+        }
+    }
+};
+
+// The fragments of one operand: W tiles of 32 rows, eight k of a row per lane.
+template <bool BIG, bool TRANSPOSED, int W> struct Fragments {
+    using S = HeadTile<BIG>;
+    typedef __attribute__((address_space(3))) const v8bf *lds_v8bf;
+    typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) v4bf *lds_v4bf;
+    static constexpr int READS = TRANSPOSED ? 2 * W : W, ADDRESSES = TRANSPOSED ? 2 * W : 4;
+    uint32_t at[ADDRESSES];
+    v8bf f[2][W];
+
+    __device__ __forceinline__ Fragments(const uint32_t slot, const int part, const int lane)   // part: of the tile's rows, 32 W each
+    {
+        const int r = lane & 31, c = lane >> 5;
+        if constexpr (TRANSPOSED) {
+            // lane l of a group of 16 supplies the address of k row k0 + (l >> 2), columns 4 (l & 3) .. + 3 and gets four k of column l;
+            // two reads (h = 0, 1) make the eight k of a fragment
+            const int rr = (lane & 15) >> 2;
+#pragma unroll
+            for (int b = 0; b < W; ++b)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int gran = (part * 32 * W + 32 * b) / 8 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+                    at[2 * b + h] = slot + (8 * c + 4 * h + rr) * (2 * S::N) + 16 * (gran ^ (4 * rr | 2 * h)) + 8 * (lane & 1);
+                }
+        } else {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) at[u] = slot + (part * 32 * W + r) * 128 + 16 * ((2 * u + c) ^ ((r >> 1) & 7));
+        }
+    }
+    __device__ __forceinline__ void read(const int u, const int i)   // read i of quarter u
+    {
+        if constexpr (TRANSPOSED) {
+            const v4bf v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_v4bf)(uintptr_t)(at[i] + 16 * u * (2 * S::N)));
+            if (i & 1) f[u & 1][i >> 1].hi = v; else f[u & 1][i >> 1].lo = v;
+        } else {
+            f[u & 1][i] = *(lds_v8bf)(uintptr_t)(at[u] + i * 32 * 128);
+        }
+    }
+    __device__ __forceinline__ void move(const uint32_t by)
+    {
+#pragma unroll
+        for (int i = 0; i < ADDRESSES; ++i) at[i] += by;
+    }
+};
+
+template <bool BIG, bool PT, bool QT>
+__device__ __forceinline__ void tile_product(const Operand &p, const Operand &q, const int n0, const int m0, const int nk, uint8_t *lds,
+                                             v16f (&acc)[HeadTile<BIG>::WP][HeadTile<BIG>::WQ])
+{
+    using S = HeadTile<BIG>;
+    constexpr int WP = S::WP, WQ = S::WQ, SLOTS = WP * WQ;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lds0 = lds_address(lds);
+    Requests<BIG, PT> rp(p, n0, nk, wave, lane);
+    Requests<BIG, QT> rq(q, m0, nk, wave, lane);
+    Fragments<BIG, PT, WP> fp(lds0, wave & 1, lane);
+    Fragments<BIG, QT, WQ> fq(lds0 + S::SLOT, wave >> 1, lane);
+    constexpr int READS = fp.READS + fq.READS;
+#pragma unroll
+    for (int a = 0; a < WP; ++a)
+#pragma unroll
+        for (int b = 0; b < WQ; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
+    auto read_one = [&](const int u, const int i) {
+        if (i < fp.READS) fp.read(u, i);
+        else fq.read(u, i - fp.READS);
+    };
+    auto advance = [](const uint32_t slot) { return slot < 3u * S::SLOT ? slot + 2u * S::SLOT : slot - 3u * S::SLOT; };   // two slots further on
+    // a quarter step: side(s) is issued after instruction s; the source order is the intended issue order
+    auto quarter = [&](const int u, auto &&side) {
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            const int a = s / WQ, b = s % WQ;
+            acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp.f[u & 1][a], fq.f[u & 1][b], acc[a][b], 0, 0, 0);
+            side(s);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto spread = [&](const int s, const int n, auto &&op) {   // operations [0, n) over the slots of a quarter step
+#pragma unroll
+        for (int k = 0; k < n; ++k)
+            if (k * SLOTS / n == s) op(k);
+    };
+    // The ring holds P(0), Q(0), P(1), Q(1), ...  Step kt: quarters 0 to 2 read the fragments of the next quarter; then stage kt + 1 must have
+    // landed and every wavefront holds the last fragments of stage kt, so behind the barrier the last quarter reads the first fragments of stage
+    // kt + 1 and asks for Q(kt + 2) in the slot of P(kt), and the first two quarters of the next step for P(kt + 3) in that of Q(kt).
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (j & 1) rq.issue(j >> 1, lds0 + j * S::SLOT, i);
+            else rp.issue(j >> 1, lds0 + j * S::SLOT, i);
+        }
+    SBN_WAIT_VMCNT(8);
+    if (nk == 1) {
+        if (rp.kleft < STAGE_K) rp.zero_tail(lds0);
+        if (rq.kleft < STAGE_K) rq.zero_tail(lds0 + S::SLOT);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < READS; ++i) read_one(0, i);
+    uint32_t sp = 0, sq = S::SLOT;
+    for (int kt = 0; kt < nk; ++kt) {
+        const uint32_t sp_next = advance(sp), sq_next = advance(sq);
+        const uint32_t free = advance(sp_next);   // of Q(kt - 1)
+#pragma unroll
+        for (int u = 0; u < 3; ++u)
+            quarter(u, [&](const int s) {
+                spread(s, READS, [&](const int k) { read_one(u + 1, k); });
+                if (u < 2) spread(s, 2, [&](const int k) { rp.issue(kt + 2, lds0 + free, 2 * u + k); });
+            });
+        SBN_WAIT_VMCNT(4);   // P(kt + 2) may fly
+        if (kt + 2 == nk) {
+            if (rp.kleft < STAGE_K) rp.zero_tail(lds0 + sp_next);
+            if (rq.kleft < STAGE_K) rq.zero_tail(lds0 + sq_next);
+        }
+        __syncthreads();
+        fp.move(sp_next - sp);
+        fq.move(sq_next - sq);
+        quarter(3, [&](const int s) {
+            spread(s, READS, [&](const int k) { read_one(0, k); });
+            spread(s, 4, [&](const int k) { rq.issue(kt + 2, lds0 + sp, k); });
+        });
+        sp = sp_next;
+        sq = sq_next;
+    }
+    SBN_WAIT_VMCNT(0);   // the surplus stages have landed
+    __syncthreads();
+}
+
+// A wavefront's 32 columns b of its result to its part of LDS in fp32: row r is column m = 32 b + r, granules of 16 bytes (four n)
+// XOR-swizzled with the row.
+template <bool BIG>
+__device__ __forceinline__ void stage_columns(const v16f (&acc)[HeadTile<BIG>::WP][HeadTile<BIG>::WQ], const int b, uint8_t *stg, const int lane)
+{
+    using S = HeadTile<BIG>;
+    const int r = lane & 31, c = lane >> 5;
+    asm volatile("" ::: "memory");   // behind the last columns' reads
+#pragma unroll
+    for (int a = 0; a < S::WP; ++a)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<v4f *>(stg + r * S::ROW + 16 * ((8 * a + 2 * q + c) ^ (r & 15))) =
+                v4f{acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
+    asm volatile("" ::: "memory");   // the reads are of what other lanes have written
+}
+template <bool BIG>
+__device__ __forceinline__ float *staged(uint8_t *stg, const int row, const int n)
+{
+    return reinterpret_cast<float *>(stg + row * HeadTile<BIG>::ROW + 16 * ((n >> 2) ^ (row & 15)) + 4 * (n & 3));
+}
+
+// Tile order.  Blocks go to the eight XCDs round-robin and every XCD has its own L2, so XCD x takes a contiguous eighth of an order in which
+// consecutive tiles form super-tiles of 8 x 8.  False for the blocks that pad the range to a multiple of eight.
+__device__ __forceinline__ bool tile_of_block(const int tiles_n, const int tiles_m, const int bid, int &tn, int &tm)
+{
+    const int nb = tiles_n * tiles_m;
+    const int per = (nb + 7) >> 3;
+    const int id = (bid & 7) * per + (bid >> 3);
+    if ((bid >> 3) >= per || id >= nb) return false;
+    const int band_tiles = 8 * tiles_n;
+    const int nbands = (tiles_m + 7) >> 3;
+    int band = id / band_tiles;
+    band = band < nbands - 1 ? band : nbands - 1;
+    const int h = band == nbands - 1 ? tiles_m - 8 * band : 8;      // tile rows of this band
+    const int rem = id - band * band_tiles;
+    const int ncols = (tiles_n + 7) >> 3;
+    int col = rem / (8 * h);
+    col = col < ncols - 1 ? col : ncols - 1;
+    const int rem2 = rem - col * 8 * h;
+    tn = 8 * col + rem2 / h;
+    tm = 8 * band + rem2 % h;
+    return true;
+}
+
+// ---- logits --------------------------------------------------------------------------------------------------------------------------
+struct LogitsArgs {
+    const uint16_t *H, *W;       // W: the piece's first row
+    int tokens, d, words;        // words: rows of W in the piece
+    int64_t v0, vocab;           // the piece's first word, words of all pieces
+    int tiles_n, tiles_m;
+    const int64_t *targets;      // with HARD
+    // with SOFT: the teacher's entries (see teacher_kernel)
+    const int32_t *at;
+    const float *q;
+    const uint32_t *map;
+    const float *some;
+    int top_k;
+    float tau;
+    // forward
+    float *m, *s1, *s2;          // [parts, tokens]: maximum, sum of exp(z - m), sum of exp((z - m) / tau)
+    float *z_target, *z_top;     // [tokens], [tokens, top_k]
+    // backward
+    const float *lse1, *lse2, *d1, *d2;
+    uint16_t *G;
+    int64_t ldg;
+};
+
+// The teacher's entries among the 32 tokens from m on and the wavefront's words from v on: each(row, word - v, entry).  A wavefront asks one bit
+// per token and 64 words first; lists are read where it is set only.
+template <int WORDS, class Each>
+__device__ __forceinline__ void entries_here(const LogitsArgs &g, const uint32_t hits, const int m, const int64_t v, const int lane, Each &&each)
+{
+    for (uint32_t left = hits; left; left &= left - 1) {
+        const int row = __builtin_ctz(left);
+        const int64_t first = (int64_t)(m + row) * g.top_k;
+        for (int j = lane; j < g.top_k; j += 64) {
+            const int64_t n = g.at[first + j] - v;
+            if (n >= 0 && n < WORDS) each(row, (int)n, first + j);
+        }
+    }
+}
+template <int WORDS>
+__device__ __forceinline__ uint32_t rows_with_entries(const LogitsArgs &g, const int t, const int64_t v)
+{
+    constexpr uint32_t MASK = WORDS == 128 ? 3u : 1u;
+    const uint32_t word = t < g.tokens ? g.map[(v >> 11) * g.tokens + t] : 0u;
+    return (uint32_t)__ballot((word >> ((v >> 6) & 31)) & MASK);   // the lanes of the upper half hold the same tokens
+}
+
+template <bool BIG, bool GRAD, bool HARD, bool SOFT>
+__global__ void __launch_bounds__(64 * HeadTile<BIG>::WAVES) logits_kernel(LogitsArgs g)
+{
+    using S = HeadTile<BIG>;
+    constexpr int WP = S::WP, WQ = S::WQ, WORDS = 32 * WP;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t dlds[];
+    int tn, tm;
+    if (!tile_of_block(g.tiles_n, g.tiles_m, blockIdx.x, tn, tm)) return;
+    v16f acc[WP][WQ];
+    const Operand p{g.W, g.d, g.words, g.d}, q{g.H, g.d, g.tokens, g.d};
+    tile_product<BIG, false, false>(p, q, tn * S::N, tm * S::M, (g.d + STAGE_K - 1) / STAGE_K, dlds, acc);
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 31, c = lane >> 5;
+    const int n0 = tn * S::N + (wave & 1) * WORDS;      // of the piece
+    const int m0 = tm * S::M + (wave >> 1) * 32 * WQ;
+    const int64_t v = g.v0 + n0;
+    uint8_t *const stg = dlds + wave * S::STAGING;
+    const int left = g.words - n0;                      // words that the wavefront has
+    const float k1 = LOG2E, k2 = SOFT ? LOG2E / g.tau : 0.0f;
+#pragma unroll
+    for (int b = 0; b < WQ; ++b) {
+        const int t = m0 + 32 * b + r;
+        const bool inside = t < g.tokens;
+        const int64_t target = HARD && inside ? g.targets[t] : -1;
+        const bool kept = HARD && target >= 0 && target < g.vocab;
+        const int64_t y = kept ? target - v : -1;       // relative to the wavefront's words
+        const bool here = y >= 0 && y < (left < WORDS ? left : WORDS);
+        const uint32_t hits = SOFT ? rows_with_entries<WORDS>(g, t, v) : 0u;
+        if constexpr (!GRAD) {
+            if (HARD && __any(here)) {
+                float z = 0.0f;
+#pragma unroll
+                for (int a = 0; a < WP; ++a)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if ((int)y == 32 * a + 8 * (i >> 2) + 4 * c + (i & 3)) z = acc[a][b][i];
+                if (here && (((int)y >> 2) & 1) == c) g.z_target[t] = z;
+            }
+            if (SOFT && hits) {
+                stage_columns<BIG>(acc, b, stg, lane);
+                entries_here<WORDS>(g, hits, m0 + 32 * b, v, lane, [&](int row, int n, int64_t e) { g.z_top[e] = *staged<BIG>(stg, row, n); });
+            }
+            if (left < WORDS) {
+#pragma unroll
+                for (int a = 0; a < WP; ++a)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (32 * a + 8 * (i >> 2) + 4 * c + (i & 3) >= left) acc[a][b][i] = -INFINITY;
+            }
+            float most = -INFINITY;
+#pragma unroll
+            for (int a = 0; a < WP; ++a)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) most = fmaxf(most, acc[a][b][i]);
+            most = fmaxf(most, __shfl_xor(most, 32));
+            const float base = most == -INFINITY ? 0.0f : most;   // no word here: sums of zeros
+            float sum1 = 0.0f, sum2 = 0.0f;
+#pragma unroll
+            for (int a = 0; a < WP; ++a)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float z = acc[a][b][i] - base;
+                    if (HARD) sum1 += exp2_fast(z * k1);
+                    if (SOFT) sum2 += exp2_fast(z * k2);
+                }
+            if (HARD) sum1 += __shfl_xor(sum1, 32);
+            if (SOFT) sum2 += __shfl_xor(sum2, 32);
+            if (inside && c == 0) {
+                const int64_t at = (int64_t)(2 * tn + (wave & 1)) * g.tokens + t;
+                g.m[at] = most;
+                if (HARD) g.s1[at] = sum1;
+                if (SOFT) g.s2[at] = sum2;
+            }
+        } else {
+            // exp(z - lse) as 2^(z log2 e - lse log2 e); a token without a share has none whatever its lse
+            float c1 = 0.0f, c2 = 0.0f, l1 = INFINITY, l2 = INFINITY;
+            if (kept) {
+                c1 = g.d1[t];
+                if (c1 != 0.0f) l1 = g.lse1[t] * LOG2E;
+            }
+            if (SOFT && inside) {
+                if (g.some[t] != 0.0f) c2 = g.d2[t] * g.tau;
+                if (c2 != 0.0f) l2 = g.lse2[t] * LOG2E;
+            }
+#pragma unroll
+            for (int a = 0; a < WP; ++a)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float z = acc[a][b][i];
+                    float e = 0.0f;
+                    if (HARD) e = c1 * exp2_fast(__builtin_fmaf(z, k1, -l1));
+                    if (SOFT) e = __builtin_fmaf(c2, exp2_fast(__builtin_fmaf(z, k2, -l2)), e);
+                    acc[a][b][i] = e;
+                }
+            if (HARD && __any(here)) {
+                const float less = here ? c1 : 0.0f;
+#pragma unroll
+                for (int a = 0; a < WP; ++a)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if ((int)y == 32 * a + 8 * (i >> 2) + 4 * c + (i & 3)) acc[a][b][i] -= less;
+            }
+            stage_columns<BIG>(acc, b, stg, lane);
+            if (SOFT && hits) {
+                entries_here<WORDS>(g, hits, m0 + 32 * b, v, lane, [&](int row, int n, int64_t e) {
+                    float *const x = staged<BIG>(stg, row, n);
+                    *x = __builtin_fmaf(-(g.d2[m0 + 32 * b + row] * g.tau), g.q[e], *x);   // every word once per token: no two lanes at one place
+                });
+                asm volatile("" ::: "memory");
+            }
+            constexpr int LPR = S::ROW / 32, J = 32 * LPR / 64;   // lanes per row, stores of 32 rows
+            const int n = 8 * (lane % LPR);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const int row = (64 / LPR) * j + lane / LPR, tt = m0 + 32 * b + row;
+                v4f lo = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n)), hi = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n + 4));
+                if (left < WORDS) {   // columns that pad a row of G
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (n + i >= left) lo[i] = 0.0f;
+                        if (n + 4 + i >= left) hi[i] = 0.0f;
+                    }
+                }
+                if (tt < g.tokens && n0 + n < g.ldg)
+                    *reinterpret_cast<uint4 *>(g.G + tt * g.ldg + n0 + n) =
+                        make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]));
+            }
+        }
+    }
+}
+
+// ---- the teacher -----------------------------------------------------------------------------------------------------------------------
+// A wavefront per token: q = softmax(a / tau) over the valid entries (an index of the vocabulary, a logit above -inf).  A word that a list
+// holds more than once counts once, with the sum of its probabilities: at[t, j] is entry j's word where it is the list's first of that word
+// and -1 elsewhere, so that no two entries of a token meet in one place later.  map[w, t]: bit i of word w says that the token has an entry
+// among the words 64 (32 w + i) .. + 63.
+struct TeacherArgs {
+    const int64_t *idx;
+    const void *logits;
+    int tokens, top_k, map_words;
+    int64_t vocab;
+    float tau;
+    int32_t *at;
+    float *q, *some;
+    uint32_t *map;
+};
+
+__device__ __forceinline__ float wave_max(float x)
+{
+#pragma unroll
+    for (int i = 1; i < 64; i *= 2) x = fmaxf(x, __shfl_xor(x, i));
+    return x;
+}
+__device__ __forceinline__ float wave_sum(float x)
+{
+#pragma unroll
+    for (int i = 1; i < 64; i *= 2) x += __shfl_xor(x, i);
+    return x;
+}
+
+template <bool BF16>
+__global__ void __launch_bounds__(256) teacher_kernel(TeacherArgs g)
+{
+    extern __shared__ __attribute__((aligned(16))) uint8_t dlds[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int t = blockIdx.x * 4 + wave;
+    int32_t *const word = reinterpret_cast<int32_t *>(dlds) + wave * (2 * g.top_k + g.map_words);
+    float *const share = reinterpret_cast<float *>(word + g.top_k);
+    uint32_t *const map = reinterpret_cast<uint32_t *>(share + g.top_k);
+    if (t >= g.tokens) return;   // a wavefront keeps to itself: no barrier below
+    const int64_t first = (int64_t)t * g.top_k;
+    float most = -INFINITY;
+    for (int j = lane; j < g.top_k; j += 64) {
+        const int64_t i = g.idx[first + j];
+        const float a = BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t *>(g.logits)[first + j] << 16) : static_cast<const float *>(g.logits)[first + j];
+        const bool valid = i >= 0 && i < g.vocab && a > -INFINITY;
+        word[j] = valid ? (int32_t)i : -1;
+        share[j] = a;
+        if (valid) most = fmaxf(most, a);
+    }
+    for (int w = lane; w < g.map_words; w += 64) map[w] = 0;
+    most = wave_max(most);
+    float total = 0.0f;
+    for (int j = lane; j < g.top_k; j += 64) {
+        const float e = word[j] >= 0 ? expf((share[j] - most) / g.tau) : 0.0f;
+        share[j] = e;
+        total += e;
+    }
+    total = wave_sum(total);
+    const bool some = most > -INFINITY;
+    asm volatile("" ::: "memory");   // LDS operations of a wavefront are done in order
+    for (int j = lane; j < g.top_k; j += 64) {
+        const int32_t w = word[j];
+        float e = share[j];
+        bool again = false;
+        if (w >= 0) {
+            for (int i = 0; i < j; ++i) again |= word[i] == w;
+            for (int i = j + 1; i < g.top_k; ++i)
+                if (word[i] == w) e += share[i];
+            if (!again) atomicOr(&map[w >> 11], 1u << ((w >> 6) & 31));
+        }
+        g.at[first + j] = again ? -1 : w;
+        g.q[first + j] = some ? e / total : 0.0f;
+    }
+    asm volatile("" ::: "memory");
+    for (int w = lane; w < g.map_words; w += 64) g.map[(int64_t)w * g.tokens + t] = map[w];
+    if (lane == 0) g.some[t] = some ? 1.0f : 0.0f;
+}
+
+// ---- losses from the parts of their sums ---------------------------------------------------------------------------------------------------
+struct JoinArgs {
+    const float *m, *s1, *s2;
+    int parts, tokens, top_k, across;   // across: tokens of a block, a power of two
+    int64_t vocab;
+    const int64_t *targets;
+    const float *z_target, *z_top, *q, *some;
+    const int32_t *at;
+    float tau;
+    float *ce, *kd, *lse1, *lse2;
+};
+
+template <bool HARD, bool SOFT>
+__global__ void __launch_bounds__(256) join_kernel(JoinArgs g)
+{
+    __shared__ float part[3][256];
+    const int slices = 256 / g.across, slice = threadIdx.x / g.across;
+    const int t = blockIdx.x * g.across + threadIdx.x % g.across;
+    const bool inside = t < g.tokens;
+    const float k2 = SOFT ? LOG2E / g.tau : 0.0f;
+    float m = -INFINITY, s1 = 0.0f, s2 = 0.0f;
+    auto add = [&](const float om, const float o1, const float o2) {
+        const float to = fmaxf(m, om);
+        if (to == -INFINITY) return;
+        const float mine = m - to, its = om - to;
+        if (HARD) s1 = s1 * exp2_fast(mine * LOG2E) + o1 * exp2_fast(its * LOG2E);
+        if (SOFT) s2 = s2 * exp2_fast(mine * k2) + o2 * exp2_fast(its * k2);
+        m = to;
+    };
+    if (inside)
+        for (int p = slice; p < g.parts; p += slices) {
+            const int64_t at = (int64_t)p * g.tokens + t;
+            add(g.m[at], HARD ? g.s1[at] : 0.0f, SOFT ? g.s2[at] : 0.0f);
+        }
+    for (int half = slices / 2; half; half /= 2) {
+        part[0][threadIdx.x] = m;
+        part[1][threadIdx.x] = s1;
+        part[2][threadIdx.x] = s2;
+        __syncthreads();
+        const int other = threadIdx.x + half * g.across;
+        if (slice < half) add(part[0][other], part[1][other], part[2][other]);
+        __syncthreads();
+    }
+    if (slice == 0) {
+        const float lse1 = m + logf(s1), lse2 = SOFT ? m / g.tau + logf(s2) : 0.0f;
+        if (inside && HARD) {
+            const int64_t y = g.targets[t];
+            g.lse1[t] = lse1;
+            g.ce[t] = y >= 0 && y < g.vocab ? lse1 - g.z_target[t] : 0.0f;
+        }
+        if (inside && SOFT) g.lse2[t] = lse2;
+        part[0][threadIdx.x] = lse2;
+    }
+    if constexpr (SOFT) {
+        __syncthreads();
+        const float lse2 = part[0][threadIdx.x % g.across];
+        float sum = 0.0f;
+        if (inside)
+            for (int j = slice; j < g.top_k; j += slices) {
+                const int64_t e = (int64_t)t * g.top_k + j;
+                const float q = g.q[e];
+                if (g.at[e] >= 0 && q > 0.0f) sum += q * (logf(q) - g.z_top[e] / g.tau + lse2);
+            }
+        for (int half = slices / 2; half; half /= 2) {
+            part[1][threadIdx.x] = sum;
+            __syncthreads();
+            if (slice < half) sum += part[1][threadIdx.x + half * g.across];
+            __syncthreads();
+        }
+        if (inside && slice == 0) g.kd[t] = g.some[t] != 0.0f ? g.tau * g.tau * sum : 0.0f;
+    }
+}
+
+// ---- gradients -------------------------------------------------------------------------------------------------------------------------
+// The two products of a piece in one launch, the longer contraction first.  The contraction of either may be cut into splits that leave
+// their sums in fp32 side by side; dH adds up over the pieces of the vocabulary in fp32 as well.
+struct GradientArgs {
+    Operand P, Q;              // P transposed; Q transposed (dW) or not (dH)
+    int q_transposed;
+    int N, M, stages;          // of the result; k stages of the whole contraction
+    int splits, per;           // stages of a split
+    uint16_t *C;               // bf16 [M, N], or null:
+    float *part;               // fp32 [splits, M, N]
+    int add;                   // to what part holds
+    int tiles_n, tiles_m, padded;
+};
+struct GradientPair {
+    GradientArgs g[2];
+    int block0[3];
+};
+
+template <bool BIG>
+__device__ __forceinline__ void gradient_epilogue(const GradientArgs &g, const v16f (&acc)[HeadTile<BIG>::WP][HeadTile<BIG>::WQ], uint8_t *lds, const int n0,
+                                                  const int m0, const int split)
+{
+    using S = HeadTile<BIG>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint8_t *const stg = lds + wave * S::STAGING;
+    const int nw = n0 + (wave & 1) * 32 * S::WP, mw = m0 + (wave >> 1) * 32 * S::WQ;
+#pragma unroll
+    for (int b = 0; b < S::WQ; ++b) {
+        stage_columns<BIG>(acc, b, stg, lane);
+        if (g.C) {
+            constexpr int LPR = S::ROW / 32, J = 32 * LPR / 64;
+            const int n = 8 * (lane % LPR);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const int row = (64 / LPR) * j + lane / LPR, m = mw + 32 * b + row;
+                const v4f lo = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n)), hi = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n + 4));
+                if (m < g.M && nw + n < g.N)
+                    *reinterpret_cast<uint4 *>(g.C + (int64_t)m * g.N + nw + n) =
+                        make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]));
+            }
+        } else {
+            constexpr int LPR = S::ROW / 16, J = 32 * LPR / 64;
+            const int n = 4 * (lane % LPR);
+            float *const part = g.part + (int64_t)split * g.M * g.N;
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const int row = (64 / LPR) * j + lane / LPR, m = mw + 32 * b + row;
+                v4f x = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n));
+                if (m < g.M && nw + n < g.N) {
+                    v4f *const to = reinterpret_cast<v4f *>(part + (int64_t)m * g.N + nw + n);
+                    if (g.add) x += *to;
+                    *to = x;
+                }
+            }
+        }
+    }
+}
+
+template <bool BIG>
+__global__ void __launch_bounds__(64 * HeadTile<BIG>::WAVES) gradient_kernel(GradientPair pair)
+{
+    using S = HeadTile<BIG>;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t dlds[];
+    const int which = (int)blockIdx.x >= pair.block0[1];
+    const GradientArgs &g = pair.g[which];
+    const int bid = (int)blockIdx.x - pair.block0[which];
+    const int split = bid / g.padded;
+    int tn, tm;
+    if (!tile_of_block(g.tiles_n, g.tiles_m, bid - split * g.padded, tn, tm)) return;
+    const int s0 = split * g.per, nk = g.stages - s0 < g.per ? g.stages - s0 : g.per;
+    if (nk <= 0) return;   // of a last piece that has fewer stages: nothing to add
+    Operand p = g.P, q = g.Q;
+    p.base += (int64_t)s0 * STAGE_K * p.ld;
+    p.k -= s0 * STAGE_K;
+    q.base += (int64_t)s0 * STAGE_K * (g.q_transposed ? q.ld : 1);
+    q.k -= s0 * STAGE_K;
+    v16f acc[S::WP][S::WQ];
+    if (g.q_transposed) tile_product<BIG, true, true>(p, q, tn * S::N, tm * S::M, nk, dlds, acc);
+    else tile_product<BIG, true, false>(p, q, tn * S::N, tm * S::M, nk, dlds, acc);
+    gradient_epilogue<BIG>(g, acc, dlds, tn * S::N, tm * S::M, split);
+}
+
+// bf16 sums of fp32 parts, in their order
+__global__ void __launch_bounds__(256) sum_parts_kernel(const float *part, int64_t n, int parts, uint16_t *out)
+{
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (i >= n) return;
+    v4f lo = *reinterpret_cast<const v4f *>(part + i), hi = *reinterpret_cast<const v4f *>(part + i + 4);
+    for (int p = 1; p < parts; ++p) {
+        lo += *reinterpret_cast<const v4f *>(part + p * n + i);
+        hi += *reinterpret_cast<const v4f *>(part + p * n + i + 4);
+    }
+    *reinterpret_cast<uint4 *>(out + i) = make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]));
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------------------------
+constexpr int PLAN_CUS = 256;                          // multiprocessors of the part: a plan depends on sizes alone
+constexpr int64_t PIECE_ELEMENTS = (int64_t)1 << 28;   // most of G at a time (512 MB)
+
+// Estimated time in us of `tiles` tiles of `stages` stages with one tile size; see the comment at tile_product
+template <bool BIG>
+float tiles_us(const int64_t tiles, const int64_t stages)
+{
+    const float step = BIG ? 1.45f : 1.05f, alone = BIG ? 1.2f : 0.6f, fixed = BIG ? 10.0f : 7.0f;
+    return std::max((float)stages * alone + fixed, (float)tiles * ((float)stages * step + fixed) / (float)((BIG ? 1 : 2) * PLAN_CUS));
+}
+int64_t tiles_of(const int64_t n, const int64_t m, const bool big) { return ceil_div(n, big ? 256 : 128) * ceil_div(m, big ? 256 : 128); }
+
+bool big_logits(const int64_t tokens, const int64_t words, const int64_t d)
+{
+    const int64_t stages = ceil_div(d, STAGE_K);
+    return tiles_us<true>(tiles_of(words, tokens, true), stages) <= tiles_us<false>(tiles_of(words, tokens, false), stages);
+}
+
+struct BackwardPlan {
+    int64_t piece;       // words at a time
+    int64_t ldg;         // row length of G
+    bool big;            // tiles of the gradients' products
+    int dw_splits, dh_splits;
+    // fp32 results that are still to be added up, [parts, rows, d] (0: the product writes bf16)
+    int dw_parts() const { return dw_splits > 1 ? dw_splits : 0; }
+    int dh_parts(int64_t vocab) const { return dh_splits > 1 || piece < vocab ? dh_splits : 0; }
+};
+
+BackwardPlan plan_backward(const int64_t tokens, const int64_t d, const int64_t vocab)
+{
+    BackwardPlan plan;
+    const int64_t most = std::min(std::max(PIECE_ELEMENTS / tokens / 256 * 256, (int64_t)256), (int64_t)1 << 22);
+    const int64_t pieces = ceil_div(vocab, most);
+    plan.piece = pieces == 1 ? vocab : ceil_div(ceil_div(vocab, pieces), 256) * 256;
+    plan.ldg = ceil_div(plan.piece, STAGE_K) * STAGE_K;
+    // fewest us over tile sizes and splits: what the products take, and what a split's parts are to write and read again at 4 TB/s
+    const int64_t dw_stages = ceil_div(tokens, STAGE_K), dh_stages = plan.ldg / STAGE_K;
+    float best = INFINITY;
+    for (int big = 0; big < 2; ++big)
+        for (int64_t sw = 1; sw <= 16; sw *= 2)
+            for (int64_t sh = 1; sh <= 64; sh *= 2) {
+                if ((sw > 1 && sw * 2 > dw_stages) || (sh > 1 && sh * 2 > dh_stages)) continue;
+                const int64_t wt = tiles_of(d, plan.piece, big) * sw, ht = tiles_of(d, tokens, big) * sh;
+                const int64_t wk = ceil_div(dw_stages, sw), hk = ceil_div(dh_stages, sh);
+                const float w = big ? tiles_us<true>(wt, wk) : tiles_us<false>(wt, wk), h = big ? tiles_us<true>(ht, hk) : tiles_us<false>(ht, hk);
+                const float alone = big ? 1.2f : 0.6f, fixed = big ? 10.0f : 7.0f, step = big ? 1.45f : 1.05f;
+                float us = std::max(std::max((float)wk, (float)hk) * alone + fixed,
+                                    ((float)wt * ((float)wk * step + fixed) + (float)ht * ((float)hk * step + fixed)) / (float)((big ? 1 : 2) * PLAN_CUS));
+                us = std::max(us, std::max(w, h));
+                if (sw > 1) us += 3.0f + (float)(8 * sw + 2) * (float)plan.piece * (float)d / 4e6f;
+                if (sh > 1) us += 3.0f + (float)(8 * sh + 2) * (float)tokens * (float)d / 4e6f;
+                if (us < best) {
+                    best = us;
+                    plan.big = big;
+                    plan.dw_splits = (int)sw;
+                    plan.dh_splits = (int)sh;
+                }
+            }
+    // no split without a stage
+    plan.dw_splits = (int)ceil_div(dw_stages, ceil_div(dw_stages, plan.dw_splits));
+    plan.dh_splits = (int)ceil_div(dh_stages, ceil_div(dh_stages, plan.dh_splits));
+    return plan;
+}
+
+// Workspace, one region after the other
+struct HeadRegions {
+    size_t bytes = 0;
+    size_t take(const size_t n)
+    {
+        const size_t at = bytes;
+        bytes += align_up(n, 256);
+        return at;
+    }
+};
+struct TeacherRegions {
+    size_t at, q, map, some;
+    TeacherRegions(HeadRegions &r, int64_t tokens, int64_t vocab, int64_t top_k)
+    {
+        at = r.take((size_t)tokens * top_k * 4);
+        q = r.take((size_t)tokens * top_k * 4);
+        map = r.take((size_t)ceil_div(vocab, 2048) * tokens * 4);
+        some = r.take((size_t)tokens * 4);
+    }
+};
+
+template <class Kernel>
+sbn_status with_lds(Kernel kernel, const int bytes)
+{
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess) return SBN_OK;
+    set_hip_error(e, "hipFuncSetAttribute");
+    return SBN_EHIP;
+}
+
+template <bool BIG, bool GRAD, bool HARD, bool SOFT>
+sbn_status launch_logits_as(LogitsArgs &g, hipStream_t stream)
+{
+    using S = HeadTile<BIG>;
+    g.tiles_n = (int)ceil_div(g.words, S::N);
+    g.tiles_m = (int)ceil_div(g.tokens, S::M);
+    static thread_local bool raised = false;
+    if (!raised) {
+        const sbn_status st = with_lds(&logits_kernel<BIG, GRAD, HARD, SOFT>, S::LDS);
+        if (st != SBN_OK) return st;
+        raised = true;
+    }
+    const int64_t blocks = ceil_div((int64_t)g.tiles_n * g.tiles_m, 8) * 8;
+    hipLaunchKernelGGL((logits_kernel<BIG, GRAD, HARD, SOFT>), dim3((unsigned)blocks), dim3(64 * S::WAVES), S::LDS, stream, g);
+    return check_launch("logits_kernel");
+}
+template <bool GRAD>
+sbn_status launch_logits(LogitsArgs &g, bool big, bool hard, bool soft, hipStream_t stream)
+{
+    if (big)
+        return !soft ? launch_logits_as<true, GRAD, true, false>(g, stream) : hard ? launch_logits_as<true, GRAD, true, true>(g, stream)
+                                                                                   : launch_logits_as<true, GRAD, false, true>(g, stream);
+    return !soft ? launch_logits_as<false, GRAD, true, false>(g, stream) : hard ? launch_logits_as<false, GRAD, true, true>(g, stream)
+                                                                                : launch_logits_as<false, GRAD, false, true>(g, stream);
+}
+
+sbn_status launch_teacher(const HeadCall &h, uint8_t *ws, const TeacherRegions &r, LogitsArgs &g, hipStream_t stream)
+{
+    g.at = reinterpret_cast<int32_t *>(ws + r.at);
+    g.q = reinterpret_cast<float *>(ws + r.q);
+    g.map = reinterpret_cast<uint32_t *>(ws + r.map);
+    g.some = reinterpret_cast<float *>(ws + r.some);
+    g.top_k = (int)h.top_k;
+    g.tau = h.tau;
+    TeacherArgs t{h.top_idx, h.top_logits, (int)h.tokens, (int)h.top_k, (int)ceil_div(h.vocab, 2048), h.vocab, h.tau,
+                  const_cast<int32_t *>(g.at), const_cast<float *>(g.q), const_cast<float *>(g.some), const_cast<uint32_t *>(g.map)};
+    const unsigned lds = 16u * (2u * t.top_k + t.map_words);
+    if (h.top_dtype == SBN_BF16) hipLaunchKernelGGL(teacher_kernel<true>, dim3((unsigned)ceil_div(h.tokens, 4)), dim3(256), lds, stream, t);
+    else hipLaunchKernelGGL(teacher_kernel<false>, dim3((unsigned)ceil_div(h.tokens, 4)), dim3(256), lds, stream, t);
+    return check_launch("teacher_kernel");
+}
+
+LogitsArgs logits_of(const HeadCall &h)
+{
+    LogitsArgs g{};
+    g.H = static_cast<const uint16_t *>(h.H);
+    g.W = static_cast<const uint16_t *>(h.W);
+    g.tokens = (int)h.tokens;
+    g.d = (int)h.d_in;
+    g.words = (int)h.vocab;
+    g.vocab = h.vocab;
+    g.targets = h.targets;
+    return g;
+}
+
+int64_t forward_parts(const HeadCall &h) { return 2 * ceil_div(h.vocab, big_logits(h.tokens, h.vocab, h.d_in) ? 256 : 128); }
+
+}  // namespace
+
+size_t head_workspace_bytes(int64_t tokens, int64_t d_in, int64_t vocab, int64_t top_k, bool backward)
+{
+    HeadCall h{};
+    h.tokens = tokens;
+    h.d_in = d_in;
+    h.vocab = vocab;
+    HeadRegions r;
+    const int64_t parts = forward_parts(h);
+    for (int i = 0; i < (top_k ? 3 : 2); ++i) r.take((size_t)parts * tokens * 4);
+    r.take((size_t)tokens * 4);
+    r.take((size_t)tokens * top_k * 4);
+    if (top_k) TeacherRegions(r, tokens, vocab, top_k);
+    if (!backward) return r.bytes;
+    HeadRegions b;
+    const BackwardPlan plan = plan_backward(tokens, d_in, vocab);
+    if (top_k) TeacherRegions(b, tokens, vocab, top_k);
+    b.take((size_t)tokens * plan.ldg * 2);
+    b.take((size_t)plan.dh_parts(vocab) * tokens * d_in * 4);
+    b.take((size_t)plan.dw_parts() * plan.piece * d_in * 4);
+    return std::max(r.bytes, b.bytes);
+}
+
+sbn_status launch_head_forward(const HeadCall &h, void *workspace, hipStream_t stream)
+{
+    const bool hard = h.targets != nullptr, soft = h.top_idx != nullptr;
+    uint8_t *const ws = static_cast<uint8_t *>(workspace);
+    HeadRegions r;
+    LogitsArgs g = logits_of(h);
+    const bool big = big_logits(h.tokens, h.vocab, h.d_in);
+    const int64_t parts = forward_parts(h);
+    auto floats = [&](const size_t n) { return reinterpret_cast<float *>(ws + r.take(n * 4)); };
+    g.m = floats((size_t)parts * h.tokens);
+    g.s1 = floats((size_t)parts * h.tokens);
+    g.s2 = soft ? floats((size_t)parts * h.tokens) : nullptr;
+    g.z_target = floats((size_t)h.tokens);
+    g.z_top = floats((size_t)h.tokens * h.top_k);
+    if (soft) {
+        const TeacherRegions tr(r, h.tokens, h.vocab, h.top_k);
+        const sbn_status st = launch_teacher(h, ws, tr, g, stream);
+        if (st != SBN_OK) return st;
+    }
+    const sbn_status st = launch_logits<false>(g, big, hard, soft, stream);
+    if (st != SBN_OK) return st;
+    JoinArgs j{g.m, g.s1, g.s2, (int)parts, (int)h.tokens, (int)h.top_k, 1, h.vocab, h.targets, g.z_target, g.z_top, g.q, g.some, g.at, h.tau,
+               h.ce, h.kd, h.lse1, h.lse2};
+    while (j.across < 32 && h.tokens / (2 * j.across) >= PLAN_CUS) j.across *= 2;
+    const dim3 grid((unsigned)ceil_div(h.tokens, j.across)), block(256);
+    if (!soft) hipLaunchKernelGGL((join_kernel<true, false>), grid, block, 0, stream, j);
+    else if (hard) hipLaunchKernelGGL((join_kernel<true, true>), grid, block, 0, stream, j);
+    else hipLaunchKernelGGL((join_kernel<false, true>), grid, block, 0, stream, j);
+    return check_launch("join_kernel");
+}
+
+template <bool BIG>
+static sbn_status launch_gradients(GradientPair &pair, hipStream_t stream)
+{
+    using S = HeadTile<BIG>;
+    if (pair.g[1].per > pair.g[0].per) std::swap(pair.g[0], pair.g[1]);
+    int64_t blocks = 0;
+    for (int i = 0; i < 2; ++i) {
+        GradientArgs &g = pair.g[i];
+        g.tiles_n = (int)ceil_div(g.N, S::N);
+        g.tiles_m = (int)ceil_div(g.M, S::M);
+        g.padded = (int)(ceil_div((int64_t)g.tiles_n * g.tiles_m, 8) * 8);
+        pair.block0[i] = (int)blocks;
+        blocks += g.N ? (int64_t)g.padded * g.splits : 0;
+    }
+    pair.block0[2] = (int)blocks;
+    static thread_local bool raised = false;
+    if (!raised) {
+        const sbn_status st = with_lds(&gradient_kernel<BIG>, S::LDS);
+        if (st != SBN_OK) return st;
+        raised = true;
+    }
+    hipLaunchKernelGGL(gradient_kernel<BIG>, dim3((unsigned)blocks), dim3(64 * S::WAVES), S::LDS, stream, pair);
+    return check_launch("gradient_kernel");
+}
+
+sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t stream)
+{
+    const bool hard = h.targets != nullptr, soft = h.top_idx != nullptr;
+    uint8_t *const ws = static_cast<uint8_t *>(workspace);
+    const BackwardPlan plan = plan_backward(h.tokens, h.d_in, h.vocab);
+    HeadRegions r;
+    LogitsArgs g = logits_of(h);
+    sbn_status st;
+    if (soft) {
+        const TeacherRegions tr(r, h.tokens, h.vocab, h.top_k);
+        st = launch_teacher(h, ws, tr, g, stream);
+        if (st != SBN_OK) return st;
+    }
+    g.lse1 = h.lse1;
+    g.lse2 = h.lse2;
+    g.d1 = h.d_ce;
+    g.d2 = h.d_kd;
+    g.G = reinterpret_cast<uint16_t *>(ws + r.take((size_t)h.tokens * plan.ldg * 2));
+    const int dh_parts = plan.dh_parts(h.vocab), dw_parts = plan.dw_parts();
+    float *const dh_part = reinterpret_cast<float *>(ws + r.take((size_t)dh_parts * h.tokens * h.d_in * 4));
+    float *const dw_part = reinterpret_cast<float *>(ws + r.take((size_t)dw_parts * plan.piece * h.d_in * 4));
+    const int d = (int)h.d_in, tokens = (int)h.tokens;
+    auto sum = [&](const float *part, int64_t n, int parts, uint16_t *out) {
+        hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)ceil_div(n, 2048)), dim3(256), 0, stream, part, n, parts, out);
+        return check_launch("sum_parts_kernel");
+    };
+    for (int64_t v0 = 0; v0 < h.vocab; v0 += plan.piece) {
+        const int words = (int)std::min(plan.piece, h.vocab - v0);
+        g.W = static_cast<const uint16_t *>(h.W) + v0 * d;
+        g.v0 = v0;
+        g.words = words;
+        g.ldg = ceil_div(words, STAGE_K) * STAGE_K;
+        st = launch_logits<true>(g, big_logits(h.tokens, words, h.d_in), hard, soft, stream);
+        if (st != SBN_OK) return st;
+        GradientPair pair{};
+        if (h.dW) {
+            GradientArgs &a = pair.g[0];
+            a.P = Operand{g.H, d, d, tokens};
+            a.Q = Operand{g.G, g.ldg, words, tokens};
+            a.q_transposed = 1;
+            a.N = d;
+            a.M = words;
+            a.stages = (int)ceil_div(tokens, STAGE_K);
+            a.splits = plan.dw_splits;
+            a.C = dw_parts ? nullptr : static_cast<uint16_t *>(h.dW) + v0 * d;
+            a.part = dw_part;
+        }
+        if (h.dH) {
+            GradientArgs &a = pair.g[1];
+            a.P = Operand{g.W, d, d, words};
+            a.Q = Operand{g.G, g.ldg, tokens, (int)g.ldg};
+            a.N = d;
+            a.M = tokens;
+            a.stages = (int)(g.ldg / STAGE_K);
+            a.splits = plan.dh_splits;
+            a.C = dh_parts ? nullptr : static_cast<uint16_t *>(h.dH);
+            a.part = dh_part;
+            a.add = v0 > 0;
+        }
+        for (GradientArgs &a : pair.g) {
+            if (!a.N) continue;
+            a.per = (int)ceil_div(a.stages, a.splits);
+        }
+        st = plan.big ? launch_gradients<true>(pair, stream) : launch_gradients<false>(pair, stream);
+        if (st != SBN_OK) return st;
+        if (h.dW && dw_parts) {
+            st = sum(dw_part, (int64_t)words * d, dw_parts, static_cast<uint16_t *>(h.dW) + v0 * d);
+            if (st != SBN_OK) return st;
+        }
+    }
+    return h.dH && dh_parts ? sum(dh_part, h.tokens * h.d_in, dh_parts, static_cast<uint16_t *>(h.dH)) : SBN_OK;
+}
+
+}  // namespace sbn

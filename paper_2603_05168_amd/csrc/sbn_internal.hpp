@@ -162,4 +162,33 @@ sbn_status launch_backward(const void *dY, int64_t tokens, int64_t d_in, int64_t
                            const int8_t *xq, const float *sx, void *dX, void *dW, int flags,
                            void *workspace, size_t ws_bytes, hipStream_t stream);
 
+// ---- output head (sbn_head.hip) ------------------------------------------------------------------
+struct HeadCall {
+    const void *H, *W;
+    int64_t tokens, d_in, vocab;
+    const int64_t *targets;    // null: no cross entropy
+    const int64_t *top_idx;    // null: no teacher
+    const void *top_logits;
+    sbn_dtype top_dtype;
+    int64_t top_k;
+    float tau;
+    float *ce, *kd;            // forward
+    float *lse1, *lse2;        // of z and of z / tau: written by the forward, read by the backward
+    const float *d_ce, *d_kd;  // backward
+    void *dH, *dW;
+};
+constexpr int64_t HEAD_MAX_TOKENS = 1 << 24, HEAD_MAX_D = 1 << 16, HEAD_MAX_VOCAB = 1 << 24, HEAD_MAX_TEACHER_VOCAB = 1 << 21, HEAD_MAX_TOP = 1024;
+size_t head_workspace_bytes(int64_t tokens, int64_t d_in, int64_t vocab, int64_t top_k, bool backward);
+sbn_status launch_head_forward(const HeadCall &h, void *workspace, hipStream_t stream);
+sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t stream);
+
+// ---- microscaled 4-bit floating point (sbn_mxfp4.hip) ---------------------------------------------
+constexpr int64_t MXFP4_MAX_COLS = 1 << 20;
+void mxfp4_bytes(int64_t rows, int64_t cols, size_t &codes, size_t &scales);
+size_t mxfp4_workspace_bytes(int64_t tokens, int64_t d_in);
+sbn_status launch_mxfp4_quantize(const void *X, sbn_dtype dtype, int64_t rows, int64_t cols, uint8_t *codes, uint8_t *scales, hipStream_t stream);
+sbn_status launch_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *Y, sbn_dtype dtype, hipStream_t stream);
+sbn_status launch_mxfp4_linear(const void *X, int64_t tokens, int64_t d_in, int64_t d_out, const uint8_t *codes, const uint8_t *scales,
+                               const float *bias, float *Y, void *workspace, hipStream_t stream);
+
 }  // namespace sbn
