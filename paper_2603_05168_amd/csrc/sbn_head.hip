@@ -314,7 +314,7 @@ struct LogitsArgs {
     float *z_target, *z_top;     // [tokens], [tokens, top_k]
     // backward
     const float *lse1, *lse2, *d1, *d2;
-    uint16_t *G;
+    uint16_t *G;                 // [tokens, ldg]
     int64_t ldg;
 };
 
@@ -340,6 +340,29 @@ __device__ __forceinline__ uint32_t rows_with_entries(const LogitsArgs &g, const
     return (uint32_t)__ballot((word >> ((v >> 6) & 31)) & MASK);   // the lanes of the upper half hold the same tokens
 }
 
+// What d_ce has in common: the significand of the first one of the first 64 tokens that counts.  G is divided by it before it is rounded to bf16 and
+// the products' sums are multiplied by it: with one d_ce for all tokens (a mean) -d_ce (1 - p) has the same rounding error in every token,
+// which sums keep (0.0039 of the norm of dH and dW at 16384 tokens, 0.0019 this way), whereas -2^e (1 - p) is exact where p is small.  Any
+// value in [1, 2) is right; ranges do not change.  Read in front of a product, looked at behind it.
+struct CommonFactor {
+    int64_t target = -1;
+    float d = 0.0f;
+    __device__ __forceinline__ CommonFactor(const int64_t *targets, const float *d1, const int tokens)
+    {
+        const int t = threadIdx.x & 63;
+        if (targets && t < tokens) {
+            target = targets[t];
+            d = d1[t];
+        }
+    }
+    __device__ __forceinline__ float value(const int64_t vocab) const
+    {
+        const uint32_t bits = __float_as_uint(d) & 0x7fffffffu;
+        const uint64_t some = __ballot(target >= 0 && target < vocab && bits >= 0x00800000u && bits < 0x7f800000u);
+        return some ? __uint_as_float((__builtin_amdgcn_readlane(bits, __builtin_ctzll(some)) & 0x007fffffu) | 0x3f800000u) : 1.0f;
+    }
+};
+
 template <bool BIG, bool GRAD, bool HARD, bool SOFT>
 __global__ void __launch_bounds__(64 * HeadTile<BIG>::WAVES) logits_kernel(LogitsArgs g)
 {
@@ -348,25 +371,43 @@ __global__ void __launch_bounds__(64 * HeadTile<BIG>::WAVES) logits_kernel(Logit
     extern __shared__ __attribute__((aligned(1024))) uint8_t dlds[];
     int tn, tm;
     if (!tile_of_block(g.tiles_n, g.tiles_m, blockIdx.x, tn, tm)) return;
-    v16f acc[WP][WQ];
-    const Operand p{g.W, g.d, g.words, g.d}, q{g.H, g.d, g.tokens, g.d};
-    tile_product<BIG, false, false>(p, q, tn * S::N, tm * S::M, (g.d + STAGE_K - 1) / STAGE_K, dlds, acc);
-
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 31, c = lane >> 5;
     const int n0 = tn * S::N + (wave & 1) * WORDS;      // of the piece
     const int m0 = tm * S::M + (wave >> 1) * 32 * WQ;
     const int64_t v = g.v0 + n0;
+    // what belongs to the lane's tokens is asked for in front of the product
+    int64_t targets[WQ];
+    float d1[WQ], lse1[WQ], d2[WQ], lse2[WQ], some[WQ];
+#pragma unroll
+    for (int b = 0; b < WQ; ++b) {
+        const int t = std::min(m0 + 32 * b + r, g.tokens - 1);
+        if (HARD) targets[b] = g.targets[t];
+        if (HARD && GRAD) {
+            d1[b] = g.d1[t];
+            lse1[b] = g.lse1[t];
+        }
+        if (SOFT && GRAD) {
+            d2[b] = g.d2[t];
+            lse2[b] = g.lse2[t];
+            some[b] = g.some[t];
+        }
+    }
+    const CommonFactor common(GRAD && HARD ? g.targets : nullptr, g.d1, g.tokens);
+    v16f acc[WP][WQ];
+    const Operand p{g.W, g.d, g.words, g.d}, q{g.H, g.d, g.tokens, g.d};
+    tile_product<BIG, false, false>(p, q, tn * S::N, tm * S::M, (g.d + STAGE_K - 1) / STAGE_K, dlds, acc);
+
     uint8_t *const stg = dlds + wave * S::STAGING;
     const int left = g.words - n0;                      // words that the wavefront has
     const float k1 = LOG2E, k2 = SOFT ? LOG2E / g.tau : 0.0f;
+    const float inv = GRAD && HARD ? 1.0f / common.value(g.vocab) : 1.0f;
 #pragma unroll
     for (int b = 0; b < WQ; ++b) {
         const int t = m0 + 32 * b + r;
         const bool inside = t < g.tokens;
-        const int64_t target = HARD && inside ? g.targets[t] : -1;
-        const bool kept = HARD && target >= 0 && target < g.vocab;
-        const int64_t y = kept ? target - v : -1;       // relative to the wavefront's words
+        const bool kept = HARD && inside && targets[b] >= 0 && targets[b] < g.vocab;
+        const int64_t y = kept ? targets[b] - v : -1;   // relative to the wavefront's words
         const bool here = y >= 0 && y < (left < WORDS ? left : WORDS);
         const uint32_t hits = SOFT ? rows_with_entries<WORDS>(g, t, v) : 0u;
         if constexpr (!GRAD) {
@@ -417,14 +458,10 @@ __global__ void __launch_bounds__(64 * HeadTile<BIG>::WAVES) logits_kernel(Logit
         } else {
             // exp(z - lse) as 2^(z log2 e - lse log2 e); a token without a share has none whatever its lse
             float c1 = 0.0f, c2 = 0.0f, l1 = INFINITY, l2 = INFINITY;
-            if (kept) {
-                c1 = g.d1[t];
-                if (c1 != 0.0f) l1 = g.lse1[t] * LOG2E;
-            }
-            if (SOFT && inside) {
-                if (g.some[t] != 0.0f) c2 = g.d2[t] * g.tau;
-                if (c2 != 0.0f) l2 = g.lse2[t] * LOG2E;
-            }
+            if (HARD && kept) c1 = d1[b] * inv;
+            if (HARD && c1 != 0.0f) l1 = lse1[b] * LOG2E;
+            if (SOFT && inside && some[b] != 0.0f) c2 = d2[b] * g.tau * inv;
+            if (SOFT && c2 != 0.0f) l2 = lse2[b] * LOG2E;
 #pragma unroll
             for (int a = 0; a < WP; ++a)
 #pragma unroll
@@ -447,7 +484,7 @@ __global__ void __launch_bounds__(64 * HeadTile<BIG>::WAVES) logits_kernel(Logit
             if (SOFT && hits) {
                 entries_here<WORDS>(g, hits, m0 + 32 * b, v, lane, [&](int row, int n, int64_t e) {
                     float *const x = staged<BIG>(stg, row, n);
-                    *x = __builtin_fmaf(-(g.d2[m0 + 32 * b + row] * g.tau), g.q[e], *x);   // every word once per token: no two lanes at one place
+                    *x = __builtin_fmaf(-(g.d2[m0 + 32 * b + row] * g.tau * inv), g.q[e], *x);   // every word once per token: no two lanes at one place
                 });
                 asm volatile("" ::: "memory");
             }
@@ -639,11 +676,15 @@ struct GradientArgs {
 struct GradientPair {
     GradientArgs g[2];
     int block0[3];
+    const int64_t *targets;    // of G's common factor (null: 1)
+    const float *d1;
+    int tokens;
+    int64_t vocab;
 };
 
 template <bool BIG>
 __device__ __forceinline__ void gradient_epilogue(const GradientArgs &g, const v16f (&acc)[HeadTile<BIG>::WP][HeadTile<BIG>::WQ], uint8_t *lds, const int n0,
-                                                  const int m0, const int split)
+                                                  const int m0, const int split, const float factor)
 {
     using S = HeadTile<BIG>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -658,7 +699,7 @@ __device__ __forceinline__ void gradient_epilogue(const GradientArgs &g, const v
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 const int row = (64 / LPR) * j + lane / LPR, m = mw + 32 * b + row;
-                const v4f lo = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n)), hi = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n + 4));
+                const v4f lo = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n)) * factor, hi = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n + 4)) * factor;
                 if (m < g.M && nw + n < g.N)
                     *reinterpret_cast<uint4 *>(g.C + (int64_t)m * g.N + nw + n) =
                         make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]));
@@ -670,7 +711,7 @@ __device__ __forceinline__ void gradient_epilogue(const GradientArgs &g, const v
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 const int row = (64 / LPR) * j + lane / LPR, m = mw + 32 * b + row;
-                v4f x = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n));
+                v4f x = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n)) * factor;
                 if (m < g.M && nw + n < g.N) {
                     v4f *const to = reinterpret_cast<v4f *>(part + (int64_t)m * g.N + nw + n);
                     if (g.add) x += *to;
@@ -699,23 +740,133 @@ __global__ void __launch_bounds__(64 * HeadTile<BIG>::WAVES) gradient_kernel(Gra
     p.k -= s0 * STAGE_K;
     q.base += (int64_t)s0 * STAGE_K * (g.q_transposed ? q.ld : 1);
     q.k -= s0 * STAGE_K;
+    const CommonFactor common(pair.targets, pair.d1, pair.tokens);
     v16f acc[S::WP][S::WQ];
     if (g.q_transposed) tile_product<BIG, true, true>(p, q, tn * S::N, tm * S::M, nk, dlds, acc);
     else tile_product<BIG, true, false>(p, q, tn * S::N, tm * S::M, nk, dlds, acc);
-    gradient_epilogue<BIG>(g, acc, dlds, tn * S::N, tm * S::M, split);
+    gradient_epilogue<BIG>(g, acc, dlds, tn * S::N, tm * S::M, split, common.value(pair.vocab));
 }
 
-// bf16 sums of fp32 parts, in their order
+// bf16 sums of fp32 parts.  A block takes 256 / SLICES groups of four values, a slice of its threads every SLICES-th part: with few values and
+// many parts (37 x 1000 in 32) one thread for all of them took 11 us.
+template <int SLICES>
 __global__ void __launch_bounds__(256) sum_parts_kernel(const float *part, int64_t n, int parts, uint16_t *out)
 {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-    if (i >= n) return;
-    v4f lo = *reinterpret_cast<const v4f *>(part + i), hi = *reinterpret_cast<const v4f *>(part + i + 4);
-    for (int p = 1; p < parts; ++p) {
-        lo += *reinterpret_cast<const v4f *>(part + p * n + i);
-        hi += *reinterpret_cast<const v4f *>(part + p * n + i + 4);
+    constexpr int ACROSS = 256 / SLICES;
+    __shared__ v4f sums[256];
+    const int slice = threadIdx.x / ACROSS;
+    const int64_t i = ((int64_t)blockIdx.x * ACROSS + threadIdx.x % ACROSS) * 4;
+    v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (i < n)
+        for (int p = slice; p < parts; p += SLICES) x += *reinterpret_cast<const v4f *>(part + p * n + i);
+    if constexpr (SLICES > 1) {
+        sums[threadIdx.x] = x;
+        __syncthreads();
+        if (slice) return;
+#pragma unroll
+        for (int s = 1; s < SLICES; ++s) x += sums[threadIdx.x + s * ACROSS];
     }
-    *reinterpret_cast<uint4 *>(out + i) = make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]));
+    if (i < n) *reinterpret_cast<uint2 *>(out + i) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+}
+
+// ---- few tokens ------------------------------------------------------------------------------------------------------------------------
+// Gradients of up to 64 tokens in one launch.  dH reads W: small tiles as above, the words cut into splits.  dW is written and little else: its
+// contraction is the tokens, at most four steps of 16, so a wavefront takes 128 words x 128 columns from registers.  A lane reads four
+// neighbouring columns (words) of eight tokens of H (G) and sorts them into four fragments by byte permutations; column j of a lane's four is
+// a product's column, so a lane's results are neighbours again and rows leave in 256 bytes.
+struct FewGradients {
+    GradientArgs dh;
+    int dh_blocks;
+    const uint16_t *H, *G;
+    int64_t ldg;
+    int tokens, d, words;
+    uint16_t *dW;
+    int across;               // groups of 128 columns
+    const int64_t *targets;
+    const float *d1;
+    int64_t vocab;
+};
+
+// fragment j: column k + j, rows first + 8 c .. + 7 (the last one again past it)
+__device__ __forceinline__ void column_fragments(const uint16_t *base, const int64_t ld, const int first, const int last, const int64_t k, const int c, v8bf (&f)[4])
+{
+    typedef unsigned v4u __attribute__((ext_vector_type(4)));
+    uint2 raw[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) raw[e] = *reinterpret_cast<const uint2 *>(base + (int64_t)std::min(first + 8 * c + e, last) * ld + k);
+    v4u o[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        o[0][p] = __builtin_amdgcn_perm(raw[2 * p + 1].x, raw[2 * p].x, 0x05040100u);
+        o[1][p] = __builtin_amdgcn_perm(raw[2 * p + 1].x, raw[2 * p].x, 0x07060302u);
+        o[2][p] = __builtin_amdgcn_perm(raw[2 * p + 1].y, raw[2 * p].y, 0x05040100u);
+        o[3][p] = __builtin_amdgcn_perm(raw[2 * p + 1].y, raw[2 * p].y, 0x07060302u);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = __builtin_bit_cast(v8bf, o[j]);
+}
+
+template <int STEPS>   // of 16 tokens
+__global__ void __launch_bounds__(256, 2) few_gradient_kernel(FewGradients g)
+{
+    using S = HeadTile<false>;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t dlds[];
+    const CommonFactor common(g.targets, g.d1, g.tokens);
+    if ((int)blockIdx.x < g.dh_blocks) {
+        const int tn = blockIdx.x % g.dh.tiles_n, split = blockIdx.x / g.dh.tiles_n;
+        const int s0 = split * g.dh.per, nk = std::min(g.dh.stages - s0, g.dh.per);
+        Operand p = g.dh.P, q = g.dh.Q;
+        p.base += (int64_t)s0 * STAGE_K * p.ld;
+        p.k -= s0 * STAGE_K;
+        q.base += s0 * STAGE_K;
+        q.k -= s0 * STAGE_K;
+        v16f acc[S::WP][S::WQ];
+        tile_product<false, true, false>(p, q, tn * S::N, 0, nk, dlds, acc);
+        gradient_epilogue<false>(g.dh, acc, dlds, tn * S::N, 0, split, common.value(g.vocab));
+        return;
+    }
+    const int lane = threadIdx.x & 63, r = lane & 31, c = lane >> 5;
+    const int id = (blockIdx.x - g.dh_blocks) * 4 + (threadIdx.x >> 6);
+    const int col = id % g.across * 128 + 4 * r, v0 = id / g.across * 128;
+    if (v0 >= g.words) return;
+    v8bf h[STEPS][4], a[STEPS][4];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        column_fragments(g.G, g.ldg, 16 * s, g.tokens - 1, std::min((int64_t)v0 + 4 * r, g.ldg - 4), c, a[s]);
+        column_fragments(g.H, g.d, 16 * s, g.tokens - 1, std::min(col, g.d - 4), c, h[s]);
+        if (16 * s + 16 > g.tokens) {   // past the last token: zeros
+            typedef unsigned v4u __attribute__((ext_vector_type(4)));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v4u x = __builtin_bit_cast(v4u, a[s][j]);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    const int left = g.tokens - (16 * s + 8 * c + 2 * p);
+                    x[p] = left >= 2 ? x[p] : left == 1 ? x[p] & 0xffffu : 0u;
+                }
+                a[s][j] = __builtin_bit_cast(v8bf, x);
+            }
+        }
+    }
+    const float factor = common.value(g.vocab);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {   // words v0 + 4 row + w
+        v16f acc[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[j][e] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s][w], h[s][j], acc[j], 0, 0, 0);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int v = v0 + 4 * (8 * (e >> 2) + 4 * c + (e & 3)) + w;
+            if (v < g.words && col < g.d)
+                *reinterpret_cast<uint2 *>(g.dW + (int64_t)v * g.d + col) =
+                    make_uint2(pack_bf16(acc[0][e] * factor, acc[1][e] * factor), pack_bf16(acc[2][e] * factor, acc[3][e] * factor));
+        }
+    }
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------------------
@@ -868,6 +1019,25 @@ LogitsArgs logits_of(const HeadCall &h)
     return g;
 }
 
+// Few tokens: splits of the words for dH, as many as give 512 blocks (two per multiprocessor) with eight stages each, and fewer where their
+// sums, [tokens, d] floats written and read again per split, would weigh more than a quarter of W
+constexpr int64_t FEW_TOKENS = 64;
+struct FewPlan {
+    int64_t ldg;
+    int stages, per, splits;   // of dH; splits 1: bf16 at once
+};
+FewPlan plan_few(const int64_t tokens, const int64_t d, const int64_t vocab)
+{
+    FewPlan p;
+    p.stages = (int)ceil_div(vocab, STAGE_K);
+    p.ldg = (int64_t)p.stages * STAGE_K;
+    int64_t splits = std::min(ceil_div(2 * PLAN_CUS, ceil_div(d, 128)), ceil_div(p.stages, 8));
+    splits = std::max((int64_t)1, std::min(splits, vocab / (16 * tokens)));
+    p.per = (int)ceil_div(p.stages, splits);
+    p.splits = (int)ceil_div(p.stages, p.per);
+    return p;
+}
+
 int64_t forward_parts(const HeadCall &h) { return 2 * ceil_div(h.vocab, big_logits(h.tokens, h.vocab, h.d_in) ? 256 : 128); }
 
 }  // namespace
@@ -886,6 +1056,13 @@ size_t head_workspace_bytes(int64_t tokens, int64_t d_in, int64_t vocab, int64_t
     if (top_k) TeacherRegions(r, tokens, vocab, top_k);
     if (!backward) return r.bytes;
     HeadRegions b;
+    if (tokens <= FEW_TOKENS) {
+        const FewPlan plan = plan_few(tokens, d_in, vocab);
+        if (top_k) TeacherRegions(b, tokens, vocab, top_k);
+        b.take((size_t)tokens * plan.ldg * 2);
+        b.take(plan.splits > 1 ? (size_t)plan.splits * tokens * d_in * 4 : 0);
+        return std::max(r.bytes, b.bytes);
+    }
     const BackwardPlan plan = plan_backward(tokens, d_in, vocab);
     if (top_k) TeacherRegions(b, tokens, vocab, top_k);
     b.take((size_t)tokens * plan.ldg * 2);
@@ -950,11 +1127,53 @@ static sbn_status launch_gradients(GradientPair &pair, hipStream_t stream)
     return check_launch("gradient_kernel");
 }
 
+static sbn_status launch_few_gradients(const HeadCall &h, const LogitsArgs &l, const FewPlan &plan, float *part, hipStream_t stream)
+{
+    FewGradients g{};
+    g.H = l.H;
+    g.G = l.G;
+    g.ldg = l.ldg;
+    g.tokens = l.tokens;
+    g.d = l.d;
+    g.words = l.words;
+    g.dW = static_cast<uint16_t *>(h.dW);
+    g.across = (int)ceil_div(h.d_in, 128);
+    g.targets = h.targets;
+    g.d1 = h.d_ce;
+    g.vocab = h.vocab;
+    GradientArgs &a = g.dh;
+    a.P = Operand{l.W, l.d, l.d, l.words};
+    a.Q = Operand{l.G, l.ldg, l.tokens, (int)l.ldg};
+    a.N = l.d;
+    a.M = l.tokens;
+    a.stages = plan.stages;
+    a.per = plan.per;
+    a.C = plan.splits > 1 ? nullptr : static_cast<uint16_t *>(h.dH);
+    a.part = part;
+    a.tiles_n = g.across;
+    g.dh_blocks = h.dH ? g.across * plan.splits : 0;
+    const int64_t blocks = g.dh_blocks + (h.dW ? ceil_div(ceil_div(h.vocab, 128) * g.across, 4) : 0);
+    const int steps = h.tokens <= 16 ? 1 : h.tokens <= 32 ? 2 : 4;
+    static thread_local bool raised = false;
+    constexpr int LDS = HeadTile<false>::LDS;
+    if (!raised) {
+        sbn_status st = with_lds(&few_gradient_kernel<1>, LDS);
+        if (st == SBN_OK) st = with_lds(&few_gradient_kernel<2>, LDS);
+        if (st == SBN_OK) st = with_lds(&few_gradient_kernel<4>, LDS);
+        if (st != SBN_OK) return st;
+        raised = true;
+    }
+    const dim3 grid((unsigned)blocks), block(256);
+    if (steps == 1) hipLaunchKernelGGL(few_gradient_kernel<1>, grid, block, LDS, stream, g);
+    else if (steps == 2) hipLaunchKernelGGL(few_gradient_kernel<2>, grid, block, LDS, stream, g);
+    else hipLaunchKernelGGL(few_gradient_kernel<4>, grid, block, LDS, stream, g);
+    return check_launch("few_gradient_kernel");
+}
+
 sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t stream)
 {
     const bool hard = h.targets != nullptr, soft = h.top_idx != nullptr;
     uint8_t *const ws = static_cast<uint8_t *>(workspace);
-    const BackwardPlan plan = plan_backward(h.tokens, h.d_in, h.vocab);
     HeadRegions r;
     LogitsArgs g = logits_of(h);
     sbn_status st;
@@ -967,15 +1186,26 @@ sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t 
     g.lse2 = h.lse2;
     g.d1 = h.d_ce;
     g.d2 = h.d_kd;
+    auto sum = [&](const float *part, int64_t n, int parts, uint16_t *out) {
+        if (n <= (int64_t)1 << 20 && parts >= 4) hipLaunchKernelGGL(sum_parts_kernel<8>, dim3((unsigned)ceil_div(n, 128)), dim3(256), 0, stream, part, n, parts, out);
+        else hipLaunchKernelGGL(sum_parts_kernel<1>, dim3((unsigned)ceil_div(n, 1024)), dim3(256), 0, stream, part, n, parts, out);
+        return check_launch("sum_parts_kernel");
+    };
+    if (h.tokens <= FEW_TOKENS) {
+        const FewPlan plan = plan_few(h.tokens, h.d_in, h.vocab);
+        g.ldg = plan.ldg;
+        g.G = reinterpret_cast<uint16_t *>(ws + r.take((size_t)h.tokens * plan.ldg * 2));
+        float *const part = reinterpret_cast<float *>(ws + r.bytes);
+        st = launch_logits<true>(g, big_logits(h.tokens, h.vocab, h.d_in), hard, soft, stream);
+        if (st == SBN_OK) st = launch_few_gradients(h, g, plan, part, stream);
+        return st != SBN_OK || !h.dH || plan.splits == 1 ? st : sum(part, h.tokens * h.d_in, plan.splits, static_cast<uint16_t *>(h.dH));
+    }
+    const BackwardPlan plan = plan_backward(h.tokens, h.d_in, h.vocab);
     g.G = reinterpret_cast<uint16_t *>(ws + r.take((size_t)h.tokens * plan.ldg * 2));
     const int dh_parts = plan.dh_parts(h.vocab), dw_parts = plan.dw_parts();
     float *const dh_part = reinterpret_cast<float *>(ws + r.take((size_t)dh_parts * h.tokens * h.d_in * 4));
     float *const dw_part = reinterpret_cast<float *>(ws + r.take((size_t)dw_parts * plan.piece * h.d_in * 4));
     const int d = (int)h.d_in, tokens = (int)h.tokens;
-    auto sum = [&](const float *part, int64_t n, int parts, uint16_t *out) {
-        hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)ceil_div(n, 2048)), dim3(256), 0, stream, part, n, parts, out);
-        return check_launch("sum_parts_kernel");
-    };
     for (int64_t v0 = 0; v0 < h.vocab; v0 += plan.piece) {
         const int words = (int)std::min(plan.piece, h.vocab - v0);
         g.W = static_cast<const uint16_t *>(h.W) + v0 * d;
@@ -985,6 +1215,10 @@ sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t 
         st = launch_logits<true>(g, big_logits(h.tokens, words, h.d_in), hard, soft, stream);
         if (st != SBN_OK) return st;
         GradientPair pair{};
+        pair.targets = h.targets;
+        pair.d1 = h.d_ce;
+        pair.tokens = tokens;
+        pair.vocab = h.vocab;
         if (h.dW) {
             GradientArgs &a = pair.g[0];
             a.P = Operand{g.H, d, d, tokens};

@@ -60,67 +60,105 @@ __device__ __forceinline__ uint32_t quantize8(const float (&x)[8], uint32_t &s)
     return w;
 }
 
-template <bool BF16>
-__global__ void __launch_bounds__(256) mxfp4_quantize_kernel(const void *X, int64_t rows, int cols, int vectors, uint32_t *codes, uint8_t *scales)
+// PER vectors of eight values per lane, 256 apart.  Scales: block by block of a row, or, for the products, [stages of 2^stage_shift columns, rows, blocks
+// of a stage].
+template <bool BF16, int PER>
+__global__ void __launch_bounds__(256) mxfp4_quantize_kernel(const void *X, uint32_t rows, int cols, uint32_t vectors, uint32_t *codes, uint8_t *scales,
+                                                                int stage_shift)
 {
-    // vectors: of eight values in a padded row, a multiple of 16
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows * vectors) return;   // whole blocks of four lanes
-    const int64_t row = i / vectors;
-    const int col = 8 * (int)(i - row * vectors);
-    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (col < cols) load8<BF16>(X, row * cols + col, x);
-    uint32_t s;
-    codes[i] = quantize8(x, s);
-    if ((threadIdx.x & 3) == 0) scales[i >> 2] = (uint8_t)s;
+    // vectors: in a padded row, a multiple of 16; all together fewer than 2^32
+    const uint32_t first = blockIdx.x * 256 * PER + threadIdx.x, all = rows * vectors;
+    float x[PER][8];
+    uint32_t row[PER], col[PER];
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+        const uint32_t i = first + 256 * p;
+        row[p] = i / vectors;
+        col[p] = 8 * (i - row[p] * vectors);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[p][e] = 0.0f;
+        if (i < all && (int)col[p] < cols) load8<BF16>(X, (int64_t)row[p] * cols + col[p], x[p]);
+    }
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+        const uint32_t i = first + 256 * p;
+        if (i >= all) return;   // whole blocks of four lanes
+        uint32_t s;
+        codes[i] = quantize8(x[p], s);
+        if ((threadIdx.x & 3) == 0) {
+            const int in_stage = stage_shift - 5;   // log2 of the blocks of a stage
+            scales[stage_shift ? ((((int64_t)(col[p] >> stage_shift)) * rows + row[p]) << in_stage) + ((col[p] >> 5) & ((1u << in_stage) - 1)) : i >> 2] = (uint8_t)s;
+        }
+    }
 }
 
-template <bool BF16>
-__global__ void __launch_bounds__(256) mxfp4_dequantize_kernel(const uint32_t *codes, const uint8_t *scales, int64_t rows, int cols, int vectors, void *Y)
+template <bool BF16, int PER>
+__global__ void __launch_bounds__(256) mxfp4_dequantize_kernel(const uint32_t *codes, const uint8_t *scales, uint32_t rows, uint32_t cols, uint32_t vectors, void *Y)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int across = cols / 8;
-    if (i >= rows * across) return;
-    const int64_t row = i / across;
-    const int v = (int)(i - row * across);
-    const uint32_t w = codes[row * vectors + v];
-    const float scale = scale_value(scales[(row * vectors + v) >> 2]);
-    typedef float v2f __attribute__((ext_vector_type(2)));
-    const v2f p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1),
-                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3)};
-    const int64_t at = row * cols + 8 * v;
-    if constexpr (BF16) {
-        uint32_t o[4];
+    const uint32_t first = blockIdx.x * 256 * PER + threadIdx.x, across = cols / 8, all = rows * across;
+    uint32_t w[PER], s[PER];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)   // exact: two significant bits, so the high half of the fp32 value
-            o[k] = __builtin_amdgcn_perm(__float_as_uint(p[k][1] * scale), __float_as_uint(p[k][0] * scale), 0x07060302u);
-        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(Y) + at) = make_uint4(o[0], o[1], o[2], o[3]);
-    } else {
-        v4f *const to = reinterpret_cast<v4f *>(static_cast<float *>(Y) + at);
-        to[0] = v4f{p[0][0] * scale, p[0][1] * scale, p[1][0] * scale, p[1][1] * scale};
-        to[1] = v4f{p[2][0] * scale, p[2][1] * scale, p[3][0] * scale, p[3][1] * scale};
+    for (int p = 0; p < PER; ++p) {
+        const uint32_t i = std::min(first + 256 * p, all - 1), row = i / across, at = row * vectors + (i - row * across);
+        w[p] = codes[at];
+        s[p] = scales[at >> 2];
+    }
+    typedef float v2f __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+        const uint32_t i = first + 256 * p;
+        if (i >= all) return;
+        const float scale = scale_value(s[p]);
+        const v2f v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[p], 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[p], 1.0f, 1),
+                          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[p], 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[p], 1.0f, 3)};
+        const int64_t at = 8 * (int64_t)i;
+        if constexpr (BF16) {
+            uint32_t o[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)   // exact: two significant bits, so the high half of the fp32 value
+                o[k] = __builtin_amdgcn_perm(__float_as_uint(v[k][1] * scale), __float_as_uint(v[k][0] * scale), 0x07060302u);
+            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(Y) + at) = make_uint4(o[0], o[1], o[2], o[3]);
+        } else {
+            v4f *const to = reinterpret_cast<v4f *>(static_cast<float *>(Y) + at);
+            to[0] = v4f{v[0][0] * scale, v[0][1] * scale, v[1][0] * scale, v[1][1] * scale};
+            to[1] = v4f{v[2][0] * scale, v[2][1] * scale, v[3][0] * scale, v[3][1] * scale};
+        }
     }
 }
 
 // ---- block tile product -----------------------------------------------------------------------------------------------------------------
-// Y[t, o] = sum_k q(X)[t, k] W[o, k] (+ bias[o]) for block tiles of 256 x 256 (o x t; eight wavefronts of 128 x 64) or 128 x 128 (four of 64 x 64, two
-// blocks per multiprocessor).  Stages of 256 k (128 bytes of a row, and its eight scales) come by LDS-DMA into two buffers; a stage is
-// consumed in quarters of 64 k, quarter u being the blocks u and 4 + u of the stage: a lane's scales of a stage are then one word, whose byte
-// u the instruction picks.
-constexpr int STAGE_BYTES = 128, STAGE_SCALES = 8;
-template <bool BIG> struct MxTile {
-    static constexpr int N = BIG ? 256 : 128, M = N, WAVES = BIG ? 8 : 4;
-    static constexpr int WP = BIG ? 4 : 2, WQ = 2;
-    static constexpr int CODES = N * STAGE_BYTES, SCALES = N * STAGE_SCALES;
-    static constexpr int STAGE = 2 * (CODES + SCALES), LDS = 2 * STAGE;      // P codes, Q codes, P scales, Q scales
-    static constexpr int ROW = WP * 128;                                     // bytes of a staged row of results
-    static_assert(WAVES * 32 * ROW <= LDS, "results are staged in the idle stages");
+// Y[t, o] = sum_k q(X)[t, k] W[o, k] (+ bias[o]) for block tiles of 256 x 256 (o x t; eight wavefronts of 128 x 64), 128 x 128 (four of 64 x 64, two
+// blocks per multiprocessor) and 64 x 64 (four of 32 x 32, four blocks).  Stages of 256 k (128 bytes of a row, a whole line) come by LDS-DMA into
+// two slots; a stage is consumed in quarters of 64 k, quarter u being the blocks u and 4 + u of the stage: a lane's four scales of a stage are
+// one word, and the instruction picks byte u.  Scales of X lie together per stage (the quantizer writes them so); those of W are rows apart,
+// so four stages of them are asked for at once: a request for 4 bytes of a row costs as much as one for its line.
+// An instruction on 4-bit operands has four times the products of one on bf16 in the same time, so its feeding and what surrounds it bound the
+// product: a stage of the large tile takes 1.44 us, 1.17 without its requests and 0.98 its matrix instructions at 2.1 GHz; a tile's first
+// stages, its way through LDS and its stores some 16 us more (4096 x 2560 -> 131072, us per tile: 37.6, 25 without stores, 21 without
+// results; 30.7 with stores past the caches).  Half the stage in three slots for two blocks per multiprocessor was slower
+// (64 bytes of a row are half a line: 81.7 us against 68.2 at 4096 x 2560 -> 6912), and so were requests spread over the stage.
+template <int WP_, int WQ_, int WM, int ROW_BYTES, int SLOTS_, int CHUNK_STAGES_> struct MxTile {
+    static constexpr int WP = WP_, WQ = WQ_, WAVES = 2 * WM;                 // 32 x 32 tiles of a wavefront
+    static constexpr int N = 64 * WP, M = 32 * WM * WQ;
+    static constexpr int BYTES = ROW_BYTES, SCALES = BYTES / 16, SLOTS = SLOTS_, CHUNK_STAGES = CHUNK_STAGES_;   // of a row and stage; of the ring
+    static constexpr int P = N * BYTES, Q = M * BYTES, SQ = M * SCALES, STAGE = P + Q + SQ;   // in this order
+    static constexpr int CHUNK_ROW = SCALES * CHUNK_STAGES, CHUNK = N * CHUNK_ROW;            // scales of W of some stages
+    static constexpr int CHUNKS = SLOTS * STAGE, LDS = CHUNKS + 2 * CHUNK;
+    static constexpr int RPI = 1024 / BYTES, PI = N / (RPI * WAVES), QI = M / (RPI * WAVES);  // requests of a wavefront and stage
+    static constexpr int REQUESTS = PI + QI + 1, CI = CHUNK / (256 * WAVES);                  // with X's scales; of a chunk
+    // results of large tiles, 64 MB and more, leave past the caches: 4096 x 2560 -> 131072 1204 us and 981 so, -> 6912 66.9 and 66.2
+    static constexpr bool PAST_CACHES = WP == 4;
+    static constexpr int OUT = WP * 128;                                     // bytes of a staged row of results
+    static_assert(WAVES * 32 * OUT <= CHUNKS, "results are staged in the idle stages");
 };
+using MxLarge = MxTile<4, 2, 4, 128, 2, 4>;
+using MxMiddle = MxTile<2, 2, 2, 128, 2, 4>;
+using MxSmall = MxTile<1, 1, 2, 128, 2, 4>;
 struct MxArgs {
-    const uint8_t *P, *Q;      // codes of W [N, pitch] and of X [M, pitch]
-    const uint8_t *sp, *sq;    // their scales, [., pitch / 16]
-    int64_t pitch;             // bytes of a row, a multiple of 64
-    int N, M;
+    const uint8_t *P, *Q;      // codes of W [N, pitch] and of X [M, qpitch]
+    const uint8_t *sp, *sq;    // their scales, [N, pitch / 16] and [stages, M, scales of a stage]
+    int64_t pitch, qpitch;     // bytes of a row: a multiple of 64 (W) and of 128 (X)
+    int N, M, stages;
     const float *bias;
     float *Y;                  // [M, N]
     int tiles_n, tiles_m;
@@ -132,11 +170,10 @@ __device__ __forceinline__ void lds_dma4_buffer(const v4i rsrc, uint32_t voff, u
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" : : "s"(lds_addr), "v"(voff), "s"(rsrc), "s"(soff) : "memory", "m0");
 }
 
-template <bool BIG>
-__global__ void __launch_bounds__(64 * MxTile<BIG>::WAVES) mxfp4_tile_kernel(MxArgs g)
+template <class S>
+__global__ void __launch_bounds__(64 * S::WAVES, 2) mxfp4_tile_kernel(MxArgs g)
 {
-    using S = MxTile<BIG>;
-    constexpr int WP = S::WP, WQ = S::WQ, SLOTS = WP * WQ;
+    constexpr int WP = S::WP, WQ = S::WQ, TILES = WP * WQ;
     extern __shared__ __attribute__((aligned(1024))) uint8_t dlds[];
     const int nb = g.tiles_n * g.tiles_m, per = (nb + 7) >> 3;
     const int id = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);   // an XCD takes a contiguous eighth
@@ -146,55 +183,66 @@ __global__ void __launch_bounds__(64 * MxTile<BIG>::WAVES) mxfp4_tile_kernel(MxA
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wn = wave & 1, wm = wave >> 1, r = lane & 31, c = lane >> 5;
     const uint32_t lds0 = lds_address(dlds);
-    const int nk = (int)((g.pitch + STAGE_BYTES - 1) / STAGE_BYTES);
-    const bool half_last = (g.pitch & (STAGE_BYTES - 1)) != 0;             // the last stage is half a stage
+    const int nk = g.stages;
 
-    // rows past the matrix, and what is past its end, read as zeros
-    const uint32_t pitch = (uint32_t)g.pitch, spitch = pitch / 16;
+    // Rows past the matrix read as zeros.  A last stage of W that is half a stage goes on into the next row: X holds zeros there.
+    const uint32_t pitch = (uint32_t)g.pitch, qpitch = (uint32_t)g.qpitch, spitch = pitch / 16;
     const int prows = std::min(S::N, g.N - n0), qrows = std::min(S::M, g.M - m0);
-    const int pbytes = prows * (int)pitch, qbytes = qrows * (int)pitch;
-    v4i pb = buffer_of(g.P + (int64_t)n0 * pitch, pbytes), qb = buffer_of(g.Q + (int64_t)m0 * pitch, qbytes);
-    v4i spb = buffer_of(g.sp + (int64_t)n0 * spitch, pbytes / 16), sqb = buffer_of(g.sq + (int64_t)m0 * spitch, qbytes / 16);
-    uint32_t off[4];   // the same of both operands
+    const int pbytes = prows * (int)pitch, qbytes = qrows * (int)qpitch;
+    v4i pb = buffer_of(g.P + (int64_t)n0 * pitch, pbytes), qb = buffer_of(g.Q + (int64_t)m0 * qpitch, qbytes);
+    const v4i spb = buffer_of(g.sp + (int64_t)n0 * spitch, pbytes / 16);
+    v4i sqb = buffer_of(g.sq + (int64_t)m0 * S::SCALES, 0);
+    const uint64_t sqstep = (uint64_t)g.M * S::SCALES;
+    // Codes: one instruction fills 1 KB, lane l granule l % G of row l / G holding granule (l % G) ^ swizzle: 16 rows of one granule lie in
+    // different banks.
+    constexpr int G = S::BYTES / 16, STEPS = G / 2;
+    auto swizzle = [](const int row) { return G == 8 ? (row >> 1) & 7 : (row >> 2) & 3; };
+    uint32_t poff[S::PI], qoff[S::QI];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = 32 * wave + 8 * i + (lane >> 3);
-        off[i] = (uint32_t)row * pitch + 16u * ((lane & 7) ^ ((row >> 1) & 7));
+    for (int i = 0; i < S::PI; ++i) {
+        const int row = S::RPI * (S::PI * wave + i) + lane / G;
+        poff[i] = (uint32_t)row * pitch + 16u * ((lane % G) ^ swizzle(row));
     }
-    const uint32_t soff = (uint32_t)(32 * wave + (lane >> 1)) * spitch + 4u * (lane & 1);
-    auto request = [&](const int kt, const int i) {   // instruction i < 10 of stage kt; past the last one zeros are deposited
+#pragma unroll
+    for (int i = 0; i < S::QI; ++i) {
+        const int row = S::RPI * (S::QI * wave + i) + lane / G;
+        qoff[i] = (uint32_t)row * qpitch + 16u * ((lane % G) ^ swizzle(row));
+    }
+    // scales of X: 256 bytes of what lies together (by two wavefronts where there are more of them, so that all have as many requests in
+    // flight); of W: rows of CHUNK_ROW bytes
+    constexpr int CL = S::CHUNK_ROW / 4;
+    const int qw = wave % (S::SQ / 256);
+    const uint32_t spoff = (uint32_t)(lane / CL) * spitch + 4u * (lane % CL);
+    auto request = [&](const int kt, const uint32_t slot, const int i) {   // instruction i of stage kt; past the last one zeros are deposited
         if (i == 0) {   // (no branch: the compiler would move the matrix instructions behind it)
             const bool some = kt < nk;
             pb[2] = some ? pbytes : 0;
             qb[2] = some ? qbytes : 0;
-            spb[2] = some ? pbytes / 16 : 0;
-            sqb[2] = some ? qbytes / 16 : 0;
+            const uint64_t base = (uint64_t)(uintptr_t)(g.sq + (int64_t)m0 * S::SCALES) + (uint64_t)kt * sqstep;
+            sqb[0] = (int)(uint32_t)base;
+            sqb[1] = (int)(uint32_t)(base >> 32);
+            sqb[2] = some ? qrows * S::SCALES : 0;
         }
-        const uint32_t at = lds0 + (kt & 1) * S::STAGE, k = (uint32_t)kt * STAGE_BYTES;
-        if (i < 4) lds_dma16_buffer(pb, off[i], k, at + wave * 4096 + i * 1024);
-        else if (i < 8) lds_dma16_buffer(qb, off[i - 4], k, at + S::CODES + wave * 4096 + (i - 4) * 1024);
-        else if (i == 8) lds_dma4_buffer(spb, soff, k / 16, at + 2 * S::CODES + wave * 256);
-        else lds_dma4_buffer(sqb, soff, k / 16, at + 2 * S::CODES + S::SCALES + wave * 256);
+        const uint32_t at = lds0 + slot, k = (uint32_t)kt * S::BYTES;
+        if (i < S::PI) lds_dma16_buffer(pb, poff[i], k, at + (S::PI * wave + i) * 1024);
+        else if (i < S::PI + S::QI) lds_dma16_buffer(qb, qoff[i - S::PI], k, at + S::P + (S::QI * wave + i - S::PI) * 1024);
+        else lds_dma4_buffer(sqb, 256 * qw + 4 * lane, 0, at + S::P + S::Q + 256 * qw);
     };
-    // the second half of a last stage that is half a stage: zeros in place of what the next row begins with
-    auto zero_tail = [&](const uint32_t at) {
-        typedef __attribute__((address_space(3))) v4i *lds_v4i;
-        asm volatile("" ::: "memory");
+    auto request_chunk = [&](const int kt) {   // scales of W of the stages kt .. kt + CHUNK_STAGES - 1
+        const uint32_t at = lds0 + S::CHUNKS + (kt / S::CHUNK_STAGES & 1) * S::CHUNK;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int gran = (lane & 7) ^ (((32 * wave + 8 * i + (lane >> 3)) >> 1) & 7);
-            if (gran >= 4) {
-                *(lds_v4i)(uintptr_t)(lds0 + at + wave * 4096 + i * 1024 + 16 * lane) = v4i{0, 0, 0, 0};
-                *(lds_v4i)(uintptr_t)(lds0 + at + S::CODES + wave * 4096 + i * 1024 + 16 * lane) = v4i{0, 0, 0, 0};
-            }
+        for (int i = 0; i < S::CI; ++i) {
+            const int row = 64 / CL * (S::CI * wave + i);
+            lds_dma4_buffer(spb, spoff, row * spitch + kt * S::SCALES, at + row * S::CHUNK_ROW);
         }
     };
-    // granule 4 c + u of a row in quarter u: u flips bits of the address
-    const uint32_t slot0 = 16 * ((4 * c) ^ ((r >> 1) & 7));
-    const uint32_t pa = lds0 + (wn * 32 * WP + r) * 128 + slot0, qa = lds0 + S::CODES + (wm * 32 * WQ + r) * 128 + slot0;
-    const uint32_t psa = lds0 + 2 * S::CODES + (wn * 32 * WP + r) * 8 + 4 * c, qsa = lds0 + 2 * S::CODES + S::SCALES + (wm * 32 * WQ + r) * 8 + 4 * c;
+    // granule G / 2 c + u of a row in step u: u flips bits of the address
+    const uint32_t slot0 = 16 * ((STEPS * c) ^ swizzle(r));
+    const uint32_t pa = lds0 + (wn * 32 * WP + r) * S::BYTES + slot0, qa = lds0 + S::P + (wm * 32 * WQ + r) * S::BYTES + slot0;
+    const uint32_t psa = lds0 + S::CHUNKS + (wn * 32 * WP + r) * S::CHUNK_ROW + STEPS * c, qsa = lds0 + S::P + S::Q + (wm * 32 * WQ + r) * S::SCALES + STEPS * c;
     typedef __attribute__((address_space(3))) const v4i *lds_v4i;
     typedef __attribute__((address_space(3))) const int *lds_int;
+    typedef __attribute__((address_space(3))) const uint16_t *lds_u16;
 
     v16f acc[WP][WQ];
 #pragma unroll
@@ -204,21 +252,24 @@ __global__ void __launch_bounds__(64 * MxTile<BIG>::WAVES) mxfp4_tile_kernel(MxA
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
     v4i fp[2][WP], fq[2][WQ];
-    int sp[WP], sq[WQ], sp_next[WP], sq_next[WQ];   // scales of a stage
+    int sp[WP], sq[WQ];   // scales of a stage
+    constexpr int READS = WP + WQ;
     auto read_one = [&](const uint32_t at, const int u, const int i) {
-        if (i < WP) fp[u & 1][i] = *(lds_v4i)(uintptr_t)((pa ^ (16 * u)) + at + i * 32 * 128);
-        else fq[u & 1][i - WP] = *(lds_v4i)(uintptr_t)((qa ^ (16 * u)) + at + (i - WP) * 32 * 128);
+        if (i < WP) fp[u & 1][i] = *(lds_v4i)(uintptr_t)((pa ^ (16 * u)) + at + i * 32 * S::BYTES);
+        else fq[u & 1][i - WP] = *(lds_v4i)(uintptr_t)((qa ^ (16 * u)) + at + (i - WP) * 32 * S::BYTES);
     };
-    auto read_scales = [&](const uint32_t at) {
+    auto read_scales = [&](const int kt, const uint32_t at) {
+        const uint32_t chunk = (kt / S::CHUNK_STAGES & 1) * S::CHUNK + (kt % S::CHUNK_STAGES) * S::SCALES;
+        auto of = [](const uint32_t a) { return G == 8 ? *(lds_int)(uintptr_t)a : (int)*(lds_u16)(uintptr_t)a; };
 #pragma unroll
-        for (int a = 0; a < WP; ++a) sp_next[a] = *(lds_int)(uintptr_t)(psa + at + a * 32 * 8);
+        for (int a = 0; a < WP; ++a) sp[a] = of(psa + chunk + a * 32 * S::CHUNK_ROW);
 #pragma unroll
-        for (int b = 0; b < WQ; ++b) sq_next[b] = *(lds_int)(uintptr_t)(qsa + at + b * 32 * 8);
+        for (int b = 0; b < WQ; ++b) sq[b] = of(qsa + at + b * 32 * S::SCALES);
     };
     auto wide = [](const v4i x) { return v8i{x[0], x[1], x[2], x[3], 0, 0, 0, 0}; };   // 4-bit operands are four registers
-    auto quarter = [&](const int u, auto &&side) {
+    auto part = [&](const int u, auto &&side) {
 #pragma unroll
-        for (int s = 0; s < SLOTS; ++s) {
+        for (int s = 0; s < TILES; ++s) {
             const int a = s / WQ, b = s % WQ;
             const v8i x = wide(fp[u & 1][a]), y = wide(fq[u & 1][b]);
             if (u == 0) acc[a][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc[a][b], 4, 4, 0, sp[a], 0, sq[b]);
@@ -229,46 +280,39 @@ __global__ void __launch_bounds__(64 * MxTile<BIG>::WAVES) mxfp4_tile_kernel(MxA
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    constexpr int READS = WP + WQ;
     auto spread = [&](const int s, const int n, auto &&op) {
 #pragma unroll
         for (int k = 0; k < n; ++k)
-            if (k * SLOTS / n == s) op(k);
+            if (k * TILES / n == s) op(k);
     };
-    // Step kt: quarters 0 to 2 read the fragments of the next quarter; then stage kt + 1 must have landed and every wavefront holds the last
-    // fragments of stage kt, so behind the barrier the last quarter reads the first fragments of stage kt + 1 and stage kt + 2 is asked for.
-    auto take_scales = [&] {
+    // Stage kt: all parts but the last read the fragments of the next part; then stage kt + 1 must have landed and every wavefront holds the
+    // last fragments of stage kt, so behind the barrier the last part reads the first fragments of stage kt + 1 and asks for stage kt + SLOTS
+    // in the slot of stage kt.
 #pragma unroll
-        for (int a = 0; a < WP; ++a) sp[a] = sp_next[a];
+    for (int st = 0; st < S::SLOTS; ++st) {
+        if (st % S::CHUNK_STAGES == 0) request_chunk(st);
 #pragma unroll
-        for (int b = 0; b < WQ; ++b) sq[b] = sq_next[b];
-    };
-#pragma unroll
-    for (int i = 0; i < 10; ++i) request(0, i);
-#pragma unroll
-    for (int i = 0; i < 10; ++i) request(1, i);
-    SBN_WAIT_VMCNT(10);
-    if (half_last && nk == 1) zero_tail(0);
+        for (int i = 0; i < S::REQUESTS; ++i) request(st, st * S::STAGE, i);
+    }
+    SBN_WAIT_VMCNT((S::SLOTS - 1) * S::REQUESTS);
     __syncthreads();
-    read_scales(0);
-    take_scales();
+    read_scales(0, 0);
 #pragma unroll
     for (int i = 0; i < READS; ++i) read_one(0, 0, i);
     uint32_t at = 0;
     for (int kt = 0; kt < nk; ++kt) {
-        const uint32_t next = S::STAGE - at;
+        const uint32_t next = at == (S::SLOTS - 1) * S::STAGE ? 0 : at + S::STAGE;
 #pragma unroll
-        for (int u = 0; u < 3; ++u)
-            quarter(u, [&](const int s) { spread(s, READS, [&](const int k) { read_one(at, u + 1, k); }); });
-        SBN_WAIT_VMCNT(0);
-        if (half_last && kt + 2 == nk) zero_tail(next);
+        for (int u = 0; u + 1 < STEPS; ++u)
+            part(u, [&](const int s) { spread(s, READS, [&](const int k) { read_one(at, u + 1, k); }); });
+        SBN_WAIT_VMCNT((S::SLOTS - 2) * S::REQUESTS);
         __syncthreads();
-        quarter(3, [&](const int s) {
-            if (s == 0) read_scales(next);
+        if ((kt + S::SLOTS) % S::CHUNK_STAGES == 0) request_chunk(kt + S::SLOTS);   // (past the last row's end: zeros)
+        part(STEPS - 1, [&](const int s) {
             spread(s, READS, [&](const int k) { read_one(next, 0, k); });
-            spread(s, 10, [&](const int k) { request(kt + 2, k); });
+            spread(s, S::REQUESTS, [&](const int k) { request(kt + S::SLOTS, at, k); });
+            if (s == TILES - 1) read_scales(kt + 1, next);   // behind their last use
         });
-        take_scales();
         at = next;
     }
     SBN_WAIT_VMCNT(0);   // the surplus stages have landed
@@ -277,8 +321,8 @@ __global__ void __launch_bounds__(64 * MxTile<BIG>::WAVES) mxfp4_tile_kernel(MxA
     // Result: 32 tokens at a time through the idle stages (granules of 16 bytes XOR-swizzled with the row), so that whole rows of the
     // wavefront's outputs leave
     typedef float v4f_u __attribute__((ext_vector_type(4), aligned(4)));
-    uint8_t *const stg = dlds + wave * 32 * S::ROW;
-    constexpr int LPR = S::ROW / 16, J = 32 * LPR / 64;
+    uint8_t *const stg = dlds + wave * 32 * S::OUT;
+    constexpr int LPR = S::OUT / 16, J = 32 * LPR / 64, SWIZZLE = LPR < 16 ? LPR - 1 : 15;
     const int nw = n0 + wn * 32 * WP, n = nw + 4 * (lane % LPR), mw = m0 + wm * 32 * WQ;
     v4f bias = {0.0f, 0.0f, 0.0f, 0.0f};
     if (g.bias)
@@ -291,18 +335,20 @@ __global__ void __launch_bounds__(64 * MxTile<BIG>::WAVES) mxfp4_tile_kernel(MxA
         for (int a = 0; a < WP; ++a)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<v4f *>(stg + r * S::ROW + 16 * ((8 * a + 2 * q + c) ^ (r & 15))) =
+                *reinterpret_cast<v4f *>(stg + r * S::OUT + 16 * ((8 * a + 2 * q + c) ^ (r & SWIZZLE))) =
                     v4f{acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
         asm volatile("" ::: "memory");
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int row = (64 / LPR) * j + lane / LPR, m = mw + 32 * b + row;
-            v4f x = *reinterpret_cast<const v4f *>(stg + row * S::ROW + 16 * ((lane % LPR) ^ (row & 15)));
+            v4f x = *reinterpret_cast<const v4f *>(stg + row * S::OUT + 16 * ((lane % LPR) ^ (row & SWIZZLE)));
             if (g.bias) x += bias;
             if (m >= g.M) continue;
             float *const to = g.Y + (int64_t)m * g.N + n;
-            if (n + 4 <= g.N) *reinterpret_cast<v4f_u *>(to) = x;
-            else
+            if (n + 4 <= g.N) {
+                if (S::PAST_CACHES) __builtin_nontemporal_store(x, reinterpret_cast<v4f_u *>(to));
+                else *reinterpret_cast<v4f_u *>(to) = x;
+            } else
 #pragma unroll
                 for (int i = 0; i < 3; ++i)
                     if (n + i < g.N) to[i] = x[i];
@@ -310,21 +356,166 @@ __global__ void __launch_bounds__(64 * MxTile<BIG>::WAVES) mxfp4_tile_kernel(MxA
     }
 }
 
-template <bool BIG>
-sbn_status launch_tile(MxArgs &g, hipStream_t stream)
+template <class S>
+sbn_status launch_tile(MxArgs g, hipStream_t stream)
 {
-    using S = MxTile<BIG>;
     g.tiles_n = (int)ceil_div(g.N, S::N);
     g.tiles_m = (int)ceil_div(g.M, S::M);
     static thread_local bool raised = false;
     if (!raised) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&mxfp4_tile_kernel<BIG>), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&mxfp4_tile_kernel<S>), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
         if (e != hipSuccess) { set_hip_error(e, "hipFuncSetAttribute"); return SBN_EHIP; }
         raised = true;
     }
     const int64_t blocks = ceil_div((int64_t)g.tiles_n * g.tiles_m, 8) * 8;
-    hipLaunchKernelGGL(mxfp4_tile_kernel<BIG>, dim3((unsigned)blocks), dim3(64 * S::WAVES), S::LDS, stream, g);
+    hipLaunchKernelGGL(mxfp4_tile_kernel<S>, dim3((unsigned)blocks), dim3(64 * S::WAVES), S::LDS, stream, g);
     return check_launch("mxfp4_tile_kernel");
+}
+
+// ---- few tokens ---------------------------------------------------------------------------------------------------------------------------
+// The same product where W is what has to be moved: a block takes 32 rows of W at a time, its wavefronts share the dimensions in stages of 256,
+// and their sums meet in LDS.  A wavefront's stages of W come by LDS-DMA into a part of its own (whole lines are asked for; a lane's operands lie in 32
+// rows), two at a time, without a barrier; the tokens' operands are read from the L2 into registers.  Quantizing them here as well, by the lane that
+// multiplies them, cost more than the launch it saved (one token x 2560 -> 6912: 8.6 us against 6.2, -> 131072: 46 against 30).
+
+constexpr int STAGE_BYTES = 128, STAGE_SCALES = 8;   // of a row and stage
+constexpr int FEW_ROWS = 32, FEW_STAGE = FEW_ROWS * (STAGE_BYTES + STAGE_SCALES), FEW_PITCH = FEW_ROWS + 4;
+constexpr int FEW_WAVES = 8, LDS_BYTES = 160 * 1024;
+int few_lds(int tokens) { return 2 * FEW_STAGE + 2 * tokens * FEW_PITCH * 4; }   // of a wavefront: two stages, its sums of two tiles
+
+template <int TG>
+__global__ void __launch_bounds__(512) mxfp4_few_kernel(MxArgs g)
+{
+    extern __shared__ __attribute__((aligned(1024))) uint8_t dlds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int r = lane & 31, c = lane >> 5;
+    const uint32_t pitch = (uint32_t)g.pitch, spitch = pitch / 16;
+    const int stages = g.stages;
+    const int tiles = (g.N + FEW_ROWS - 1) / FEW_ROWS;
+    const uint32_t lds0 = lds_address(dlds) + wave * 2 * FEW_STAGE;
+    float *const sums = reinterpret_cast<float *>(dlds + waves * 2 * FEW_STAGE);   // [2][waves][g.M][FEW_PITCH]
+    uint32_t off[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = 8 * i + (lane >> 3);
+        off[i] = (uint32_t)row * pitch + 16u * ((lane & 7) ^ ((row >> 1) & 7));
+    }
+    const uint32_t soff = (uint32_t)(lane >> 1) * spitch + 4u * (lane & 1);
+    // W of a stage, to buffer e
+    auto request = [&](const int tile, const int st, const int e) {
+        const int64_t o0 = (int64_t)tile * FEW_ROWS;
+        const int rows = std::min(FEW_ROWS, g.N - (int)o0);
+        const v4i pb = buffer_of(g.P + o0 * pitch, rows * (int)pitch), spb = buffer_of(g.sp + o0 * spitch, rows * (int)spitch);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lds_dma16_buffer(pb, off[i], (uint32_t)st * STAGE_BYTES, lds0 + e * FEW_STAGE + i * 1024);
+        lds_dma4_buffer(spb, soff, (uint32_t)st * STAGE_SCALES, lds0 + e * FEW_STAGE + FEW_ROWS * STAGE_BYTES);
+    };
+    v4i q[2][TG][4], p[2][4];
+    int sq[2][TG], sp[2];
+    // the tokens' operands of a stage
+    auto load_tokens = [&](const int st, const int e) {
+#pragma unroll
+        for (int i = 0; i < TG; ++i) {
+            const int64_t t = std::min(32 * i + r, g.M - 1);   // past the last the last one again
+            const uint8_t *const row = g.Q + t * g.qpitch + st * STAGE_BYTES + 64 * c;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) q[e][i][u] = *reinterpret_cast<const v4i *>(row + 16 * u);
+            sq[e][i] = *reinterpret_cast<const int *>(g.sq + ((int64_t)st * g.M + t) * STAGE_SCALES + 4 * c);
+        }
+    };
+    typedef __attribute__((address_space(3))) const v4i *lds_v4i;
+    typedef __attribute__((address_space(3))) const int *lds_int;
+    auto read_words = [&](const int e) {
+        const uint32_t at = lds0 + e * FEW_STAGE;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) p[e][u] = *(lds_v4i)(uintptr_t)(at + r * 128 + 16 * ((4 * c + u) ^ ((r >> 1) & 7)));
+        sp[e] = *(lds_int)(uintptr_t)(at + FEW_ROWS * STAGE_BYTES + 8 * r + 4 * c);
+    };
+    v16f acc[TG];
+    auto wide = [](const v4i x) { return v8i{x[0], x[1], x[2], x[3], 0, 0, 0, 0}; };
+    auto multiply = [&](const int e) {
+#pragma unroll
+        for (int i = 0; i < TG; ++i) {
+            acc[i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(p[e][0]), wide(q[e][i][0]), acc[i], 4, 4, 0, sp[e], 0, sq[e][i]);
+            acc[i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(p[e][1]), wide(q[e][i][1]), acc[i], 4, 4, 1, sp[e], 1, sq[e][i]);
+            acc[i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(p[e][2]), wide(q[e][i][2]), acc[i], 4, 4, 2, sp[e], 2, sq[e][i]);
+            acc[i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(p[e][3]), wide(q[e][i][3]), acc[i], 4, 4, 3, sp[e], 3, sq[e][i]);
+        }
+    };
+    // A wavefront's stages wave, wave + waves, ... of a tile, two at a time
+    auto request_two = [&](const int tile, const int st) {
+        request(tile, st, 0);
+        if (st + waves < stages) request(tile, st + waves, 1);
+    };
+    const bool kept = stages <= 2 * waves;   // the tokens' operands stay in registers from tile to tile
+    int tile = blockIdx.x;
+    request_two(tile, wave);
+    for (int parity = 0; tile < tiles; tile += gridDim.x, parity ^= 1) {
+#pragma unroll
+        for (int i = 0; i < TG; ++i)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) acc[i][x] = 0.0f;
+        for (int st = wave; st < stages; st += 2 * waves) {
+            const bool two = st + waves < stages;
+            if (!kept || tile == (int)blockIdx.x) {
+                load_tokens(st, 0);
+                if (two) load_tokens(st + waves, 1);
+            }
+            SBN_WAIT_VMCNT(0);
+            asm volatile("" ::: "memory");   // the words have landed
+            read_words(0);
+            if (two) read_words(1);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // and are out of LDS before the next ones are asked for
+            if (st + 2 * waves < stages) request_two(tile, st + 2 * waves);
+            else if (tile + (int)gridDim.x < tiles) request_two(tile + gridDim.x, wave);
+            multiply(0);
+            if (two) multiply(1);
+        }
+        float *const part = sums + (parity * waves + wave) * g.M * FEW_PITCH;
+#pragma unroll
+        for (int i = 0; i < TG; ++i)
+            if (32 * i + r < g.M)
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    *reinterpret_cast<v4f *>(part + (32 * i + r) * FEW_PITCH + 8 * x + 4 * c) = v4f{acc[i][4 * x], acc[i][4 * x + 1], acc[i][4 * x + 2], acc[i][4 * x + 3]};
+        // (asynchronous loads go on: no __syncthreads, which would wait for them.  One barrier per tile: the sums of the tile after the next
+        // one are written behind the next one's barrier)
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        typedef float v4f_u __attribute__((ext_vector_type(4), aligned(4)));
+        for (int at = threadIdx.x; at < 8 * g.M; at += blockDim.x) {
+            const int t = at >> 3, n = 4 * (at & 7);
+            v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int w = 0; w < waves; ++w) x += *reinterpret_cast<const v4f *>(sums + ((parity * waves + w) * g.M + t) * FEW_PITCH + n);
+            const int o = tile * FEW_ROWS + n;
+            float *const to = g.Y + (int64_t)t * g.N + o;
+            if (o + 4 <= g.N) {
+                if (g.bias) x += *reinterpret_cast<const v4f_u *>(g.bias + o);
+                *reinterpret_cast<v4f_u *>(to) = x;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    if (o + i < g.N) to[i] = x[i] + (g.bias ? g.bias[o + i] : 0.0f);
+            }
+        }
+    }
+}
+
+template <int TG>
+sbn_status launch_few(const MxArgs &g, hipStream_t stream)
+{
+    // as many wavefronts as have the same number of stages, up to eight, or as many as LDS has room for
+    const int most = std::min(FEW_WAVES, LDS_BYTES / few_lds(g.M)), waves = (int)ceil_div(g.stages, ceil_div(g.stages, most));
+    static thread_local bool raised = false;
+    if (!raised) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&mxfp4_few_kernel<TG>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES);
+        if (e != hipSuccess) { set_hip_error(e, "hipFuncSetAttribute"); return SBN_EHIP; }
+        raised = true;
+    }
+    // as many blocks as fit the device, with the same number of tiles each
+    const int lds = waves * few_lds(g.M), fit = std::max(1, std::min(LDS_BYTES / lds, 16 / waves));
+    const int64_t tiles = ceil_div(g.N, FEW_ROWS), rounds = ceil_div(tiles, 256 * fit);
+    hipLaunchKernelGGL(mxfp4_few_kernel<TG>, dim3((unsigned)ceil_div(tiles, rounds)), dim3(64 * waves), lds, stream, g);
+    return check_launch("mxfp4_few_kernel");
 }
 
 int64_t padded(int64_t cols) { return ceil_div(cols, PAD) * PAD; }
@@ -337,43 +528,78 @@ void mxfp4_bytes(int64_t rows, int64_t cols, size_t &codes, size_t &scales)
     scales = (size_t)(rows * padded(cols) / GROUP);
 }
 
+// X in the workspace: rows of whole stages (256 columns) of codes, then the scales stage by stage
+static int64_t stages_of(int64_t d_in) { return ceil_div(d_in, 256); }
+static size_t x_code_bytes(int64_t tokens, int64_t d_in) { return align_up((size_t)(tokens * stages_of(d_in) * STAGE_BYTES), 256); }
 size_t mxfp4_workspace_bytes(int64_t tokens, int64_t d_in)
 {
-    size_t codes, scales;
-    mxfp4_bytes(tokens, d_in, codes, scales);
-    return align_up(codes, 256) + align_up(scales, 256);
+    return x_code_bytes(tokens, d_in) + align_up((size_t)(tokens * stages_of(d_in) * STAGE_SCALES), 256);
+}
+
+// Bound by what they move.  131072 x 2560 of bf16, us with 1 / 2 / 4 vectors per lane: quantize 177 / 169 / 180 (5.0 TB/s, what a copy reaches), back
+// 150 / 134 / 131 (6.5); few blocks keep one vector per lane
+template <bool BF16>
+static void launch_quantize(const void *X, int64_t rows, int64_t cols, int64_t vectors, uint8_t *codes, uint8_t *scales, int stage_shift, hipStream_t stream)
+{
+    uint32_t *const words = reinterpret_cast<uint32_t *>(codes);
+    const int64_t blocks = ceil_div(rows * vectors, 256);
+    if (blocks >= 4096)
+        hipLaunchKernelGGL((mxfp4_quantize_kernel<BF16, 2>), dim3((unsigned)ceil_div(blocks, 2)), dim3(256), 0, stream, X, (uint32_t)rows, (int)cols, (uint32_t)vectors, words,
+                           scales, stage_shift);
+    else
+        hipLaunchKernelGGL((mxfp4_quantize_kernel<BF16, 1>), dim3((unsigned)blocks), dim3(256), 0, stream, X, (uint32_t)rows, (int)cols, (uint32_t)vectors, words, scales,
+                           stage_shift);
 }
 
 sbn_status launch_mxfp4_quantize(const void *X, sbn_dtype dtype, int64_t rows, int64_t cols, uint8_t *codes, uint8_t *scales, hipStream_t stream)
 {
-    const int64_t vectors = padded(cols) / 8;
-    const dim3 grid((unsigned)ceil_div(rows * vectors, 256)), block(256);
-    uint32_t *const words = reinterpret_cast<uint32_t *>(codes);
-    if (dtype == SBN_BF16) hipLaunchKernelGGL(mxfp4_quantize_kernel<true>, grid, block, 0, stream, X, rows, (int)cols, (int)vectors, words, scales);
-    else hipLaunchKernelGGL(mxfp4_quantize_kernel<false>, grid, block, 0, stream, X, rows, (int)cols, (int)vectors, words, scales);
+    if (dtype == SBN_BF16) launch_quantize<true>(X, rows, cols, padded(cols) / 8, codes, scales, 0, stream);
+    else launch_quantize<false>(X, rows, cols, padded(cols) / 8, codes, scales, 0, stream);
     return check_launch("mxfp4_quantize_kernel");
+}
+
+template <bool BF16>
+static void launch_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *Y, hipStream_t stream)
+{
+    const uint32_t *const words = reinterpret_cast<const uint32_t *>(codes);
+    const int64_t blocks = ceil_div(rows * (cols / 8), 256);
+    const uint32_t vectors = (uint32_t)(padded(cols) / 8);
+    if (blocks >= 4096)
+        hipLaunchKernelGGL((mxfp4_dequantize_kernel<BF16, 4>), dim3((unsigned)ceil_div(blocks, 4)), dim3(256), 0, stream, words, scales, (uint32_t)rows, (uint32_t)cols, vectors, Y);
+    else
+        hipLaunchKernelGGL((mxfp4_dequantize_kernel<BF16, 1>), dim3((unsigned)blocks), dim3(256), 0, stream, words, scales, (uint32_t)rows, (uint32_t)cols, vectors, Y);
 }
 
 sbn_status launch_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *Y, sbn_dtype dtype, hipStream_t stream)
 {
-    const int64_t vectors = padded(cols) / 8;
-    const dim3 grid((unsigned)ceil_div(rows * (cols / 8), 256)), block(256);
-    const uint32_t *const words = reinterpret_cast<const uint32_t *>(codes);
-    if (dtype == SBN_BF16) hipLaunchKernelGGL(mxfp4_dequantize_kernel<true>, grid, block, 0, stream, words, scales, rows, (int)cols, (int)vectors, Y);
-    else hipLaunchKernelGGL(mxfp4_dequantize_kernel<false>, grid, block, 0, stream, words, scales, rows, (int)cols, (int)vectors, Y);
+    if (dtype == SBN_BF16) launch_dequantize<true>(codes, scales, rows, cols, Y, stream);
+    else launch_dequantize<false>(codes, scales, rows, cols, Y, stream);
     return check_launch("mxfp4_dequantize_kernel");
+}
+
+// Estimated us of a product in tiles of `edge`: one tile alone, or every multiprocessor's share of them, `each` us of the multiprocessor.  The
+// figures are fits to products of 65 to 8192 tokens, 1000 -> 20000, 2560 -> 6912 and 131072, 4096 -> 4096 (2560 -> 6912, us, small / middle /
+// large: 128 tokens 10.4 / 14.7 / 24.1, 512 21.3 / 18.7 / 28.6, 4096 110 / 81 / 68).
+static float tiles_us(const MxArgs &g, const int edge, const float alone, const float each)
+{
+    return std::max(alone, each * (float)ceil_div(ceil_div(g.N, edge) * ceil_div(g.M, edge), 256));
 }
 
 sbn_status launch_mxfp4_linear(const void *X, int64_t tokens, int64_t d_in, int64_t d_out, const uint8_t *codes, const uint8_t *scales, const float *bias,
                                float *Y, void *workspace, hipStream_t stream)
 {
-    size_t code_bytes, scale_bytes;
-    mxfp4_bytes(tokens, d_in, code_bytes, scale_bytes);
-    uint8_t *const xc = static_cast<uint8_t *>(workspace), *const xs = xc + align_up(code_bytes, 256);
-    const sbn_status st = launch_mxfp4_quantize(X, SBN_BF16, tokens, d_in, xc, xs, stream);
+    const int64_t stages = stages_of(d_in);
+    uint8_t *const xc = static_cast<uint8_t *>(workspace), *const xs = xc + x_code_bytes(tokens, d_in);
+    launch_quantize<true>(X, tokens, d_in, stages * 32, xc, xs, 8, stream);
+    const sbn_status st = check_launch("mxfp4_quantize_kernel");
     if (st != SBN_OK) return st;
-    MxArgs g{codes, xc, scales, xs, padded(d_in) / 2, (int)d_out, (int)tokens, bias, Y, 0, 0};
-    return launch_tile<false>(g, stream);
+    MxArgs g{codes, xc, scales, xs, padded(d_in) / 2, stages * STAGE_BYTES, (int)d_out, (int)tokens, (int)stages, bias, Y, 0, 0};
+    // 64 tokens, few and small tiles: 2560 -> 6912 8.9 and 10.4 us, 4096 -> 4096 10.8 and 12.6
+    if (tokens <= 32) return launch_few<1>(g, stream);
+    if (tokens <= 64) return launch_few<2>(g, stream);
+    const float large = tiles_us(g, 256, 1.05f * stages + 12.0f, 1.44f * stages + 16.0f), middle = tiles_us(g, 128, 0.65f * stages + 6.2f, 0.48f * stages + 6.5f),
+                small = tiles_us(g, 64, 0.38f * stages + 4.6f, 0.28f * stages + 1.1f);
+    return large <= std::min(middle, small) ? launch_tile<MxLarge>(g, stream) : middle <= small ? launch_tile<MxMiddle>(g, stream) : launch_tile<MxSmall>(g, stream);
 }
 
 }  // namespace sbn
