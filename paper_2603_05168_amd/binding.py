@@ -126,12 +126,26 @@ def _load_fastcall(path=os.path.join(_HERE, "_fastcall.so")):
         return None
     address = lambda f: ctypes.cast(f, ctypes.c_void_p).value   # noqa: E731
     module.bind(address(_lib.sbn_sparse_ternary_linear), address(_lib.sbn_sparse_ternary_linear_grouped))
+    module.bind_head(*(address(f) for f in (
+        _lib.sbn_head_cross_entropy, _lib.sbn_head_cross_entropy_backward, _lib.sbn_head_distill, _lib.sbn_head_distill_backward, _lib.sbn_mxfp4_quantize,
+        _lib.sbn_mxfp4_dequantize, _lib.sbn_mxfp4_linear, _lib.sbn_head_workspace_bytes, _lib.sbn_mxfp4_bytes, _lib.sbn_mxfp4_workspace_bytes)))
     return module
 
 
 _fastcall = _load_fastcall()
 _fast_linear = _fastcall.linear if _fastcall else lambda *args: None
 _fast_grouped = _fastcall.grouped if _fastcall else lambda *args: None
+
+
+def _fast(name):
+    """A call of the output head in C++: its status, or None where the Python code beside it is to do it."""
+    return getattr(_fastcall, name) if _fastcall else lambda *args: None
+
+
+_fast_head_ce, _fast_head_ce_backward = _fast("head_ce"), _fast("head_ce_backward")
+_fast_head_distill, _fast_head_distill_backward = _fast("head_distill"), _fast("head_distill_backward")
+_fast_mxfp4_quantize, _fast_mxfp4_dequantize, _fast_mxfp4_linear = _fast("mxfp4_quantize"), _fast("mxfp4_dequantize"), _fast("mxfp4_linear")
+_fast_head_bytes, _fast_mxfp4_bytes, _fast_mxfp4_workspace_bytes = _fast("head_bytes"), _fast("mxfp4_bytes"), _fast("mxfp4_workspace_bytes")
 
 
 def lib_path() -> str:
@@ -468,12 +482,22 @@ def _expect(name, t, shape, *dtypes):
     return t
 
 
+def _on_gpu(*tensors):
+    """A host address given to a kernel is a fault of the device."""
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise ValueError("tensors must be on the GPU")
+
+
 def _bytes_of(ws):
     return ws.numel() * ws.element_size()
 
 
 def sbn_head_workspace_bytes(tokens: int, d_in: int, vocab: int, top_k: int = 0, backward: bool = True) -> int:
     """Workspace of the forward calls of the output head, and of their backward calls where `backward` is set."""
+    nbytes = _fast_head_bytes(tokens, d_in, vocab, top_k, int(backward))
+    if nbytes is not None:
+        return nbytes
     out = ctypes.c_size_t(0)
     _check(_lib.sbn_head_workspace_bytes(tokens, d_in, vocab, top_k, int(backward), ctypes.byref(out)), "sbn_head_workspace_bytes")
     return out.value
@@ -493,16 +517,28 @@ def _head_sizes(H, W, targets, ce, dH=None, dW=None):
 
 def sbn_head_cross_entropy(H, W, targets, ce, lse, workspace):
     """ce, lse (fp32 [tokens]) of z = H W^T against targets (int64; outside the vocabulary: left out), the logits never stored."""
+    status = _fast_head_ce(H, W, targets, ce, lse, workspace)
+    if status is not None:
+        if status:
+            _check(status, "sbn_head_cross_entropy")
+        return
     tokens, d_in, vocab = _head_sizes(H, W, targets, ce)
     _expect("lse", lse, (tokens,), torch.float32)
+    _on_gpu(H, W, targets, ce, lse, workspace)
     _check(_lib.sbn_head_cross_entropy(_ptr(H), _ptr(W), _ptr(targets), tokens, d_in, vocab, _ptr(ce), _ptr(lse), _ptr(workspace),
                                        _bytes_of(workspace), _stream()), "sbn_head_cross_entropy")
 
 
 def sbn_head_cross_entropy_backward(H, W, targets, lse, d_ce, workspace, dH=None, dW=None):
     """dH, dW (bf16, overwritten; None: not wanted) for the gradient d_ce (fp32 [tokens]) of ce."""
+    status = _fast_head_ce_backward(H, W, targets, lse, d_ce, workspace, dH, dW)
+    if status is not None:
+        if status:
+            _check(status, "sbn_head_cross_entropy_backward")
+        return
     tokens, d_in, vocab = _head_sizes(H, W, targets, d_ce, dH, dW)
     _expect("lse", lse, (tokens,), torch.float32)
+    _on_gpu(H, W, targets, lse, d_ce, workspace, dH, dW)
     _check(_lib.sbn_head_cross_entropy_backward(_ptr(H), _ptr(W), _ptr(targets), _ptr(lse), _ptr(d_ce), tokens, d_in, vocab, _ptr(dH), _ptr(dW),
                                                 _ptr(workspace), _bytes_of(workspace), _stream()), "sbn_head_cross_entropy_backward")
 
@@ -517,20 +553,32 @@ def _teacher(top_idx, top_logits, tokens):
 def sbn_head_distill(H, W, top_idx, top_logits, tau: float, kd, lse, workspace, targets=None, ce=None):
     """kd (fp32 [tokens]) against the teacher's entries top_idx (int64) and top_logits (fp32 or bf16), both [tokens, k], at temperature
     tau; lse fp32 [2, tokens]; with targets and ce the cross entropy from the same pass."""
+    status = _fast_head_distill(H, W, top_idx, top_logits, tau, kd, lse, workspace, targets, ce)
+    if status is not None:
+        if status:
+            _check(status, "sbn_head_distill")
+        return
     tokens, d_in, vocab = _head_sizes(H, W, targets, ce)
     dtype, top_k = _teacher(top_idx, top_logits, tokens)
     _expect("kd", kd, (tokens,), torch.float32)
     _expect("lse", lse, (2, tokens), torch.float32)
+    _on_gpu(H, W, top_idx, top_logits, kd, lse, workspace, targets, ce)
     _check(_lib.sbn_head_distill(_ptr(H), _ptr(W), _ptr(top_idx), _ptr(top_logits), dtype, top_k, tau, _ptr(targets), tokens, d_in, vocab,
                                  _ptr(kd), _ptr(ce), _ptr(lse), _ptr(workspace), _bytes_of(workspace), _stream()), "sbn_head_distill")
 
 
 def sbn_head_distill_backward(H, W, top_idx, top_logits, tau: float, lse, d_kd, workspace, targets=None, d_ce=None, dH=None, dW=None):
     """dH, dW (bf16, overwritten; None: not wanted) for the gradients d_kd and, with targets, d_ce of the two losses."""
+    status = _fast_head_distill_backward(H, W, top_idx, top_logits, tau, lse, d_kd, workspace, targets, d_ce, dH, dW)
+    if status is not None:
+        if status:
+            _check(status, "sbn_head_distill_backward")
+        return
     tokens, d_in, vocab = _head_sizes(H, W, targets, d_ce, dH, dW)
     dtype, top_k = _teacher(top_idx, top_logits, tokens)
     _expect("d_kd", d_kd, (tokens,), torch.float32)
     _expect("lse", lse, (2, tokens), torch.float32)
+    _on_gpu(H, W, top_idx, top_logits, lse, d_kd, workspace, targets, d_ce, dH, dW)
     _check(_lib.sbn_head_distill_backward(_ptr(H), _ptr(W), _ptr(top_idx), _ptr(top_logits), dtype, top_k, tau, _ptr(targets), _ptr(lse),
                                           _ptr(d_kd), _ptr(d_ce), tokens, d_in, vocab, _ptr(dH), _ptr(dW), _ptr(workspace),
                                           _bytes_of(workspace), _stream()), "sbn_head_distill_backward")
@@ -538,6 +586,9 @@ def sbn_head_distill_backward(H, W, top_idx, top_logits, tau: float, lse, d_kd, 
 
 def sbn_mxfp4_bytes(rows: int, cols: int):
     """Bytes of the codes and of the scales of a [rows, cols] matrix."""
+    nbytes = _fast_mxfp4_bytes(rows, cols)
+    if nbytes is not None:
+        return nbytes
     codes, scales = ctypes.c_size_t(0), ctypes.c_size_t(0)
     _check(_lib.sbn_mxfp4_bytes(rows, cols, ctypes.byref(codes), ctypes.byref(scales)), "sbn_mxfp4_bytes")
     return codes.value, scales.value
@@ -555,21 +606,36 @@ def _mxfp4(codes, scales, rows, cols):
 
 def sbn_mxfp4_quantize(X, codes, scales):
     """X (fp32 or bf16 [rows, cols]) to microscaled 4-bit codes and block scales (uint8)."""
+    status = _fast_mxfp4_quantize(X, codes, scales)
+    if status is not None:
+        if status:
+            _check(status, "sbn_mxfp4_quantize")
+        return
     rows, cols = X.shape
     _expect("X", X, (rows, cols), torch.float32, torch.bfloat16)
     _mxfp4(codes, scales, rows, cols)
+    _on_gpu(X, codes, scales)
     _check(_lib.sbn_mxfp4_quantize(_ptr(X), _dtype_code(X), rows, cols, _ptr(codes), _ptr(scales), _stream()), "sbn_mxfp4_quantize")
 
 
 def sbn_mxfp4_dequantize(codes, scales, Y):
     """The values that codes and scales stand for, exactly, into Y (fp32 or bf16 [rows, cols])."""
+    status = _fast_mxfp4_dequantize(codes, scales, Y)
+    if status is not None:
+        if status:
+            _check(status, "sbn_mxfp4_dequantize")
+        return
     rows, cols = Y.shape
     _expect("Y", Y, (rows, cols), torch.float32, torch.bfloat16)
     _mxfp4(codes, scales, rows, cols)
+    _on_gpu(codes, scales, Y)
     _check(_lib.sbn_mxfp4_dequantize(_ptr(codes), _ptr(scales), rows, cols, _ptr(Y), _dtype_code(Y), _stream()), "sbn_mxfp4_dequantize")
 
 
 def sbn_mxfp4_workspace_bytes(tokens: int, d_in: int) -> int:
+    nbytes = _fast_mxfp4_workspace_bytes(tokens, d_in)
+    if nbytes is not None:
+        return nbytes
     out = ctypes.c_size_t(0)
     _check(_lib.sbn_mxfp4_workspace_bytes(tokens, d_in, ctypes.byref(out)), "sbn_mxfp4_workspace_bytes")
     return out.value
@@ -577,11 +643,17 @@ def sbn_mxfp4_workspace_bytes(tokens: int, d_in: int) -> int:
 
 def sbn_mxfp4_linear(X, codes, scales, Y, workspace, bias=None):
     """Y (fp32 [tokens, d_out]) = q(X) W^T (+ bias): X bf16, quantized on the way; W as codes and scales."""
+    status = _fast_mxfp4_linear(X, codes, scales, Y, workspace, bias)
+    if status is not None:
+        if status:
+            _check(status, "sbn_mxfp4_linear")
+        return
     (tokens, d_in), d_out = X.shape, Y.shape[1]
     _expect("X", X, (tokens, d_in), torch.bfloat16)
     _expect("Y", Y, (tokens, d_out), torch.float32)
     _expect("bias", bias, (d_out,), torch.float32)
     _mxfp4(codes, scales, d_out, d_in)
+    _on_gpu(X, codes, scales, Y, workspace, bias)
     _check(_lib.sbn_mxfp4_linear(_ptr(X), tokens, d_in, d_out, _ptr(codes), _ptr(scales), _ptr(bias), _ptr(Y), _ptr(workspace),
                                  _bytes_of(workspace), _stream()), "sbn_mxfp4_linear")
 

@@ -276,3 +276,31 @@ def test_graph_replay():
             assert torch.equal(v, eager[k]), k
         again = run(case, 2.0)
         assert torch.equal(again["dW"], eager["dW"])
+
+
+def test_marshalling_in_python_gives_the_same(monkeypatch):
+    import paper_2603_05168_amd.binding as b
+    case = make(40, 128, 900, 950, top=5)
+    fast = run(case, 2.0) | {"alone": run(case)["dW"]}
+    for name in [n for n in dir(b) if n.startswith("_fast_")]:
+        monkeypatch.setattr(b, name, lambda *args: None)
+    slow = run(case, 2.0) | {"alone": run(case)["dW"]}
+    for k in fast:
+        assert torch.equal(fast[k], slow[k]), k
+
+
+def test_refusals_reach_the_caller():
+    s = sbn()
+    case = {k: v.to(DEV) for k, v in make(40, 128, 900, 950, top=5).items()}
+    f = torch.zeros(40, device=DEV)
+    small = s.new_workspace(256)
+    for call in (lambda: s.sbn_head_cross_entropy(case["H"], case["W"], case["targets"], f, f, small),
+                 lambda: s.sbn_head_distill(case["H"], case["W"], case["top_idx"], case["top_logits"], 2.0, f, torch.zeros(2, 40, device=DEV), small)):
+        with pytest.raises(s.SbnError) as e:
+            call()
+        assert e.value.status == s.SBN_ESIZE
+    with pytest.raises(s.SbnError) as e:
+        s.sbn_head_distill(case["H"], case["W"], case["top_idx"], case["top_logits"], 0.0, f, torch.zeros(2, 40, device=DEV), small)
+    assert e.value.status == s.SBN_EINVAL
+    with pytest.raises(ValueError):
+        s.sbn_head_cross_entropy(case["H"], case["W"].t().contiguous().t(), case["targets"], f, f, small)

@@ -128,3 +128,23 @@ def test_mxfp4_sizes():
         sbn.sbn_mxfp4_quantize(X.half(), torch.zeros(3 * 128, dtype=torch.uint8), torch.zeros(24, dtype=torch.uint8))
     with pytest.raises(ValueError):
         sbn.sbn_mxfp4_quantize(torch.zeros(136, 3).t(), torch.zeros(3 * 128, dtype=torch.uint8), torch.zeros(24, dtype=torch.uint8))
+
+
+def test_host_tensors_are_refused_and_declined_by_the_marshalling():
+    import paper_2603_05168_amd.binding as b
+    H, W = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(10, 64, dtype=torch.bfloat16)
+    y, f, ws = torch.zeros(4, dtype=torch.int64), torch.zeros(4), torch.zeros(1 << 16, dtype=torch.uint8)
+    idx, a, lse = torch.zeros(4, 3, dtype=torch.int64), torch.zeros(4, 3), torch.zeros(2, 4)
+    X, codes, scales, Y = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(10 * 64, dtype=torch.uint8), torch.zeros(40, dtype=torch.uint8), torch.zeros(4, 10)
+    for name, fast, args in [
+            ("sbn_head_cross_entropy", b._fast_head_ce, (H, W, y, f, f, ws)),
+            ("sbn_head_cross_entropy_backward", b._fast_head_ce_backward, (H, W, y, f, f, ws, H, W)),
+            ("sbn_head_distill", b._fast_head_distill, (H, W, idx, a, 1.0, f, lse, ws, y, f)),
+            ("sbn_head_distill_backward", b._fast_head_distill_backward, (H, W, idx, a, 1.0, lse, f, ws, y, f, H, W)),
+            ("sbn_mxfp4_quantize", b._fast_mxfp4_quantize, (W, codes, scales)),
+            ("sbn_mxfp4_dequantize", b._fast_mxfp4_dequantize, (codes, scales, W)),
+            ("sbn_mxfp4_linear", b._fast_mxfp4_linear, (X, codes, scales, Y, ws, None))]:
+        assert fast(*args) is None and fast(*args[:-1]) is None and fast(*args[:-1], 7) is None, name
+        with pytest.raises(ValueError, match="GPU"):
+            getattr(b, name)(*args)
+    assert b._fast_head_bytes(0, 64, 10, 0, 1) is None and b._fast_mxfp4_bytes(1.0, 8) is None and b._fast_mxfp4_workspace_bytes(1 << 70, 8) is None
