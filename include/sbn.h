@@ -447,6 +447,14 @@ sbn_status sbn_mxfp4_workspace_bytes(int64_t tokens, int64_t d_in, size_t *bytes
 sbn_status sbn_mxfp4_linear(const void *X, int64_t tokens, int64_t d_in, int64_t d_out, const void *codes, const void *scales,
                             const float *bias, float *Y, void *workspace, size_t ws_bytes, void *stream);
 
+/*
+ * Test hook: the sizes of the block tiles that the output head takes, so that a test reaches the edges of each whatever an estimate
+ * chooses: 0, 1, 2 for tiles of 64, 128 and 256; for the gradients 3 for the kernel of up to 64 tokens as well; negative for the
+ * library's choice.  (A product in 4-bit floating point of up to 64 tokens takes its own kernel only by that choice.)  Workspaces are to be asked
+ * for anew.  Process-wide; not for use while calls are being enqueued from other threads.
+ */
+void sbn_test_set_head_tiles(int logits, int gradients, int mxfp4);
+
 /* Text of the last HIP error seen by this thread ("" if none). */
 const char *sbn_last_error(void);
 

@@ -73,6 +73,8 @@ def _load():
     lib.sbn_rmsnorm_act_quant.argtypes = [vp, i64, i64, vp, ctypes.c_float, vp, vp, vp, vp]
     lib.sbn_test_set_spin_limits.restype = None
     lib.sbn_test_set_spin_limits.argtypes = [cint, cint]
+    lib.sbn_test_set_head_tiles.restype = None
+    lib.sbn_test_set_head_tiles.argtypes = [cint, cint, cint]
     lib.sbn_test_linear_kernel.restype = cint
     lib.sbn_test_linear_kernel.argtypes = [cint, cint, pp, pp, pi64, pi64, pi64, cint, cint, pp, pp, pp, pp, pp, vp]
     lib.sbn_test_self_kernel.restype = cint
@@ -656,6 +658,11 @@ def sbn_mxfp4_linear(X, codes, scales, Y, workspace, bias=None):
     _on_gpu(X, codes, scales, Y, workspace, bias)
     _check(_lib.sbn_mxfp4_linear(_ptr(X), tokens, d_in, d_out, _ptr(codes), _ptr(scales), _ptr(bias), _ptr(Y), _ptr(workspace),
                                  _bytes_of(workspace), _stream()), "sbn_mxfp4_linear")
+
+
+def sbn_test_set_head_tiles(logits: int = -1, gradients: int = -1, mxfp4: int = -1):
+    """Test hook: block tiles of the output head (0, 1, 2; gradients 3: the kernel of up to 64 tokens; negative: the library's choice)."""
+    _lib.sbn_test_set_head_tiles(logits, gradients, mxfp4)
 
 
 def new_workspace(nbytes: int, device="cuda") -> torch.Tensor:

@@ -8,6 +8,7 @@
 // way out, and both gradients' products read G.  All products run on the bf16 matrix cores (v_mfma_f32_32x32x16_bf16, fp32
 // accumulation).  Nothing is added atomically: results do not depend on the order of blocks.
 #include <algorithm>
+#include <atomic>
 
 #include "sbn_internal.hpp"
 #include "sbn_mfma.hpp"
@@ -29,20 +30,34 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp
 
 // ---- block tile product -------------------------------------------------------------------------------------------------------------
-// acc[n, m] = sum_k P[n, k] Q[m, k] for a block tile of 256 x 256 (eight wavefronts of 128 x 64) or 128 x 128 (four of 64 x 64, two blocks
-// per multiprocessor).  Either operand lies with k contiguous ([rows, ld]) or the other way round ([k, ld], "transposed": read from LDS by
-// ds_read_b64_tr_b16).  Stages of 64 k come by LDS-DMA into a ring of five slots that the operands take in turns, so that P lies in LDS two
-// stages ahead and Q one; a stage is consumed in quarters of 16 k, the fragments of the next quarter are read and the requests for later
-// stages issued between the matrix instructions of the current one.
+// acc[n, m] = sum_k P[n, k] Q[m, k] for a block tile of 256 x 256 (eight wavefronts of 128 x 64), 128 x 128 (four of 64 x 64, two blocks per
+// multiprocessor) or 64 x 64 (four of 32 x 32, two blocks).  Either operand lies with k contiguous ([rows, ld]) or the other way round ([k, ld],
+// "transposed": read from LDS by ds_read_b64_tr_b16).  Stages of 64 k come by LDS-DMA into a ring of 2 AHEAD + 1 slots that the operands
+// take in turns, so that P lies in LDS AHEAD stages ahead and Q one less; a stage is consumed in quarters of 16 k, the fragments of the next
+// quarter are read and the requests for later stages issued between the matrix instructions of the current one.
 constexpr int STAGE_K = 64;
-template <bool BIG> struct HeadTile {
-    static constexpr int N = BIG ? 256 : 128, M = N;
-    static constexpr int WAVES = BIG ? 8 : 4, WN = 2, WM = WAVES / WN;       // wavefronts along n and m
-    static constexpr int WP = N / WN / 32, WQ = M / WM / 32;                 // 32 x 32 tiles of a wavefront: 4 x 2 or 2 x 2
-    static constexpr int SLOT = N * STAGE_K * 2, SLOTS = 5;                  // one operand's share of a stage
-    static constexpr int LDS = SLOTS * SLOT, STAGING = 4 * SLOT / WAVES;     // the last: of a wavefront, for its result
-    static constexpr int ROW = WP * 128;                                     // bytes of a staged row of fp32 results
+enum { TINY, SMALL, BIG };
+template <int SIZE> struct HeadTile {
+    static constexpr int N = SIZE == BIG ? 256 : SIZE == SMALL ? 128 : 64, M = N;
+    static constexpr int WAVES = SIZE == BIG ? 8 : 4, WN = 2, WM = WAVES / WN;   // wavefronts along n and m
+    static constexpr int WP = N / WN / 32, WQ = M / WM / 32;                     // 32 x 32 tiles of a wavefront: 4 x 2, 2 x 2 or 1 x 1
+    static constexpr int AHEAD = SIZE == TINY ? 4 : 2;
+    static constexpr int SLOT = N * STAGE_K * 2, SLOTS = 2 * AHEAD + 1;          // one operand's share of a stage
+    static constexpr int REQUESTS = SLOT / (1024 * WAVES);                       // of a wavefront, operand and stage
+    static constexpr int LDS = SLOTS * SLOT;
+    // results leave through the ring's last slot, some rows (columns m) of a wavefront at a time: a next tile's first stages may be in the others
+    static constexpr int ROW = WP * 128, STAGING = SLOT / WAVES, ROWS = STAGING / ROW;
+    static constexpr int STAGED = (SLOTS - 1) * SLOT;
 };
+
+// The lane, as a value that the compiler knows nothing of: what a tile's parts derive from it is made again in each of them, for all of it at once
+// does not fit the registers
+__device__ __forceinline__ int lane_here()
+{
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
 
 struct Operand {
     const uint16_t *base;   // row 0, k 0
@@ -50,23 +65,26 @@ struct Operand {
     int rows, k;            // what the matrix has (k: from the product's first k on)
 };
 
-// The requests of one operand: four instructions of 1 KB per wavefront and stage.  Rows and k past the matrix read as zeros or as what
-// zero_tail overwrites; stages past the last fetch nothing.  A buffer's size has 32 bits and ends with the rows of the tile.
-template <bool BIG, bool TRANSPOSED> struct Requests {
-    using S = HeadTile<BIG>;
+// The requests of one operand: instructions of 1 KB.  Rows and k past the matrix read as zeros or as what zero_tail overwrites; stages past the
+// last fetch nothing.  A buffer's size has 32 bits and ends with the rows of the tile.
+template <int SIZE, bool TRANSPOSED> struct Requests {
+    using S = HeadTile<SIZE>;
+    static constexpr int I = S::REQUESTS;
     v4i buffer;
-    uint32_t off[4], bytes, bytes_last;
+    uint32_t off[I], bytes, bytes_last;
     uint64_t step;
-    int nk, kleft, wave, lane;
+    int nk, kleft, wave;
 
-    __device__ __forceinline__ Requests(const Operand &op, int row0, int nk_, int wave_, int lane_) : nk(nk_), wave(wave_), lane(lane_)
+    __device__ __forceinline__ void set(const Operand &op, int row0, int nk_, int wave_, int lane)
     {
+        nk = __builtin_amdgcn_readfirstlane(nk_);
+        wave = wave_;
         const uint32_t pitch = 2u * (uint32_t)op.ld;
         kleft = op.k - (nk - 1) * STAGE_K;
         kleft = kleft < STAGE_K ? kleft : STAGE_K;
         if constexpr (TRANSPOSED) {
-            // a stage is 64 k rows of S::N values, one instruction fills 1024 bytes of them; slot s of row k holds granule s ^ f(k),
-            // f = 4 (k & 3) | 2 ((k >> 2) & 1): the four k rows that a transposing read of 16 lanes takes lie in different banks
+            // a stage is 64 k rows of S::N values; slot s of row k holds granule s ^ f(k), f = 4 (k & 3) | 2 ((k >> 2) & 1): the four k rows that a
+            // transposing read of 16 lanes takes lie in different banks
             auto up_to_end = [&](const int k) { return (uint32_t)std::min((uint64_t)k * pitch - 2u * (uint32_t)row0, (uint64_t)0xfffffff0u); };
             bytes = up_to_end(STAGE_K);
             bytes_last = up_to_end(kleft);
@@ -75,9 +93,9 @@ template <bool BIG, bool TRANSPOSED> struct Requests {
             buffer = buffer_of(op.base + row0, nk > 1 ? bytes : bytes_last);
             constexpr int GPR = S::N / 8, RPI = 64 / GPR;   // granules of a k row, k rows per instruction
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int k = RPI * (4 * wave + i) + lane / GPR;
-                const int gran = (lane % GPR) ^ (4 * (k & 3) | 2 * ((k >> 2) & 1));
+            for (int i = 0; i < I; ++i) {
+                const int k = RPI * (I * wave + i) + lane / GPR;
+                const int gran = (lane % GPR) ^ (4 * (k & 3) | 2 * ((k >> 2) & 1)) % GPR;
                 off[i] = (uint32_t)k * pitch + 16u * gran;
             }
         } else {
@@ -88,21 +106,22 @@ template <bool BIG, bool TRANSPOSED> struct Requests {
             step = 2 * STAGE_K;
             buffer = buffer_of(op.base + (int64_t)row0 * op.ld, nk > 1 ? bytes : bytes_last);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = 32 * wave + 8 * i + (lane >> 3);
+            for (int i = 0; i < I; ++i) {
+                const int row = 8 * (I * wave + i) + (lane >> 3);
                 off[i] = (uint32_t)row * pitch + 16u * ((lane & 7) ^ ((row >> 1) & 7));
             }
         }
     }
-    // instruction i of stage kt; the fourth moves on to the next stage
+    // instruction i of stage kt; the last one moves on to the next stage
     __device__ __forceinline__ void issue(const int kt, const uint32_t slot, const int i)
     {
-        lds_dma16_buffer(buffer, off[i], 0, slot + wave * 4096 + i * 1024);
-        if (i < 3) return;
+        lds_dma16_buffer(buffer, off[i], 0, slot + (I * wave + i) * 1024);
+        if (i + 1 < I) return;
         const uint64_t base = ((uint64_t)(uint32_t)buffer[1] << 32 | (uint32_t)buffer[0]) + step;
-        buffer[0] = (int)(uint32_t)base;
-        buffer[1] = (int)(uint32_t)(base >> 32);
-        buffer[2] = kt + 2 < nk ? (int)bytes : kt + 2 == nk ? (int)bytes_last : 0;
+        // (the same in all lanes; where the compiler does not see it, it would not hold them in scalar registers)
+        buffer[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)base);
+        buffer[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(base >> 32));
+        buffer[2] = __builtin_amdgcn_readfirstlane(kt + 2 < nk ? (int)bytes : kt + 2 == nk ? (int)bytes_last : 0);
     }
     // k of the last stage past a row's end: the next row was fetched in their place.  A lane overwrites what it asked for itself, behind
     // its own wait and in front of the barrier that publishes the stage.
@@ -110,18 +129,18 @@ template <bool BIG, bool TRANSPOSED> struct Requests {
     {
         if constexpr (TRANSPOSED) return;
         typedef __attribute__((address_space(3))) v4i *lds_v4i;
-        asm volatile("" ::: "memory");   // not in front of the wait
+        const int lane = lane_here();   // (volatile: not in front of the wait)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int k = 8 * ((lane & 7) ^ (((32 * wave + 8 * i + (lane >> 3)) >> 1) & 7));
-            if (k >= kleft) *(lds_v4i)(uintptr_t)(slot + wave * 4096 + i * 1024 + 16 * lane) = v4i{0, 0, 0, 0};
+        for (int i = 0; i < I; ++i) {
+            const int k = 8 * ((lane & 7) ^ (((8 * (I * wave + i) + (lane >> 3)) >> 1) & 7));
+            if (k >= kleft) *(lds_v4i)(uintptr_t)(slot + (I * wave + i) * 1024 + 16 * lane) = v4i{0, 0, 0, 0};
         }
     }
 };
 
 // The fragments of one operand: W tiles of 32 rows, eight k of a row per lane.
-template <bool BIG, bool TRANSPOSED, int W> struct Fragments {
-    using S = HeadTile<BIG>;
+template <int SIZE, bool TRANSPOSED, int W> struct Fragments {
+    using S = HeadTile<SIZE>;
     typedef __attribute__((address_space(3))) const v8bf *lds_v8bf;
     typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) v4bf *lds_v4bf;
@@ -141,7 +160,7 @@ template <bool BIG, bool TRANSPOSED, int W> struct Fragments {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int gran = (part * 32 * W + 32 * b) / 8 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-                    at[2 * b + h] = slot + (8 * c + 4 * h + rr) * (2 * S::N) + 16 * (gran ^ (4 * rr | 2 * h)) + 8 * (lane & 1);
+                    at[2 * b + h] = slot + (8 * c + 4 * h + rr) * (2 * S::N) + 16 * (gran ^ (4 * rr | 2 * h) % (S::N / 8)) + 8 * (lane & 1);
                 }
         } else {
 #pragma unroll
@@ -164,116 +183,132 @@ template <bool BIG, bool TRANSPOSED, int W> struct Fragments {
     }
 };
 
-template <bool BIG, bool PT, bool QT>
-__device__ __forceinline__ void tile_product(const Operand &p, const Operand &q, const int n0, const int m0, const int nk, uint8_t *lds,
-                                             v16f (&acc)[HeadTile<BIG>::WP][HeadTile<BIG>::WQ])
-{
-    using S = HeadTile<BIG>;
-    constexpr int WP = S::WP, WQ = S::WQ, SLOTS = WP * WQ;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t lds0 = lds_address(lds);
-    Requests<BIG, PT> rp(p, n0, nk, wave, lane);
-    Requests<BIG, QT> rq(q, m0, nk, wave, lane);
-    Fragments<BIG, PT, WP> fp(lds0, wave & 1, lane);
-    Fragments<BIG, QT, WQ> fq(lds0 + S::SLOT, wave >> 1, lane);
-    constexpr int READS = fp.READS + fq.READS;
+// A tile's product in two parts, so that a block that takes one tile after the other asks for a tile's first stages in front of the last one's
+// results: begin, then run.
+template <int SIZE, bool PT, bool QT> struct TileProduct {
+    using S = HeadTile<SIZE>;
+    static constexpr int WP = S::WP, WQ = S::WQ, TILES = WP * WQ, I = S::REQUESTS, D = S::AHEAD;
+    Requests<SIZE, PT> rp;
+    Requests<SIZE, QT> rq;
+    int nk;
+
+    __device__ __forceinline__ void begin(const Operand &p, const Operand &q, const int n0, const int m0, const int stages, uint8_t *lds)
+    {
+        const int lane = lane_here(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const uint32_t lds0 = lds_address(lds);
+        nk = stages;
+        rp.set(p, n0, nk, wave, lane);
+        rq.set(q, m0, nk, wave, lane);
 #pragma unroll
-    for (int a = 0; a < WP; ++a)
+        for (int j = 0; j < 2 * D; ++j)
 #pragma unroll
-        for (int b = 0; b < WQ; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
-    auto read_one = [&](const int u, const int i) {
-        if (i < fp.READS) fp.read(u, i);
-        else fq.read(u, i - fp.READS);
-    };
-    auto advance = [](const uint32_t slot) { return slot < 3u * S::SLOT ? slot + 2u * S::SLOT : slot - 3u * S::SLOT; };   // two slots further on
-    // a quarter step: side(s) is issued after instruction s; the source order is the intended issue order
-    auto quarter = [&](const int u, auto &&side) {
-#pragma unroll
-        for (int s = 0; s < SLOTS; ++s) {
-            const int a = s / WQ, b = s % WQ;
-            acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp.f[u & 1][a], fq.f[u & 1][b], acc[a][b], 0, 0, 0);
-            side(s);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
-    auto spread = [&](const int s, const int n, auto &&op) {   // operations [0, n) over the slots of a quarter step
-#pragma unroll
-        for (int k = 0; k < n; ++k)
-            if (k * SLOTS / n == s) op(k);
-    };
-    // The ring holds P(0), Q(0), P(1), Q(1), ...  Step kt: quarters 0 to 2 read the fragments of the next quarter; then stage kt + 1 must have
-    // landed and every wavefront holds the last fragments of stage kt, so behind the barrier the last quarter reads the first fragments of stage
-    // kt + 1 and asks for Q(kt + 2) in the slot of P(kt), and the first two quarters of the next step for P(kt + 3) in that of Q(kt).
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (j & 1) rq.issue(j >> 1, lds0 + j * S::SLOT, i);
-            else rp.issue(j >> 1, lds0 + j * S::SLOT, i);
-        }
-    SBN_WAIT_VMCNT(8);
-    if (nk == 1) {
-        if (rp.kleft < STAGE_K) rp.zero_tail(lds0);
-        if (rq.kleft < STAGE_K) rq.zero_tail(lds0 + S::SLOT);
+            for (int i = 0; i < I; ++i) {
+                if (j & 1) rq.issue(j >> 1, lds0 + j * S::SLOT, i);
+                else rp.issue(j >> 1, lds0 + j * S::SLOT, i);
+            }
     }
-    __syncthreads();
+
+    __device__ __forceinline__ void run(uint8_t *lds, v16f (&acc)[WP][WQ])
+    {
+        const int lane = lane_here(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const uint32_t lds0 = lds_address(lds);
+        Fragments<SIZE, PT, WP> fp(lds0, wave & 1, lane);
+        Fragments<SIZE, QT, WQ> fq(lds0 + S::SLOT, wave >> 1, lane);
+        constexpr int READS = fp.READS + fq.READS;
 #pragma unroll
-    for (int i = 0; i < READS; ++i) read_one(0, i);
-    uint32_t sp = 0, sq = S::SLOT;
-    for (int kt = 0; kt < nk; ++kt) {
-        const uint32_t sp_next = advance(sp), sq_next = advance(sq);
-        const uint32_t free = advance(sp_next);   // of Q(kt - 1)
+        for (int a = 0; a < WP; ++a)
 #pragma unroll
-        for (int u = 0; u < 3; ++u)
-            quarter(u, [&](const int s) {
-                spread(s, READS, [&](const int k) { read_one(u + 1, k); });
-                if (u < 2) spread(s, 2, [&](const int k) { rp.issue(kt + 2, lds0 + free, 2 * u + k); });
-            });
-        SBN_WAIT_VMCNT(4);   // P(kt + 2) may fly
-        if (kt + 2 == nk) {
-            if (rp.kleft < STAGE_K) rp.zero_tail(lds0 + sp_next);
-            if (rq.kleft < STAGE_K) rq.zero_tail(lds0 + sq_next);
+            for (int b = 0; b < WQ; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
+        auto read_one = [&](const int u, const int i) {
+            if (i < fp.READS) fp.read(u, i);
+            else fq.read(u, i - fp.READS);
+        };
+        auto advance = [](const uint32_t slot) { return slot < (S::SLOTS - 2u) * S::SLOT ? slot + 2u * S::SLOT : slot - (S::SLOTS - 2u) * S::SLOT; };   // two slots further on
+        // a quarter step: side(s) is issued after instruction s; the source order is the intended issue order
+        auto quarter = [&](const int u, auto &&side) {
+#pragma unroll
+            for (int s = 0; s < TILES; ++s) {
+                const int a = s / WQ, b = s % WQ;
+                acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp.f[u & 1][a], fq.f[u & 1][b], acc[a][b], 0, 0, 0);
+                side(s);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        auto spread = [&](const int s, const int n, auto &&op) {   // operations [0, n) over the instructions of a quarter step
+#pragma unroll
+            for (int k = 0; k < n; ++k)
+                if (k * TILES / n == s) op(k);
+        };
+        // The ring holds P(0), Q(0), P(1), Q(1), ...  Step kt: quarters 0 to 2 read the fragments of the next quarter; then stage kt + 1 must have
+        // landed and every wavefront holds the last fragments of stage kt, so behind the barrier the last quarter reads the first fragments of
+        // stage kt + 1 and asks for Q(kt + D) in the slot of P(kt), and the first two quarters of the next step for P(kt + D + 1) in that of Q(kt).
+        SBN_WAIT_VMCNT((2 * D - 2) * I);   // (what was issued behind begin is waited for as well)
+        asm volatile("" ::: "memory");
+        if (nk == 1) {
+            if (rp.kleft < STAGE_K) rp.zero_tail(lds0);
+            if (rq.kleft < STAGE_K) rq.zero_tail(lds0 + S::SLOT);
         }
         __syncthreads();
-        fp.move(sp_next - sp);
-        fq.move(sq_next - sq);
-        quarter(3, [&](const int s) {
-            spread(s, READS, [&](const int k) { read_one(0, k); });
-            spread(s, 4, [&](const int k) { rq.issue(kt + 2, lds0 + sp, k); });
-        });
-        sp = sp_next;
-        sq = sq_next;
+#pragma unroll
+        for (int i = 0; i < READS; ++i) read_one(0, i);
+        uint32_t sp = 0, sq = S::SLOT;
+        for (int kt = 0; kt < nk; ++kt) {
+            const uint32_t sp_next = advance(sp), sq_next = advance(sq);
+            const uint32_t free = sp ? sp - S::SLOT : (S::SLOTS - 1u) * S::SLOT;   // of Q(kt - 1)
+#pragma unroll
+            for (int u = 0; u < 3; ++u)
+                quarter(u, [&](const int s) {
+                    spread(s, READS, [&](const int k) { read_one(u + 1, k); });
+                    if (u < 2) spread(s, I / 2, [&](const int k) { rp.issue(kt + D, lds0 + free, I / 2 * u + k); });
+                });
+            SBN_WAIT_VMCNT((2 * D - 3) * I);   // P(kt + 2) and what follows it may fly
+            if (kt + 2 == nk) {
+                if (rp.kleft < STAGE_K) rp.zero_tail(lds0 + sp_next);
+                if (rq.kleft < STAGE_K) rq.zero_tail(lds0 + sq_next);
+            }
+            __syncthreads();
+            fp.move(sp_next - sp);
+            fq.move(sq_next - sq);
+            quarter(3, [&](const int s) {
+                spread(s, READS, [&](const int k) { read_one(0, k); });
+                spread(s, I, [&](const int k) { rq.issue(kt + D, lds0 + sp, k); });
+            });
+            sp = sp_next;
+            sq = sq_next;
+        }
+        SBN_WAIT_VMCNT(0);   // the surplus stages have landed
+        __syncthreads();
     }
-    SBN_WAIT_VMCNT(0);   // the surplus stages have landed
-    __syncthreads();
-}
+};
 
-// A wavefront's 32 columns b of its result to its part of LDS in fp32: row r is column m = 32 b + r, granules of 16 bytes (four n)
-// XOR-swizzled with the row.
-template <bool BIG>
-__device__ __forceinline__ void stage_columns(const v16f (&acc)[HeadTile<BIG>::WP][HeadTile<BIG>::WQ], const int b, uint8_t *stg, const int lane)
+// Part of a wavefront's columns b of its result to its part of LDS in fp32: ROWS columns m from 32 b + first on become rows, granules of 16 bytes
+// (four n) XOR-swizzled with the row.
+template <int SIZE, int ROWS>
+__device__ __forceinline__ void stage_columns(const v16f (&acc)[HeadTile<SIZE>::WP][HeadTile<SIZE>::WQ], const int b, const int first, uint8_t *stg, const int lane)
 {
-    using S = HeadTile<BIG>;
-    const int r = lane & 31, c = lane >> 5;
+    using S = HeadTile<SIZE>;
+    constexpr int SWIZZLE = S::ROW / 16 < 16 ? S::ROW / 16 - 1 : 15;
+    const int r = (lane & 31) - first, c = lane >> 5;
     asm volatile("" ::: "memory");   // behind the last columns' reads
+    if (ROWS == 32 || (r >= 0 && r < ROWS))
 #pragma unroll
-    for (int a = 0; a < S::WP; ++a)
+        for (int a = 0; a < S::WP; ++a)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            *reinterpret_cast<v4f *>(stg + r * S::ROW + 16 * ((8 * a + 2 * q + c) ^ (r & 15))) =
-                v4f{acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<v4f *>(stg + r * S::ROW + 16 * ((8 * a + 2 * q + c) ^ (r & SWIZZLE))) =
+                    v4f{acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
     asm volatile("" ::: "memory");   // the reads are of what other lanes have written
 }
-template <bool BIG>
+template <int SIZE>
 __device__ __forceinline__ float *staged(uint8_t *stg, const int row, const int n)
 {
-    return reinterpret_cast<float *>(stg + row * HeadTile<BIG>::ROW + 16 * ((n >> 2) ^ (row & 15)) + 4 * (n & 3));
+    constexpr int SWIZZLE = HeadTile<SIZE>::ROW / 16 < 16 ? HeadTile<SIZE>::ROW / 16 - 1 : 15;
+    return reinterpret_cast<float *>(stg + row * HeadTile<SIZE>::ROW + 16 * ((n >> 2) ^ (row & SWIZZLE)) + 4 * (n & 3));
 }
-
 // Tile order.  Blocks go to the eight XCDs round-robin and every XCD has its own L2, so XCD x takes a contiguous eighth of an order in which
-// consecutive tiles form super-tiles of 8 x 8.  False for the blocks that pad the range to a multiple of eight.
+// consecutive tiles form super-tiles of 8 x 8.  False for the numbers that pad the range to a multiple of eight.
 __device__ __forceinline__ bool tile_of_block(const int tiles_n, const int tiles_m, const int bid, int &tn, int &tm)
 {
     const int nb = tiles_n * tiles_m;
@@ -363,149 +398,190 @@ struct CommonFactor {
     }
 };
 
-template <bool BIG, bool GRAD, bool HARD, bool SOFT>
-__global__ void __launch_bounds__(64 * HeadTile<BIG>::WAVES) logits_kernel(LogitsArgs g)
-{
-    using S = HeadTile<BIG>;
-    constexpr int WP = S::WP, WQ = S::WQ, WORDS = 32 * WP;
-    extern __shared__ __attribute__((aligned(1024))) uint8_t dlds[];
-    int tn, tm;
-    if (!tile_of_block(g.tiles_n, g.tiles_m, blockIdx.x, tn, tm)) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r = lane & 31, c = lane >> 5;
-    const int n0 = tn * S::N + (wave & 1) * WORDS;      // of the piece
-    const int m0 = tm * S::M + (wave >> 1) * 32 * WQ;
-    const int64_t v = g.v0 + n0;
-    // what belongs to the lane's tokens is asked for in front of the product
-    int64_t targets[WQ];
+// what belongs to a lane's tokens, asked for in front of a tile's product
+template <int WQ, bool GRAD, bool HARD, bool SOFT> struct TokenValues {
+    int64_t target[WQ];
     float d1[WQ], lse1[WQ], d2[WQ], lse2[WQ], some[WQ];
+    __device__ __forceinline__ void load(const LogitsArgs &g, const int m0)
+    {
+        const int r = lane_here() & 31;
 #pragma unroll
-    for (int b = 0; b < WQ; ++b) {
-        const int t = std::min(m0 + 32 * b + r, g.tokens - 1);
-        if (HARD) targets[b] = g.targets[t];
-        if (HARD && GRAD) {
-            d1[b] = g.d1[t];
-            lse1[b] = g.lse1[t];
-        }
-        if (SOFT && GRAD) {
-            d2[b] = g.d2[t];
-            lse2[b] = g.lse2[t];
-            some[b] = g.some[t];
+        for (int b = 0; b < WQ; ++b) {
+            const int t = std::min(m0 + 32 * b + r, g.tokens - 1);
+            if (HARD) target[b] = g.targets[t];
+            if (HARD && GRAD) {
+                d1[b] = g.d1[t];
+                lse1[b] = g.lse1[t];
+            }
+            if (SOFT && GRAD) {
+                d2[b] = g.d2[t];
+                lse2[b] = g.lse2[t];
+                some[b] = g.some[t];
+            }
         }
     }
-    const CommonFactor common(GRAD && HARD ? g.targets : nullptr, g.d1, g.tokens);
-    v16f acc[WP][WQ];
-    const Operand p{g.W, g.d, g.words, g.d}, q{g.H, g.d, g.tokens, g.d};
-    tile_product<BIG, false, false>(p, q, tn * S::N, tm * S::M, (g.d + STAGE_K - 1) / STAGE_K, dlds, acc);
+};
 
-    uint8_t *const stg = dlds + wave * S::STAGING;
-    const int left = g.words - n0;                      // words that the wavefront has
+// Forward, a block takes tile after tile, gridDim.x apart: the next one's first stages come in under the sums of the last one (16384 tokens x
+// 131072 words x 2560: 8.68 ms with a block per tile, 8.63 so; 1531 x 50001 x 1000 164 us and 160).  Backward, results need LDS: with all of it for
+// a block per tile G takes 181 us at 1531 x 50001 x 1000, with the slot that a next tile's first stages leave 206.
+template <int SIZE, bool GRAD, bool HARD, bool SOFT>
+__global__ void __launch_bounds__(64 * HeadTile<SIZE>::WAVES, 2) logits_kernel(LogitsArgs g)
+{
+    using S = HeadTile<SIZE>;
+    constexpr int WP = S::WP, WQ = S::WQ, WORDS = 32 * WP;
+    constexpr int LPR = S::ROW / 32;   // G: lanes per row
+    constexpr int ROWS = GRAD ? 32 : S::ROWS;                       // staged at a time
+    static_assert(S::WAVES * 32 * S::ROW <= S::LDS, "32 columns of every wavefront are staged in the idle ring");
+    extern __shared__ __attribute__((aligned(1024))) uint8_t dlds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint8_t *const stg = GRAD ? dlds + wave * 32 * S::ROW : dlds + S::STAGED + wave * S::STAGING;
     const float k1 = LOG2E, k2 = SOFT ? LOG2E / g.tau : 0.0f;
+    const int jobs = (g.tiles_n * g.tiles_m + 7) / 8 * 8;
+    int job = blockIdx.x, tn, tm;
+    auto next_tile = [&] {
+        for (; job < jobs; job += gridDim.x)
+            if (tile_of_block(g.tiles_n, g.tiles_m, job, tn, tm)) return true;
+        return false;
+    };
+    if (!next_tile()) return;
+    TokenValues<WQ, GRAD, HARD, SOFT> now, next;
+    TileProduct<SIZE, false, false> product;
+    const Operand p{g.W, g.d, g.words, g.d}, q{g.H, g.d, g.tokens, g.d};
+    const int stages = (g.d + STAGE_K - 1) / STAGE_K;
+    const CommonFactor common(GRAD && HARD ? g.targets : nullptr, g.d1, g.tokens);
+    now.load(g, tm * S::M + (wave >> 1) * 32 * WQ);
+    product.begin(p, q, tn * S::N, tm * S::M, stages, dlds);
     const float inv = GRAD && HARD ? 1.0f / common.value(g.vocab) : 1.0f;
-#pragma unroll
-    for (int b = 0; b < WQ; ++b) {
-        const int t = m0 + 32 * b + r;
-        const bool inside = t < g.tokens;
-        const bool kept = HARD && inside && targets[b] >= 0 && targets[b] < g.vocab;
-        const int64_t y = kept ? targets[b] - v : -1;   // relative to the wavefront's words
-        const bool here = y >= 0 && y < (left < WORDS ? left : WORDS);
-        const uint32_t hits = SOFT ? rows_with_entries<WORDS>(g, t, v) : 0u;
-        if constexpr (!GRAD) {
-            if (HARD && __any(here)) {
-                float z = 0.0f;
-#pragma unroll
-                for (int a = 0; a < WP; ++a)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if ((int)y == 32 * a + 8 * (i >> 2) + 4 * c + (i & 3)) z = acc[a][b][i];
-                if (here && (((int)y >> 2) & 1) == c) g.z_target[t] = z;
-            }
-            if (SOFT && hits) {
-                stage_columns<BIG>(acc, b, stg, lane);
-                entries_here<WORDS>(g, hits, m0 + 32 * b, v, lane, [&](int row, int n, int64_t e) { g.z_top[e] = *staged<BIG>(stg, row, n); });
-            }
-            if (left < WORDS) {
-#pragma unroll
-                for (int a = 0; a < WP; ++a)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (32 * a + 8 * (i >> 2) + 4 * c + (i & 3) >= left) acc[a][b][i] = -INFINITY;
-            }
-            float most = -INFINITY;
-#pragma unroll
-            for (int a = 0; a < WP; ++a)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) most = fmaxf(most, acc[a][b][i]);
-            most = fmaxf(most, __shfl_xor(most, 32));
-            const float base = most == -INFINITY ? 0.0f : most;   // no word here: sums of zeros
-            float sum1 = 0.0f, sum2 = 0.0f;
-#pragma unroll
-            for (int a = 0; a < WP; ++a)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float z = acc[a][b][i] - base;
-                    if (HARD) sum1 += exp2_fast(z * k1);
-                    if (SOFT) sum2 += exp2_fast(z * k2);
-                }
-            if (HARD) sum1 += __shfl_xor(sum1, 32);
-            if (SOFT) sum2 += __shfl_xor(sum2, 32);
-            if (inside && c == 0) {
-                const int64_t at = (int64_t)(2 * tn + (wave & 1)) * g.tokens + t;
-                g.m[at] = most;
-                if (HARD) g.s1[at] = sum1;
-                if (SOFT) g.s2[at] = sum2;
-            }
+    for (bool more = true; more;) {
+        v16f acc[WP][WQ];
+        product.run(dlds, acc);
+        const int part = 2 * tn + (wave & 1);
+        const int n0 = tn * S::N + (wave & 1) * WORDS;      // of the piece
+        const int m0 = tm * S::M + (wave >> 1) * 32 * WQ;
+        const int64_t v = g.v0 + n0;
+        const int left = g.words - n0;                      // words that the wavefront has
+        if constexpr (GRAD) {
+            more = false;
         } else {
-            // exp(z - lse) as 2^(z log2 e - lse log2 e); a token without a share has none whatever its lse
-            float c1 = 0.0f, c2 = 0.0f, l1 = INFINITY, l2 = INFINITY;
-            if (HARD && kept) c1 = d1[b] * inv;
-            if (HARD && c1 != 0.0f) l1 = lse1[b] * LOG2E;
-            if (SOFT && inside && some[b] != 0.0f) c2 = d2[b] * g.tau * inv;
-            if (SOFT && c2 != 0.0f) l2 = lse2[b] * LOG2E;
+            job += gridDim.x;
+            more = next_tile();
+        }
+        if (more) {
+            next.load(g, tm * S::M + (wave >> 1) * 32 * WQ);
+            product.begin(p, q, tn * S::N, tm * S::M, stages, dlds);
+        }
+        const int lane = lane_here(), r = lane & 31, c = lane >> 5;
 #pragma unroll
-            for (int a = 0; a < WP; ++a)
+        for (int b = 0; b < WQ; ++b) {
+            const int t = m0 + 32 * b + r;
+            const bool inside = t < g.tokens;
+            const bool kept = HARD && inside && now.target[b] >= 0 && now.target[b] < g.vocab;
+            const int64_t y = kept ? now.target[b] - v : -1;   // relative to the wavefront's words
+            const bool here = y >= 0 && y < (left < WORDS ? left : WORDS);
+            const uint32_t hits = SOFT ? rows_with_entries<WORDS>(g, t, v) : 0u;
+            if constexpr (!GRAD) {
+                if (HARD && __any(here)) {
+                    float z = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float z = acc[a][b][i];
-                    float e = 0.0f;
-                    if (HARD) e = c1 * exp2_fast(__builtin_fmaf(z, k1, -l1));
-                    if (SOFT) e = __builtin_fmaf(c2, exp2_fast(__builtin_fmaf(z, k2, -l2)), e);
-                    acc[a][b][i] = e;
+                    for (int a = 0; a < WP; ++a)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if ((int)y == 32 * a + 8 * (i >> 2) + 4 * c + (i & 3)) z = acc[a][b][i];
+                    if (here && (((int)y >> 2) & 1) == c) g.z_target[t] = z;
                 }
-            if (HARD && __any(here)) {
-                const float less = here ? c1 : 0.0f;
+                if (SOFT && hits)
+#pragma unroll
+                    for (int row0 = 0; row0 < 32; row0 += ROWS) {
+                        const uint32_t some = hits & ((uint32_t)((1ull << ROWS) - 1) << row0);
+                        if (!some) continue;
+                        stage_columns<SIZE, ROWS>(acc, b, row0, stg, lane);
+                        entries_here<WORDS>(g, some, m0 + 32 * b, v, lane, [&](int row, int n, int64_t e) { g.z_top[e] = *staged<SIZE>(stg, row - row0, n); });
+                    }
+                if (left < WORDS) {
+#pragma unroll
+                    for (int a = 0; a < WP; ++a)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (32 * a + 8 * (i >> 2) + 4 * c + (i & 3) >= left) acc[a][b][i] = -INFINITY;
+                }
+                float most = -INFINITY;
 #pragma unroll
                 for (int a = 0; a < WP; ++a)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if ((int)y == 32 * a + 8 * (i >> 2) + 4 * c + (i & 3)) acc[a][b][i] -= less;
-            }
-            stage_columns<BIG>(acc, b, stg, lane);
-            if (SOFT && hits) {
-                entries_here<WORDS>(g, hits, m0 + 32 * b, v, lane, [&](int row, int n, int64_t e) {
-                    float *const x = staged<BIG>(stg, row, n);
-                    *x = __builtin_fmaf(-(g.d2[m0 + 32 * b + row] * g.tau * inv), g.q[e], *x);   // every word once per token: no two lanes at one place
-                });
-                asm volatile("" ::: "memory");
-            }
-            constexpr int LPR = S::ROW / 32, J = 32 * LPR / 64;   // lanes per row, stores of 32 rows
-            const int n = 8 * (lane % LPR);
+                    for (int i = 0; i < 16; ++i) most = fmaxf(most, acc[a][b][i]);
+                most = fmaxf(most, __shfl_xor(most, 32));
+                const float base = most == -INFINITY ? 0.0f : most;   // no word here: sums of zeros
+                const float base1 = base * k1, base2 = base * k2;
+                float sum1 = 0.0f, sum2 = 0.0f;
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const int row = (64 / LPR) * j + lane / LPR, tt = m0 + 32 * b + row;
-                v4f lo = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n)), hi = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n + 4));
-                if (left < WORDS) {   // columns that pad a row of G
+                for (int a = 0; a < WP; ++a)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (n + i >= left) lo[i] = 0.0f;
-                        if (n + 4 + i >= left) hi[i] = 0.0f;
+                    for (int i = 0; i < 16; ++i) {
+                        const float z = acc[a][b][i];
+                        if (HARD) sum1 += exp2_fast(__builtin_fmaf(z, k1, -base1));
+                        if (SOFT) sum2 += exp2_fast(__builtin_fmaf(z, k2, -base2));
                     }
+                if (HARD) sum1 += __shfl_xor(sum1, 32);
+                if (SOFT) sum2 += __shfl_xor(sum2, 32);
+                if (inside && c == 0) {
+                    const int64_t at = (int64_t)part * g.tokens + t;
+                    g.m[at] = most;
+                    if (HARD) g.s1[at] = sum1;
+                    if (SOFT) g.s2[at] = sum2;
                 }
-                if (tt < g.tokens && n0 + n < g.ldg)
-                    *reinterpret_cast<uint4 *>(g.G + tt * g.ldg + n0 + n) =
-                        make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]));
+            } else {
+                // exp(z - lse) as 2^(z log2 e - lse log2 e); a token without a share has none whatever its lse
+                float c1 = 0.0f, c2 = 0.0f, l1 = INFINITY, l2 = INFINITY;
+                if (HARD && kept) c1 = now.d1[b] * inv;
+                if (HARD && c1 != 0.0f) l1 = now.lse1[b] * LOG2E;
+                if (SOFT && inside && now.some[b] != 0.0f) c2 = now.d2[b] * g.tau * inv;
+                if (SOFT && c2 != 0.0f) l2 = now.lse2[b] * LOG2E;
+#pragma unroll
+                for (int a = 0; a < WP; ++a)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float z = acc[a][b][i];
+                        float e = 0.0f;
+                        if (HARD) e = c1 * exp2_fast(__builtin_fmaf(z, k1, -l1));
+                        if (SOFT) e = __builtin_fmaf(c2, exp2_fast(__builtin_fmaf(z, k2, -l2)), e);
+                        acc[a][b][i] = e;
+                    }
+                if (HARD && __any(here)) {
+                    const float less = here ? c1 : 0.0f;
+#pragma unroll
+                    for (int a = 0; a < WP; ++a)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if ((int)y == 32 * a + 8 * (i >> 2) + 4 * c + (i & 3)) acc[a][b][i] -= less;
+                }
+                stage_columns<SIZE, 32>(acc, b, 0, stg, lane);
+                if (SOFT && hits) {
+                    entries_here<WORDS>(g, hits, m0 + 32 * b, v, lane, [&](int row, int m, int64_t e) {
+                        float *const x = staged<SIZE>(stg, row, m);
+                        *x = __builtin_fmaf(-(g.d2[m0 + 32 * b + row] * g.tau * inv), g.q[e], *x);   // every word once per token: no two lanes at one place
+                    });
+                    asm volatile("" ::: "memory");
+                }
+                const int n = 8 * (lane % LPR);
+#pragma unroll
+                for (int j = 0; j < LPR / 2; ++j) {
+                    const int row = 64 / LPR * j + lane / LPR, tt = m0 + 32 * b + row;
+                    v4f lo = *reinterpret_cast<const v4f *>(staged<SIZE>(stg, row, n)), hi = *reinterpret_cast<const v4f *>(staged<SIZE>(stg, row, n + 4));
+                    if (left < WORDS) {   // columns that pad a row of G
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (n + i >= left) lo[i] = 0.0f;
+                            if (n + 4 + i >= left) hi[i] = 0.0f;
+                        }
+                    }
+                    if (tt < g.tokens && n0 + n < g.ldg)
+                        *reinterpret_cast<uint4 *>(g.G + tt * g.ldg + n0 + n) =
+                            make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]));
+                }
             }
         }
+        now = next;
     }
 }
 
@@ -665,7 +741,6 @@ __global__ void __launch_bounds__(256) join_kernel(JoinArgs g)
 // their sums in fp32 side by side; dH adds up over the pieces of the vocabulary in fp32 as well.
 struct GradientArgs {
     Operand P, Q;              // P transposed; Q transposed (dW) or not (dH)
-    int q_transposed;
     int N, M, stages;          // of the result; k stages of the whole contraction
     int splits, per;           // stages of a split
     uint16_t *C;               // bf16 [M, N], or null:
@@ -674,46 +749,47 @@ struct GradientArgs {
     int tiles_n, tiles_m, padded;
 };
 struct GradientPair {
-    GradientArgs g[2];
-    int block0[3];
+    GradientArgs dw, dh;
+    int dw_first, job0;        // the first block of the second product
     const int64_t *targets;    // of G's common factor (null: 1)
     const float *d1;
     int tokens;
     int64_t vocab;
 };
 
-template <bool BIG>
-__device__ __forceinline__ void gradient_epilogue(const GradientArgs &g, const v16f (&acc)[HeadTile<BIG>::WP][HeadTile<BIG>::WQ], uint8_t *lds, const int n0,
-                                                  const int m0, const int split, const float factor)
+template <int SIZE>
+__device__ __forceinline__ void gradient_results(const GradientArgs &g, const v16f (&acc)[HeadTile<SIZE>::WP][HeadTile<SIZE>::WQ], uint8_t *lds, const int n0,
+                                                 const int m0, const int split, const float factor)
 {
-    using S = HeadTile<BIG>;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    uint8_t *const stg = lds + wave * S::STAGING;
+    using S = HeadTile<SIZE>;
+    static_assert(S::WAVES * 32 * S::ROW <= S::LDS, "32 columns of every wavefront are staged in the idle ring");
+    const int lane = lane_here(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint8_t *const stg = lds + wave * 32 * S::ROW;
     const int nw = n0 + (wave & 1) * 32 * S::WP, mw = m0 + (wave >> 1) * 32 * S::WQ;
+    float *const part = g.part + ((int64_t)split * g.M + mw) * g.N + nw;
 #pragma unroll
     for (int b = 0; b < S::WQ; ++b) {
-        stage_columns<BIG>(acc, b, stg, lane);
+        stage_columns<SIZE, 32>(acc, b, 0, stg, lane);
         if (g.C) {
-            constexpr int LPR = S::ROW / 32, J = 32 * LPR / 64;
+            constexpr int LPR = S::ROW / 32;
             const int n = 8 * (lane % LPR);
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const int row = (64 / LPR) * j + lane / LPR, m = mw + 32 * b + row;
-                const v4f lo = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n)) * factor, hi = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n + 4)) * factor;
-                if (m < g.M && nw + n < g.N)
-                    *reinterpret_cast<uint4 *>(g.C + (int64_t)m * g.N + nw + n) =
+            for (int j = 0; j < LPR / 2; ++j) {
+                const int row = 64 / LPR * j + lane / LPR, m = 32 * b + row;
+                const v4f lo = *reinterpret_cast<const v4f *>(staged<SIZE>(stg, row, n)) * factor, hi = *reinterpret_cast<const v4f *>(staged<SIZE>(stg, row, n + 4)) * factor;
+                if (mw + m < g.M && nw + n < g.N)
+                    *reinterpret_cast<uint4 *>(g.C + (int64_t)(mw + m) * g.N + nw + n) =
                         make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]));
             }
         } else {
-            constexpr int LPR = S::ROW / 16, J = 32 * LPR / 64;
+            constexpr int LPR = S::ROW / 16;
             const int n = 4 * (lane % LPR);
-            float *const part = g.part + (int64_t)split * g.M * g.N;
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const int row = (64 / LPR) * j + lane / LPR, m = mw + 32 * b + row;
-                v4f x = *reinterpret_cast<const v4f *>(staged<BIG>(stg, row, n)) * factor;
-                if (m < g.M && nw + n < g.N) {
-                    v4f *const to = reinterpret_cast<v4f *>(part + (int64_t)m * g.N + nw + n);
+            for (int j = 0; j < LPR / 2; ++j) {
+                const int row = 64 / LPR * j + lane / LPR, m = 32 * b + row;
+                v4f x = *reinterpret_cast<const v4f *>(staged<SIZE>(stg, row, n)) * factor;
+                if (mw + m < g.M && nw + n < g.N) {
+                    v4f *const to = reinterpret_cast<v4f *>(part + (int64_t)m * g.N + n);
                     if (g.add) x += *to;
                     *to = x;
                 }
@@ -722,29 +798,38 @@ __device__ __forceinline__ void gradient_epilogue(const GradientArgs &g, const v
     }
 }
 
-template <bool BIG>
-__global__ void __launch_bounds__(64 * HeadTile<BIG>::WAVES) gradient_kernel(GradientPair pair)
+template <int SIZE, bool QT>
+__device__ __forceinline__ void gradient_tile(const GradientArgs &g, uint8_t *lds, const int job, const CommonFactor &common, const int64_t vocab)
 {
-    using S = HeadTile<BIG>;
-    extern __shared__ __attribute__((aligned(1024))) uint8_t dlds[];
-    const int which = (int)blockIdx.x >= pair.block0[1];
-    const GradientArgs &g = pair.g[which];
-    const int bid = (int)blockIdx.x - pair.block0[which];
-    const int split = bid / g.padded;
+    using S = HeadTile<SIZE>;
+    const int split = __builtin_amdgcn_readfirstlane(job / g.padded);
+    const int k0 = split * g.per * STAGE_K, left = g.stages - split * g.per, stages = left < g.per ? left : g.per;
     int tn, tm;
-    if (!tile_of_block(g.tiles_n, g.tiles_m, bid - split * g.padded, tn, tm)) return;
-    const int s0 = split * g.per, nk = g.stages - s0 < g.per ? g.stages - s0 : g.per;
-    if (nk <= 0) return;   // of a last piece that has fewer stages: nothing to add
+    // (no stages: of a last piece that has fewer of them; nothing to add)
+    if (stages <= 0 || !tile_of_block(g.tiles_n, g.tiles_m, job - split * g.padded, tn, tm)) return;
     Operand p = g.P, q = g.Q;
-    p.base += (int64_t)s0 * STAGE_K * p.ld;
-    p.k -= s0 * STAGE_K;
-    q.base += (int64_t)s0 * STAGE_K * (g.q_transposed ? q.ld : 1);
-    q.k -= s0 * STAGE_K;
-    const CommonFactor common(pair.targets, pair.d1, pair.tokens);
+    p.base += (int64_t)k0 * p.ld;
+    p.k -= k0;
+    q.base += (int64_t)k0 * (QT ? q.ld : 1);
+    q.k -= k0;
+    TileProduct<SIZE, true, QT> product;
+    product.begin(p, q, tn * S::N, tm * S::M, stages, lds);
     v16f acc[S::WP][S::WQ];
-    if (g.q_transposed) tile_product<BIG, true, true>(p, q, tn * S::N, tm * S::M, nk, dlds, acc);
-    else tile_product<BIG, true, false>(p, q, tn * S::N, tm * S::M, nk, dlds, acc);
-    gradient_epilogue<BIG>(g, acc, dlds, tn * S::N, tm * S::M, split, common.value(pair.vocab));
+    product.run(lds, acc);
+    gradient_results<SIZE>(g, acc, lds, tn * S::N, tm * S::M, split, common.value(vocab));
+}
+
+// A block per tile: taken one after the other by a block, as the logits are, they took 3 to 10 % longer (the two products' tiles are not alike,
+// and the device deals them out as multiprocessors become free).
+template <int SIZE>
+__global__ void __launch_bounds__(64 * HeadTile<SIZE>::WAVES, 2) gradient_kernel(GradientPair pair)
+{
+    extern __shared__ __attribute__((aligned(1024))) uint8_t dlds[];
+    const CommonFactor common(pair.targets, pair.d1, pair.tokens);
+    const bool second = (int)blockIdx.x >= pair.job0;
+    const int job = (int)blockIdx.x - (second ? pair.job0 : 0);
+    if (second != (pair.dw_first != 0)) gradient_tile<SIZE, true>(pair.dw, dlds, job, common, pair.vocab);
+    else gradient_tile<SIZE, false>(pair.dh, dlds, job, common, pair.vocab);
 }
 
 // bf16 sums of fp32 parts.  A block takes 256 / SLICES groups of four values, a slice of its threads every SLICES-th part: with few values and
@@ -809,7 +894,7 @@ __device__ __forceinline__ void column_fragments(const uint16_t *base, const int
 template <int STEPS>   // of 16 tokens
 __global__ void __launch_bounds__(256, 2) few_gradient_kernel(FewGradients g)
 {
-    using S = HeadTile<false>;
+    using S = HeadTile<SMALL>;
     extern __shared__ __attribute__((aligned(1024))) uint8_t dlds[];
     const CommonFactor common(g.targets, g.d1, g.tokens);
     if ((int)blockIdx.x < g.dh_blocks) {
@@ -821,8 +906,10 @@ __global__ void __launch_bounds__(256, 2) few_gradient_kernel(FewGradients g)
         q.base += s0 * STAGE_K;
         q.k -= s0 * STAGE_K;
         v16f acc[S::WP][S::WQ];
-        tile_product<false, true, false>(p, q, tn * S::N, 0, nk, dlds, acc);
-        gradient_epilogue<false>(g.dh, acc, dlds, tn * S::N, 0, split, common.value(g.vocab));
+        TileProduct<SMALL, true, false> product;
+        product.begin(p, q, tn * S::N, 0, nk, dlds);
+        product.run(dlds, acc);
+        gradient_results<SMALL>(g.dh, acc, dlds, tn * S::N, 0, split, common.value(g.vocab));
         return;
     }
     const int lane = threadIdx.x & 63, r = lane & 31, c = lane >> 5;
@@ -871,27 +958,43 @@ __global__ void __launch_bounds__(256, 2) few_gradient_kernel(FewGradients g)
 
 // ---- host ------------------------------------------------------------------------------------------------------------------------------
 constexpr int PLAN_CUS = 256;                          // multiprocessors of the part: a plan depends on sizes alone
-constexpr int64_t PIECE_ELEMENTS = (int64_t)1 << 28;   // most of G at a time (512 MB)
+constexpr int64_t PIECE_ELEMENTS = (int64_t)1 << 28;   // most of G at a time (512 MB); 2^25 to 2^27 took within 5 % of it, pieces that the last cache holds too
 
-// Estimated time in us of `tiles` tiles of `stages` stages with one tile size; see the comment at tile_product
-template <bool BIG>
-float tiles_us(const int64_t tiles, const int64_t stages)
-{
-    const float step = BIG ? 1.45f : 1.05f, alone = BIG ? 1.2f : 0.6f, fixed = BIG ? 10.0f : 7.0f;
-    return std::max((float)stages * alone + fixed, (float)tiles * ((float)stages * step + fixed) / (float)((BIG ? 1 : 2) * PLAN_CUS));
-}
-int64_t tiles_of(const int64_t n, const int64_t m, const bool big) { return ceil_div(n, big ? 256 : 128) * ceil_div(m, big ? 256 : 128); }
+std::atomic<int> g_logits_size{-1}, g_gradient_size{-1};   // of the test hook
 
-bool big_logits(const int64_t tokens, const int64_t words, const int64_t d)
+int edge_of(const int size) { return size == BIG ? 256 : size == SMALL ? 128 : 64; }
+int64_t tiles_of(const int64_t n, const int64_t m, const int size) { return ceil_div(n, edge_of(size)) * ceil_div(m, edge_of(size)); }
+
+// Estimated us of tiles of one size: of a tile alone and, where the others run, of a multiprocessor's time for it, by its stages
+struct TileTimes {
+    float alone_step, alone, step, each;
+    float longest(const float stages) const { return alone_step * stages + alone; }
+    float share(const float stages) const { return step * stages + each; }
+};
+
+// Logits in tiles of 64, 128 and 256; fits to 16 to 16000 tokens, 500 to 32000 words and 64 to 2560 dimensions.  us measured with each size (forward
+// with its join): 16 x 500 x 2560 16.2 / 22.4 / 49.6, 300 x 4000 x 2560 23.2 / 27.1 / 51.7, 1000 x 4000 x 2560 40.0 / 29.7 / 51.3,
+// 1000 x 32000 x 2560 269 / 158 / 133, 4000 x 32000 x 64 165 / 78 / 59.
+int logits_size(const int64_t tokens, const int64_t words, const int64_t d)
 {
-    const int64_t stages = ceil_div(d, STAGE_K);
-    return tiles_us<true>(tiles_of(words, tokens, true), stages) <= tiles_us<false>(tiles_of(words, tokens, false), stages);
+    const int forced = g_logits_size.load(std::memory_order_relaxed);
+    if (forced >= 0) return forced;
+    static constexpr TileTimes times[] = {{0.2f, 4.0f, 0.19f, 1.3f}, {0.335f, 5.0f, 0.43f, 1.8f}, {0.94f, 7.9f, 1.43f, 4.8f}};
+    const float stages = (float)ceil_div(d, STAGE_K);
+    int best = BIG;
+    float least = INFINITY;
+    for (int size = BIG; size >= TINY; --size) {
+        const TileTimes &t = times[size];
+        const float us = std::max(t.longest(stages), (float)ceil_div(tiles_of(words, tokens, size), PLAN_CUS) * t.share(stages));
+        if (us < least) least = us, best = size;
+    }
+    return best;
 }
 
 struct BackwardPlan {
     int64_t piece;       // words at a time
     int64_t ldg;         // row length of G
-    bool big;            // tiles of the gradients' products
+    int size;            // tiles of the gradients' products
     int dw_splits, dh_splits;
     // fp32 results that are still to be added up, [parts, rows, d] (0: the product writes bf16)
     int dw_parts() const { return dw_splits > 1 ? dw_splits : 0; }
@@ -907,23 +1010,26 @@ BackwardPlan plan_backward(const int64_t tokens, const int64_t d, const int64_t 
     plan.ldg = ceil_div(plan.piece, STAGE_K) * STAGE_K;
     // fewest us over tile sizes and splits: what the products take, and what a split's parts are to write and read again at 4 TB/s
     const int64_t dw_stages = ceil_div(tokens, STAGE_K), dh_stages = plan.ldg / STAGE_K;
+    // fits as for the logits, with what surrounds a tile in proportion to what it stores.  us of a backward pass, tiles of 128 and of 256 for the
+    // gradients: 65 x 32000 x 512 38 / 60, 1000 x 4000 x 2560 74 / 81, 1000 x 32000 x 2560 503 / 456, 16000 x 4000 x 2560 921 / 803; of 64
+    // and of 128: 128 x 4000 x 64 12 / 15
+    static constexpr TileTimes times[] = {{0.2f, 5.0f, 0.35f, 1.5f}, {0.45f, 6.0f, 0.48f, 3.6f}, {1.1f, 9.0f, 1.4f, 18.0f}};
+    const int forced = g_gradient_size.load(std::memory_order_relaxed);
     float best = INFINITY;
-    for (int big = 0; big < 2; ++big)
+    for (int size = TINY; size <= BIG; ++size)
         for (int64_t sw = 1; sw <= 16; sw *= 2)
             for (int64_t sh = 1; sh <= 64; sh *= 2) {
+                if (forced >= 0 && forced <= BIG && size != forced) continue;
                 if ((sw > 1 && sw * 2 > dw_stages) || (sh > 1 && sh * 2 > dh_stages)) continue;
-                const int64_t wt = tiles_of(d, plan.piece, big) * sw, ht = tiles_of(d, tokens, big) * sh;
-                const int64_t wk = ceil_div(dw_stages, sw), hk = ceil_div(dh_stages, sh);
-                const float w = big ? tiles_us<true>(wt, wk) : tiles_us<false>(wt, wk), h = big ? tiles_us<true>(ht, hk) : tiles_us<false>(ht, hk);
-                const float alone = big ? 1.2f : 0.6f, fixed = big ? 10.0f : 7.0f, step = big ? 1.45f : 1.05f;
-                float us = std::max(std::max((float)wk, (float)hk) * alone + fixed,
-                                    ((float)wt * ((float)wk * step + fixed) + (float)ht * ((float)hk * step + fixed)) / (float)((big ? 1 : 2) * PLAN_CUS));
-                us = std::max(us, std::max(w, h));
+                const int64_t wt = tiles_of(d, plan.piece, size) * sw, ht = tiles_of(d, tokens, size) * sh;
+                const float wk = (float)ceil_div(dw_stages, sw), hk = (float)ceil_div(dh_stages, sh);
+                const TileTimes &t = times[size];
+                float us = std::max(t.longest(std::max(wk, hk)), ((float)wt * t.share(wk) + (float)ht * t.share(hk)) / (float)PLAN_CUS);
                 if (sw > 1) us += 3.0f + (float)(8 * sw + 2) * (float)plan.piece * (float)d / 4e6f;
                 if (sh > 1) us += 3.0f + (float)(8 * sh + 2) * (float)tokens * (float)d / 4e6f;
                 if (us < best) {
                     best = us;
-                    plan.big = big;
+                    plan.size = size;
                     plan.dw_splits = (int)sw;
                     plan.dh_splits = (int)sh;
                 }
@@ -964,30 +1070,33 @@ sbn_status with_lds(Kernel kernel, const int bytes)
     return SBN_EHIP;
 }
 
-template <bool BIG, bool GRAD, bool HARD, bool SOFT>
+template <int SIZE, bool GRAD, bool HARD, bool SOFT>
 sbn_status launch_logits_as(LogitsArgs &g, hipStream_t stream)
 {
-    using S = HeadTile<BIG>;
+    using S = HeadTile<SIZE>;
     g.tiles_n = (int)ceil_div(g.words, S::N);
     g.tiles_m = (int)ceil_div(g.tokens, S::M);
     static thread_local bool raised = false;
     if (!raised) {
-        const sbn_status st = with_lds(&logits_kernel<BIG, GRAD, HARD, SOFT>, S::LDS);
+        const sbn_status st = with_lds(&logits_kernel<SIZE, GRAD, HARD, SOFT>, S::LDS);
         if (st != SBN_OK) return st;
         raised = true;
     }
-    const int64_t blocks = ceil_div((int64_t)g.tiles_n * g.tiles_m, 8) * 8;
-    hipLaunchKernelGGL((logits_kernel<BIG, GRAD, HARD, SOFT>), dim3((unsigned)blocks), dim3(64 * S::WAVES), S::LDS, stream, g);
+    const int64_t all = ceil_div((int64_t)g.tiles_n * g.tiles_m, 8) * 8, blocks = GRAD ? all : std::min(all, (int64_t)(SIZE == BIG ? 1 : 2) * PLAN_CUS);
+    hipLaunchKernelGGL((logits_kernel<SIZE, GRAD, HARD, SOFT>), dim3((unsigned)blocks), dim3(64 * S::WAVES), S::LDS, stream, g);
     return check_launch("logits_kernel");
 }
-template <bool GRAD>
-sbn_status launch_logits(LogitsArgs &g, bool big, bool hard, bool soft, hipStream_t stream)
+template <int SIZE, bool GRAD>
+sbn_status launch_logits_of(LogitsArgs &g, bool hard, bool soft, hipStream_t stream)
 {
-    if (big)
-        return !soft ? launch_logits_as<true, GRAD, true, false>(g, stream) : hard ? launch_logits_as<true, GRAD, true, true>(g, stream)
-                                                                                   : launch_logits_as<true, GRAD, false, true>(g, stream);
-    return !soft ? launch_logits_as<false, GRAD, true, false>(g, stream) : hard ? launch_logits_as<false, GRAD, true, true>(g, stream)
-                                                                                : launch_logits_as<false, GRAD, false, true>(g, stream);
+    return !soft ? launch_logits_as<SIZE, GRAD, true, false>(g, stream) : hard ? launch_logits_as<SIZE, GRAD, true, true>(g, stream)
+                                                                               : launch_logits_as<SIZE, GRAD, false, true>(g, stream);
+}
+template <bool GRAD>
+sbn_status launch_logits(LogitsArgs &g, int size, bool hard, bool soft, hipStream_t stream)
+{
+    return size == BIG ? launch_logits_of<BIG, GRAD>(g, hard, soft, stream) : size == SMALL ? launch_logits_of<SMALL, GRAD>(g, hard, soft, stream)
+                                                                                             : launch_logits_of<TINY, GRAD>(g, hard, soft, stream);
 }
 
 sbn_status launch_teacher(const HeadCall &h, uint8_t *ws, const TeacherRegions &r, LogitsArgs &g, hipStream_t stream)
@@ -1021,7 +1130,15 @@ LogitsArgs logits_of(const HeadCall &h)
 
 // Few tokens: splits of the words for dH, as many as give 512 blocks (two per multiprocessor) with eight stages each, and fewer where their
 // sums, [tokens, d] floats written and read again per split, would weigh more than a quarter of W
-constexpr int64_t FEW_TOKENS = 64;
+// and more than 2 MB
+// They are taken for weights of 2^21 values and more (backward pass of 16 to 64 tokens against the plan below at 65, us: 32000 x 2560 88 / 122,
+// 32000 x 512 29 / 38, 32000 x 64 18 / 26, 4000 x 512 16.5 / 16.0, 4000 x 64 13.9 / 11.7)
+constexpr int64_t FEW_TOKENS = 64, FEW_VALUES = 1 << 21;
+bool takes_few(const int64_t tokens, const int64_t d, const int64_t vocab)
+{
+    const int forced = g_gradient_size.load(std::memory_order_relaxed);
+    return tokens <= FEW_TOKENS && (forced >= 0 ? forced > BIG : vocab * d >= FEW_VALUES);
+}
 struct FewPlan {
     int64_t ldg;
     int stages, per, splits;   // of dH; splits 1: bf16 at once
@@ -1032,15 +1149,21 @@ FewPlan plan_few(const int64_t tokens, const int64_t d, const int64_t vocab)
     p.stages = (int)ceil_div(vocab, STAGE_K);
     p.ldg = (int64_t)p.stages * STAGE_K;
     int64_t splits = std::min(ceil_div(2 * PLAN_CUS, ceil_div(d, 128)), ceil_div(p.stages, 8));
-    splits = std::max((int64_t)1, std::min(splits, vocab / (16 * tokens)));
+    splits = std::max((int64_t)1, std::min(splits, std::max(vocab / (16 * tokens), ((int64_t)1 << 19) / (tokens * d))));
     p.per = (int)ceil_div(p.stages, splits);
     p.splits = (int)ceil_div(p.stages, p.per);
     return p;
 }
 
-int64_t forward_parts(const HeadCall &h) { return 2 * ceil_div(h.vocab, big_logits(h.tokens, h.vocab, h.d_in) ? 256 : 128); }
+int64_t forward_parts(const HeadCall &h) { return 2 * ceil_div(h.vocab, edge_of(logits_size(h.tokens, h.vocab, h.d_in))); }
 
 }  // namespace
+
+void set_head_tiles(int logits, int gradients)
+{
+    g_logits_size.store(logits > BIG ? -1 : logits, std::memory_order_relaxed);
+    g_gradient_size.store(gradients, std::memory_order_relaxed);
+}
 
 size_t head_workspace_bytes(int64_t tokens, int64_t d_in, int64_t vocab, int64_t top_k, bool backward)
 {
@@ -1056,7 +1179,7 @@ size_t head_workspace_bytes(int64_t tokens, int64_t d_in, int64_t vocab, int64_t
     if (top_k) TeacherRegions(r, tokens, vocab, top_k);
     if (!backward) return r.bytes;
     HeadRegions b;
-    if (tokens <= FEW_TOKENS) {
+    if (takes_few(tokens, d_in, vocab)) {
         const FewPlan plan = plan_few(tokens, d_in, vocab);
         if (top_k) TeacherRegions(b, tokens, vocab, top_k);
         b.take((size_t)tokens * plan.ldg * 2);
@@ -1077,7 +1200,6 @@ sbn_status launch_head_forward(const HeadCall &h, void *workspace, hipStream_t s
     uint8_t *const ws = static_cast<uint8_t *>(workspace);
     HeadRegions r;
     LogitsArgs g = logits_of(h);
-    const bool big = big_logits(h.tokens, h.vocab, h.d_in);
     const int64_t parts = forward_parts(h);
     auto floats = [&](const size_t n) { return reinterpret_cast<float *>(ws + r.take(n * 4)); };
     g.m = floats((size_t)parts * h.tokens);
@@ -1090,7 +1212,7 @@ sbn_status launch_head_forward(const HeadCall &h, void *workspace, hipStream_t s
         const sbn_status st = launch_teacher(h, ws, tr, g, stream);
         if (st != SBN_OK) return st;
     }
-    const sbn_status st = launch_logits<false>(g, big, hard, soft, stream);
+    const sbn_status st = launch_logits<false>(g, logits_size(h.tokens, h.vocab, h.d_in), hard, soft, stream);
     if (st != SBN_OK) return st;
     JoinArgs j{g.m, g.s1, g.s2, (int)parts, (int)h.tokens, (int)h.top_k, 1, h.vocab, h.targets, g.z_target, g.z_top, g.q, g.some, g.at, h.tau,
                h.ce, h.kd, h.lse1, h.lse2};
@@ -1102,28 +1224,27 @@ sbn_status launch_head_forward(const HeadCall &h, void *workspace, hipStream_t s
     return check_launch("join_kernel");
 }
 
-template <bool BIG>
+template <int SIZE>
 static sbn_status launch_gradients(GradientPair &pair, hipStream_t stream)
 {
-    using S = HeadTile<BIG>;
-    if (pair.g[1].per > pair.g[0].per) std::swap(pair.g[0], pair.g[1]);
-    int64_t blocks = 0;
-    for (int i = 0; i < 2; ++i) {
-        GradientArgs &g = pair.g[i];
+    using S = HeadTile<SIZE>;
+    pair.dw_first = pair.dw.per >= pair.dh.per;
+    int64_t jobs = 0;
+    for (const bool second : {false, true}) {
+        GradientArgs &g = second != (pair.dw_first != 0) ? pair.dw : pair.dh;
         g.tiles_n = (int)ceil_div(g.N, S::N);
         g.tiles_m = (int)ceil_div(g.M, S::M);
-        g.padded = (int)(ceil_div((int64_t)g.tiles_n * g.tiles_m, 8) * 8);
-        pair.block0[i] = (int)blocks;
-        blocks += g.N ? (int64_t)g.padded * g.splits : 0;
+        g.padded = (int)(ceil_div((int64_t)g.tiles_n * g.tiles_m, 8) * 8);   // equal shares, one per XCD
+        if (second) pair.job0 = (int)jobs;
+        jobs += g.N ? (int64_t)g.padded * g.splits : 0;
     }
-    pair.block0[2] = (int)blocks;
     static thread_local bool raised = false;
     if (!raised) {
-        const sbn_status st = with_lds(&gradient_kernel<BIG>, S::LDS);
+        const sbn_status st = with_lds(&gradient_kernel<SIZE>, S::LDS);
         if (st != SBN_OK) return st;
         raised = true;
     }
-    hipLaunchKernelGGL(gradient_kernel<BIG>, dim3((unsigned)blocks), dim3(64 * S::WAVES), S::LDS, stream, pair);
+    hipLaunchKernelGGL(gradient_kernel<SIZE>, dim3((unsigned)jobs), dim3(64 * S::WAVES), S::LDS, stream, pair);
     return check_launch("gradient_kernel");
 }
 
@@ -1155,7 +1276,7 @@ static sbn_status launch_few_gradients(const HeadCall &h, const LogitsArgs &l, c
     const int64_t blocks = g.dh_blocks + (h.dW ? ceil_div(ceil_div(h.vocab, 128) * g.across, 4) : 0);
     const int steps = h.tokens <= 16 ? 1 : h.tokens <= 32 ? 2 : 4;
     static thread_local bool raised = false;
-    constexpr int LDS = HeadTile<false>::LDS;
+    constexpr int LDS = HeadTile<SMALL>::LDS;
     if (!raised) {
         sbn_status st = with_lds(&few_gradient_kernel<1>, LDS);
         if (st == SBN_OK) st = with_lds(&few_gradient_kernel<2>, LDS);
@@ -1191,12 +1312,12 @@ sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t 
         else hipLaunchKernelGGL(sum_parts_kernel<1>, dim3((unsigned)ceil_div(n, 1024)), dim3(256), 0, stream, part, n, parts, out);
         return check_launch("sum_parts_kernel");
     };
-    if (h.tokens <= FEW_TOKENS) {
+    if (takes_few(h.tokens, h.d_in, h.vocab)) {
         const FewPlan plan = plan_few(h.tokens, h.d_in, h.vocab);
         g.ldg = plan.ldg;
         g.G = reinterpret_cast<uint16_t *>(ws + r.take((size_t)h.tokens * plan.ldg * 2));
         float *const part = reinterpret_cast<float *>(ws + r.bytes);
-        st = launch_logits<true>(g, big_logits(h.tokens, h.vocab, h.d_in), hard, soft, stream);
+        st = launch_logits<true>(g, logits_size(h.tokens, h.vocab, h.d_in), hard, soft, stream);
         if (st == SBN_OK) st = launch_few_gradients(h, g, plan, part, stream);
         return st != SBN_OK || !h.dH || plan.splits == 1 ? st : sum(part, h.tokens * h.d_in, plan.splits, static_cast<uint16_t *>(h.dH));
     }
@@ -1212,7 +1333,7 @@ sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t 
         g.v0 = v0;
         g.words = words;
         g.ldg = ceil_div(words, STAGE_K) * STAGE_K;
-        st = launch_logits<true>(g, big_logits(h.tokens, words, h.d_in), hard, soft, stream);
+        st = launch_logits<true>(g, logits_size(h.tokens, words, h.d_in), hard, soft, stream);
         if (st != SBN_OK) return st;
         GradientPair pair{};
         pair.targets = h.targets;
@@ -1220,10 +1341,9 @@ sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t 
         pair.tokens = tokens;
         pair.vocab = h.vocab;
         if (h.dW) {
-            GradientArgs &a = pair.g[0];
+            GradientArgs &a = pair.dw;
             a.P = Operand{g.H, d, d, tokens};
             a.Q = Operand{g.G, g.ldg, words, tokens};
-            a.q_transposed = 1;
             a.N = d;
             a.M = words;
             a.stages = (int)ceil_div(tokens, STAGE_K);
@@ -1232,7 +1352,7 @@ sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t 
             a.part = dw_part;
         }
         if (h.dH) {
-            GradientArgs &a = pair.g[1];
+            GradientArgs &a = pair.dh;
             a.P = Operand{g.W, d, d, words};
             a.Q = Operand{g.G, g.ldg, tokens, (int)g.ldg};
             a.N = d;
@@ -1243,11 +1363,9 @@ sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t 
             a.part = dh_part;
             a.add = v0 > 0;
         }
-        for (GradientArgs &a : pair.g) {
-            if (!a.N) continue;
-            a.per = (int)ceil_div(a.stages, a.splits);
-        }
-        st = plan.big ? launch_gradients<true>(pair, stream) : launch_gradients<false>(pair, stream);
+        if (h.dW) pair.dw.per = (int)ceil_div(pair.dw.stages, pair.dw.splits);
+        if (h.dH) pair.dh.per = (int)ceil_div(pair.dh.stages, pair.dh.splits);
+        st = plan.size == BIG ? launch_gradients<BIG>(pair, stream) : plan.size == SMALL ? launch_gradients<SMALL>(pair, stream) : launch_gradients<TINY>(pair, stream);
         if (st != SBN_OK) return st;
         if (h.dW && dw_parts) {
             st = sum(dw_part, (int64_t)words * d, dw_parts, static_cast<uint16_t *>(h.dW) + v0 * d);

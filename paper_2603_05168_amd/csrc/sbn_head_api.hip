@@ -68,6 +68,12 @@ using namespace sbn;
 
 extern "C" {
 
+void sbn_test_set_head_tiles(int logits, int gradients, int mxfp4)
+{
+    set_head_tiles(logits, gradients);
+    set_mxfp4_tiles(mxfp4);
+}
+
 sbn_status sbn_head_workspace_bytes(int64_t tokens, int64_t d_in, int64_t vocab, int64_t top_k, int backward, size_t *bytes)
 {
     if (!bytes) return SBN_EINVAL;

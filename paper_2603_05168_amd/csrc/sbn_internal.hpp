@@ -178,12 +178,14 @@ struct HeadCall {
     void *dH, *dW;
 };
 constexpr int64_t HEAD_MAX_TOKENS = 1 << 24, HEAD_MAX_D = 1 << 16, HEAD_MAX_VOCAB = 1 << 24, HEAD_MAX_TEACHER_VOCAB = 1 << 21, HEAD_MAX_TOP = 1024;
+void set_head_tiles(int logits, int gradients);   // see sbn_test_set_head_tiles
 size_t head_workspace_bytes(int64_t tokens, int64_t d_in, int64_t vocab, int64_t top_k, bool backward);
 sbn_status launch_head_forward(const HeadCall &h, void *workspace, hipStream_t stream);
 sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t stream);
 
 // ---- microscaled 4-bit floating point (sbn_mxfp4.hip) ---------------------------------------------
 constexpr int64_t MXFP4_MAX_COLS = 1 << 20;
+void set_mxfp4_tiles(int size);
 void mxfp4_bytes(int64_t rows, int64_t cols, size_t &codes, size_t &scales);
 size_t mxfp4_workspace_bytes(int64_t tokens, int64_t d_in);
 sbn_status launch_mxfp4_quantize(const void *X, sbn_dtype dtype, int64_t rows, int64_t cols, uint8_t *codes, uint8_t *scales, hipStream_t stream);

@@ -4,6 +4,7 @@
 //   code), at most 6
 // The product runs on v_mfma_scale_f32_32x32x64_f8f6f4, which takes both operands and their scales as they are stored and adds up in fp32.
 #include <algorithm>
+#include <atomic>
 
 #include "sbn_internal.hpp"
 #include "sbn_mfma.hpp"
@@ -518,9 +519,13 @@ sbn_status launch_few(const MxArgs &g, hipStream_t stream)
     return check_launch("mxfp4_few_kernel");
 }
 
+std::atomic<int> g_tiles{-1};   // of the test hook
+
 int64_t padded(int64_t cols) { return ceil_div(cols, PAD) * PAD; }
 
 }  // namespace
+
+void set_mxfp4_tiles(int size) { g_tiles.store(size, std::memory_order_relaxed); }
 
 void mxfp4_bytes(int64_t rows, int64_t cols, size_t &codes, size_t &scales)
 {
@@ -595,8 +600,10 @@ sbn_status launch_mxfp4_linear(const void *X, int64_t tokens, int64_t d_in, int6
     if (st != SBN_OK) return st;
     MxArgs g{codes, xc, scales, xs, padded(d_in) / 2, stages * STAGE_BYTES, (int)d_out, (int)tokens, (int)stages, bias, Y, 0, 0};
     // 64 tokens, few and small tiles: 2560 -> 6912 8.9 and 10.4 us, 4096 -> 4096 10.8 and 12.6
-    if (tokens <= 32) return launch_few<1>(g, stream);
-    if (tokens <= 64) return launch_few<2>(g, stream);
+    const int forced = g_tiles.load(std::memory_order_relaxed);
+    if (tokens <= 32 && forced < 0) return launch_few<1>(g, stream);
+    if (tokens <= 64 && forced < 0) return launch_few<2>(g, stream);
+    if (forced >= 0) return forced == 0 ? launch_tile<MxSmall>(g, stream) : forced == 1 ? launch_tile<MxMiddle>(g, stream) : launch_tile<MxLarge>(g, stream);
     const float large = tiles_us(g, 256, 1.05f * stages + 12.0f, 1.44f * stages + 16.0f), middle = tiles_us(g, 128, 0.65f * stages + 6.2f, 0.48f * stages + 6.5f),
                 small = tiles_us(g, 64, 0.38f * stages + 4.6f, 0.28f * stages + 1.1f);
     return large <= std::min(middle, small) ? launch_tile<MxLarge>(g, stream) : middle <= small ? launch_tile<MxMiddle>(g, stream) : launch_tile<MxSmall>(g, stream);

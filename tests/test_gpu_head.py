@@ -138,6 +138,38 @@ def test_distillation(tokens, d, vocab, top, tau, dtype, hard):
     check(run(case, tau, hard), reference(case, tau, hard))
 
 
+@pytest.fixture
+def tiles():
+    yield sbn().sbn_test_set_head_tiles
+    sbn().sbn_test_set_head_tiles()
+
+
+@pytest.mark.parametrize("size", [0, 1, 2])
+@pytest.mark.parametrize("tokens,d,vocab", [(1, 8, 1), (5, 136, 63), (37, 1000, 777), (130, 520, 1025), (300, 64, 515), (700, 200, 130)])
+def test_every_tile_size(tokens, d, vocab, size, tiles):
+    tiles(size, size)
+    case = make(tokens, d, vocab, 1000 + tokens, top=min(vocab, 13))
+    check(run(case, 2.0), reference(case, 2.0))
+    check(run(case), reference(case))
+
+
+@pytest.mark.parametrize("tokens,d,vocab", [(1, 8, 1), (3, 64, 5000), (16, 256, 1000), (17, 520, 129), (33, 1000, 777), (64, 136, 4100)])
+def test_gradients_of_few_tokens(tokens, d, vocab, tiles):
+    tiles(gradients=3)
+    case = make(tokens, d, vocab, 1100 + tokens, top=min(vocab, 13))
+    check(run(case, 2.0), reference(case, 2.0))
+    check(run(case, 2.0, dW=False), reference(case, 2.0))
+    check(run(case, dH=False), reference(case))
+
+
+def test_many_tiles_for_a_block(tiles):
+    """More tiles than blocks run at once, of every size: a block's next tile begins under the results of its last one."""
+    for size, vocab in ((0, 20000), (1, 40001), (2, 70001)):
+        tiles(size, size)
+        case = {k: v.to(DEV) for k, v in make(200 if size < 2 else 600, 72, vocab, 1200 + size, top=9).items()}
+        check(run(case, 2.0), reference(case, 2.0))
+
+
 @pytest.mark.parametrize("what", ["all left out", "beyond the vocabulary", "lowest", "far logits", "one kept", "no gradient"])
 def test_cross_entropy_masks(what):
     case = make(70, 192, 900, 300)

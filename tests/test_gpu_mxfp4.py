@@ -103,6 +103,19 @@ LINEAR = [(1, 8, 1, False), (1, 128, 5, True), (1, 2560, 1000, False), (1, 1000,
           (130, 1000, 391, True), (300, 1288, 515, False), (515, 512, 1026, True)]
 
 
+@pytest.fixture
+def tiles():
+    yield sbn().sbn_test_set_head_tiles
+    sbn().sbn_test_set_head_tiles()
+
+
+@pytest.mark.parametrize("size", [0, 1, 2])
+@pytest.mark.parametrize("tokens,d_in,d_out,bias", [(1, 8, 1, True), (33, 264, 129, False), (130, 1000, 391, True), (300, 1288, 515, False), (600, 136, 260, True)])
+def test_linear_in_every_tile_size(tokens, d_in, d_out, bias, size, tiles):
+    tiles(mxfp4=size)
+    test_linear(tokens, d_in, d_out, bias)
+
+
 @pytest.mark.parametrize("tokens,d_in,d_out,bias", LINEAR)
 def test_linear(tokens, d_in, d_out, bias):
     s = sbn()
