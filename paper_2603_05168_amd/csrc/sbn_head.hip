@@ -675,50 +675,60 @@ struct JoinArgs {
     float *ce, *kd, *lse1, *lse2;
 };
 
+// A block takes `across` tokens; the slices of a token, 256 / across threads, share its parts and entries.  Their sums meet by shuffles and once in LDS.
 template <bool HARD, bool SOFT>
 __global__ void __launch_bounds__(256) join_kernel(JoinArgs g)
 {
-    __shared__ float part[3][256];
-    const int slices = 256 / g.across, slice = threadIdx.x / g.across;
+    __shared__ float waves[4][4][64];
+    const int slices = 256 / g.across, slice = threadIdx.x / g.across, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int t = blockIdx.x * g.across + threadIdx.x % g.across;
     const bool inside = t < g.tokens;
     const float k2 = SOFT ? LOG2E / g.tau : 0.0f;
+    int64_t y = -1;
+    float z_target = 0.0f;
+    if (HARD && inside) {
+        y = g.targets[t];
+        z_target = g.z_target[t];   // of a token that counts
+    }
     float m = -INFINITY, s1 = 0.0f, s2 = 0.0f;
     auto add = [&](const float om, const float o1, const float o2) {
-        const float to = fmaxf(m, om);
-        if (to == -INFINITY) return;
-        const float mine = m - to, its = om - to;
+        const float to = fmaxf(m, om), base = to == -INFINITY ? 0.0f : to;
+        const float mine = m - base, its = om - base;
         if (HARD) s1 = s1 * exp2_fast(mine * LOG2E) + o1 * exp2_fast(its * LOG2E);
         if (SOFT) s2 = s2 * exp2_fast(mine * k2) + o2 * exp2_fast(its * k2);
         m = to;
     };
-    if (inside)
-        for (int p = slice; p < g.parts; p += slices) {
-            const int64_t at = (int64_t)p * g.tokens + t;
-            add(g.m[at], HARD ? g.s1[at] : 0.0f, SOFT ? g.s2[at] : 0.0f);
+    for (int p = slice; p < g.parts; p += 4 * slices) {
+        float om[4], o1[4], o2[4];   // asked for together
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t at = (int64_t)std::min(p + i * slices, g.parts - 1) * g.tokens + std::min(t, g.tokens - 1);
+            om[i] = p + i * slices < g.parts ? g.m[at] : -INFINITY;
+            o1[i] = HARD ? g.s1[at] : 0.0f;
+            o2[i] = SOFT ? g.s2[at] : 0.0f;
         }
-    for (int half = slices / 2; half; half /= 2) {
-        part[0][threadIdx.x] = m;
-        part[1][threadIdx.x] = s1;
-        part[2][threadIdx.x] = s2;
-        __syncthreads();
-        const int other = threadIdx.x + half * g.across;
-        if (slice < half) add(part[0][other], part[1][other], part[2][other]);
-        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (om[i] > -INFINITY) add(om[i], o1[i], o2[i]);
     }
-    if (slice == 0) {
-        const float lse1 = m + logf(s1), lse2 = SOFT ? m / g.tau + logf(s2) : 0.0f;
-        if (inside && HARD) {
-            const int64_t y = g.targets[t];
+    for (int x = g.across; x < 64; x *= 2) add(__shfl_xor(m, x), __shfl_xor(s1, x), __shfl_xor(s2, x));   // the same sum in both lanes
+    waves[0][wave][lane] = m;
+    waves[1][wave][lane] = s1;
+    waves[2][wave][lane] = s2;
+    __syncthreads();
+    m = -INFINITY;
+    s1 = s2 = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) add(waves[0][w][lane], waves[1][w][lane], waves[2][w][lane]);
+    const float lse1 = HARD ? m + logf(s1) : 0.0f, lse2 = SOFT ? m / g.tau + logf(s2) : 0.0f;
+    if (inside && slice == 0) {
+        if (HARD) {
             g.lse1[t] = lse1;
-            g.ce[t] = y >= 0 && y < g.vocab ? lse1 - g.z_target[t] : 0.0f;
+            g.ce[t] = y >= 0 && y < g.vocab ? lse1 - z_target : 0.0f;
         }
-        if (inside && SOFT) g.lse2[t] = lse2;
-        part[0][threadIdx.x] = lse2;
+        if (SOFT) g.lse2[t] = lse2;
     }
     if constexpr (SOFT) {
-        __syncthreads();
-        const float lse2 = part[0][threadIdx.x % g.across];
         float sum = 0.0f;
         if (inside)
             for (int j = slice; j < g.top_k; j += slices) {
@@ -726,13 +736,13 @@ __global__ void __launch_bounds__(256) join_kernel(JoinArgs g)
                 const float q = g.q[e];
                 if (g.at[e] >= 0 && q > 0.0f) sum += q * (logf(q) - g.z_top[e] / g.tau + lse2);
             }
-        for (int half = slices / 2; half; half /= 2) {
-            part[1][threadIdx.x] = sum;
-            __syncthreads();
-            if (slice < half) sum += part[1][threadIdx.x + half * g.across];
-            __syncthreads();
+        for (int x = g.across; x < 64; x *= 2) sum += __shfl_xor(sum, x);
+        waves[3][wave][lane] = sum;
+        __syncthreads();
+        if (inside && slice == 0) {
+            sum = waves[3][0][lane] + waves[3][1][lane] + waves[3][2][lane] + waves[3][3][lane];
+            g.kd[t] = g.some[t] != 0.0f ? g.tau * g.tau * sum : 0.0f;
         }
-        if (inside && slice == 0) g.kd[t] = g.some[t] != 0.0f ? g.tau * g.tau * sum : 0.0f;
     }
 }
 
