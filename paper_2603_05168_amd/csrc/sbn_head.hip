@@ -812,11 +812,21 @@ template <int SIZE, bool QT>
 __device__ __forceinline__ void gradient_tile(const GradientArgs &g, uint8_t *lds, const int job, const CommonFactor &common, const int64_t vocab)
 {
     using S = HeadTile<SIZE>;
-    const int split = __builtin_amdgcn_readfirstlane(job / g.padded);
+    int split, tn, tm;
+    if (g.splits % 8 == 0) {
+        // all tiles of a split on one XCD: they read the same k of both operands, which only one L2 asks for then (1531 x 50001 x 1000, where
+        // a split's 24 tiles lay on all of them: 1.26 GB read)
+        const int tiles = g.tiles_n * g.tiles_m, i = job >> 3, tile = i % tiles;
+        split = (job & 7) + 8 * (i / tiles);
+        tn = tile / g.tiles_m;
+        tm = tile - tn * g.tiles_m;
+    } else {
+        split = job / g.padded;
+        if (!tile_of_block(g.tiles_n, g.tiles_m, job - split * g.padded, tn, tm)) return;
+    }
+    split = __builtin_amdgcn_readfirstlane(split);
     const int k0 = split * g.per * STAGE_K, left = g.stages - split * g.per, stages = left < g.per ? left : g.per;
-    int tn, tm;
-    // (no stages: of a last piece that has fewer of them; nothing to add)
-    if (stages <= 0 || !tile_of_block(g.tiles_n, g.tiles_m, job - split * g.padded, tn, tm)) return;
+    if (stages <= 0) return;   // of a last piece that has fewer of them; nothing to add
     Operand p = g.P, q = g.Q;
     p.base += (int64_t)k0 * p.ld;
     p.k -= k0;
@@ -1018,7 +1028,7 @@ BackwardPlan plan_backward(const int64_t tokens, const int64_t d, const int64_t 
     const int64_t pieces = ceil_div(vocab, most);
     plan.piece = pieces == 1 ? vocab : ceil_div(ceil_div(vocab, pieces), 256) * 256;
     plan.ldg = ceil_div(plan.piece, STAGE_K) * STAGE_K;
-    // fewest us over tile sizes and splits: what the products take, and what a split's parts are to write and read again at 4 TB/s
+    // fewest us over tile sizes and splits: what the products take, and what a split's parts are to read again at 4 TB/s
     const int64_t dw_stages = ceil_div(tokens, STAGE_K), dh_stages = plan.ldg / STAGE_K;
     // fits as for the logits, with what surrounds a tile in proportion to what it stores.  us of a backward pass, tiles of 128 and of 256 for the
     // gradients: 65 x 32000 x 512 38 / 60, 1000 x 4000 x 2560 74 / 81, 1000 x 32000 x 2560 503 / 456, 16000 x 4000 x 2560 921 / 803; of 64
@@ -1035,8 +1045,8 @@ BackwardPlan plan_backward(const int64_t tokens, const int64_t d, const int64_t 
                 const float wk = (float)ceil_div(dw_stages, sw), hk = (float)ceil_div(dh_stages, sh);
                 const TileTimes &t = times[size];
                 float us = std::max(t.longest(std::max(wk, hk)), ((float)wt * t.share(wk) + (float)ht * t.share(hk)) / (float)PLAN_CUS);
-                if (sw > 1) us += 3.0f + (float)(8 * sw + 2) * (float)plan.piece * (float)d / 4e6f;
-                if (sh > 1) us += 3.0f + (float)(8 * sh + 2) * (float)tokens * (float)d / 4e6f;
+                if (sw > 1) us += 3.0f + (float)(4 * sw + 2) * (float)plan.piece * (float)d / 4e6f;
+                if (sh > 1) us += 3.0f + (float)(4 * sh + 2) * (float)tokens * (float)d / 4e6f;
                 if (us < best) {
                     best = us;
                     plan.size = size;
@@ -1244,7 +1254,7 @@ static sbn_status launch_gradients(GradientPair &pair, hipStream_t stream)
         GradientArgs &g = second != (pair.dw_first != 0) ? pair.dw : pair.dh;
         g.tiles_n = (int)ceil_div(g.N, S::N);
         g.tiles_m = (int)ceil_div(g.M, S::M);
-        g.padded = (int)(ceil_div((int64_t)g.tiles_n * g.tiles_m, 8) * 8);   // equal shares, one per XCD
+        g.padded = g.splits % 8 == 0 ? g.tiles_n * g.tiles_m : (int)(ceil_div((int64_t)g.tiles_n * g.tiles_m, 8) * 8);   // equal shares, one per XCD
         if (second) pair.job0 = (int)jobs;
         jobs += g.N ? (int64_t)g.padded * g.splits : 0;
     }
