@@ -3,8 +3,8 @@
 //   ce = lse(z) - z_y,                                         lse(x) = log sum_v exp x_v
 //   kd = tau^2 sum_v q_v (log q_v - (z_v / tau - lse(z / tau))),   q = softmax(a / tau) over the teacher's entries
 //   G  = d_ce (softmax(z) - onehot(y)) + d_kd tau (softmax(z / tau) - q),   dH = G W,   dW = G^T H
-// Forward: one product whose tiles leave a maximum and sums of exponentials per token and 128 (64) words of the vocabulary; they are joined
-// in a fixed order.  Backward: the vocabulary is cut into pieces; the logits of a piece are made once more, turned into G (bf16) on their
+// Forward: one product whose tiles leave a maximum and sums of exponentials per token and the words of a wavefront (128, 64 or 32); they
+// are joined in a fixed order.  Backward: the vocabulary is cut into pieces; the logits of a piece are made once more, turned into G (bf16) on their
 // way out, and both gradients' products read G.  All products run on the bf16 matrix cores (v_mfma_f32_32x32x16_bf16, fp32
 // accumulation).  Nothing is added atomically: results do not depend on the order of blocks.
 #include <algorithm>
@@ -425,6 +425,10 @@ template <int WQ, bool GRAD, bool HARD, bool SOFT> struct TokenValues {
 // Forward, a block takes tile after tile, gridDim.x apart: the next one's first stages come in under the sums of the last one (16384 tokens x
 // 131072 words x 2560: 8.68 ms with a block per tile, 8.63 so; 1531 x 50001 x 1000 164 us and 160).  Backward, results need LDS: with all of it for
 // a block per tile G takes 181 us at 1531 x 50001 x 1000, with the slot that a next tile's first stages leave 206.
+// Many tokens are bound by the matrix pipe at the clock that power leaves: 2048 x 32000 x 2560 262 to 296 us (1.13 to 1.28 PFLOP/s, the pipe busy
+// in 71 % of the cycles), 16384 tokens x 131072 8.7 ms forward (1.26) and 9.6 in eight pieces backward (1.14), where G leaves; with few dimensions
+// a tile's sums and results weigh as much as its product (1531 x 50001 x 1000: 0.9 and 0.87, the pipe busy in 44 % of the backward pass).  One
+// token by the stream of W: 131072 x 2560 112 us, 6.0 TB/s.
 template <int SIZE, bool GRAD, bool HARD, bool SOFT>
 __global__ void __launch_bounds__(64 * HeadTile<SIZE>::WAVES, 2) logits_kernel(LogitsArgs g)
 {
@@ -590,6 +594,7 @@ __global__ void __launch_bounds__(64 * HeadTile<SIZE>::WAVES, 2) logits_kernel(L
 // holds more than once counts once, with the sum of its probabilities: at[t, j] is entry j's word where it is the list's first of that word
 // and -1 elsewhere, so that no two entries of a token meet in one place later.  map[w, t]: bit i of word w says that the token has an entry
 // among the words 64 (32 w + i) .. + 63.
+// Latency and the search of the list: 4096 tokens x 64 entries 13 us, 37 x 7 4.2.
 struct TeacherArgs {
     const int64_t *idx;
     const void *logits;
@@ -676,6 +681,7 @@ struct JoinArgs {
 };
 
 // A block takes `across` tokens; the slices of a token, 256 / across threads, share its parts and entries.  Their sums meet by shuffles and once in LDS.
+// Bound by its reads: 16384 tokens x 1024 parts (134 MB) 33 us, 4.1 TB/s; few tokens by one chain of reads, 3.4 us at 16 x 1000.
 template <bool HARD, bool SOFT>
 __global__ void __launch_bounds__(256) join_kernel(JoinArgs g)
 {
@@ -840,7 +846,9 @@ __device__ __forceinline__ void gradient_tile(const GradientArgs &g, uint8_t *ld
 }
 
 // A block per tile: taken one after the other by a block, as the logits are, they took 3 to 10 % longer (the two products' tiles are not alike,
-// and the device deals them out as multiprocessors become free).
+// and the device deals them out as multiprocessors become free).  Bound by the matrix pipe: 16384 tokens x 16384 words x 2560 in 2.1 ms (1.3 PFLOP/s;
+// large library products of these two forms reach 0.91 and 0.97), 1531 x 50001 x 1000 in 290 to 320 us (1.0), where dW has 24 stages to a tile
+// and some 18 us beside them.
 template <int SIZE>
 __global__ void __launch_bounds__(64 * HeadTile<SIZE>::WAVES, 2) gradient_kernel(GradientPair pair)
 {
@@ -854,6 +862,7 @@ __global__ void __launch_bounds__(64 * HeadTile<SIZE>::WAVES, 2) gradient_kernel
 
 // bf16 sums of fp32 parts.  A block takes 256 / SLICES groups of four values, a slice of its threads every SLICES-th part: with few values and
 // many parts (37 x 1000 in 32) one thread for all of them took 11 us.
+// 16384 x 2560 40 us: 252 MB at 6.2 TB/s.
 template <int SLICES>
 __global__ void __launch_bounds__(256) sum_parts_kernel(const float *part, int64_t n, int parts, uint16_t *out)
 {
@@ -879,6 +888,7 @@ __global__ void __launch_bounds__(256) sum_parts_kernel(const float *part, int64
 // contraction is the tokens, at most four steps of 16, so a wavefront takes 128 words x 128 columns from registers.  A lane reads four
 // neighbouring columns (words) of eight tokens of H (G) and sorts them into four fragments by byte permutations; column j of a lane's four is
 // a product's column, so a lane's results are neighbours again and rows leave in 256 bytes.
+// Bound by what it moves: 37 x 32001 x 1000 34 us for 64 MB read and 66 written, 3.9 TB/s.
 struct FewGradients {
     GradientArgs dh;
     int dh_blocks;
