@@ -888,10 +888,11 @@ __global__ void __launch_bounds__(256) sum_parts_kernel(const float *part, int64
 // contraction is the tokens, at most four steps of 16, so a wavefront takes 128 words x 128 columns from registers.  A lane reads four
 // neighbouring columns (words) of eight tokens of H (G) and sorts them into four fragments by byte permutations; column j of a lane's four is
 // a product's column, so a lane's results are neighbours again and rows leave in 256 bytes.
-// Bound by what it moves: 37 x 32001 x 1000 34 us for 64 MB read and 66 written, 3.9 TB/s.
+// Bound by what it moves: 37 x 32001 x 1000 27 us for 71 MB read and 72 written, 5.3 TB/s.  An XCD takes neighbouring tiles: rows that are not whole
+// lines share them (dealt out in turns, W came 1.8 times: 34 us), and tiles of one split share G (64 x 32000 x 2560, whole lines: 4 us).
 struct FewGradients {
     GradientArgs dh;
-    int dh_blocks;
+    int dh_blocks, dw_per;   // multiples of eight; of the others, an XCD's share
     const uint16_t *H, *G;
     int64_t ldg;
     int tokens, d, words;
@@ -928,7 +929,9 @@ __global__ void __launch_bounds__(256, 2) few_gradient_kernel(FewGradients g)
     extern __shared__ __attribute__((aligned(1024))) uint8_t dlds[];
     const CommonFactor common(g.targets, g.d1, g.tokens);
     if ((int)blockIdx.x < g.dh_blocks) {
-        const int tn = blockIdx.x % g.dh.tiles_n, split = blockIdx.x / g.dh.tiles_n;
+        const int id = ((int)blockIdx.x & 7) * (g.dh_blocks >> 3) + ((int)blockIdx.x >> 3);
+        const int tn = id % g.dh.tiles_n, split = id / g.dh.tiles_n;
+        if (split >= g.dh.splits) return;
         const int s0 = split * g.dh.per, nk = std::min(g.dh.stages - s0, g.dh.per);
         Operand p = g.dh.P, q = g.dh.Q;
         p.base += (int64_t)s0 * STAGE_K * p.ld;
@@ -943,7 +946,8 @@ __global__ void __launch_bounds__(256, 2) few_gradient_kernel(FewGradients g)
         return;
     }
     const int lane = threadIdx.x & 63, r = lane & 31, c = lane >> 5;
-    const int id = (blockIdx.x - g.dh_blocks) * 4 + (threadIdx.x >> 6);
+    const int job = (int)blockIdx.x - g.dh_blocks;
+    const int id = ((job & 7) * g.dw_per + (job >> 3)) * 4 + (threadIdx.x >> 6);
     const int col = id % g.across * 128 + 4 * r, v0 = id / g.across * 128;
     if (v0 >= g.words) return;
     v8bf h[STEPS][4], a[STEPS][4];
@@ -1302,8 +1306,10 @@ static sbn_status launch_few_gradients(const HeadCall &h, const LogitsArgs &l, c
     a.C = plan.splits > 1 ? nullptr : static_cast<uint16_t *>(h.dH);
     a.part = part;
     a.tiles_n = g.across;
-    g.dh_blocks = h.dH ? g.across * plan.splits : 0;
-    const int64_t blocks = g.dh_blocks + (h.dW ? ceil_div(ceil_div(h.vocab, 128) * g.across, 4) : 0);
+    a.splits = plan.splits;
+    g.dh_blocks = h.dH ? (g.across * plan.splits + 7) / 8 * 8 : 0;
+    g.dw_per = h.dW ? (int)ceil_div(ceil_div(h.vocab, 128) * g.across, 4 * 8) : 0;
+    const int64_t blocks = g.dh_blocks + 8 * (int64_t)g.dw_per;
     const int steps = h.tokens <= 16 ? 1 : h.tokens <= 32 ? 2 : 4;
     static thread_local bool raised = false;
     constexpr int LDS = HeadTile<SMALL>::LDS;
