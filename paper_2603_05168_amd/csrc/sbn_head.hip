@@ -307,14 +307,9 @@ __device__ __forceinline__ float *staged(uint8_t *stg, const int row, const int 
     constexpr int SWIZZLE = HeadTile<SIZE>::ROW / 16 < 16 ? HeadTile<SIZE>::ROW / 16 - 1 : 15;
     return reinterpret_cast<float *>(stg + row * HeadTile<SIZE>::ROW + 16 * ((n >> 2) ^ (row & SWIZZLE)) + 4 * (n & 3));
 }
-// Tile order.  Blocks go to the eight XCDs round-robin and every XCD has its own L2, so XCD x takes a contiguous eighth of an order in which
-// consecutive tiles form super-tiles of 8 x 8.  False for the numbers that pad the range to a multiple of eight.
-__device__ __forceinline__ bool tile_of_block(const int tiles_n, const int tiles_m, const int bid, int &tn, int &tm)
+// Tile order: consecutive tiles form super-tiles of 8 x 8
+__device__ __forceinline__ void tile_in_order(const int tiles_n, const int tiles_m, const int id, int &tn, int &tm)
 {
-    const int nb = tiles_n * tiles_m;
-    const int per = (nb + 7) >> 3;
-    const int id = (bid & 7) * per + (bid >> 3);
-    if ((bid >> 3) >= per || id >= nb) return false;
     const int band_tiles = 8 * tiles_n;
     const int nbands = (tiles_m + 7) >> 3;
     int band = id / band_tiles;
@@ -327,6 +322,19 @@ __device__ __forceinline__ bool tile_of_block(const int tiles_n, const int tiles
     const int rem2 = rem - col * 8 * h;
     tn = 8 * col + rem2 / h;
     tm = 8 * band + rem2 % h;
+}
+// Blocks go to the eight XCDs round-robin and every XCD has its own L2, so XCD x takes a contiguous eighth of `all` in order.  The numbers that pad
+// them to a multiple of eight get one past the end.
+__device__ __forceinline__ int place_of_block(const int all, const int bid)
+{
+    const int per = (all + 7) >> 3, at = bid >> 3;
+    return at < per ? (bid & 7) * per + at : all;
+}
+__device__ __forceinline__ bool tile_of_block(const int tiles_n, const int tiles_m, const int bid, int &tn, int &tm)
+{
+    const int id = place_of_block(tiles_n * tiles_m, bid);
+    if (id >= tiles_n * tiles_m) return false;
+    tile_in_order(tiles_n, tiles_m, id, tn, tm);
     return true;
 }
 
@@ -762,7 +770,7 @@ struct GradientArgs {
     uint16_t *C;               // bf16 [M, N], or null:
     float *part;               // fp32 [splits, M, N]
     int add;                   // to what part holds
-    int tiles_n, tiles_m, padded;
+    int tiles_n, tiles_m;
 };
 struct GradientPair {
     GradientArgs dw, dh;
@@ -818,18 +826,14 @@ template <int SIZE, bool QT>
 __device__ __forceinline__ void gradient_tile(const GradientArgs &g, uint8_t *lds, const int job, const CommonFactor &common, const int64_t vocab)
 {
     using S = HeadTile<SIZE>;
-    int split, tn, tm;
-    if (g.splits % 8 == 0) {
-        // all tiles of a split on one XCD: they read the same k of both operands, which only one L2 asks for then (1531 x 50001 x 1000, where
-        // a split's 24 tiles lay on all of them: 1.26 GB read)
-        const int tiles = g.tiles_n * g.tiles_m, i = job >> 3, tile = i % tiles;
-        split = (job & 7) + 8 * (i / tiles);
-        tn = tile / g.tiles_m;
-        tm = tile - tn * g.tiles_m;
-    } else {
-        split = job / g.padded;
-        if (!tile_of_block(g.tiles_n, g.tiles_m, job - split * g.padded, tn, tm)) return;
-    }
+    // The tiles of a split follow one another and so lie on as few XCDs as there are for each: they read the same k of both operands, which only these
+    // L2s ask for then (dH of 1531 x 50001 x 1000 in four splits of 24 tiles: 863 MB read with every split on all XCDs, 420 so).  The tiles of dW
+    // that share the same words' G, the larger operand where tokens are few, follow one another.
+    const int tiles = g.tiles_n * g.tiles_m, id = place_of_block(tiles * g.splits, job);
+    if (id >= tiles * g.splits) return;
+    int split = id / tiles, tn, tm;
+    if constexpr (QT) tile_in_order(g.tiles_m, g.tiles_n, id - split * tiles, tm, tn);
+    else tile_in_order(g.tiles_n, g.tiles_m, id - split * tiles, tn, tm);
     split = __builtin_amdgcn_readfirstlane(split);
     const int k0 = split * g.per * STAGE_K, left = g.stages - split * g.per, stages = left < g.per ? left : g.per;
     if (stages <= 0) return;   // of a last piece that has fewer of them; nothing to add
@@ -1035,6 +1039,10 @@ struct BackwardPlan {
     int dh_parts(int64_t vocab) const { return dh_splits > 1 || piece < vocab ? dh_splits : 0; }
 };
 
+// Rows of G lie an odd number of lines apart, so that those of a stage go to all channels of a L2 (16384 tokens in pieces of 16384 words: 34.5 ms a
+// step with the lines of a row alone, 34.1 so)
+int64_t pitch_of(const int64_t cols) { return (cols / STAGE_K | 1) * STAGE_K; }
+
 BackwardPlan plan_backward(const int64_t tokens, const int64_t d, const int64_t vocab)
 {
     BackwardPlan plan;
@@ -1222,7 +1230,7 @@ size_t head_workspace_bytes(int64_t tokens, int64_t d_in, int64_t vocab, int64_t
     }
     const BackwardPlan plan = plan_backward(tokens, d_in, vocab);
     if (top_k) TeacherRegions(b, tokens, vocab, top_k);
-    b.take((size_t)tokens * plan.ldg * 2);
+    b.take((size_t)tokens * pitch_of(plan.ldg) * 2);
     b.take((size_t)plan.dh_parts(vocab) * tokens * d_in * 4);
     b.take((size_t)plan.dw_parts() * plan.piece * d_in * 4);
     return std::max(r.bytes, b.bytes);
@@ -1268,9 +1276,8 @@ static sbn_status launch_gradients(GradientPair &pair, hipStream_t stream)
         GradientArgs &g = second != (pair.dw_first != 0) ? pair.dw : pair.dh;
         g.tiles_n = (int)ceil_div(g.N, S::N);
         g.tiles_m = (int)ceil_div(g.M, S::M);
-        g.padded = g.splits % 8 == 0 ? g.tiles_n * g.tiles_m : (int)(ceil_div((int64_t)g.tiles_n * g.tiles_m, 8) * 8);   // equal shares, one per XCD
         if (second) pair.job0 = (int)jobs;
-        jobs += g.N ? (int64_t)g.padded * g.splits : 0;
+        jobs += g.N ? ceil_div((int64_t)g.tiles_n * g.tiles_m * g.splits, 8) * 8 : 0;   // equal shares, one per XCD
     }
     static thread_local bool raised = false;
     if (!raised) {
@@ -1358,7 +1365,7 @@ sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t 
         return st != SBN_OK || !h.dH || plan.splits == 1 ? st : sum(part, h.tokens * h.d_in, plan.splits, static_cast<uint16_t *>(h.dH));
     }
     const BackwardPlan plan = plan_backward(h.tokens, h.d_in, h.vocab);
-    g.G = reinterpret_cast<uint16_t *>(ws + r.take((size_t)h.tokens * plan.ldg * 2));
+    g.G = reinterpret_cast<uint16_t *>(ws + r.take((size_t)h.tokens * pitch_of(plan.ldg) * 2));
     const int dh_parts = plan.dh_parts(h.vocab), dw_parts = plan.dw_parts();
     float *const dh_part = reinterpret_cast<float *>(ws + r.take((size_t)dh_parts * h.tokens * h.d_in * 4));
     float *const dw_part = reinterpret_cast<float *>(ws + r.take((size_t)dw_parts * plan.piece * h.d_in * 4));
@@ -1368,7 +1375,8 @@ sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t 
         g.W = static_cast<const uint16_t *>(h.W) + v0 * d;
         g.v0 = v0;
         g.words = words;
-        g.ldg = ceil_div(words, STAGE_K) * STAGE_K;
+        const int64_t cols = ceil_div(words, STAGE_K) * STAGE_K;
+        g.ldg = pitch_of(cols);
         st = launch_logits<true>(g, logits_size(h.tokens, words, h.d_in), hard, soft, stream);
         if (st != SBN_OK) return st;
         GradientPair pair{};
@@ -1390,10 +1398,10 @@ sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t 
         if (h.dH) {
             GradientArgs &a = pair.dh;
             a.P = Operand{g.W, d, d, words};
-            a.Q = Operand{g.G, g.ldg, tokens, (int)g.ldg};
+            a.Q = Operand{g.G, g.ldg, tokens, (int)cols};
             a.N = d;
             a.M = tokens;
-            a.stages = (int)(g.ldg / STAGE_K);
+            a.stages = (int)(cols / STAGE_K);
             a.splits = plan.dh_splits;
             a.C = dh_parts ? nullptr : static_cast<uint16_t *>(h.dH);
             a.part = dh_part;
