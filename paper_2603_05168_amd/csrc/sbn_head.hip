@@ -358,6 +358,7 @@ struct LogitsArgs {
     // backward
     const float *lse1, *lse2, *d1, *d2;
     uint16_t *G;                 // [tokens, ldg]
+    uint16_t *rest;              // [tokens, ldg]: what rounding to bf16 left over of G; null: not asked for (tiles of 64 alone)
     int64_t ldg;
 };
 
@@ -405,6 +406,13 @@ struct CommonFactor {
         return some ? __uint_as_float((__builtin_amdgcn_readlane(bits, __builtin_ctzll(some)) & 0x007fffffu) | 0x3f800000u) : 1.0f;
     }
 };
+
+// What two rounded values left over, rounded in turn; nothing of one that has no finite value
+__device__ __forceinline__ uint32_t rest_of(const uint32_t rounded, const float lo, const float hi)
+{
+    const float a = __builtin_bit_cast(float, rounded << 16), b = __builtin_bit_cast(float, rounded & 0xffff0000u);
+    return pack_bf16(__builtin_fabsf(a) < INFINITY ? lo - a : 0.0f, __builtin_fabsf(b) < INFINITY ? hi - b : 0.0f);
+}
 
 // what belongs to a lane's tokens, asked for in front of a tile's product
 template <int WQ, bool GRAD, bool HARD, bool SOFT> struct TokenValues {
@@ -587,9 +595,13 @@ __global__ void __launch_bounds__(64 * HeadTile<SIZE>::WAVES, 2) logits_kernel(L
                             if (n + 4 + i >= left) hi[i] = 0.0f;
                         }
                     }
-                    if (tt < g.tokens && n0 + n < g.ldg)
-                        *reinterpret_cast<uint4 *>(g.G + tt * g.ldg + n0 + n) =
-                            make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]));
+                    if (tt < g.tokens && n0 + n < g.ldg) {
+                        const uint4 words = make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]));
+                        *reinterpret_cast<uint4 *>(g.G + tt * g.ldg + n0 + n) = words;
+                        if (SIZE == TINY && g.rest != nullptr)
+                            *reinterpret_cast<uint4 *>(g.rest + tt * g.ldg + n0 + n) = make_uint4(rest_of(words.x, lo[0], lo[1]), rest_of(words.y, lo[2], lo[3]),
+                                                                                                  rest_of(words.z, hi[0], hi[1]), rest_of(words.w, hi[2], hi[3]));
+                    }
                 }
             }
         }
@@ -899,7 +911,7 @@ struct FewGradients {
     int dh_blocks, dw_per;   // multiples of eight; of the others, an XCD's share
     const uint16_t *H, *G;
     int64_t ldg;
-    int tokens, d, words;
+    int tokens, rows, d, words;   // rows of G: as many as tokens, or, with their rests behind them, twice as many
     uint16_t *dW;
     int across;               // groups of 128 columns
     const int64_t *targets;
@@ -907,13 +919,17 @@ struct FewGradients {
     int64_t vocab;
 };
 
-// fragment j: column k + j, rows first + 8 c .. + 7 (the last one again past it)
-__device__ __forceinline__ void column_fragments(const uint16_t *base, const int64_t ld, const int first, const int last, const int64_t k, const int c, v8bf (&f)[4])
+// fragment j: column k + j, rows first + 8 c .. + 7 (the last one again past it; those from `wrap` on are the first ones again)
+__device__ __forceinline__ void column_fragments(const uint16_t *base, const int64_t ld, const int first, const int last, const int wrap, const int64_t k, const int c,
+                                                 v8bf (&f)[4])
 {
     typedef unsigned v4u __attribute__((ext_vector_type(4)));
     uint2 raw[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) raw[e] = *reinterpret_cast<const uint2 *>(base + (int64_t)std::min(first + 8 * c + e, last) * ld + k);
+    for (int e = 0; e < 8; ++e) {
+        const int row = std::min(first + 8 * c + e, last);
+        raw[e] = *reinterpret_cast<const uint2 *>(base + (int64_t)(row < wrap ? row : row - wrap) * ld + k);
+    }
     v4u o[4];
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
@@ -957,16 +973,16 @@ __global__ void __launch_bounds__(256, 2) few_gradient_kernel(FewGradients g)
     v8bf h[STEPS][4], a[STEPS][4];
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-        column_fragments(g.G, g.ldg, 16 * s, g.tokens - 1, std::min((int64_t)v0 + 4 * r, g.ldg - 4), c, a[s]);
-        column_fragments(g.H, g.d, 16 * s, g.tokens - 1, std::min(col, g.d - 4), c, h[s]);
-        if (16 * s + 16 > g.tokens) {   // past the last token: zeros
+        column_fragments(g.G, g.ldg, 16 * s, g.rows - 1, g.rows, std::min((int64_t)v0 + 4 * r, g.ldg - 4), c, a[s]);
+        column_fragments(g.H, g.d, 16 * s, g.rows - 1, g.tokens, std::min(col, g.d - 4), c, h[s]);
+        if (16 * s + 16 > g.rows) {   // past the last row: zeros
             typedef unsigned v4u __attribute__((ext_vector_type(4)));
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 v4u x = __builtin_bit_cast(v4u, a[s][j]);
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
-                    const int left = g.tokens - (16 * s + 8 * c + 2 * p);
+                    const int left = g.rows - (16 * s + 8 * c + 2 * p);
                     x[p] = left >= 2 ? x[p] : left == 1 ? x[p] & 0xffffu : 0u;
                 }
                 a[s][j] = __builtin_bit_cast(v8bf, x);
@@ -1176,10 +1192,16 @@ LogitsArgs logits_of(const HeadCall &h)
 // They are taken for weights of 2^21 values and more (backward pass of 16 to 64 tokens against the plan below at 65, us: 32000 x 2560 88 / 122,
 // 32000 x 512 29 / 38, 32000 x 64 18 / 26, 4000 x 512 16.5 / 16.0, 4000 x 64 13.9 / 11.7)
 constexpr int64_t FEW_TOKENS = 64, FEW_VALUES = 1 << 21;
+// Up to REST_TOKENS tokens dW takes G with what its rounding to bf16 left over: a step of 16 has room for the rests.  With one or two tokens a word's
+// row is one token's H times one value, for the target nearly -d_ce, which a power of two holds exactly; the rounding of the other words' G
+// then made dW's error up to 1.8 times what rounding the result costs (0.0006 of its norm against 0.0003).  Heads of fewer than 2^21 values take
+// this way as well then, 1.5 to 2.5 us more (8 tokens, 1000 x 64 10.3 and 12.4 us, 2000 x 1000 16.2 and 16.7).
+constexpr int REST_TOKENS = 8;
+int64_t rows_of_g(const int64_t tokens) { return tokens <= REST_TOKENS ? 2 * tokens : tokens; }
 bool takes_few(const int64_t tokens, const int64_t d, const int64_t vocab)
 {
     const int forced = g_gradient_size.load(std::memory_order_relaxed);
-    return tokens <= FEW_TOKENS && (forced >= 0 ? forced > BIG : vocab * d >= FEW_VALUES);
+    return tokens <= FEW_TOKENS && (forced >= 0 ? forced > BIG : tokens <= REST_TOKENS || vocab * d >= FEW_VALUES);
 }
 struct FewPlan {
     int64_t ldg;
@@ -1224,7 +1246,7 @@ size_t head_workspace_bytes(int64_t tokens, int64_t d_in, int64_t vocab, int64_t
     if (takes_few(tokens, d_in, vocab)) {
         const FewPlan plan = plan_few(tokens, d_in, vocab);
         if (top_k) TeacherRegions(b, tokens, vocab, top_k);
-        b.take((size_t)tokens * plan.ldg * 2);
+        b.take((size_t)rows_of_g(tokens) * plan.ldg * 2);
         b.take(plan.splits > 1 ? (size_t)plan.splits * tokens * d_in * 4 : 0);
         return std::max(r.bytes, b.bytes);
     }
@@ -1296,6 +1318,7 @@ static sbn_status launch_few_gradients(const HeadCall &h, const LogitsArgs &l, c
     g.G = l.G;
     g.ldg = l.ldg;
     g.tokens = l.tokens;
+    g.rows = l.rest != nullptr ? 2 * l.tokens : l.tokens;
     g.d = l.d;
     g.words = l.words;
     g.dW = static_cast<uint16_t *>(h.dW);
@@ -1317,7 +1340,7 @@ static sbn_status launch_few_gradients(const HeadCall &h, const LogitsArgs &l, c
     g.dh_blocks = h.dH ? (g.across * plan.splits + 7) / 8 * 8 : 0;
     g.dw_per = h.dW ? (int)ceil_div(ceil_div(h.vocab, 128) * g.across, 4 * 8) : 0;
     const int64_t blocks = g.dh_blocks + 8 * (int64_t)g.dw_per;
-    const int steps = h.tokens <= 16 ? 1 : h.tokens <= 32 ? 2 : 4;
+    const int steps = g.rows <= 16 ? 1 : g.rows <= 32 ? 2 : 4;
     static thread_local bool raised = false;
     constexpr int LDS = HeadTile<SMALL>::LDS;
     if (!raised) {
@@ -1358,9 +1381,10 @@ sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t 
     if (takes_few(h.tokens, h.d_in, h.vocab)) {
         const FewPlan plan = plan_few(h.tokens, h.d_in, h.vocab);
         g.ldg = plan.ldg;
-        g.G = reinterpret_cast<uint16_t *>(ws + r.take((size_t)h.tokens * plan.ldg * 2));
+        g.G = reinterpret_cast<uint16_t *>(ws + r.take((size_t)rows_of_g(h.tokens) * plan.ldg * 2));
+        if (rows_of_g(h.tokens) > h.tokens && h.dW) g.rest = g.G + h.tokens * plan.ldg;
         float *const part = reinterpret_cast<float *>(ws + r.bytes);
-        st = launch_logits<true>(g, logits_size(h.tokens, h.vocab, h.d_in), hard, soft, stream);
+        st = launch_logits<true>(g, g.rest != nullptr ? TINY : logits_size(h.tokens, h.vocab, h.d_in), hard, soft, stream);
         if (st == SBN_OK) st = launch_few_gradients(h, g, plan, part, stream);
         return st != SBN_OK || !h.dH || plan.splits == 1 ? st : sum(part, h.tokens * h.d_in, plan.splits, static_cast<uint16_t *>(h.dH));
     }

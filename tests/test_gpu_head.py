@@ -336,3 +336,35 @@ def test_refusals_reach_the_caller():
     assert e.value.status == s.SBN_EINVAL
     with pytest.raises(ValueError):
         s.sbn_head_cross_entropy(case["H"], case["W"].t().contiguous().t(), case["targets"], f, f, small)
+
+
+@pytest.mark.parametrize("tokens,d,vocab", [(1, 648, 5674), (2, 648, 5674), (2, 8, 1), (3, 72, 65), (7, 136, 1000), (8, 1000, 129), (8, 128, 20000)])
+def test_weight_gradient_of_up_to_eight_tokens_is_rounded_once(tokens, d, vocab):
+    # G is taken with what its rounding left over: it is off by 2^-16 relative instead of 2^-8
+    case = make(tokens, d, vocab, 900 + tokens)
+    case["targets"].clamp_(min=0)
+    case["d_ce"].fill_(1 / tokens)
+    H, W = case["H"].double(), case["W"].double()
+    z = H @ W.t()
+    dz = d * FP32_STEP * (H.abs() @ W.abs().t()).amax()
+    G = torch.softmax(z, 1)
+    dG = G / tokens * 2 * (dz + 32 * FP32_STEP * (z.abs().amax() + 20))
+    G[torch.arange(tokens), case["targets"]] -= 1
+    G /= tokens
+    dG += BF16_HALF ** 2 * (G.abs() + dG) + 1e-37
+    want = G.t() @ H
+    off = dG.t() @ H.abs() + 2 * tokens * FP32_STEP * (G.abs().t() @ H.abs()) + 1e-37
+    off = (off + BF16_HALF * want.abs()) * (1 + BF16_HALF)
+    for grads in ({"dH": False}, {}):
+        got = run(case, **grads)["dW"].double().cpu()
+        assert not (~((got - want).abs() <= off)).any()
+
+
+def test_weight_gradient_beyond_the_range_of_bf16_stays_infinite():
+    # a value that rounds to infinity leaves no rest that would make the sum a NaN
+    case = make(1, 64, 1000, 950)
+    case["targets"][0] = 3
+    case["d_ce"][0] = 3.4e38
+    case["W"][3] = -case["W"][3].abs() * case["H"][0].sign() * 4    # an unlikely target: G is nearly -d_ce there
+    got = run(case)["dW"].float().cpu()
+    assert not got[3].isnan().any() and (got[3].isinf() | (got[3].abs() > 0) | (case["H"][0] == 0)).all()
