@@ -1026,20 +1026,25 @@ struct TileTimes {
     float share(const float stages) const { return step * stages + each; }
 };
 
-// Logits in tiles of 64, 128 and 256; fits to 16 to 16000 tokens, 500 to 32000 words and 64 to 2560 dimensions.  us measured with each size (forward
-// with its join): 16 x 500 x 2560 16.2 / 22.4 / 49.6, 300 x 4000 x 2560 23.2 / 27.1 / 51.7, 1000 x 4000 x 2560 40.0 / 29.7 / 51.3,
-// 1000 x 32000 x 2560 269 / 158 / 133, 4000 x 32000 x 64 165 / 78 / 59.
+// Logits in tiles of 64, 128 and 256; fits to 16 to 1500 tokens, 3000 to 100000 words and 128 to 4096 dimensions (0.3 % over the best of the three on
+// average, 15 at most).  Rows that are not whole lines of 128 bytes cost a stage's fetches a second line each, small tiles most.  us measured with
+// each size (forward with its join): 16 x 500 x 2560 16.2 / 22.4 / 49.6, 300 x 4000 x 2560 23.2 / 27.1 / 51.7, 1000 x 4000 x 2560 40.0 / 29.7 /
+// 51.3, 1000 x 32000 x 2560 269 / 158 / 133, 4000 x 32000 x 64 165 / 78 / 59, 169 x 37331 x 3280 99 / 86 / 64, 400 x 100000 x 3280 696 / 466 / 327.
 int logits_size(const int64_t tokens, const int64_t words, const int64_t d)
 {
     const int forced = g_logits_size.load(std::memory_order_relaxed);
     if (forced >= 0) return forced;
-    static constexpr TileTimes times[] = {{0.2f, 4.0f, 0.19f, 1.3f}, {0.335f, 5.0f, 0.43f, 1.8f}, {0.94f, 7.9f, 1.43f, 4.8f}};
+    static constexpr TileTimes times[] = {{0.22f, 2.9f, 0.2f, 1.8f}, {0.41f, 4.0f, 0.41f, 2.2f}, {0.92f, 6.9f, 1.15f, 6.4f}};
+    static constexpr float ragged[] = {1.3f, 1.18f, 1.03f};
     const float stages = (float)ceil_div(d, STAGE_K);
     int best = BIG;
     float least = INFINITY;
     for (int size = BIG; size >= TINY; --size) {
         const TileTimes &t = times[size];
-        const float us = std::max(t.longest(stages), (float)ceil_div(tiles_of(words, tokens, size), PLAN_CUS) * t.share(stages));
+        const float alone = t.longest(stages), share = t.share(d % STAGE_K ? ragged[size] * stages : stages);
+        const int64_t tiles = tiles_of(words, tokens, size);
+        // (few of them do not slow each other down)
+        const float us = std::max(alone, tiles <= PLAN_CUS ? alone + (share - alone) * (float)tiles / PLAN_CUS : (float)ceil_div(tiles, PLAN_CUS) * share);
         if (us < least) least = us, best = size;
     }
     return best;
