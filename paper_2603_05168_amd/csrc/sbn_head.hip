@@ -1073,10 +1073,11 @@ BackwardPlan plan_backward(const int64_t tokens, const int64_t d, const int64_t 
     plan.ldg = ceil_div(plan.piece, STAGE_K) * STAGE_K;
     // fewest us over tile sizes and splits: what the products take, and what a split's parts are to read again at 4 TB/s
     const int64_t dw_stages = ceil_div(tokens, STAGE_K), dh_stages = plan.ldg / STAGE_K;
-    // fits as for the logits, with what surrounds a tile in proportion to what it stores.  us of a backward pass, tiles of 128 and of 256 for the
-    // gradients: 65 x 32000 x 512 38 / 60, 1000 x 4000 x 2560 74 / 81, 1000 x 32000 x 2560 503 / 456, 16000 x 4000 x 2560 921 / 803; of 64
-    // and of 128: 128 x 4000 x 64 12 / 15
-    static constexpr TileTimes times[] = {{0.2f, 5.0f, 0.35f, 1.5f}, {0.45f, 6.0f, 0.48f, 3.6f}, {1.1f, 9.0f, 1.4f, 18.0f}};
+    // fits to 70 to 5000 tokens, 1500 to 100000 words and 128 to 3280 dimensions, with what surrounds a tile in proportion to what it stores.  us of a
+    // backward pass, tiles of 128 and of 256 for the gradients: 65 x 32000 x 512 38 / 60, 1000 x 4000 x 2560 74 / 81, 1000 x 32000 x 2560 503 /
+    // 456, 130 x 100000 x 3280 846 / 598, 16000 x 4000 x 2560 921 / 803; of 64 and of 128: 128 x 4000 x 64 12 / 15
+    static constexpr TileTimes times[] = {{0.2f, 5.0f, 0.33f, 1.4f}, {0.45f, 6.0f, 0.44f, 3.35f}, {1.1f, 9.0f, 1.42f, 14.5f}};
+    static constexpr float ragged[] = {1.5f, 1.3f, 1.0f};   // of what surrounds a tile: rows that are not whole lines leave in parts of them
     const int forced = g_gradient_size.load(std::memory_order_relaxed);
     float best = INFINITY;
     for (int size = TINY; size <= BIG; ++size)
@@ -1087,7 +1088,12 @@ BackwardPlan plan_backward(const int64_t tokens, const int64_t d, const int64_t 
                 const int64_t wt = tiles_of(d, plan.piece, size) * sw, ht = tiles_of(d, tokens, size) * sh;
                 const float wk = (float)ceil_div(dw_stages, sw), hk = (float)ceil_div(dh_stages, sh);
                 const TileTimes &t = times[size];
-                float us = std::max(t.longest(std::max(wk, hk)), ((float)wt * t.share(wk) + (float)ht * t.share(hk)) / (float)PLAN_CUS);
+                const float more = d % STAGE_K ? (ragged[size] - 1.0f) * t.each : 0.0f;
+                // a long tile beside those of a full device takes longer (fewer splits of dH than this asks for: 130 x 100000 x 2560 750 us,
+                // 200 x 100000 x 2560 733; 501 and 508 so)
+                const float most = std::max(wk, hk), busy = std::min(1.0f, (float)(wt + ht) / (float)((size == BIG ? 1 : 2) * PLAN_CUS));
+                const float longest = t.longest(most * (1.0f + 0.4f * busy));
+                float us = std::max(longest, ((float)wt * t.share(wk) + (float)ht * t.share(hk) + (float)(wt + ht) * more) / (float)PLAN_CUS);
                 if (sw > 1) us += 3.0f + (float)(4 * sw + 2) * (float)plan.piece * (float)d / 4e6f;
                 if (sh > 1) us += 3.0f + (float)(4 * sh + 2) * (float)tokens * (float)d / 4e6f;
                 if (us < best) {
