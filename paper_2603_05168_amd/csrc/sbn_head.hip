@@ -358,7 +358,7 @@ struct LogitsArgs {
     // backward
     const float *lse1, *lse2, *d1, *d2;
     uint16_t *G;                 // [tokens, ldg]
-    uint16_t *rest;              // [tokens, ldg]: what rounding to bf16 left over of G; null: not asked for (tiles of 64 alone)
+    uint16_t *rest;              // [tokens, ldg]: what rounding to bf16 left over of G; null: not asked for (tiles of 64 and 128 alone)
     int64_t ldg;
 };
 
@@ -598,7 +598,7 @@ __global__ void __launch_bounds__(64 * HeadTile<SIZE>::WAVES, 2) logits_kernel(L
                     if (tt < g.tokens && n0 + n < g.ldg) {
                         const uint4 words = make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]));
                         *reinterpret_cast<uint4 *>(g.G + tt * g.ldg + n0 + n) = words;
-                        if (SIZE == TINY && g.rest != nullptr)
+                        if (SIZE != BIG && g.rest != nullptr)
                             *reinterpret_cast<uint4 *>(g.rest + tt * g.ldg + n0 + n) = make_uint4(rest_of(words.x, lo[0], lo[1]), rest_of(words.y, lo[2], lo[3]),
                                                                                                   rest_of(words.z, hi[0], hi[1]), rest_of(words.w, hi[2], hi[3]));
                     }
@@ -904,14 +904,15 @@ __global__ void __launch_bounds__(256) sum_parts_kernel(const float *part, int64
 // contraction is the tokens, at most four steps of 16, so a wavefront takes 128 words x 128 columns from registers.  A lane reads four
 // neighbouring columns (words) of eight tokens of H (G) and sorts them into four fragments by byte permutations; column j of a lane's four is
 // a product's column, so a lane's results are neighbours again and rows leave in 256 bytes.
-// Bound by what it moves: 37 x 32001 x 1000 27 us for 71 MB read and 72 written, 5.3 TB/s.  An XCD takes neighbouring tiles: rows that are not whole
-// lines share them (dealt out in turns, W came 1.8 times: 34 us), and tiles of one split share G (64 x 32000 x 2560, whole lines: 4 us).
+// Bound by what it moves: 37 x 32001 x 1000 27 us for 71 MB read and 72 written, 5.3 TB/s (33 where it takes G's rests as well).  An XCD takes
+// neighbouring tiles: rows that are not whole lines share them (dealt out in turns, W came 1.8 times: 34 us), and tiles of one split share G
+// (64 x 32000 x 2560, whole lines: 4 us).
 struct FewGradients {
     GradientArgs dh;
     int dh_blocks, dw_per;   // multiples of eight; of the others, an XCD's share
-    const uint16_t *H, *G;
+    const uint16_t *H, *G, *rest;
     int64_t ldg;
-    int tokens, rows, d, words;   // rows of G: as many as tokens, or, with their rests behind them, twice as many
+    int tokens, d, words;
     uint16_t *dW;
     int across;               // groups of 128 columns
     const int64_t *targets;
@@ -919,30 +920,50 @@ struct FewGradients {
     int64_t vocab;
 };
 
-// fragment j: column k + j, rows first + 8 c .. + 7 (the last one again past it; those from `wrap` on are the first ones again)
-__device__ __forceinline__ void column_fragments(const uint16_t *base, const int64_t ld, const int first, const int last, const int wrap, const int64_t k, const int c,
-                                                 v8bf (&f)[4])
+// fragment j: column k + j of COLUMNS, rows first + 8 c .. + 7 (the last one again past it)
+template <int COLUMNS>
+__device__ __forceinline__ void column_fragments(const uint16_t *base, const int64_t ld, const int first, const int last, const int64_t k, const int c, v8bf (&f)[COLUMNS])
 {
     typedef unsigned v4u __attribute__((ext_vector_type(4)));
-    uint2 raw[8];
+    uint32_t raw[8][COLUMNS / 2];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int row = std::min(first + 8 * c + e, last);
-        raw[e] = *reinterpret_cast<const uint2 *>(base + (int64_t)(row < wrap ? row : row - wrap) * ld + k);
-    }
-    v4u o[4];
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-        o[0][p] = __builtin_amdgcn_perm(raw[2 * p + 1].x, raw[2 * p].x, 0x05040100u);
-        o[1][p] = __builtin_amdgcn_perm(raw[2 * p + 1].x, raw[2 * p].x, 0x07060302u);
-        o[2][p] = __builtin_amdgcn_perm(raw[2 * p + 1].y, raw[2 * p].y, 0x05040100u);
-        o[3][p] = __builtin_amdgcn_perm(raw[2 * p + 1].y, raw[2 * p].y, 0x07060302u);
+        const uint16_t *const row = base + (int64_t)std::min(first + 8 * c + e, last) * ld + k;
+        if constexpr (COLUMNS == 4) {
+            const uint2 x = *reinterpret_cast<const uint2 *>(row);
+            raw[e][0] = x.x;
+            raw[e][1] = x.y;
+        } else raw[e][0] = *reinterpret_cast<const uint32_t *>(row);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) f[j] = __builtin_bit_cast(v8bf, o[j]);
+    for (int j = 0; j < COLUMNS; ++j) {
+        v4u o;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) o[p] = __builtin_amdgcn_perm(raw[2 * p + 1][j / 2], raw[2 * p][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+        f[j] = __builtin_bit_cast(v8bf, o);
+    }
+}
+// the same with zeros past the last one
+template <int COLUMNS>
+__device__ __forceinline__ void token_fragments(const uint16_t *base, const int64_t ld, const int first, const int tokens, const int64_t k, const int c, v8bf (&f)[COLUMNS])
+{
+    column_fragments(base, ld, first, tokens - 1, k, c, f);
+    if (first + 16 > tokens) {
+        typedef unsigned v4u __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int j = 0; j < COLUMNS; ++j) {
+            v4u x = __builtin_bit_cast(v4u, f[j]);
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const int left = tokens - (first + 8 * c + 2 * p);
+                x[p] = left >= 2 ? x[p] : left == 1 ? x[p] & 0xffffu : 0u;
+            }
+            f[j] = __builtin_bit_cast(v8bf, x);
+        }
+    }
 }
 
-template <int STEPS>   // of 16 tokens
+template <int STEPS, bool REST>   // of 16 tokens; with what rounding left over of G
 __global__ void __launch_bounds__(256, 2) few_gradient_kernel(FewGradients g)
 {
     using S = HeadTile<SMALL>;
@@ -970,42 +991,45 @@ __global__ void __launch_bounds__(256, 2) few_gradient_kernel(FewGradients g)
     const int id = ((job & 7) * g.dw_per + (job >> 3)) * 4 + (threadIdx.x >> 6);
     const int col = id % g.across * 128 + 4 * r, v0 = id / g.across * 128;
     if (v0 >= g.words) return;
-    v8bf h[STEPS][4], a[STEPS][4];
+    constexpr int AT_ONCE = STEPS >= 3 && REST ? 2 : 4;   // words of a lane: what the registers hold
+    v8bf h[STEPS][4], a[STEPS][AT_ONCE], b[REST ? STEPS : 1][AT_ONCE];
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-        column_fragments(g.G, g.ldg, 16 * s, g.rows - 1, g.rows, std::min((int64_t)v0 + 4 * r, g.ldg - 4), c, a[s]);
-        column_fragments(g.H, g.d, 16 * s, g.rows - 1, g.tokens, std::min(col, g.d - 4), c, h[s]);
-        if (16 * s + 16 > g.rows) {   // past the last row: zeros
-            typedef unsigned v4u __attribute__((ext_vector_type(4)));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v4u x = __builtin_bit_cast(v4u, a[s][j]);
-#pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                    const int left = g.rows - (16 * s + 8 * c + 2 * p);
-                    x[p] = left >= 2 ? x[p] : left == 1 ? x[p] & 0xffffu : 0u;
-                }
-                a[s][j] = __builtin_bit_cast(v8bf, x);
-            }
-        }
-    }
+    for (int s = 0; s < STEPS; ++s) column_fragments(g.H, g.d, 16 * s, g.tokens - 1, std::min(col, g.d - 4), c, h[s]);
     const float factor = common.value(g.vocab);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {   // words v0 + 4 row + w
-        v16f acc[4];
+    for (int w0 = 0; w0 < 4; w0 += AT_ONCE) {
+        const int64_t k = std::min((int64_t)v0 + 4 * r, g.ldg - 4) + w0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[j][e] = 0.0f;
-#pragma unroll
-            for (int s = 0; s < STEPS; ++s) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s][w], h[s][j], acc[j], 0, 0, 0);
+        for (int s = 0; s < STEPS; ++s) {
+            int half = c;
+            if (AT_ONCE == 2) {   // neither all of them asked for at once nor their addresses kept: the registers hold no more
+                asm volatile("" : "+v"(half));
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            token_fragments(g.G, g.ldg, 16 * s, g.tokens, k, half, a[s]);
+            if constexpr (REST) token_fragments(g.rest, g.ldg, 16 * s, g.tokens, k, half, b[s]);
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int v = v0 + 4 * (8 * (e >> 2) + 4 * c + (e & 3)) + w;
-            if (v < g.words && col < g.d)
-                *reinterpret_cast<uint2 *>(g.dW + (int64_t)v * g.d + col) =
-                    make_uint2(pack_bf16(acc[0][e] * factor, acc[1][e] * factor), pack_bf16(acc[2][e] * factor, acc[3][e] * factor));
+        for (int w = 0; w < AT_ONCE; ++w) {   // words v0 + 4 row + w0 + w
+            if (AT_ONCE == 2) __builtin_amdgcn_sched_barrier(0);
+            v16f acc[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[j][e] = 0.0f;
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) {
+                    acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s][w], h[s][j], acc[j], 0, 0, 0);
+                    if constexpr (REST) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[s][w], h[s][j], acc[j], 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int v = v0 + 4 * (8 * (e >> 2) + 4 * c + (e & 3)) + w0 + w;
+                if (v < g.words && col < g.d)
+                    *reinterpret_cast<uint2 *>(g.dW + (int64_t)v * g.d + col) =
+                        make_uint2(pack_bf16(acc[0][e] * factor, acc[1][e] * factor), pack_bf16(acc[2][e] * factor, acc[3][e] * factor));
+            }
         }
     }
 }
@@ -1203,30 +1227,38 @@ LogitsArgs logits_of(const HeadCall &h)
 // They are taken for weights of 2^21 values and more (backward pass of 16 to 64 tokens against the plan below at 65, us: 32000 x 2560 88 / 122,
 // 32000 x 512 29 / 38, 32000 x 64 18 / 26, 4000 x 512 16.5 / 16.0, 4000 x 64 13.9 / 11.7)
 constexpr int64_t FEW_TOKENS = 64, FEW_VALUES = 1 << 21;
-// Up to REST_TOKENS tokens dW takes G with what its rounding to bf16 left over: a step of 16 has room for the rests.  With one or two tokens a word's
-// row is one token's H times one value, for the target nearly -d_ce, which a power of two holds exactly; the rounding of the other words' G
-// then made dW's error up to 1.8 times what rounding the result costs (0.0006 of its norm against 0.0003).  Heads of fewer than 2^21 values take
-// this way as well then, 1.5 to 2.5 us more (8 tokens, 1000 x 64 10.3 and 12.4 us, 2000 x 1000 16.2 and 16.7).
+// The gradients of few tokens take G with what its rounding to bf16 left over, as rows behind those of G: of dH a tile has room for them, of dW they
+// are read beside G.  With few tokens a result is one or a few of G's values times H or W and has their rounding in full, on top of its own: the
+// errors of dH and dW of a distillation of 37 tokens were 0.0025 of their norms, 0.0017 so (what rounding the results costs), and with one
+// or two tokens, whose own targets' -d_ce needs no rounding, those of cross entropy 0.0006 and 0.0003.  Cross entropy of more tokens
+// has little of it (its largest values are near -d_ce, see CommonFactor), and many tokens of either average it out.  It costs 11 us of the 74 of a
+// distillation of 37 tokens x 32001 x 1000, and the small heads that take this way for it 1.5 to 2.5 us (8 tokens: 1000 x 64 10.3 and 12.4,
+// 2000 x 1000 16.2 and 16.7).
 constexpr int REST_TOKENS = 8;
-int64_t rows_of_g(const int64_t tokens) { return tokens <= REST_TOKENS ? 2 * tokens : tokens; }
-bool takes_few(const int64_t tokens, const int64_t d, const int64_t vocab)
+bool takes_rest(const int64_t tokens, const bool soft) { return tokens <= (soft ? FEW_TOKENS : REST_TOKENS); }
+bool takes_few(const int64_t tokens, const int64_t d, const int64_t vocab, const bool soft)
 {
     const int forced = g_gradient_size.load(std::memory_order_relaxed);
-    return tokens <= FEW_TOKENS && (forced >= 0 ? forced > BIG : tokens <= REST_TOKENS || vocab * d >= FEW_VALUES);
+    return tokens <= FEW_TOKENS && (forced >= 0 ? forced > BIG : takes_rest(tokens, soft) || vocab * d >= FEW_VALUES);
 }
 struct FewPlan {
     int64_t ldg;
-    int stages, per, splits;   // of dH; splits 1: bf16 at once
+    int stages, per, splits;   // of dH
+    int rows;                  // of G
+    int parts;                 // fp32 [parts, tokens, d] of dH; 1: bf16 at once
 };
-FewPlan plan_few(const int64_t tokens, const int64_t d, const int64_t vocab)
+FewPlan plan_few(const int64_t tokens, const int64_t d, const int64_t vocab, const bool soft)
 {
     FewPlan p;
+    const bool rest = takes_rest(tokens, soft);
+    p.rows = (int)(rest ? 2 * tokens : tokens);
     p.stages = (int)ceil_div(vocab, STAGE_K);
     p.ldg = (int64_t)p.stages * STAGE_K;
     int64_t splits = std::min(ceil_div(2 * PLAN_CUS, ceil_div(d, 128)), ceil_div(p.stages, 8));
     splits = std::max((int64_t)1, std::min(splits, std::max(vocab / (16 * tokens), ((int64_t)1 << 19) / (tokens * d))));
     p.per = (int)ceil_div(p.stages, splits);
     p.splits = (int)ceil_div(p.stages, p.per);
+    p.parts = rest ? 2 * p.splits : p.splits;
     return p;
 }
 
@@ -1254,11 +1286,11 @@ size_t head_workspace_bytes(int64_t tokens, int64_t d_in, int64_t vocab, int64_t
     if (top_k) TeacherRegions(r, tokens, vocab, top_k);
     if (!backward) return r.bytes;
     HeadRegions b;
-    if (takes_few(tokens, d_in, vocab)) {
-        const FewPlan plan = plan_few(tokens, d_in, vocab);
+    if (takes_few(tokens, d_in, vocab, top_k != 0)) {
+        const FewPlan plan = plan_few(tokens, d_in, vocab, top_k != 0);
         if (top_k) TeacherRegions(b, tokens, vocab, top_k);
-        b.take((size_t)rows_of_g(tokens) * plan.ldg * 2);
-        b.take(plan.splits > 1 ? (size_t)plan.splits * tokens * d_in * 4 : 0);
+        b.take((size_t)plan.rows * plan.ldg * 2);
+        b.take(plan.parts > 1 ? (size_t)plan.parts * tokens * d_in * 4 : 0);
         return std::max(r.bytes, b.bytes);
     }
     const BackwardPlan plan = plan_backward(tokens, d_in, vocab);
@@ -1322,6 +1354,20 @@ static sbn_status launch_gradients(GradientPair &pair, hipStream_t stream)
     return check_launch("gradient_kernel");
 }
 
+template <int STEPS, bool REST>
+static sbn_status launch_few_as(const FewGradients &g, const int64_t blocks, hipStream_t stream)
+{
+    constexpr int LDS = HeadTile<SMALL>::LDS;
+    static thread_local bool raised = false;
+    if (!raised) {
+        const sbn_status st = with_lds(&few_gradient_kernel<STEPS, REST>, LDS);
+        if (st != SBN_OK) return st;
+        raised = true;
+    }
+    hipLaunchKernelGGL((few_gradient_kernel<STEPS, REST>), dim3((unsigned)blocks), dim3(256), LDS, stream, g);
+    return check_launch("few_gradient_kernel");
+}
+
 static sbn_status launch_few_gradients(const HeadCall &h, const LogitsArgs &l, const FewPlan &plan, float *part, hipStream_t stream)
 {
     FewGradients g{};
@@ -1329,7 +1375,7 @@ static sbn_status launch_few_gradients(const HeadCall &h, const LogitsArgs &l, c
     g.G = l.G;
     g.ldg = l.ldg;
     g.tokens = l.tokens;
-    g.rows = l.rest != nullptr ? 2 * l.tokens : l.tokens;
+    g.rest = l.rest;
     g.d = l.d;
     g.words = l.words;
     g.dW = static_cast<uint16_t *>(h.dW);
@@ -1339,33 +1385,23 @@ static sbn_status launch_few_gradients(const HeadCall &h, const LogitsArgs &l, c
     g.vocab = h.vocab;
     GradientArgs &a = g.dh;
     a.P = Operand{l.W, l.d, l.d, l.words};
-    a.Q = Operand{l.G, l.ldg, l.tokens, (int)l.ldg};
+    a.Q = Operand{l.G, l.ldg, plan.rows, (int)l.ldg};
     a.N = l.d;
-    a.M = l.tokens;
+    a.M = plan.rows;   // (a split's rests are a part of their own)
     a.stages = plan.stages;
     a.per = plan.per;
-    a.C = plan.splits > 1 ? nullptr : static_cast<uint16_t *>(h.dH);
+    a.C = plan.parts > 1 ? nullptr : static_cast<uint16_t *>(h.dH);
     a.part = part;
     a.tiles_n = g.across;
     a.splits = plan.splits;
     g.dh_blocks = h.dH ? (g.across * plan.splits + 7) / 8 * 8 : 0;
     g.dw_per = h.dW ? (int)ceil_div(ceil_div(h.vocab, 128) * g.across, 4 * 8) : 0;
     const int64_t blocks = g.dh_blocks + 8 * (int64_t)g.dw_per;
-    const int steps = g.rows <= 16 ? 1 : g.rows <= 32 ? 2 : 4;
-    static thread_local bool raised = false;
-    constexpr int LDS = HeadTile<SMALL>::LDS;
-    if (!raised) {
-        sbn_status st = with_lds(&few_gradient_kernel<1>, LDS);
-        if (st == SBN_OK) st = with_lds(&few_gradient_kernel<2>, LDS);
-        if (st == SBN_OK) st = with_lds(&few_gradient_kernel<4>, LDS);
-        if (st != SBN_OK) return st;
-        raised = true;
-    }
-    const dim3 grid((unsigned)blocks), block(256);
-    if (steps == 1) hipLaunchKernelGGL(few_gradient_kernel<1>, grid, block, LDS, stream, g);
-    else if (steps == 2) hipLaunchKernelGGL(few_gradient_kernel<2>, grid, block, LDS, stream, g);
-    else hipLaunchKernelGGL(few_gradient_kernel<4>, grid, block, LDS, stream, g);
-    return check_launch("few_gradient_kernel");
+    const bool rest = l.rest != nullptr;
+    if (h.tokens <= 16) return rest ? launch_few_as<1, true>(g, blocks, stream) : launch_few_as<1, false>(g, blocks, stream);
+    if (h.tokens <= 32) return rest ? launch_few_as<2, true>(g, blocks, stream) : launch_few_as<2, false>(g, blocks, stream);
+    if (h.tokens <= 48) return rest ? launch_few_as<3, true>(g, blocks, stream) : launch_few_as<3, false>(g, blocks, stream);
+    return rest ? launch_few_as<4, true>(g, blocks, stream) : launch_few_as<4, false>(g, blocks, stream);
 }
 
 sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t stream)
@@ -1389,15 +1425,16 @@ sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t 
         else hipLaunchKernelGGL(sum_parts_kernel<1>, dim3((unsigned)ceil_div(n, 1024)), dim3(256), 0, stream, part, n, parts, out);
         return check_launch("sum_parts_kernel");
     };
-    if (takes_few(h.tokens, h.d_in, h.vocab)) {
-        const FewPlan plan = plan_few(h.tokens, h.d_in, h.vocab);
+    if (takes_few(h.tokens, h.d_in, h.vocab, soft)) {
+        const FewPlan plan = plan_few(h.tokens, h.d_in, h.vocab, soft);
         g.ldg = plan.ldg;
-        g.G = reinterpret_cast<uint16_t *>(ws + r.take((size_t)rows_of_g(h.tokens) * plan.ldg * 2));
-        if (rows_of_g(h.tokens) > h.tokens && h.dW) g.rest = g.G + h.tokens * plan.ldg;
+        g.G = reinterpret_cast<uint16_t *>(ws + r.take((size_t)plan.rows * plan.ldg * 2));
+        if (plan.rows > h.tokens) g.rest = g.G + h.tokens * plan.ldg;
         float *const part = reinterpret_cast<float *>(ws + r.bytes);
-        st = launch_logits<true>(g, g.rest != nullptr ? TINY : logits_size(h.tokens, h.vocab, h.d_in), hard, soft, stream);
+        const int size = logits_size(h.tokens, h.vocab, h.d_in);
+        st = launch_logits<true>(g, g.rest != nullptr ? std::min(size, (int)SMALL) : size, hard, soft, stream);
         if (st == SBN_OK) st = launch_few_gradients(h, g, plan, part, stream);
-        return st != SBN_OK || !h.dH || plan.splits == 1 ? st : sum(part, h.tokens * h.d_in, plan.splits, static_cast<uint16_t *>(h.dH));
+        return st != SBN_OK || !h.dH || plan.parts == 1 ? st : sum(part, h.tokens * h.d_in, plan.parts, static_cast<uint16_t *>(h.dH));
     }
     const BackwardPlan plan = plan_backward(h.tokens, h.d_in, h.vocab);
     g.G = reinterpret_cast<uint16_t *>(ws + r.take((size_t)h.tokens * pitch_of(plan.ldg) * 2));

@@ -368,3 +368,17 @@ def test_weight_gradient_beyond_the_range_of_bf16_stays_infinite():
     case["W"][3] = -case["W"][3].abs() * case["H"][0].sign() * 4    # an unlikely target: G is nearly -d_ce there
     got = run(case)["dW"].float().cpu()
     assert not got[3].isnan().any() and (got[3].isinf() | (got[3].abs() > 0) | (case["H"][0] == 0)).all()
+
+
+@pytest.mark.parametrize("hard", [True, False])
+@pytest.mark.parametrize("tokens,d,vocab,top", [(2, 64, 1000, 3), (9, 136, 63, 7), (17, 256, 3000, 2), (37, 1000, 5001, 7), (48, 72, 515, 1), (64, 648, 4001, 33)])
+def test_gradients_of_a_short_distillation_are_rounded_once(tokens, d, vocab, top, hard):
+    # up to 64 tokens G is taken with what its rounding left over, for either product: the errors are those of rounding the results, which are
+    # at most 2^-8 relative and 2^-8 / sqrt(3) in the mean of many where all are as large, with room for the rest of the bound
+    case, tau = make(tokens, d, vocab, 1000 + tokens, top=top), 2.0
+    ref, got = reference(case, tau, hard), run(case, tau, hard)
+    for name in ("dH", "dW"):
+        want = ref[name]
+        once = want.bfloat16().double()
+        off, least = (got[name].cpu().double() - want).norm(), (once - want).norm()
+        assert off <= 1.1 * least + 2.0 ** -12 * want.norm()
