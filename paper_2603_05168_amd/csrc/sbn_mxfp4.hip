@@ -67,8 +67,9 @@ template <bool BF16, int PER>
 __global__ void __launch_bounds__(256) mxfp4_quantize_kernel(const void *X, uint32_t rows, int cols, uint32_t vectors, uint32_t *codes, uint8_t *scales,
                                                                 int stage_shift)
 {
-    // vectors: in a padded row, a multiple of 16; all together fewer than 2^32
-    const uint32_t first = blockIdx.x * 256 * PER + threadIdx.x, all = rows * vectors;
+    // vectors: in a padded row, a multiple of 16.  All together they are at most 2^32 (2^27 tokens of a product, whose rows are padded to 256 columns): the
+    // last one's number has 32 bits, their count may have 33
+    const uint32_t first = blockIdx.x * 256 * PER + threadIdx.x, last = rows * vectors - 1;
     float x[PER][8];
     uint32_t row[PER], col[PER];
 #pragma unroll
@@ -78,12 +79,12 @@ __global__ void __launch_bounds__(256) mxfp4_quantize_kernel(const void *X, uint
         col[p] = 8 * (i - row[p] * vectors);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[p][e] = 0.0f;
-        if (i < all && (int)col[p] < cols) load8<BF16>(X, (int64_t)row[p] * cols + col[p], x[p]);
+        if (i <= last && (int)col[p] < cols) load8<BF16>(X, (int64_t)row[p] * cols + col[p], x[p]);
     }
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
         const uint32_t i = first + 256 * p;
-        if (i >= all) return;   // whole blocks of four lanes
+        if (i > last) return;   // whole blocks of four lanes
         uint32_t s;
         codes[i] = quantize8(x[p], s);
         if ((threadIdx.x & 3) == 0) {
