@@ -455,6 +455,9 @@ sbn_status sbn_mxfp4_linear(const void *X, int64_t tokens, int64_t d_in, int64_t
  */
 void sbn_test_set_head_tiles(int logits, int gradients, int mxfp4);
 
+/* Test hook, host only: the block tiles (0, 1, 2 as above) that sbn_mxfp4_linear takes for more than 64 tokens, and the threads of that launch. */
+sbn_status sbn_test_chosen_mxfp4_tile(int64_t tokens, int64_t d_in, int64_t d_out, int *size, int64_t *threads);
+
 /* Text of the last HIP error seen by this thread ("" if none). */
 const char *sbn_last_error(void);
 

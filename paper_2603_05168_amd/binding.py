@@ -75,6 +75,8 @@ def _load():
     lib.sbn_test_set_spin_limits.argtypes = [cint, cint]
     lib.sbn_test_set_head_tiles.restype = None
     lib.sbn_test_set_head_tiles.argtypes = [cint, cint, cint]
+    lib.sbn_test_chosen_mxfp4_tile.restype = cint
+    lib.sbn_test_chosen_mxfp4_tile.argtypes = [i64, i64, i64, ctypes.POINTER(cint), pi64]
     lib.sbn_test_linear_kernel.restype = cint
     lib.sbn_test_linear_kernel.argtypes = [cint, cint, pp, pp, pi64, pi64, pi64, cint, cint, pp, pp, pp, pp, pp, vp]
     lib.sbn_test_self_kernel.restype = cint
@@ -663,6 +665,13 @@ def sbn_mxfp4_linear(X, codes, scales, Y, workspace, bias=None):
 def sbn_test_set_head_tiles(logits: int = -1, gradients: int = -1, mxfp4: int = -1):
     """Test hook: block tiles of the output head (0, 1, 2; gradients 3: the kernel of up to 64 tokens; negative: the library's choice)."""
     _lib.sbn_test_set_head_tiles(logits, gradients, mxfp4)
+
+
+def sbn_test_chosen_mxfp4_tile(tokens: int, d_in: int, d_out: int):
+    """Test hook: the block tiles (0, 1, 2) of a 4-bit product of more than 64 tokens, and the threads of its launch."""
+    size, threads = ctypes.c_int(0), ctypes.c_int64(0)
+    _check(_lib.sbn_test_chosen_mxfp4_tile(tokens, d_in, d_out, ctypes.byref(size), ctypes.byref(threads)), "sbn_test_chosen_mxfp4_tile")
+    return size.value, threads.value
 
 
 def new_workspace(nbytes: int, device="cuda") -> torch.Tensor:

@@ -60,6 +60,13 @@ sbn_status check_mxfp4(int64_t rows, int64_t cols)
     return cols % 8 != 0 || cols > MXFP4_MAX_COLS || rows > ((int64_t)1 << 34) / (ceil_div(cols, 128) * 128) ? SBN_EUNSUPPORTED : SBN_OK;
 }
 
+sbn_status check_mxfp4_product(int64_t tokens, int64_t d_in, int64_t d_out)
+{
+    sbn_status st = check_mxfp4(tokens, d_in);
+    if (st == SBN_OK) st = check_mxfp4(d_out, d_in);
+    return st != SBN_OK ? st : tokens * d_out >= (int64_t)1 << 38 ? SBN_EUNSUPPORTED : SBN_OK;
+}
+
 }  // namespace
 
 }  // namespace sbn
@@ -72,6 +79,14 @@ void sbn_test_set_head_tiles(int logits, int gradients, int mxfp4)
 {
     set_head_tiles(logits, gradients);
     set_mxfp4_tiles(mxfp4);
+}
+
+sbn_status sbn_test_chosen_mxfp4_tile(int64_t tokens, int64_t d_in, int64_t d_out, int *size, int64_t *threads)
+{
+    if (!size || !threads) return SBN_EINVAL;
+    const sbn_status st = check_mxfp4_product(tokens, d_in, d_out);
+    if (st == SBN_OK) *threads = mxfp4_tile_threads(tokens, d_in, d_out, size);
+    return st;
 }
 
 sbn_status sbn_head_workspace_bytes(int64_t tokens, int64_t d_in, int64_t vocab, int64_t top_k, int backward, size_t *bytes)
@@ -177,10 +192,8 @@ sbn_status sbn_mxfp4_linear(const void *X, int64_t tokens, int64_t d_in, int64_t
                             void *workspace, size_t ws_bytes, void *stream)
 {
     if (!X || !codes || !scales || !Y || !workspace) return SBN_EINVAL;
-    sbn_status st = check_mxfp4(tokens, d_in);
-    if (st == SBN_OK) st = check_mxfp4(d_out, d_in);
+    const sbn_status st = check_mxfp4_product(tokens, d_in, d_out);
     if (st != SBN_OK) return st;
-    if (tokens * d_out >= (int64_t)1 << 38) return SBN_EUNSUPPORTED;
     if (!aligned(X, 16) || !aligned(codes, 16) || !aligned(scales, 4) || !aligned(bias, 4) || !aligned(Y, 16) || !aligned(workspace, 256)) return SBN_EALIGN;
     if (ws_bytes < mxfp4_workspace_bytes(tokens, d_in)) return SBN_ESIZE;
     return launch_mxfp4_linear(X, tokens, d_in, d_out, static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales), bias, Y, workspace,

@@ -186,6 +186,7 @@ sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t 
 // ---- microscaled 4-bit floating point (sbn_mxfp4.hip) ---------------------------------------------
 constexpr int64_t MXFP4_MAX_COLS = 1 << 20;
 void set_mxfp4_tiles(int size);
+int64_t mxfp4_tile_threads(int64_t tokens, int64_t d_in, int64_t d_out, int *size);   // see sbn_test_chosen_mxfp4_tile
 void mxfp4_bytes(int64_t rows, int64_t cols, size_t &codes, size_t &scales);
 size_t mxfp4_workspace_bytes(int64_t tokens, int64_t d_in);
 sbn_status launch_mxfp4_quantize(const void *X, sbn_dtype dtype, int64_t rows, int64_t cols, uint8_t *codes, uint8_t *scales, hipStream_t stream);

@@ -5,6 +5,7 @@
 // The product runs on v_mfma_scale_f32_32x32x64_f8f6f4, which takes both operands and their scales as they are stored and adds up in fp32.
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 
 #include "sbn_internal.hpp"
 #include "sbn_mfma.hpp"
@@ -358,6 +359,8 @@ __global__ void __launch_bounds__(64 * S::WAVES, 2) mxfp4_tile_kernel(MxArgs g)
     }
 }
 
+template <class S> int64_t tile_blocks(int64_t N, int64_t M) { return ceil_div(ceil_div(N, S::N) * ceil_div(M, S::M), 8) * 8; }
+
 template <class S>
 sbn_status launch_tile(MxArgs g, hipStream_t stream)
 {
@@ -369,8 +372,7 @@ sbn_status launch_tile(MxArgs g, hipStream_t stream)
         if (e != hipSuccess) { set_hip_error(e, "hipFuncSetAttribute"); return SBN_EHIP; }
         raised = true;
     }
-    const int64_t blocks = ceil_div((int64_t)g.tiles_n * g.tiles_m, 8) * 8;
-    hipLaunchKernelGGL(mxfp4_tile_kernel<S>, dim3((unsigned)blocks), dim3(64 * S::WAVES), S::LDS, stream, g);
+    hipLaunchKernelGGL(mxfp4_tile_kernel<S>, dim3((unsigned)tile_blocks<S>(g.N, g.M)), dim3(64 * S::WAVES), S::LDS, stream, g);
     return check_launch("mxfp4_tile_kernel");
 }
 
@@ -584,12 +586,30 @@ sbn_status launch_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, 
     return check_launch("mxfp4_dequantize_kernel");
 }
 
-// Estimated us of a product in tiles of `edge`: one tile alone, or every multiprocessor's share of them, `each` us of the multiprocessor.  The
+// Estimated us of a product in tiles of one size: one tile alone, or every multiprocessor's share of them, `each` us of the multiprocessor.  The
 // figures are fits to products of 65 to 8192 tokens, 1000 -> 20000, 2560 -> 6912 and 131072, 4096 -> 4096 (2560 -> 6912, us, small / middle /
-// large: 128 tokens 10.4 / 14.7 / 24.1, 512 21.3 / 18.7 / 28.6, 4096 110 / 81 / 68).
-static float tiles_us(const MxArgs &g, const int edge, const float alone, const float each)
+// large: 128 tokens 10.4 / 14.7 / 24.1, 512 21.3 / 18.7 / 28.6, 4096 110 / 81 / 68).  A launch has fewer than 2^32 threads, so some 2^36 outputs and
+// more do not go to the small tiles (the large ones have room for all that a call takes).
+template <class S>
+static float tiles_us(const int64_t N, const int64_t M, const float alone, const float each)
 {
-    return std::max(alone, each * (float)ceil_div(ceil_div(g.N, edge) * ceil_div(g.M, edge), 256));
+    if (tile_blocks<S>(N, M) * 64 * S::WAVES >= (int64_t)1 << 32) return INFINITY;
+    return std::max(alone, each * (float)ceil_div(ceil_div(N, S::N) * ceil_div(M, S::M), 256));
+}
+
+// 0, 1, 2: small, middle, large tiles
+static int choose_tile(const int64_t N, const int64_t M, const int64_t stages)
+{
+    const float large = tiles_us<MxLarge>(N, M, 1.05f * stages + 12.0f, 1.44f * stages + 16.0f), middle = tiles_us<MxMiddle>(N, M, 0.65f * stages + 6.2f, 0.48f * stages + 6.5f),
+                small = tiles_us<MxSmall>(N, M, 0.38f * stages + 4.6f, 0.28f * stages + 1.1f);
+    return large <= std::min(middle, small) ? 2 : middle <= small ? 1 : 0;
+}
+
+int64_t mxfp4_tile_threads(int64_t tokens, int64_t d_in, int64_t d_out, int *size)
+{
+    *size = choose_tile(d_out, tokens, stages_of(d_in));
+    return *size == 0 ? tile_blocks<MxSmall>(d_out, tokens) * 64 * MxSmall::WAVES
+                      : *size == 1 ? tile_blocks<MxMiddle>(d_out, tokens) * 64 * MxMiddle::WAVES : tile_blocks<MxLarge>(d_out, tokens) * 64 * MxLarge::WAVES;
 }
 
 sbn_status launch_mxfp4_linear(const void *X, int64_t tokens, int64_t d_in, int64_t d_out, const uint8_t *codes, const uint8_t *scales, const float *bias,
@@ -605,10 +625,8 @@ sbn_status launch_mxfp4_linear(const void *X, int64_t tokens, int64_t d_in, int6
     const int forced = g_tiles.load(std::memory_order_relaxed);
     if (tokens <= 32 && forced < 0) return launch_few<1>(g, stream);
     if (tokens <= 64 && forced < 0) return launch_few<2>(g, stream);
-    if (forced >= 0) return forced == 0 ? launch_tile<MxSmall>(g, stream) : forced == 1 ? launch_tile<MxMiddle>(g, stream) : launch_tile<MxLarge>(g, stream);
-    const float large = tiles_us(g, 256, 1.05f * stages + 12.0f, 1.44f * stages + 16.0f), middle = tiles_us(g, 128, 0.65f * stages + 6.2f, 0.48f * stages + 6.5f),
-                small = tiles_us(g, 64, 0.38f * stages + 4.6f, 0.28f * stages + 1.1f);
-    return large <= std::min(middle, small) ? launch_tile<MxLarge>(g, stream) : middle <= small ? launch_tile<MxMiddle>(g, stream) : launch_tile<MxSmall>(g, stream);
+    const int size = forced >= 0 ? forced : choose_tile(g.N, g.M, stages);
+    return size == 0 ? launch_tile<MxSmall>(g, stream) : size == 1 ? launch_tile<MxMiddle>(g, stream) : launch_tile<MxLarge>(g, stream);
 }
 
 }  // namespace sbn

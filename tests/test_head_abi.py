@@ -148,3 +148,18 @@ def test_host_tensors_are_refused_and_declined_by_the_marshalling():
         with pytest.raises(ValueError, match="GPU"):
             getattr(b, name)(*args)
     assert b._fast_head_bytes(0, 64, 10, 0, 1) is None and b._fast_mxfp4_bytes(1.0, 8) is None and b._fast_mxfp4_workspace_bytes(1 << 70, 8) is None
+
+
+def test_4bit_products_launch_fewer_than_4_billion_threads():
+    """Whatever sizes the call takes; the estimate alone prefers small tiles in some of these."""
+    wide = 1 << 27
+    for tokens, d_in, d_out in [(513, 64, wide), (512, 64, wide), (511, 64, wide), (577, 128, wide), (1025, 64, wide), (2047, 8, wide), (wide, 8, 2047), (wide, 64, 513),
+                                (4161, 1024, 1 << 24), (1 << 19, 64, (1 << 19) - 1), (65, 1 << 20, 1 << 14), (300001, 64, 300001)]:
+        size, threads = sbn.sbn_test_chosen_mxfp4_tile(tokens, d_in, d_out)
+        edge = (64, 128, 256)[size]
+        least = -(-tokens // edge) * -(-d_out // edge) * (512 if size == 2 else 256)
+        assert least <= threads < 2 ** 32, (tokens, d_in, d_out, size)
+    assert sbn.sbn_test_chosen_mxfp4_tile(128, 2560, 6912)[0] == 0 and sbn.sbn_test_chosen_mxfp4_tile(4096, 2560, 6912)[0] == 2
+    for bad in ((0, 64, 64), (64, 63, 64), (1 << 19, 64, 1 << 19)):
+        with pytest.raises(sbn.SbnError):
+            sbn.sbn_test_chosen_mxfp4_tile(*bad)
