@@ -880,12 +880,12 @@ __global__ void __launch_bounds__(64 * HeadTile<SIZE>::WAVES, 2) gradient_kernel
 // many parts (37 x 1000 in 32) one thread for all of them took 11 us.
 // 16384 x 2560 40 us: 252 MB at 6.2 TB/s.
 template <int SLICES>
-__global__ void __launch_bounds__(256) sum_parts_kernel(const float *part, int64_t n, int parts, uint16_t *out)
+__global__ void __launch_bounds__(256) sum_parts_kernel(const float *part, int64_t n, int parts, uint16_t *out, int64_t first)
 {
     constexpr int ACROSS = 256 / SLICES;
     __shared__ v4f sums[256];
     const int slice = threadIdx.x / ACROSS;
-    const int64_t i = ((int64_t)blockIdx.x * ACROSS + threadIdx.x % ACROSS) * 4;
+    const int64_t i = first + ((int64_t)blockIdx.x * ACROSS + threadIdx.x % ACROSS) * 4;
     v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
     if (i < n)
         for (int p = slice; p < parts; p += SLICES) x += *reinterpret_cast<const v4f *>(part + p * n + i);
@@ -1421,8 +1421,12 @@ sbn_status launch_head_backward(const HeadCall &h, void *workspace, hipStream_t 
     g.d1 = h.d_ce;
     g.d2 = h.d_kd;
     auto sum = [&](const float *part, int64_t n, int parts, uint16_t *out) {
-        if (n <= (int64_t)1 << 20 && parts >= 4) hipLaunchKernelGGL(sum_parts_kernel<8>, dim3((unsigned)ceil_div(n, 128)), dim3(256), 0, stream, part, n, parts, out);
-        else hipLaunchKernelGGL(sum_parts_kernel<1>, dim3((unsigned)ceil_div(n, 1024)), dim3(256), 0, stream, part, n, parts, out);
+        if (n <= (int64_t)1 << 20 && parts >= 4) hipLaunchKernelGGL(sum_parts_kernel<8>, dim3((unsigned)ceil_div(n, 128)), dim3(256), 0, stream, part, n, parts, out, (int64_t)0);
+        else   // 2^32 values at a time: a launch has fewer than 2^32 threads
+            for (int64_t first = 0; first < n; first += (int64_t)1 << 32) {
+                const int64_t here = std::min(n - first, (int64_t)1 << 32);
+                hipLaunchKernelGGL(sum_parts_kernel<1>, dim3((unsigned)ceil_div(here, 1024)), dim3(256), 0, stream, part, n, parts, out, first);
+            }
         return check_launch("sum_parts_kernel");
     };
     if (takes_few(h.tokens, h.d_in, h.vocab, soft)) {
