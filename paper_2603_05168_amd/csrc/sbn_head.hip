@@ -735,7 +735,7 @@ __global__ void __launch_bounds__(256) join_kernel(JoinArgs g)
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (om[i] > -INFINITY) add(om[i], o1[i], o2[i]);
+            if (p + i * slices < g.parts) add(om[i], o1[i], o2[i]);   // also where the maximum is -inf: the part may be of NaN, which no maximum shows
     }
     for (int x = g.across; x < 64; x *= 2) add(__shfl_xor(m, x), __shfl_xor(s1, x), __shfl_xor(s2, x));   // the same sum in both lanes
     waves[0][wave][lane] = m;

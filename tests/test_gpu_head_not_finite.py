@@ -1,0 +1,60 @@
+"""Losses of the output head where logits are not finite: a NaN or +inf among a token's logits makes its loss NaN, one of -inf has no share."""
+import pytest
+import torch
+
+from gpu_util import sbn
+from test_gpu_head import check, make, reference, run
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(params=[0, 1, 2])
+def tiles(request):
+    sbn().sbn_test_set_head_tiles(request.param, request.param)
+    yield
+    sbn().sbn_test_set_head_tiles()
+
+
+def losses(case, tau, **over):
+    return {k: v.cpu() for k, v in run({**case, **over}, tau).items() if k in ("ce", "kd", "lse1", "lse2")}
+
+
+# one word in a last part of its own; whole parts, wherever tiles of 64, 128 and 256 begin; a word among others; all words
+@pytest.mark.parametrize("words", [slice(256, 257), slice(0, 128), slice(128, 256), slice(32, 64), slice(70, 71), slice(0, 257)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_words_that_are_not_finite(words, value, tiles):
+    case = make(9, 64, 257, 1, top=5)
+    case["H"][:, 0], case["W"][:, 0] = 1.0, 0.0       # (an infinity reaches the logit as such)
+    case["targets"][:] = torch.arange(9) + 3
+    case["top_idx"][:] = torch.arange(5) + 20
+    before = losses(case, 2.0)
+    check(before, reference(case, 2.0))
+    W = case["W"].clone()
+    W[words, 0] = value
+    for tau in (None, 2.0):
+        got = losses(case, tau, W=W)
+        assert len(got) == (2 if tau is None else 4)
+        for name, x in got.items():
+            assert x.isnan().all(), (name, x)
+
+
+def test_a_token_that_is_not_finite(tiles):
+    case = make(9, 64, 300, 2, top=5)
+    case["targets"][:] = torch.arange(9)
+    H = case["H"].clone()
+    H[4, 7] = float("nan")
+    for tau in (None, 2.0):
+        want, got = losses(case, tau), losses(case, tau, H=H)
+        others = torch.arange(9) != 4
+        for name in want:
+            assert got[name][4].isnan() and torch.equal(got[name][others], want[name][others]), name
+
+
+def test_words_of_minus_infinity_have_no_share(tiles):
+    case = make(9, 64, 300, 3, top=5)
+    case["H"][:, 0], case["W"][:, 0] = 1.0, 0.0
+    case["targets"][:], case["top_idx"][:] = torch.arange(9), torch.arange(5)
+    W = case["W"].clone()
+    W[200:, 0] = -float("inf")
+    short = {**case, "W": case["W"][:200].contiguous()}
+    check(losses(case, 2.0, W=W), reference(short, 2.0))
