@@ -397,7 +397,8 @@ sbn_status sbn_test_takes_blocks(int count, const int64_t *tokens, const int64_t
  *   targets    device, int64 [tokens]; a target outside [0, vocab) leaves its token out: ce 0, no share in the gradients
  *   top_idx    device, int64 [tokens, top_k];  top_logits  device, fp32 or bf16 [tokens, top_k].  An entry whose index is outside
  *              [0, vocab) or whose logit is -inf is missing; a token with no entry has kd 0 and no share in the gradients; an
- *              index that a token's list holds more than once counts with the sum of its probabilities
+ *              index that a token's list holds more than once counts with the sum of its probabilities; an entry that is not missing and whose
+ *              logit is +inf or NaN makes its token's kd, and what it adds to the gradients, NaN
  *   ce, kd     device, fp32 [tokens]; written
  *   lse        device, fp32 [tokens] (cross_entropy: lse(z)) or [2, tokens] (distill: lse(z), written where targets are given, then
  *              lse(z / tau)); written by the forward, read by the backward

@@ -610,8 +610,8 @@ __global__ void __launch_bounds__(64 * HeadTile<SIZE>::WAVES, 2) logits_kernel(L
 }
 
 // ---- the teacher -----------------------------------------------------------------------------------------------------------------------
-// A wavefront per token: q = softmax(a / tau) over the valid entries (an index of the vocabulary, a logit above -inf).  A word that a list
-// holds more than once counts once, with the sum of its probabilities: at[t, j] is entry j's word where it is the list's first of that word
+// A wavefront per token: q = softmax(a / tau) over the valid entries (an index of the vocabulary, a logit that is not -inf; a NaN or +inf makes the
+// token's q NaN).  A word that a list holds more than once counts once, with the sum of its probabilities: at[t, j] is entry j's word where it is the list's first of that word
 // and -1 elsewhere, so that no two entries of a token meet in one place later.  map[w, t]: bit i of word w says that the token has an entry
 // among the words 64 (32 w + i) .. + 63.
 // Latency and the search of the list: 4096 tokens x 64 entries 13 us, 37 x 7 4.2.
@@ -651,10 +651,12 @@ __global__ void __launch_bounds__(256) teacher_kernel(TeacherArgs g)
     if (t >= g.tokens) return;   // a wavefront keeps to itself: no barrier below
     const int64_t first = (int64_t)t * g.top_k;
     float most = -INFINITY;
+    bool mine = false;
     for (int j = lane; j < g.top_k; j += 64) {
         const int64_t i = g.idx[first + j];
         const float a = BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t *>(g.logits)[first + j] << 16) : static_cast<const float *>(g.logits)[first + j];
-        const bool valid = i >= 0 && i < g.vocab && a > -INFINITY;
+        const bool valid = i >= 0 && i < g.vocab && a != -INFINITY;
+        mine |= valid;
         word[j] = valid ? (int32_t)i : -1;
         share[j] = a;
         if (valid) most = fmaxf(most, a);
@@ -668,7 +670,7 @@ __global__ void __launch_bounds__(256) teacher_kernel(TeacherArgs g)
         total += e;
     }
     total = wave_sum(total);
-    const bool some = most > -INFINITY;
+    const bool some = __any(mine);
     asm volatile("" ::: "memory");   // LDS operations of a wavefront are done in order
     for (int j = lane; j < g.top_k; j += 64) {
         const int32_t w = word[j];
@@ -760,7 +762,7 @@ __global__ void __launch_bounds__(256) join_kernel(JoinArgs g)
             for (int j = slice; j < g.top_k; j += slices) {
                 const int64_t e = (int64_t)t * g.top_k + j;
                 const float q = g.q[e];
-                if (g.at[e] >= 0 && q > 0.0f) sum += q * (logf(q) - g.z_top[e] / g.tau + lse2);
+                if (g.at[e] >= 0 && q != 0.0f) sum += q * (logf(q) - g.z_top[e] / g.tau + lse2);
             }
         for (int x = g.across; x < 64; x *= 2) sum += __shfl_xor(sum, x);
         waves[3][wave][lane] = sum;

@@ -1,4 +1,5 @@
-"""Losses of the output head where logits are not finite: a NaN or +inf among a token's logits makes its loss NaN, one of -inf has no share."""
+"""Losses of the output head where logits are not finite: a NaN or +inf among a token's or its teacher's logits makes its loss NaN, one of -inf has no
+share."""
 import pytest
 import torch
 
@@ -58,3 +59,23 @@ def test_words_of_minus_infinity_have_no_share(tiles):
     W[200:, 0] = -float("inf")
     short = {**case, "W": case["W"][:200].contiguous()}
     check(losses(case, 2.0, W=W), reference(short, 2.0))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("top,entries", [(1, slice(0, 1)), (5, slice(2, 3)), (5, slice(0, 5)), (130, slice(129, 130))])
+def test_teacher_logits_that_are_not_finite(top, entries, value, dtype):
+    case = make(9, 64, 300, 4, top=top, dtype=dtype)
+    broken = {**case, "top_logits": case["top_logits"].clone()}
+    broken["top_logits"][4, entries] = value
+    want, got = run(case, 2.0), run(broken, 2.0)
+    others = torch.arange(9) != 4
+    assert got["kd"][4].isnan() and torch.equal(got["kd"][others], want["kd"][others])
+    assert got["dH"][4].isnan().all() and torch.equal(got["dH"][others], want["dH"][others])
+    assert got["dW"][case["top_idx"][4]].isnan().all()
+    for name in ("ce", "lse1", "lse2"):
+        assert torch.equal(got[name], want[name]), name
+    # of an entry that is missing it is not looked at
+    broken["top_idx"] = case["top_idx"].clone()
+    broken["top_idx"][4, entries] = 300
+    check(run(broken, 2.0), reference(broken | {"top_logits": case["top_logits"]}, 2.0))
