@@ -79,3 +79,24 @@ def test_teacher_logits_that_are_not_finite(top, entries, value, dtype):
     broken["top_idx"] = case["top_idx"].clone()
     broken["top_idx"][4, entries] = 300
     check(run(broken, 2.0), reference(broken | {"top_logits": case["top_logits"]}, 2.0))
+
+
+@pytest.mark.parametrize("tokens", [2, 5, 8])
+def test_gradients_beyond_the_range_of_bf16_are_infinite(tokens):
+    # d_ce 3.4e38 lies between the largest bf16 and infinity, nearer the latter, and the first token's 1.0 leaves the common factor at 1: G is
+    # infinite at the last token's target, and what its rounding left over must not make a NaN of that
+    case = make(tokens, 64, 1000, 5)
+    last = tokens - 1
+    case["targets"][:] = torch.arange(tokens) + 10
+    case["targets"][last] = 3
+    case["d_ce"][:] = 1.0
+    case["d_ce"][last] = 3.4e38
+    case["H"][last] = torch.where(case["H"][last] == 0, 1.0, case["H"][last])
+    case["W"][3] = -case["W"][3].abs().clamp(min=0.01) * case["H"][last].sign() * 4    # an unlikely target: its softmax is nearly 0
+    assert torch.softmax(case["H"].double() @ case["W"].double().t(), 1)[last, 3] < 1e-4
+    assert torch.tensor(3.4e38).bfloat16().isinf()
+    got = run(case)
+    infinite = torch.tensor(float("inf"))
+    assert torch.equal(got["dW"][3].float().cpu(), -infinite * case["H"][last].float())
+    assert torch.equal(got["dH"][last].float().cpu(), -infinite * case["W"][3].float())
+    assert got["dH"][:last].isfinite().all() and got["dW"][10:10 + last].isfinite().all()
