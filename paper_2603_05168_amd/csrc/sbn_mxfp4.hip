@@ -140,23 +140,24 @@ __global__ void __launch_bounds__(256) mxfp4_dequantize_kernel(const uint32_t *c
 // stages, its way through LDS and its stores some 16 us more (4096 x 2560 -> 131072, us per tile: 37.6, 25 without stores, 21 without
 // results; 30.7 with stores past the caches).  Half the stage in three slots for two blocks per multiprocessor was slower
 // (64 bytes of a row are half a line: 81.7 us against 68.2 at 4096 x 2560 -> 6912), and so were requests spread over the stage.
-template <int WP_, int WQ_, int WM, int ROW_BYTES, int SLOTS_, int CHUNK_STAGES_> struct MxTile {
+constexpr int STAGE_BYTES = 128, STAGE_SCALES = 8;   // of a row and stage
+template <int WP_, int WQ_, int WM> struct MxTile {
     static constexpr int WP = WP_, WQ = WQ_, WAVES = 2 * WM;                 // 32 x 32 tiles of a wavefront
     static constexpr int N = 64 * WP, M = 32 * WM * WQ;
-    static constexpr int BYTES = ROW_BYTES, SCALES = BYTES / 16, SLOTS = SLOTS_, CHUNK_STAGES = CHUNK_STAGES_;   // of a row and stage; of the ring
-    static constexpr int P = N * BYTES, Q = M * BYTES, SQ = M * SCALES, STAGE = P + Q + SQ;   // in this order
-    static constexpr int CHUNK_ROW = SCALES * CHUNK_STAGES, CHUNK = N * CHUNK_ROW;            // scales of W of some stages
-    static constexpr int CHUNKS = SLOTS * STAGE, LDS = CHUNKS + 2 * CHUNK;
-    static constexpr int RPI = 1024 / BYTES, PI = N / (RPI * WAVES), QI = M / (RPI * WAVES);  // requests of a wavefront and stage
+    static constexpr int CHUNK_STAGES = 4;                                   // whose scales of W come together
+    static constexpr int P = N * STAGE_BYTES, Q = M * STAGE_BYTES, SQ = M * STAGE_SCALES, STAGE = P + Q + SQ;   // in this order
+    static constexpr int CHUNK_ROW = STAGE_SCALES * CHUNK_STAGES, CHUNK = N * CHUNK_ROW;      // scales of W of some stages
+    static constexpr int CHUNKS = 2 * STAGE, LDS = CHUNKS + 2 * CHUNK;
+    static constexpr int PI = N / (8 * WAVES), QI = M / (8 * WAVES);                          // requests (8 rows each) of a wavefront and stage
     static constexpr int REQUESTS = PI + QI + 1, CI = CHUNK / (256 * WAVES);                  // with X's scales; of a chunk
     // results of large tiles, 64 MB and more, leave past the caches: 4096 x 2560 -> 131072 1204 us and 981 so, -> 6912 66.9 and 66.2
     static constexpr bool PAST_CACHES = WP == 4;
     static constexpr int OUT = WP * 128;                                     // bytes of a staged row of results
     static_assert(WAVES * 32 * OUT <= CHUNKS, "results are staged in the idle stages");
 };
-using MxLarge = MxTile<4, 2, 4, 128, 2, 4>;
-using MxMiddle = MxTile<2, 2, 2, 128, 2, 4>;
-using MxSmall = MxTile<1, 1, 2, 128, 2, 4>;
+using MxLarge = MxTile<4, 2, 4>;
+using MxMiddle = MxTile<2, 2, 2>;
+using MxSmall = MxTile<1, 1, 2>;
 struct MxArgs {
     const uint8_t *P, *Q;      // codes of W [N, pitch] and of X [M, qpitch]
     const uint8_t *sp, *sq;    // their scales, [N, pitch / 16] and [stages, M, scales of a stage]
@@ -194,22 +195,21 @@ __global__ void __launch_bounds__(64 * S::WAVES, 2) mxfp4_tile_kernel(MxArgs g)
     const int pbytes = prows * (int)pitch, qbytes = qrows * (int)qpitch;
     v4i pb = buffer_of(g.P + (int64_t)n0 * pitch, pbytes), qb = buffer_of(g.Q + (int64_t)m0 * qpitch, qbytes);
     const v4i spb = buffer_of(g.sp + (int64_t)n0 * spitch, pbytes / 16);
-    v4i sqb = buffer_of(g.sq + (int64_t)m0 * S::SCALES, 0);
-    const uint64_t sqstep = (uint64_t)g.M * S::SCALES;
-    // Codes: one instruction fills 1 KB, lane l granule l % G of row l / G holding granule (l % G) ^ swizzle: 16 rows of one granule lie in
+    v4i sqb = buffer_of(g.sq + (int64_t)m0 * STAGE_SCALES, 0);
+    const uint64_t sqstep = (uint64_t)g.M * STAGE_SCALES;
+    // Codes: one instruction fills 1 KB, lane l granule l % 8 of row l / 8 holding granule (l % 8) ^ swizzle: 16 rows of one granule lie in
     // different banks.
-    constexpr int G = S::BYTES / 16, STEPS = G / 2;
-    auto swizzle = [](const int row) { return G == 8 ? (row >> 1) & 7 : (row >> 2) & 3; };
+    auto swizzle = [](const int row) { return (row >> 1) & 7; };
     uint32_t poff[S::PI], qoff[S::QI];
 #pragma unroll
     for (int i = 0; i < S::PI; ++i) {
-        const int row = S::RPI * (S::PI * wave + i) + lane / G;
-        poff[i] = (uint32_t)row * pitch + 16u * ((lane % G) ^ swizzle(row));
+        const int row = 8 * (S::PI * wave + i) + lane / 8;
+        poff[i] = (uint32_t)row * pitch + 16u * ((lane % 8) ^ swizzle(row));
     }
 #pragma unroll
     for (int i = 0; i < S::QI; ++i) {
-        const int row = S::RPI * (S::QI * wave + i) + lane / G;
-        qoff[i] = (uint32_t)row * qpitch + 16u * ((lane % G) ^ swizzle(row));
+        const int row = 8 * (S::QI * wave + i) + lane / 8;
+        qoff[i] = (uint32_t)row * qpitch + 16u * ((lane % 8) ^ swizzle(row));
     }
     // scales of X: 256 bytes of what lies together (by two wavefronts where there are more of them, so that all have as many requests in
     // flight); of W: rows of CHUNK_ROW bytes
@@ -221,12 +221,12 @@ __global__ void __launch_bounds__(64 * S::WAVES, 2) mxfp4_tile_kernel(MxArgs g)
             const bool some = kt < nk;
             pb[2] = some ? pbytes : 0;
             qb[2] = some ? qbytes : 0;
-            const uint64_t base = (uint64_t)(uintptr_t)(g.sq + (int64_t)m0 * S::SCALES) + (uint64_t)kt * sqstep;
+            const uint64_t base = (uint64_t)(uintptr_t)(g.sq + (int64_t)m0 * STAGE_SCALES) + (uint64_t)kt * sqstep;
             sqb[0] = (int)(uint32_t)base;
             sqb[1] = (int)(uint32_t)(base >> 32);
-            sqb[2] = some ? qrows * S::SCALES : 0;
+            sqb[2] = some ? qrows * STAGE_SCALES : 0;
         }
-        const uint32_t at = lds0 + slot, k = (uint32_t)kt * S::BYTES;
+        const uint32_t at = lds0 + slot, k = (uint32_t)kt * STAGE_BYTES;
         if (i < S::PI) lds_dma16_buffer(pb, poff[i], k, at + (S::PI * wave + i) * 1024);
         else if (i < S::PI + S::QI) lds_dma16_buffer(qb, qoff[i - S::PI], k, at + S::P + (S::QI * wave + i - S::PI) * 1024);
         else lds_dma4_buffer(sqb, 256 * qw + 4 * lane, 0, at + S::P + S::Q + 256 * qw);
@@ -236,16 +236,15 @@ __global__ void __launch_bounds__(64 * S::WAVES, 2) mxfp4_tile_kernel(MxArgs g)
 #pragma unroll
         for (int i = 0; i < S::CI; ++i) {
             const int row = 64 / CL * (S::CI * wave + i);
-            lds_dma4_buffer(spb, spoff, row * spitch + kt * S::SCALES, at + row * S::CHUNK_ROW);
+            lds_dma4_buffer(spb, spoff, row * spitch + kt * STAGE_SCALES, at + row * S::CHUNK_ROW);
         }
     };
-    // granule G / 2 c + u of a row in step u: u flips bits of the address
-    const uint32_t slot0 = 16 * ((STEPS * c) ^ swizzle(r));
-    const uint32_t pa = lds0 + (wn * 32 * WP + r) * S::BYTES + slot0, qa = lds0 + S::P + (wm * 32 * WQ + r) * S::BYTES + slot0;
-    const uint32_t psa = lds0 + S::CHUNKS + (wn * 32 * WP + r) * S::CHUNK_ROW + STEPS * c, qsa = lds0 + S::P + S::Q + (wm * 32 * WQ + r) * S::SCALES + STEPS * c;
+    // granule 4 c + u of a row in quarter u: u flips bits of the address
+    const uint32_t slot0 = 16 * ((4 * c) ^ swizzle(r));
+    const uint32_t pa = lds0 + (wn * 32 * WP + r) * STAGE_BYTES + slot0, qa = lds0 + S::P + (wm * 32 * WQ + r) * STAGE_BYTES + slot0;
+    const uint32_t psa = lds0 + S::CHUNKS + (wn * 32 * WP + r) * S::CHUNK_ROW + 4 * c, qsa = lds0 + S::P + S::Q + (wm * 32 * WQ + r) * STAGE_SCALES + 4 * c;
     typedef __attribute__((address_space(3))) const v4i *lds_v4i;
     typedef __attribute__((address_space(3))) const int *lds_int;
-    typedef __attribute__((address_space(3))) const uint16_t *lds_u16;
 
     v16f acc[WP][WQ];
 #pragma unroll
@@ -258,19 +257,18 @@ __global__ void __launch_bounds__(64 * S::WAVES, 2) mxfp4_tile_kernel(MxArgs g)
     int sp[WP], sq[WQ];   // scales of a stage
     constexpr int READS = WP + WQ;
     auto read_one = [&](const uint32_t at, const int u, const int i) {
-        if (i < WP) fp[u & 1][i] = *(lds_v4i)(uintptr_t)((pa ^ (16 * u)) + at + i * 32 * S::BYTES);
-        else fq[u & 1][i - WP] = *(lds_v4i)(uintptr_t)((qa ^ (16 * u)) + at + (i - WP) * 32 * S::BYTES);
+        if (i < WP) fp[u & 1][i] = *(lds_v4i)(uintptr_t)((pa ^ (16 * u)) + at + i * 32 * STAGE_BYTES);
+        else fq[u & 1][i - WP] = *(lds_v4i)(uintptr_t)((qa ^ (16 * u)) + at + (i - WP) * 32 * STAGE_BYTES);
     };
     auto read_scales = [&](const int kt, const uint32_t at) {
-        const uint32_t chunk = (kt / S::CHUNK_STAGES & 1) * S::CHUNK + (kt % S::CHUNK_STAGES) * S::SCALES;
-        auto of = [](const uint32_t a) { return G == 8 ? *(lds_int)(uintptr_t)a : (int)*(lds_u16)(uintptr_t)a; };
+        const uint32_t chunk = (kt / S::CHUNK_STAGES & 1) * S::CHUNK + (kt % S::CHUNK_STAGES) * STAGE_SCALES;
 #pragma unroll
-        for (int a = 0; a < WP; ++a) sp[a] = of(psa + chunk + a * 32 * S::CHUNK_ROW);
+        for (int a = 0; a < WP; ++a) sp[a] = *(lds_int)(uintptr_t)(psa + chunk + a * 32 * S::CHUNK_ROW);
 #pragma unroll
-        for (int b = 0; b < WQ; ++b) sq[b] = of(qsa + at + b * 32 * S::SCALES);
+        for (int b = 0; b < WQ; ++b) sq[b] = *(lds_int)(uintptr_t)(qsa + at + b * 32 * STAGE_SCALES);
     };
     auto wide = [](const v4i x) { return v8i{x[0], x[1], x[2], x[3], 0, 0, 0, 0}; };   // 4-bit operands are four registers
-    auto part = [&](const int u, auto &&side) {
+    auto quarter = [&](const int u, auto &&side) {
 #pragma unroll
         for (int s = 0; s < TILES; ++s) {
             const int a = s / WQ, b = s % WQ;
@@ -288,32 +286,32 @@ __global__ void __launch_bounds__(64 * S::WAVES, 2) mxfp4_tile_kernel(MxArgs g)
         for (int k = 0; k < n; ++k)
             if (k * TILES / n == s) op(k);
     };
-    // Stage kt: all parts but the last read the fragments of the next part; then stage kt + 1 must have landed and every wavefront holds the
-    // last fragments of stage kt, so behind the barrier the last part reads the first fragments of stage kt + 1 and asks for stage kt + SLOTS
+    // Stage kt: quarters 0 to 2 read the fragments of the next quarter; then stage kt + 1 must have landed and every wavefront holds the
+    // last fragments of stage kt, so behind the barrier the last quarter reads the first fragments of stage kt + 1 and asks for stage kt + 2
     // in the slot of stage kt.
 #pragma unroll
-    for (int st = 0; st < S::SLOTS; ++st) {
-        if (st % S::CHUNK_STAGES == 0) request_chunk(st);
+    for (int st = 0; st < 2; ++st) {
+        if (st == 0) request_chunk(0);
 #pragma unroll
         for (int i = 0; i < S::REQUESTS; ++i) request(st, st * S::STAGE, i);
     }
-    SBN_WAIT_VMCNT((S::SLOTS - 1) * S::REQUESTS);
+    SBN_WAIT_VMCNT(S::REQUESTS);
     __syncthreads();
     read_scales(0, 0);
 #pragma unroll
     for (int i = 0; i < READS; ++i) read_one(0, 0, i);
     uint32_t at = 0;
     for (int kt = 0; kt < nk; ++kt) {
-        const uint32_t next = at == (S::SLOTS - 1) * S::STAGE ? 0 : at + S::STAGE;
+        const uint32_t next = at ? 0 : S::STAGE;
 #pragma unroll
-        for (int u = 0; u + 1 < STEPS; ++u)
-            part(u, [&](const int s) { spread(s, READS, [&](const int k) { read_one(at, u + 1, k); }); });
-        SBN_WAIT_VMCNT((S::SLOTS - 2) * S::REQUESTS);
+        for (int u = 0; u < 3; ++u)
+            quarter(u, [&](const int s) { spread(s, READS, [&](const int k) { read_one(at, u + 1, k); }); });
+        SBN_WAIT_VMCNT(0);
         __syncthreads();
-        if ((kt + S::SLOTS) % S::CHUNK_STAGES == 0) request_chunk(kt + S::SLOTS);   // (past the last row's end: zeros)
-        part(STEPS - 1, [&](const int s) {
+        if ((kt + 2) % S::CHUNK_STAGES == 0) request_chunk(kt + 2);   // (past the last row's end: zeros)
+        quarter(3, [&](const int s) {
             spread(s, READS, [&](const int k) { read_one(next, 0, k); });
-            spread(s, S::REQUESTS, [&](const int k) { request(kt + S::SLOTS, at, k); });
+            spread(s, S::REQUESTS, [&](const int k) { request(kt + 2, at, k); });
             if (s == TILES - 1) read_scales(kt + 1, next);   // behind their last use
         });
         at = next;
@@ -383,7 +381,6 @@ sbn_status launch_tile(MxArgs g, hipStream_t stream)
 // multiplies them, cost more than the launch it saved (one token x 2560 -> 6912: 8.6 us against 6.2, -> 131072: 46 against 30).
 // 2560 -> 131072 takes 28 us at one token, 6.3 TB/s of codes and scales: the read stream of the board; -> 6912 at 32 tokens 5.0, a launch and its chain.
 
-constexpr int STAGE_BYTES = 128, STAGE_SCALES = 8;   // of a row and stage
 constexpr int FEW_ROWS = 32, FEW_STAGE = FEW_ROWS * (STAGE_BYTES + STAGE_SCALES), FEW_PITCH = FEW_ROWS + 4;
 constexpr int FEW_WAVES = 8, LDS_BYTES = 160 * 1024;
 int few_lds(int tokens) { return 2 * FEW_STAGE + 2 * tokens * FEW_PITCH * 4; }   // of a wavefront: two stages, its sums of two tiles
