@@ -405,8 +405,10 @@ sbn_status sbn_test_takes_blocks(int count, const int64_t *tokens, const int64_t
  *   dH, dW     device, bf16 [tokens, d_in] / [vocab, d_in], 16-byte aligned, overwritten; either may be NULL
  *   targets, ce, d_ce of the distillation calls: all given (both losses from one pass over W) or all NULL
  *   workspace  device, 256-byte aligned, >= sbn_head_workspace_bytes(tokens, d_in, vocab, top_k, backward); top_k 0 for cross entropy
- * Arithmetic: products on bf16 operands with fp32 accumulation, maxima, sums and losses in fp32; G is rounded to bf16 once as the operand
- * of its products, whose sums are fp32 until they are rounded to dH and dW.  No atomics: a call repeated gives the same bits.
+ * Arithmetic: products on bf16 operands with fp32 accumulation, maxima, sums and losses in fp32.  G is rounded to bf16 as the operand of its
+ * products, divided by a factor in [1, 2) taken from the first d_ce that counts and that the products' sums are multiplied by; up to 16
+ * tokens (64 of a distillation) what that rounding leaves over is a second operand, rounded in turn.  Sums are fp32 until they are rounded to
+ * dH and dW.  No atomics: a call repeated gives the same bits.
  * H and W must be finite, also in tokens that are left out.
  * Errors: SBN_EINVAL (null, non-positive size, tau not positive and finite), SBN_EALIGN, SBN_ESIZE, SBN_EUNSUPPORTED (d_in % 8 != 0, d_in >
  * 2^16, tokens or vocab > 2^24, tokens * vocab > 2^38, either times d_in > 2^34, top_k > 1024, vocab > 2^21 with a teacher), SBN_EHIP.

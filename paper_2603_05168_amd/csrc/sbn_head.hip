@@ -1230,13 +1230,18 @@ LogitsArgs logits_of(const HeadCall &h)
 // 32000 x 512 29 / 38, 32000 x 64 18 / 26, 4000 x 512 16.5 / 16.0, 4000 x 64 13.9 / 11.7)
 constexpr int64_t FEW_TOKENS = 64, FEW_VALUES = 1 << 21;
 // The gradients of few tokens take G with what its rounding to bf16 left over, as rows behind those of G: of dH a tile has room for them, of dW they
-// are read beside G.  With few tokens a result is one or a few of G's values times H or W and has their rounding in full, on top of its own: the
-// errors of dH and dW of a distillation of 37 tokens were 0.0025 of their norms, 0.0017 so (what rounding the results costs), and with one
-// or two tokens, whose own targets' -d_ce needs no rounding, those of cross entropy 0.0006 and 0.0003.  Cross entropy of more tokens
-// has little of it (its largest values are near -d_ce, see CommonFactor), and many tokens of either average it out.  It costs 11 us of the 74 of a
-// distillation of 37 tokens x 32001 x 1000, and the small heads that take this way for it 1.5 to 2.5 us (8 tokens: 1000 x 64 10.3 and 12.4,
-// 2000 x 1000 16.2 and 16.7).
-constexpr int REST_TOKENS = 8;
+// are read beside G.  A result then has its own rounding alone; without the rests G's comes on top, which many tokens do not average out: G's
+// largest values, the targets' and the teacher's, stand nearly alone in a row of dH and of dW.  Errors of dH and dW in 1e-4 of their norms, without
+// and with the rests (rounding the results alone costs 16 to 17; the same at 64, 512 and 2048 tokens, a little more with a few):
+//   distillation 23 and 17;  cross entropy, d_ce alike in all tokens 17 to 18 and 17 (see CommonFactor), d_ce of any values 23 to 27 and 17
+// Cross entropy with d_ce alike has its targets' values unrounded, and where few tokens count these are most of dW: then dW without the rests
+// is off by up to 1.8 times as much as with them (1.4 at 16 tokens, 1.2 at 18 and more, over 140 sizes).
+// The price, backward pass in us without and with the rests, d x words 256 x 2000 and 2560 x 32000:
+//   cross entropy  16 tokens 11.3 / 14.5 and 87 / 89, 32 tokens 11.5 / 15 and 89 / 98, 64 tokens 12 / 18.6 and 101 / 123
+//   distillation   16 tokens 16.4 / 19.8 and 91 / 94, 64 tokens 18.7 / 26 and 105 / 128
+// So a distillation takes them as far as this way goes, cross entropy as long as the tokens are one step of the matrix instruction.  More tokens
+// are bound by the matrix pipe, and the rests would be two of eight products more.
+constexpr int REST_TOKENS = 16;
 bool takes_rest(const int64_t tokens, const bool soft) { return tokens <= (soft ? FEW_TOKENS : REST_TOKENS); }
 bool takes_few(const int64_t tokens, const int64_t d, const int64_t vocab, const bool soft)
 {
@@ -1399,8 +1404,8 @@ static sbn_status launch_few_gradients(const HeadCall &h, const LogitsArgs &l, c
     g.dh_blocks = h.dH ? (g.across * plan.splits + 7) / 8 * 8 : 0;
     g.dw_per = h.dW ? (int)ceil_div(ceil_div(h.vocab, 128) * g.across, 4 * 8) : 0;
     const int64_t blocks = g.dh_blocks + 8 * (int64_t)g.dw_per;
+    if (h.tokens <= REST_TOKENS) return launch_few_as<1, true>(g, blocks, stream);
     const bool rest = l.rest != nullptr;
-    if (h.tokens <= 16) return rest ? launch_few_as<1, true>(g, blocks, stream) : launch_few_as<1, false>(g, blocks, stream);
     if (h.tokens <= 32) return rest ? launch_few_as<2, true>(g, blocks, stream) : launch_few_as<2, false>(g, blocks, stream);
     if (h.tokens <= 48) return rest ? launch_few_as<3, true>(g, blocks, stream) : launch_few_as<3, false>(g, blocks, stream);
     return rest ? launch_few_as<4, true>(g, blocks, stream) : launch_few_as<4, false>(g, blocks, stream);
