@@ -1038,7 +1038,9 @@ __global__ void __launch_bounds__(256, 2) few_gradient_kernel(FewGradients g)
 
 // ---- host ------------------------------------------------------------------------------------------------------------------------------
 constexpr int PLAN_CUS = 256;                          // multiprocessors of the part: a plan depends on sizes alone
-constexpr int64_t PIECE_ELEMENTS = (int64_t)1 << 28;   // most of G at a time (512 MB); 2^25 to 2^27 took within 5 % of it, pieces that the last cache holds too
+// Most of G at a time (512 MB and what pads its rows), but for more than 2^20 tokens, whose pieces have 256 words, and for up to 64 tokens, which take
+// the vocabulary whole.  2^25 to 2^27 took within 5 % of it, pieces that the last cache holds too
+constexpr int64_t PIECE_ELEMENTS = (int64_t)1 << 28;
 
 std::atomic<int> g_logits_size{-1}, g_gradient_size{-1};   // of the test hook
 

@@ -163,3 +163,12 @@ def test_4bit_products_launch_fewer_than_4_billion_threads():
     for bad in ((0, 64, 64), (64, 63, 64), (1 << 19, 64, 1 << 19)):
         with pytest.raises(sbn.SbnError):
             sbn.sbn_test_chosen_mxfp4_tile(*bad)
+
+
+@pytest.mark.parametrize("tokens,vocab,top_k,held", [
+    (16384, 131072, 0, (2 ** 14, 2 ** 14 + 64)), (2 ** 19, 5000, 0, (2 ** 19, 512 + 64)), (2 ** 20, 5000, 0, (2 ** 20, 256 + 64)), (2 ** 24, 256, 0, (2 ** 24, 256 + 64)),
+    (64, 2 ** 24, 0, (64, 2 ** 24)), (16, 2 ** 24, 0, (2 * 16, 2 ** 24)), (64, 2 ** 21, 8, (2 * 64, 2 ** 21))])
+def test_head_workspace_holds_one_piece_of_the_gradient_of_the_logits(tokens, vocab, top_k, held):
+    # pieces of 2^28 logits or 256 words, rows an odd number of lines apart; of few tokens the vocabulary, with the rests' rows
+    nbytes, G = sbn.sbn_head_workspace_bytes(tokens, 8, vocab, top_k), 2 * held[0] * held[1]
+    assert G <= nbytes <= G + 4 * 8 * tokens + 2 ** 22   # dH in fp32 over the pieces, splits of few tokens and the teacher's lists
