@@ -434,6 +434,8 @@ sbn_status sbn_head_distill_backward(const void *H, const void *W, const int64_t
  *   scales  rows of ceil(cols / 128) * 4 bytes, one per block: s stands for 2^(s - 127)
  * Columns that pad a row are zeros, a block of zeros has s = 0.  quantize takes s = max(e - 2, 0), e the exponent field (as of fp32) of the
  * block's largest magnitude, and of every value / 2^(s - 127) the nearest code, ties to the even one, magnitudes above 6 to 6.
+ * Values must be finite: a block with a NaN or an infinity gets codes and a scale below 255 that stand for nothing in particular (a NaN does not
+ * survive); other blocks, and a product's other tokens, are not touched.
  *   X, Y    device, fp32 or bf16 [rows, cols], 16-byte aligned; dequantize is exact in both types
  *   codes   device, 16-byte aligned;  scales  device, 4-byte aligned: sbn_mxfp4_bytes() bytes each, no scale of 255
  * linear: Y[t,o] = sum_k q(X)[t,k] W[o,k] (+ bias[o]), q(X) the values that quantize makes of X, products exact, sums in fp32

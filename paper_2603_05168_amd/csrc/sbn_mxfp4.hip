@@ -43,7 +43,8 @@ __device__ __forceinline__ void load8(const void *src, const int64_t at, float (
     }
 }
 
-// codes of eight values (a word), s: scale of the block that four neighbouring lanes hold
+// codes of eight values (a word), s: scale of the block that four neighbouring lanes hold.  Values are finite: the maximum drops a NaN, which the
+// conversion turns into a 6; of an infinity s is 253.
 __device__ __forceinline__ uint32_t quantize8(const float (&x)[8], uint32_t &s)
 {
     float most = 0.0f;

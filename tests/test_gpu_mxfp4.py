@@ -185,3 +185,28 @@ def test_linear_in_a_graph_and_on_another_stream():
             s.sbn_mxfp4_linear(X, codes, scales, other, ws)
             torch.cuda.synchronize()
             assert torch.equal(other, eager)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_a_block_that_is_not_finite_touches_no_other(value, dtype):
+    s = sbn()
+    g = torch.Generator().manual_seed(9)
+    X = torch.randn(9, 264, generator=g).to(dtype)
+    broken = X.clone()
+    broken[4, 70], broken[4, 71], broken[8, 263] = value, -value, value     # blocks 2 and 8 of rows of 12
+    codes, scales = hip_quantize(X.to(DEV))
+    c, sc = hip_quantize(broken.to(DEV))
+    assert (sc < 255).all()
+    same = torch.ones(9, 12, dtype=torch.bool, device=DEV)
+    same[4, 2] = same[8, 8] = False
+    assert torch.equal(sc[same], scales[same]) and torch.equal(c.view(9, 12, 16)[same], codes.view(9, 12, 16)[same])
+    W = hip_quantize(torch.randn(300, 264, generator=g).to(DEV))
+    for rows in (9, 9 * 40):   # both kernels of the product
+        Y = [torch.full((rows, 300), float("nan"), device=DEV) for _ in range(2)]
+        for x, y in zip((X, broken), Y):
+            x = x.bfloat16().repeat(rows // 9, 1).to(DEV)
+            s.sbn_mxfp4_linear(x, *W, y, s.new_workspace(s.sbn_mxfp4_workspace_bytes(rows, 264)))
+        others = torch.arange(rows, device=DEV) % 9
+        others = (others != 4) & (others != 8)
+        assert torch.equal(Y[0][others], Y[1][others])
