@@ -140,7 +140,9 @@ __global__ void __launch_bounds__(256) mxfp4_dequantize_kernel(const uint32_t *c
 // product: a stage of the large tile takes 1.44 us, 1.17 without its requests and 0.98 its matrix instructions at 2.1 GHz; a tile's first
 // stages, its way through LDS and its stores some 16 us more (4096 x 2560 -> 131072, us per tile: 37.6, 25 without stores, 21 without
 // results; 30.7 with stores past the caches).  Half the stage in three slots for two blocks per multiprocessor was slower
-// (64 bytes of a row are half a line: 81.7 us against 68.2 at 4096 x 2560 -> 6912), and so were requests spread over the stage.
+// (64 bytes of a row are half a line: 81.7 us against 68.2 at 4096 x 2560 -> 6912), and so were requests spread over the stage.  Counters at that
+// size (60 us): matrix pipe 24 % of the cycles, conflicts in 31 % of the LDS cycles (W's scales lie 32 bytes apart: four rows of a read to a bank, at
+// least), 146 MB read for 15 (tiles in row order: W for every row of tiles and XCD).
 constexpr int STAGE_BYTES = 128, STAGE_SCALES = 8;   // of a row and stage
 template <int WP_, int WQ_, int WM> struct MxTile {
     static constexpr int WP = WP_, WQ = WQ_, WAVES = 2 * WM;                 // 32 x 32 tiles of a wavefront
@@ -151,7 +153,8 @@ template <int WP_, int WQ_, int WM> struct MxTile {
     static constexpr int CHUNKS = 2 * STAGE, LDS = CHUNKS + 2 * CHUNK;
     static constexpr int PI = N / (8 * WAVES), QI = M / (8 * WAVES);                          // requests (8 rows each) of a wavefront and stage
     static constexpr int REQUESTS = PI + QI + 1, CI = CHUNK / (256 * WAVES);                  // with X's scales; of a chunk
-    // results of large tiles, 64 MB and more, leave past the caches: 4096 x 2560 -> 131072 1204 us and 981 so, -> 6912 66.9 and 66.2
+    // results of the large tiles, taken from some 40 MB on, leave past the caches, us through them and past: 4096 x 2560 -> 131072 1204 and 981, -> 6912 65.9
+    // and 65.5, -> 2560 33.0 and 31.1; 1500 x 2560 -> 6912 30.8 and 28.4
     static constexpr bool PAST_CACHES = WP == 4;
     static constexpr int OUT = WP * 128;                                     // bytes of a staged row of results
     static_assert(WAVES * 32 * OUT <= CHUNKS, "results are staged in the idle stages");
