@@ -453,6 +453,82 @@ sbn_status sbn_mxfp4_linear(const void *X, int64_t tokens, int64_t d_in, int64_t
                             const float *bias, float *Y, void *workspace, size_t ws_bytes, void *stream);
 
 /*
+ * RMS and layer norm of rows, in front of a layer or where a block's rows are added to the residual stream, and their gradients.  With
+ *   S = X (+ residual, rounded to the rows' type),   mu = mean S (layer 0: no mean is taken off),   r = 1 / sqrt(mean (S - mu)^2 + eps),   h = (S - mu) r
+ *   Y  = h gain (+ bias)
+ *   dX = r (a - mean a (layer 0: not taken off) - h mean(a h)) (+ d_residual),   a = dY gain,   dgain = sum_t dY h,   dbias = sum_t dY
+ * X of the backward is what was normalised: sum_out where the forward had a residual.
+ *   X, residual, Y, sum_out, dY, d_residual, dX   device, rows of one type (dtype: fp32 or bf16) [tokens, d_in]
+ *   residual, sum_out     both given or both NULL; sum_out may be X or residual, Y may be X or residual unless that is sum_out
+ *   gain, bias            device, fp32 [d_in]; NULL: 1 and 0
+ *   dX, dgain, dbias      device, overwritten; NULL: not wanted (not all three); dX may be dY or d_residual; d_residual NULL: none.  dgain, dbias fp32 [d_in]
+ *   workspace             device, 256-byte aligned, >= sbn_norm_workspace_bytes(tokens, d_in)
+ * Pointers are aligned to their values; d_in is any number up to 16384.  Arithmetic in fp32 (r of the RMS form forward in double, rounded once: where
+ * gain is given and bias is not, Y in bf16 is xn_out of sbn_rmsnorm_act_quant), results rounded once.  No atomics: a call repeated gives the same bits.
+ * A row with a NaN or an infinity is NaN in Y and dX, other rows are not touched by it; dgain and dbias are sums over all rows.
+ * Errors: SBN_EINVAL, SBN_EALIGN, SBN_ESIZE, SBN_EUNSUPPORTED (d_in > 16384, tokens > 2^24), SBN_EHIP.
+ */
+sbn_status sbn_norm(const void *X, const void *residual, sbn_dtype dtype, int64_t tokens, int64_t d_in, const float *gain, const float *bias, float eps, int layer,
+                    void *Y, void *sum_out, void *stream);
+sbn_status sbn_norm_workspace_bytes(int64_t tokens, int64_t d_in, size_t *bytes);
+sbn_status sbn_norm_backward(const void *X, const void *dY, const void *d_residual, sbn_dtype dtype, int64_t tokens, int64_t d_in, const float *gain, float eps,
+                             int layer, void *dX, float *dgain, float *dbias, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * The way in: rows of a table by token, and the gradient of the table.
+ *   Y[t,:] = scale E[ids[t],:],   dE[v,:] = scale sum_{t: ids[t] = v} dY[t,:]
+ *   E, dE      device, fp32 or bf16 (table_dtype) [vocab, d_in];  Y, dY  device, fp32 or bf16 (y_dtype) [tokens, d_in]
+ *   ids        device, int64 [tokens]; a token whose id is outside [0, vocab) gets zeros and has no share in the gradient
+ *   accumulate 0: every row of dE is written, those that no token names with zeros; else the sums are added to what dE holds (a table that is the
+ *              head's matrix as well: after sbn_head_*_backward), and rows that no token names are not touched
+ *   workspace  device, 256-byte aligned, >= sbn_embedding_workspace_bytes(tokens, d_in, vocab)
+ * Pointers are aligned to their values; d_in is any number.  Sums are fp32, multiplied by scale, then rounded once (accumulate: after the addition).
+ * The tokens of an id are added in their own order, in runs whose sums are added in turn; no atomics on values: a call repeated gives the same bits.
+ * Errors: SBN_EINVAL, SBN_EALIGN, SBN_ESIZE, SBN_EUNSUPPORTED (tokens or vocab > 2^24, d_in > 2^16, tokens or vocab times d_in > 2^34), SBN_EHIP.
+ */
+sbn_status sbn_embedding(const void *E, sbn_dtype table_dtype, int64_t vocab, int64_t d_in, const int64_t *ids, int64_t tokens, float scale, void *Y, sbn_dtype y_dtype,
+                         void *stream);
+sbn_status sbn_embedding_workspace_bytes(int64_t tokens, int64_t d_in, int64_t vocab, size_t *bytes);
+sbn_status sbn_embedding_backward(const void *dY, sbn_dtype y_dtype, const int64_t *ids, int64_t tokens, int64_t vocab, int64_t d_in, float scale, int accumulate,
+                                  void *dE, sbn_dtype table_dtype, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * The step from gradients to new weights (Table of hyperparameters: AdamW with a clipped gradient norm), over `count` tensors at once.  HOST arrays of
+ * length count; tensors of a call share their types.
+ *   norm:  out[0] = sqrt(sum over all values of all gradients, squared),   out[1] = min(1, max_norm / out[0]), NaN where the norm is not finite
+ *   step:  g scaled by *clip first (NULL: as it is),   m' = beta1 m + (1 - beta1) g,   v' = beta2 v + ((1 - beta2) g) g
+ *          p' = p (1 - lr weight_decay[i]) - lr / (1 - beta1^t) m' / (sqrt(v' / (1 - beta2^t)) + eps),   t = *step
+ *   params      device, fp32 or bf16, updated;  grads  device, fp32 or bf16, read
+ *   m, v        device, fp32, updated (m_scales and v_scales NULL), or moments in 8 bits: m and v hold a byte per value, m_scales and v_scales one per 32
+ *               values, sbn_adamw_state_bytes() each (the codes padded to whole 32); all bytes zero: all moments zero
+ *   weight_decay  HOST, NULL: none
+ *   lr, step    device, one fp32 and one int64 >= 1: read when the kernels run, so a captured step may be replayed with others
+ *   clip        device, one fp32, as out[1] above, or NULL; where it is not finite, nothing is changed: no step is made of gradients that are not finite
+ *   seed        HOST, NULL: bf16 weights and 8-bit moments are rounded to nearest, ties to even; else they are rounded stochastically, by 16 bits
+ *               for each from a hash of *seed, *step, the tensor's place in the call and the value's place in the tensor.  An update below half a step of
+ *               bf16, or a v that falls by less than half a step of its code, is lost by the one and kept on average by the other.
+ *   workspace   device, 256-byte aligned, >= sbn_grad_norm_workspace_bytes(count, sizes)
+ * Moments in 8 bits.  32 consecutive values of a tensor share a byte e, the exponent field (as of fp32) of their largest magnitude (one more where its
+ * mantissa is above 1.875), at least 15 (m) or 31 (v).  With c the low seven bits of m's code, or v's code, a value is 0 for c = 0, else the fp32 number
+ * of pattern (c + 8 (e - 15 or 31)) << 20: three bits of mantissa, 15 or 31 binades; m's top bit is the sign.  Values below are 0 for m, and the
+ * lowest code for a v that is not 0.  Every value is exact in bf16.
+ * Pointers are aligned to their values, codes to 8 bytes.  No params, m, v or scales may share memory with another of its own list (SBN_EINVAL), nor
+ * with another list.  Arithmetic in fp32, each operation rounded (the norm in double).  No atomics: a call repeated gives the same bits.  A gradient
+ * that is not finite and no clip: its weight and moments in fp32 are not finite after; moments in 8 bits of its 32 values stand for nothing in particular.
+ * Errors: SBN_EINVAL (null, sizes not positive, beta outside [0, 1), eps or weight_decay not finite, max_norm not positive), SBN_EALIGN, SBN_ESIZE,
+ * SBN_EUNSUPPORTED (count > 4096, a tensor of more than 2^31 values), SBN_EHIP.
+ */
+sbn_status sbn_grad_norm_workspace_bytes(int count, const int64_t *sizes, size_t *bytes);
+sbn_status sbn_grad_norm(int count, const void *const *grads, sbn_dtype dtype, const int64_t *sizes, float max_norm, float *out, void *workspace, size_t ws_bytes,
+                         void *stream);
+sbn_status sbn_adamw_state_bytes(int64_t n, size_t *codes, size_t *scales);
+/* The values that moments in 8 bits stand for, exactly, in fp32 or bf16; second: v, else m. */
+sbn_status sbn_adamw_state_values(const void *codes, const uint8_t *scales, int64_t n, int second, void *out, sbn_dtype dtype, void *stream);
+sbn_status sbn_adamw_step(int count, void *const *params, sbn_dtype param_dtype, const void *const *grads, sbn_dtype grad_dtype, void *const *m, void *const *v,
+                          uint8_t *const *m_scales, uint8_t *const *v_scales, const int64_t *sizes, const float *weight_decay, const float *lr, const int64_t *step,
+                          double beta1, double beta2, double eps, const float *clip, const uint64_t *seed, void *stream);
+
+/*
  * Test hook: the sizes of the block tiles that the output head takes, so that a test reaches the edges of each whatever an estimate
  * chooses: 0, 1, 2 for tiles of 64, 128 and 256; for the gradients 3 for the kernel of up to 64 tokens as well; negative for the
  * library's choice.  (A product in 4-bit floating point of up to 64 tokens takes its own kernel only by that choice.)  Workspaces are to be asked

@@ -107,6 +107,19 @@ def _load():
     lib.sbn_mxfp4_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(sz)]
     lib.sbn_mxfp4_linear.restype = cint
     lib.sbn_mxfp4_linear.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, vp, sz, vp]
+    f32, f64, pvp = ctypes.c_float, ctypes.c_double, ctypes.POINTER(ctypes.c_float)
+    for name, types in (("sbn_norm", [vp, vp, cint, i64, i64, vp, vp, f32, cint, vp, vp, vp]),
+                        ("sbn_norm_workspace_bytes", [i64, i64, ctypes.POINTER(sz)]),
+                        ("sbn_norm_backward", [vp, vp, vp, cint, i64, i64, vp, f32, cint, vp, vp, vp, vp, sz, vp]),
+                        ("sbn_embedding", [vp, cint, i64, i64, vp, i64, f32, vp, cint, vp]),
+                        ("sbn_embedding_workspace_bytes", [i64, i64, i64, ctypes.POINTER(sz)]),
+                        ("sbn_embedding_backward", [vp, cint, vp, i64, i64, i64, f32, cint, vp, cint, vp, sz, vp]),
+                        ("sbn_grad_norm_workspace_bytes", [cint, pi64, ctypes.POINTER(sz)]),
+                        ("sbn_grad_norm", [cint, pp, cint, pi64, f32, vp, vp, sz, vp]),
+                        ("sbn_adamw_state_bytes", [i64, ctypes.POINTER(sz), ctypes.POINTER(sz)]),
+                        ("sbn_adamw_state_values", [vp, vp, i64, cint, vp, cint, vp]),
+                        ("sbn_adamw_step", [cint, pp, cint, pp, cint, pp, pp, pp, pp, pi64, pvp, vp, vp, f64, f64, f64, vp, ctypes.POINTER(ctypes.c_uint64), vp])):
+        getattr(lib, name).restype, getattr(lib, name).argtypes = cint, types
     lib.sbn_mask_flips.restype = cint
     lib.sbn_mask_flips.argtypes = [vp, vp, i64, i64, cint, cint, vp, vp, sz, vp]
     return lib
@@ -660,6 +673,182 @@ def sbn_mxfp4_linear(X, codes, scales, Y, workspace, bias=None):
     _on_gpu(X, codes, scales, Y, workspace, bias)
     _check(_lib.sbn_mxfp4_linear(_ptr(X), tokens, d_in, d_out, _ptr(codes), _ptr(scales), _ptr(bias), _ptr(Y), _ptr(workspace),
                                  _bytes_of(workspace), _stream()), "sbn_mxfp4_linear")
+
+
+def _here(*tensors):
+    """Tensors of a call lie on the current device: its stream is the one that the kernels run on."""
+    _on_gpu(*tensors)
+    device = (_current_device or torch.cuda.current_device)()
+    for t in tensors:
+        if t is not None and t.device.index != device:
+            raise ValueError(f"tensors must be on the current device (cuda:{device}), not on {t.device}")
+
+
+def _size_query(fn, where, *args):
+    out = ctypes.c_size_t(0)
+    _check(fn(*args, ctypes.byref(out)), where)
+    return out.value
+
+
+def _row_type(name, t):
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"{name} must be float32 or bfloat16")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    return _dtype_code(t)
+
+
+def sbn_norm(X, Y, gain=None, bias=None, eps: float = 1e-6, layer: bool = False, residual=None, sum_out=None):
+    """Y = the RMS norm (layer: layer norm) of the rows of X, or of X + residual, which is then given back in sum_out; gain, bias fp32."""
+    dtype, shape = _row_type("X", X), X.shape
+    for name, t in (("X", X), ("Y", Y), ("residual", residual), ("sum_out", sum_out)):
+        _expect(name, t, shape, X.dtype)
+    _expect("gain", gain, shape[1:], torch.float32)
+    _expect("bias", bias, shape[1:], torch.float32)
+    _here(X, Y, gain, bias, residual, sum_out)
+    _check(_lib.sbn_norm(_ptr(X), _ptr(residual), dtype, *shape, _ptr(gain), _ptr(bias), eps, int(layer), _ptr(Y), _ptr(sum_out), _stream()), "sbn_norm")
+
+
+def sbn_norm_workspace_bytes(tokens: int, d_in: int) -> int:
+    return _size_query(_lib.sbn_norm_workspace_bytes, "sbn_norm_workspace_bytes", tokens, d_in)
+
+
+def sbn_norm_backward(X, dY, workspace, dX=None, dgain=None, dbias=None, gain=None, eps: float = 1e-6, layer: bool = False, d_residual=None):
+    """dX (+ d_residual), dgain and dbias (fp32) of sbn_norm for the gradient dY of its Y; X is what was normalised.  None: not wanted."""
+    dtype, shape = _row_type("X", X), X.shape
+    for name, t in (("X", X), ("dY", dY), ("dX", dX), ("d_residual", d_residual)):
+        _expect(name, t, shape, X.dtype)
+    for name, t in (("gain", gain), ("dgain", dgain), ("dbias", dbias)):
+        _expect(name, t, shape[1:], torch.float32)
+    _here(X, dY, workspace, dX, dgain, dbias, gain, d_residual)
+    _check(_lib.sbn_norm_backward(_ptr(X), _ptr(dY), _ptr(d_residual), dtype, *shape, _ptr(gain), eps, int(layer), _ptr(dX), _ptr(dgain), _ptr(dbias),
+                                  _ptr(workspace), _bytes_of(workspace), _stream()), "sbn_norm_backward")
+
+
+def _embedding(table_name, table, rows_name, rows, ids):
+    """Types and sizes of a table and of the rows that go with ids."""
+    types = _row_type(table_name, table), _row_type(rows_name, rows)
+    (vocab, d), tokens = table.shape, ids.numel()
+    _expect(table_name, table, (vocab, d), table.dtype)
+    _expect(rows_name, rows, (tokens, d), rows.dtype)
+    _expect("ids", ids, (tokens,), torch.int64)
+    return (*types, vocab, d, tokens)
+
+
+def sbn_embedding(E, ids, Y, scale: float = 1.0):
+    """Y[t,:] = scale E[ids[t],:] (fp32 or bf16 each); zeros where the id (int64) is outside the table."""
+    table, rows, vocab, d, tokens = _embedding("E", E, "Y", Y, ids)
+    _here(E, ids, Y)
+    _check(_lib.sbn_embedding(_ptr(E), table, vocab, d, _ptr(ids), tokens, scale, _ptr(Y), rows, _stream()), "sbn_embedding")
+
+
+def sbn_embedding_workspace_bytes(tokens: int, d_in: int, vocab: int) -> int:
+    return _size_query(_lib.sbn_embedding_workspace_bytes, "sbn_embedding_workspace_bytes", tokens, d_in, vocab)
+
+
+def sbn_embedding_backward(dY, ids, dE, workspace, scale: float = 1.0, accumulate: bool = False):
+    """dE[v,:] = scale sum of dY[t,:] over the tokens of id v: every row written, or (accumulate) the sums added to what dE holds."""
+    table, rows, vocab, d, tokens = _embedding("dE", dE, "dY", dY, ids)
+    _here(dY, ids, dE, workspace)
+    _check(_lib.sbn_embedding_backward(_ptr(dY), rows, _ptr(ids), tokens, vocab, d, scale, int(accumulate), _ptr(dE), table, _ptr(workspace), _bytes_of(workspace),
+                                       _stream()), "sbn_embedding_backward")
+
+
+def _tensors(name, tensors, *dtypes, like=None):
+    """A non-empty list of contiguous tensors of one of these types, as many values each as those of `like`."""
+    tensors = list(tensors)
+    if not tensors or (like is not None and len(tensors) != len(like)):
+        raise ValueError(f"{name} must be a list of {len(like) if like is not None else 'one or more'} tensors")
+    for i, t in enumerate(tensors):
+        if t.dtype not in dtypes or t.dtype != tensors[0].dtype:
+            raise TypeError(f"{name} must all be {' or all '.join(str(d).removeprefix('torch.') for d in dtypes)}")
+        if not t.is_contiguous() or (like is not None and t.numel() != like[i]):
+            raise ValueError(f"{name}[{i}] must be contiguous" + (f" and have {like[i]} values, not {t.numel()}" if like is not None else ""))
+    _here(*tensors)
+    return tensors
+
+
+def sbn_grad_norm_workspace_bytes(sizes) -> int:
+    """Workspace of the norm of gradients of so many values each."""
+    return _size_query(_lib.sbn_grad_norm_workspace_bytes, "sbn_grad_norm_workspace_bytes", len(sizes), _i64_array(sizes))
+
+
+class GradNormGroup:
+    """Host-side argument arrays of sbn_grad_norm, marshalled once and reusable."""
+
+    def __init__(self, grads, workspace):
+        self.keep = _tensors("grads", grads, torch.float32, torch.bfloat16)
+        _here(workspace)
+        self.count, self.dtype = len(self.keep), _dtype_code(self.keep[0])
+        self.grads, self.sizes, self.workspace = _ptr_array(self.keep), _i64_array([g.numel() for g in self.keep]), workspace
+
+    def run(self, max_norm: float, out):
+        _expect("out", out, (2,), torch.float32)
+        ws = self.workspace
+        _here(out, ws)
+        _check(_lib.sbn_grad_norm(self.count, self.grads, self.dtype, self.sizes, max_norm, _ptr(out), _ptr(ws), _bytes_of(ws), _stream()), "sbn_grad_norm")
+
+
+def sbn_grad_norm(grads, max_norm: float, out, workspace):
+    """out (fp32 [2]) = the norm of all gradients, and the factor that brings it down to max_norm (at most 1; NaN where the norm is not finite)."""
+    GradNormGroup(grads, workspace).run(max_norm, out)
+
+
+def sbn_adamw_state_bytes(n: int):
+    """Bytes of the codes and of the scales of n moments in 8 bits."""
+    codes, scales = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(_lib.sbn_adamw_state_bytes(n, ctypes.byref(codes), ctypes.byref(scales)), "sbn_adamw_state_bytes")
+    return codes.value, scales.value
+
+
+def sbn_adamw_state_values(codes, scales, out, second: bool = False):
+    """The values that moments in 8 bits stand for, exactly, into out (fp32 or bf16, any shape); second: of v, else of m."""
+    _expect("out", out, out.shape, torch.float32, torch.bfloat16)
+    for name, t, nbytes in zip(("codes", "scales"), (codes, scales), sbn_adamw_state_bytes(out.numel())):
+        _expect(name, t, (nbytes,), torch.uint8)
+    _here(codes, scales, out)
+    _check(_lib.sbn_adamw_state_values(_ptr(codes), _ptr(scales), out.numel(), int(second), _ptr(out), _dtype_code(out), _stream()), "sbn_adamw_state_values")
+
+
+class AdamWGroup:
+    """Host-side argument arrays of sbn_adamw_step, marshalled once and reusable.  Lists hold one tensor per weight: params and grads fp32 or bf16, m and v
+    fp32, or (with m_scales and v_scales) the bytes of moments in 8 bits; weight_decay is a number, or one per weight."""
+
+    def __init__(self, params, grads, m, v, m_scales=None, v_scales=None, weight_decay=0.0, betas=(0.9, 0.95), eps: float = 1e-8):
+        params = _tensors("params", params, torch.float32, torch.bfloat16)
+        sizes = [p.numel() for p in params]
+        grads = _tensors("grads", grads, torch.float32, torch.bfloat16, like=sizes)
+        if (m_scales is None) != (v_scales is None):
+            raise ValueError("m_scales and v_scales are both given or neither")
+        bits8 = m_scales is not None
+        codes, scales = zip(*(sbn_adamw_state_bytes(n) for n in sizes)) if bits8 else (sizes, None)
+        m, v = (_tensors(name, t, torch.uint8 if bits8 else torch.float32, like=codes) for name, t in (("m", m), ("v", v)))
+        if bits8:
+            m_scales, v_scales = (_tensors(name, t, torch.uint8, like=scales) for name, t in (("m_scales", m_scales), ("v_scales", v_scales)))
+        decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * len(params)
+        if len(decay) != len(params):
+            raise ValueError(f"weight_decay must be a number or {len(params)} of them")
+        self.count, self.sizes = len(params), _i64_array(sizes)
+        self.types = _dtype_code(params[0]), _dtype_code(grads[0])
+        self.params, self.grads, self.m, self.v = (_ptr_array(t) for t in (params, grads, m, v))
+        self.m_scales, self.v_scales = (_ptr_array(t) if bits8 else None for t in (m_scales, v_scales))
+        self.decay = (ctypes.c_float * len(decay))(*decay)
+        self.betas, self.eps = betas, eps
+        self.keep = (params, grads, m, v, m_scales, v_scales)
+
+    def run(self, lr, step, clip=None, seed: int | None = None):
+        """One step: lr (fp32 [1]), step (int64 [1], counted from 1) and clip (fp32 [1], or None) on the device; seed: round stochastically."""
+        _expect("lr", lr, (1,), torch.float32)
+        _expect("step", step, (1,), torch.int64)
+        _expect("clip", clip, (1,), torch.float32)
+        _here(lr, step, clip, self.keep[0][0])
+        _check(_lib.sbn_adamw_step(self.count, self.params, self.types[0], self.grads, self.types[1], self.m, self.v, self.m_scales, self.v_scales, self.sizes,
+                                   self.decay, _ptr(lr), _ptr(step), *self.betas, self.eps, _ptr(clip),
+                                   None if seed is None else ctypes.byref(ctypes.c_uint64(seed)), _stream()), "sbn_adamw_step")
+
+
+def sbn_adamw_step(params, grads, m, v, lr, step, m_scales=None, v_scales=None, weight_decay=0.0, betas=(0.9, 0.95), eps: float = 1e-8, clip=None, seed=None):
+    AdamWGroup(params, grads, m, v, m_scales, v_scales, weight_decay, betas, eps).run(lr, step, clip, seed)
 
 
 def sbn_test_set_head_tiles(logits: int = -1, gradients: int = -1, mxfp4: int = -1):

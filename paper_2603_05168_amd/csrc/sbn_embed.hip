@@ -1,0 +1,347 @@
+// Embedding: the rows of a table that the tokens name, and the gradient of the table.
+//
+//   Y[t,:] = scale E[ids[t],:]             (zeros where the id is outside the table)
+//   dE[v,:] = scale sum_{t: ids[t] = v} dY[t,:]   (+ dE[v,:])
+// Both are bound by memory: the forward moves the rows, the gradient reads dY once and writes the whole table (or, where it is added to one,
+// the rows that are named).
+//
+// The gradient goes by sorted tokens, so that no two writers meet and a repeated call gives the same bits:
+//   sort_kernel   puts the tokens in order of their ids, tokens of one id in their own order.  Ids go to blocks round-robin, which spreads the
+//                 frequent ones; a block looks through all ids, counts those of lower blocks (where its share of the order begins) and its own,
+//                 and places these.
+//   sum_kernel    walks the order in pieces of PIECE tokens, which balances the work however often an id occurs.  An id whose tokens all lie in
+//                 a piece is written there; of one that crosses pieces each leaves a partial sum in fp32.
+//   join_kernel   adds the partial sums of such an id in the order of the pieces.
+#include <algorithm>
+
+#include "sbn_internal.hpp"
+#include "sbn_rows.hpp"
+
+namespace sbn {
+
+namespace {
+
+constexpr int SORT_THREADS = 1024;
+constexpr int SORT_IDS = 8;                              // consecutive ids of a thread
+constexpr int SORT_TILE = SORT_THREADS * SORT_IDS;
+constexpr int SORT_OWN = 16384;                          // ids of the table that one sorting block has at most: their counts lie in LDS
+constexpr int PIECE = 16;                                // tokens of a piece
+
+// the sorting blocks are 2^sort_shift() and share out the ids of the table
+inline int sort_shift(int64_t vocab)
+{
+    int shift = 8;
+    while (vocab > (int64_t)SORT_OWN << shift) ++shift;
+    return shift;
+}
+
+// a wavefront copies a row
+template <sbn_dtype TABLE, sbn_dtype OUT> __global__ void __launch_bounds__(256) embedding_kernel(const void *E, const int64_t *ids, int64_t tokens, int64_t vocab,
+                                                                                                  int64_t d, float scale, void *Y)
+{
+    constexpr int U = unit_of(TABLE, OUT);
+    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t >= tokens) return;
+    const int64_t id = ids[t];
+    const bool inside = id >= 0 && id < vocab;
+    const void *from = static_cast<const typename Row<TABLE>::value *>(E) + (inside ? id : 0) * d;
+    void *to = static_cast<typename Row<OUT>::value *>(Y) + t * d;
+    for (int64_t u = threadIdx.x & 63; u * U < d; u += 64) {
+        float f[U] = {};
+        if (inside) {
+            load_unit<TABLE, U>(from, u, d, f);
+#pragma unroll
+            for (int k = 0; k < U; ++k) f[k] *= scale;
+        }
+        store_unit<OUT, U>(to, u, d, f);
+    }
+}
+
+struct SortArgs {
+    const int64_t *ids;
+    int64_t tokens, vocab;
+    int *begin;          // [blocks * own + 1]: where the tokens of id k * blocks + b begin in the order, at b * own + k
+    int *order;          // [tokens]: the tokens
+    int *order_ids;      // [tokens]: their ids
+    int own, shift;      // ids of a block; log2 of the blocks
+};
+
+// exclusive sum over the block's threads; total: of all of them
+__device__ __forceinline__ int block_scan(int x, int *scratch, int &total)
+{
+    int s = x;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int o = __shfl_up(s, off, 64);
+        if ((int)(threadIdx.x & 63) >= off) s += o;
+    }
+    __syncthreads();   // the scratch may still be read
+    if ((threadIdx.x & 63) == 63) scratch[threadIdx.x >> 6] = s;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+    for (int w = 0; w < SORT_THREADS / 64; ++w) {
+        const int o = scratch[w];
+        before += w < (int)(threadIdx.x >> 6) ? o : 0;
+        total += o;
+    }
+    return before + s - x;
+}
+
+__global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
+{
+    extern __shared__ int next[];                // [own]: counts, then where the next token of an id goes
+    __shared__ int scratch[SORT_THREADS / 64];
+    __shared__ uint2 found[SORT_TILE];           // (which of the block's ids, token), in the order of the tokens
+    const int block = blockIdx.x;
+    for (int k = threadIdx.x; k < s.own; k += SORT_THREADS) next[k] = 0;
+    __syncthreads();
+    int lower = 0;
+    for (int64_t t = threadIdx.x; t < s.tokens; t += SORT_THREADS) {
+        const int64_t id = s.ids[t];
+        if (id < 0 || id >= s.vocab) continue;
+        const int b = (int)id & ((1 << s.shift) - 1);
+        lower += b < block;
+        if (b == block) atomicAdd(&next[id >> s.shift], 1);   // whole numbers: in any order
+    }
+    int at;
+    block_scan(lower, scratch, at);
+    // from counts to beginnings: each thread a run of ids
+    const int run = (s.own + SORT_THREADS - 1) / SORT_THREADS;
+    const int k0 = min(s.own, (int)threadIdx.x * run), k1 = min(s.own, k0 + run);
+    int mine = 0, all;
+    for (int k = k0; k < k1; ++k) mine += next[k];
+    int begin = at + block_scan(mine, scratch, all);
+    for (int k = k0; k < k1; ++k) {
+        const int count = next[k];
+        next[k] = begin;
+        s.begin[(int64_t)block * s.own + k] = begin;
+        begin += count;
+    }
+    if (block == (int)gridDim.x - 1 && threadIdx.x == 0) s.begin[(int64_t)gridDim.x * s.own] = at + all;
+    if (!all) return;
+    for (int64_t tile = 0; tile < s.tokens; tile += SORT_TILE) {
+        // the tile's tokens of this block, side by side and in their order
+        const int64_t t0 = tile + (int64_t)threadIdx.x * SORT_IDS;
+        int count = 0, total;
+        int id[SORT_IDS];
+#pragma unroll
+        for (int j = 0; j < SORT_IDS; ++j) {
+            id[j] = -1;
+            if (t0 + j < s.tokens) {
+                const int64_t v = s.ids[t0 + j];
+                if (v >= 0 && v < s.vocab && ((int)v & ((1 << s.shift) - 1)) == block) id[j] = (int)(v >> s.shift);
+            }
+            count += id[j] >= 0;
+        }
+        int to = block_scan(count, scratch, total);
+#pragma unroll
+        for (int j = 0; j < SORT_IDS; ++j)
+            if (id[j] >= 0) found[to++] = make_uint2(id[j], (unsigned)(t0 + j));
+        __syncthreads();
+        // one wavefront places them, 64 at a time: a token goes behind those of its id among the lanes in front
+        if (threadIdx.x < 64) {
+            int bits = 32 - __builtin_clz(s.own);
+            for (int i = threadIdx.x; i - (int)threadIdx.x < total; i += 64) {
+                const bool live = i < total;
+                const uint2 f = live ? found[i] : make_uint2(0, 0);
+                unsigned long long same = __ballot(live);
+                for (int b = 0; b < bits; ++b) {
+                    const unsigned long long set = __ballot(f.x >> b & 1);
+                    same &= f.x >> b & 1 ? set : ~set;
+                }
+                const int before = __popcll(same & ((1ull << threadIdx.x) - 1));
+                const int place = live ? next[f.x] + before : 0;
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                if (live) {
+                    s.order[place] = (int)f.y;
+                    s.order_ids[place] = (int)(f.x << s.shift) + block;
+                    if (before == __popcll(same) - 1) next[f.x] = place + 1;
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            }
+        }
+        __syncthreads();
+    }
+}
+
+struct SumArgs {
+    const void *dY;
+    void *dE;
+    const int *begin, *order, *order_ids;
+    float *partials;     // [pieces][2][d]: of the id that the piece begins with, of the one that it ends with
+    int64_t vocab, d;
+    int own, shift, accumulate, pieces;
+    float scale;
+    __device__ __forceinline__ const int *begin_of(int64_t id) const { return begin + (id & ((1 << shift) - 1)) * own + (id >> shift); }
+    __device__ __forceinline__ int total() const { return begin[(int64_t)own << shift]; }   // tokens whose id is in the table
+};
+
+template <sbn_dtype TABLE, int U> __device__ __forceinline__ void write_gradient(const SumArgs &s, int id, int64_t unit, const float (&sum)[U])
+{
+    void *row = static_cast<typename Row<TABLE>::value *>(s.dE) + (int64_t)id * s.d;
+    float f[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) f[k] = sum[k] * s.scale;
+    if (s.accumulate) {
+        float old[U];
+        load_unit<TABLE, U>(row, unit, s.d, old);
+#pragma unroll
+        for (int k = 0; k < U; ++k) f[k] += old[k];
+    }
+    store_unit<TABLE, U>(row, unit, s.d, f);
+}
+
+// blocks below `pieces`: one piece each; those behind: 64 rows of the table each, of which they clear those that no token names
+template <sbn_dtype TABLE, sbn_dtype OUT> __global__ void __launch_bounds__(256) sum_kernel(const SumArgs s)
+{
+    constexpr int U = unit_of(TABLE, OUT);
+    if ((int)blockIdx.x >= s.pieces) {
+        const int64_t v0 = (int64_t)(blockIdx.x - s.pieces) * 64;
+        const u32x4 zero = {0, 0, 0, 0};
+        for (int64_t v = v0 + (threadIdx.x >> 6); v < min(v0 + 64, s.vocab); v += 4) {
+            const int *b = s.begin_of(v);
+            if (b[0] != b[1]) continue;
+            void *row = static_cast<typename Row<TABLE>::value *>(s.dE) + v * s.d;
+            for (int64_t vec = threadIdx.x & 63; vec * Row<TABLE>::E < s.d; vec += 64) store_vec<TABLE>(row, vec, s.d, zero);
+        }
+        return;
+    }
+    const int total = s.total();
+    const int piece = blockIdx.x, p0 = piece * PIECE, p1 = min(total, p0 + PIECE);
+    if (p0 >= p1) return;
+    const bool begun = p0 > 0 && s.order_ids[p0 - 1] == s.order_ids[p0];          // the first id's tokens begin in an earlier piece
+    const bool goes_on = p1 < total && s.order_ids[p1 - 1] == s.order_ids[p1];    // the last id's go on in the next
+    for (int64_t u = threadIdx.x; u * U < s.d; u += 256) {
+        float sum[U] = {};
+        int first = p0;   // of the present id in this piece
+        for (int p = p0; p < p1; ++p) {
+            float f[U];
+            load_unit<OUT, U>(static_cast<const typename Row<OUT>::value *>(s.dY) + (int64_t)s.order[p] * s.d, u, s.d, f);
+#pragma unroll
+            for (int k = 0; k < U; ++k) sum[k] += f[k];
+            const int id = s.order_ids[p];
+            const bool last = p + 1 == p1;
+            if (!last && s.order_ids[p + 1] == id) continue;
+            if (first == p0 && begun)
+                store_unit<SBN_F32, U>(s.partials + (int64_t)piece * 2 * s.d, u, s.d, sum);
+            else if (last && goes_on)
+                store_unit<SBN_F32, U>(s.partials + ((int64_t)piece * 2 + 1) * s.d, u, s.d, sum);
+            else
+                write_gradient<TABLE, U>(s, id, u, sum);
+#pragma unroll
+            for (int k = 0; k < U; ++k) sum[k] = 0.0f;
+            first = p + 1;
+        }
+    }
+}
+
+// one block to a piece in which an id begins that goes on behind it
+template <sbn_dtype TABLE> __global__ void __launch_bounds__(256) join_kernel(const SumArgs s)
+{
+    constexpr int U = Row<TABLE>::E;
+    const int total = s.total();
+    const int piece = blockIdx.x, p0 = piece * PIECE, p1 = p0 + PIECE;
+    if (p1 >= total) return;
+    const int id = s.order_ids[p1];
+    if (s.order_ids[p1 - 1] != id) return;
+    if (p0 > 0 && s.order_ids[p0 - 1] == id) return;   // begins earlier
+    const int end = s.begin_of(id)[1];
+    const int64_t u = (int64_t)blockIdx.y * 256 + threadIdx.x;
+    if (u * U >= s.d) return;
+    float sum[U];
+    load_unit<SBN_F32, U>(s.partials + ((int64_t)piece * 2 + 1) * s.d, u, s.d, sum);
+    for (int64_t q = piece + 1; q * PIECE < end; ++q) {
+        float f[U];
+        load_unit<SBN_F32, U>(s.partials + q * 2 * s.d, u, s.d, f);
+#pragma unroll
+        for (int k = 0; k < U; ++k) sum[k] += f[k];
+    }
+    write_gradient<TABLE, U>(s, id, u, sum);
+}
+
+struct Carved {
+    size_t begin, order, order_ids, partials, total;
+};
+Carved carve(int64_t tokens, int64_t d, int64_t vocab)
+{
+    Carved c;
+    size_t at = 0;
+    const auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at = align_up(at + bytes, 256);
+        return here;
+    };
+    const int shift = sort_shift(vocab);
+    c.begin = take((size_t)((ceil_div(vocab, (int64_t)1 << shift) << shift) + 1) * sizeof(int));
+    c.order = take((size_t)tokens * sizeof(int));
+    c.order_ids = take((size_t)tokens * sizeof(int));
+    c.partials = take((size_t)ceil_div(tokens, PIECE) * 2 * d * sizeof(float));
+    c.total = at;
+    return c;
+}
+
+template <sbn_dtype TABLE, sbn_dtype OUT> sbn_status sum_as(const SumArgs &s, hipStream_t stream)
+{
+    const int64_t clearing = s.accumulate ? 0 : ceil_div(s.vocab, 64);
+    hipLaunchKernelGGL((sum_kernel<TABLE, OUT>), dim3((unsigned)(s.pieces + clearing)), dim3(256), 0, stream, s);
+    if (s.pieces > 1)
+        hipLaunchKernelGGL(join_kernel<TABLE>, dim3((unsigned)s.pieces - 1, (unsigned)ceil_div(ceil_div(s.d, Row<TABLE>::E), 256)), dim3(256), 0, stream, s);
+    return check_launch("sum_kernel");
+}
+
+}  // namespace
+
+size_t embedding_workspace_bytes(int64_t tokens, int64_t d, int64_t vocab) { return carve(tokens, d, vocab).total; }
+
+sbn_status launch_embedding(const void *E, sbn_dtype table, int64_t vocab, int64_t d, const int64_t *ids, int64_t tokens, float scale, void *Y, sbn_dtype out,
+                            hipStream_t stream)
+{
+    const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(tokens, 4)), dim3(256), 0, stream, E, ids, tokens, vocab, d, scale, Y); };
+    if (table == SBN_BF16)
+        out == SBN_BF16 ? launch(embedding_kernel<SBN_BF16, SBN_BF16>) : launch(embedding_kernel<SBN_BF16, SBN_F32>);
+    else
+        out == SBN_BF16 ? launch(embedding_kernel<SBN_F32, SBN_BF16>) : launch(embedding_kernel<SBN_F32, SBN_F32>);
+    return check_launch("embedding_kernel");
+}
+
+sbn_status launch_embedding_backward(const void *dY, sbn_dtype out, const int64_t *ids, int64_t tokens, int64_t vocab, int64_t d, float scale, bool accumulate,
+                                     void *dE, sbn_dtype table, void *workspace, hipStream_t stream)
+{
+    const Carved c = carve(tokens, d, vocab);
+    char *ws = static_cast<char *>(workspace);
+    SortArgs o{};
+    o.ids = ids;
+    o.tokens = tokens;
+    o.vocab = vocab;
+    o.begin = reinterpret_cast<int *>(ws + c.begin);
+    o.order = reinterpret_cast<int *>(ws + c.order);
+    o.order_ids = reinterpret_cast<int *>(ws + c.order_ids);
+    o.shift = sort_shift(vocab);
+    o.own = (int)ceil_div(vocab, (int64_t)1 << o.shift);
+    const size_t lds = (size_t)o.own * sizeof(int);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(sort_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, SORT_OWN * sizeof(int));
+    if (e != hipSuccess) {
+        set_hip_error(e, "hipFuncSetAttribute(sort_kernel)");
+        return SBN_EHIP;
+    }
+    hipLaunchKernelGGL(sort_kernel, dim3(1u << o.shift), dim3(SORT_THREADS), lds, stream, o);
+    SumArgs s{};
+    s.dY = dY;
+    s.dE = dE;
+    s.begin = o.begin;
+    s.order = o.order;
+    s.order_ids = o.order_ids;
+    s.partials = reinterpret_cast<float *>(ws + c.partials);
+    s.vocab = vocab;
+    s.d = d;
+    s.own = o.own;
+    s.shift = o.shift;
+    s.accumulate = accumulate;
+    s.pieces = (int)ceil_div(tokens, PIECE);
+    s.scale = scale;
+    if (table == SBN_BF16) return out == SBN_BF16 ? sum_as<SBN_BF16, SBN_BF16>(s, stream) : sum_as<SBN_BF16, SBN_F32>(s, stream);
+    return out == SBN_BF16 ? sum_as<SBN_F32, SBN_BF16>(s, stream) : sum_as<SBN_F32, SBN_F32>(s, stream);
+}
+
+}  // namespace sbn

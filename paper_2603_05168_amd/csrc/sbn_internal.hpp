@@ -194,4 +194,42 @@ sbn_status launch_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, 
 sbn_status launch_mxfp4_linear(const void *X, int64_t tokens, int64_t d_in, int64_t d_out, const uint8_t *codes, const uint8_t *scales,
                                const float *bias, float *Y, void *workspace, hipStream_t stream);
 
+// ---- norms of rows with their gradients (sbn_norm.hip) --------------------------------------------
+constexpr int64_t NORM_MAX_D = 16384, ROWS_MAX = 1 << 24;
+size_t norm_workspace_bytes(int64_t tokens, int64_t d);
+sbn_status launch_norm(const void *X, const void *residual, sbn_dtype dtype, int64_t tokens, int64_t d, const float *gain, const float *bias, float eps, bool layer,
+                       void *Y, void *sum_out, hipStream_t stream);
+sbn_status launch_norm_backward(const void *X, const void *dY, const void *d_residual, sbn_dtype dtype, int64_t tokens, int64_t d, const float *gain, float eps,
+                                bool layer, void *dX, float *dgain, float *dbias, void *workspace, hipStream_t stream);
+
+// ---- embedding with its gradient (sbn_embed.hip) ---------------------------------------------------
+size_t embedding_workspace_bytes(int64_t tokens, int64_t d, int64_t vocab);
+sbn_status launch_embedding(const void *E, sbn_dtype table, int64_t vocab, int64_t d, const int64_t *ids, int64_t tokens, float scale, void *Y, sbn_dtype out,
+                            hipStream_t stream);
+sbn_status launch_embedding_backward(const void *dY, sbn_dtype out, const int64_t *ids, int64_t tokens, int64_t vocab, int64_t d, float scale, bool accumulate,
+                                     void *dE, sbn_dtype table, void *workspace, hipStream_t stream);
+
+// ---- optimizer step (sbn_optim.hip) -----------------------------------------------------------------
+struct AdamWCall {
+    int count;
+    void *const *params;
+    sbn_dtype param_dtype;
+    const void *const *grads;
+    sbn_dtype grad_dtype;
+    void *const *m, *const *v;
+    uint8_t *const *m_scales, *const *v_scales;   // null: moments in fp32
+    const int64_t *sizes;
+    const float *weight_decay;                    // host, null: none
+    const float *lr;
+    const int64_t *step;
+    double beta1, beta2, eps;
+    const float *clip;                            // null: gradients as they are
+    const uint64_t *seed;                         // host, null: round to nearest
+};
+constexpr int OPTIM_MAX_TENSORS = 4096;
+size_t grad_norm_workspace_bytes(int count, const int64_t *sizes);
+sbn_status launch_grad_norm(int count, const void *const *grads, sbn_dtype dtype, const int64_t *sizes, float max_norm, float *out, void *workspace, hipStream_t stream);
+sbn_status launch_adamw(const AdamWCall &c, hipStream_t stream);
+sbn_status launch_adamw_state_values(const void *codes, const uint8_t *scales, int64_t n, bool second, void *out, sbn_dtype dtype, hipStream_t stream);
+
 }  // namespace sbn

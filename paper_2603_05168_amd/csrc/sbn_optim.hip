@@ -1,0 +1,331 @@
+// The optimizer step over many tensors: the norm of all gradients, and AdamW with moments in fp32 or in 8 bits.
+//
+//   m' = beta1 m + (1 - beta1) g,   v' = beta2 v + ((1 - beta2) g) g          (g scaled first where a factor is given)
+//   p' = p (1 - lr decay) - (lr / (1 - beta1^t)) m' / (sqrt(v' / (1 - beta2^t)) + eps)
+// Bound by memory: bf16 weights and gradients with fp32 moments move 22 bytes per weight, with moments in 8 bits 10.1.
+//
+// Moments in 8 bits: 32 consecutive values share an exponent e (a byte, as of fp32), that of their largest magnitude.  A code is the upper part of
+// the fp32 pattern, exponent and three bits of mantissa, counted from the pattern `below` binades under e: rounding is an addition below the cut,
+// and codes and values are a shift and a sum apart.  m: a sign and seven bits (15 binades), v: eight bits (31 binades).  Code 0 is 0; a v that is
+// not zero keeps the lowest code, so that what it divides does not blow up.
+#include <algorithm>
+#include <cmath>
+
+#include "sbn_internal.hpp"
+#include "sbn_rows.hpp"
+
+namespace sbn {
+
+namespace {
+
+constexpr int64_t CHUNK_VALUES = 8192;   // values of a block
+constexpr int THREADS = 256;
+
+struct AdamWItem {
+    void *p;
+    const void *g;
+    void *m, *v;
+    uint8_t *m_scales, *v_scales;
+    int64_t n;
+    int first_block;
+    float decay;
+};
+constexpr int ADAMW_LAUNCH_MAX = 60;   // tensors of a launch: their table is a kernel argument
+
+struct AdamWArgs {
+    AdamWItem items[ADAMW_LAUNCH_MAX];
+    const float *lr, *clip;
+    const int64_t *step;
+    double beta1, beta2;
+    float eps;
+    uint32_t seed_low, seed_high;
+    int count, first_item;   // first_item: place in the call of items[0]
+};
+static_assert(sizeof(AdamWArgs) <= 4096, "kernel arguments");
+
+// 32 random bits of a counter and two keys: two rounds of a multiplication between shifts, the multipliers from the digits of the golden ratio and
+// of pi.  The rounding needs no more than bits that are even on average and not the same for neighbours, moments or steps.
+__device__ __forceinline__ uint32_t mix(uint32_t x, uint32_t key0, uint32_t key1)
+{
+    x ^= key0;
+    x = (x ^ (x >> 16)) * 0x9E3779B1u;
+    x = (x ^ (x >> 15)) + key1;
+    x *= 0x85A308D3u;
+    return x ^ (x >> 16);
+}
+
+constexpr int M_BELOW = 15, V_BELOW = 31;
+
+template <int BELOW> __device__ __forceinline__ float value_of(uint32_t code, uint32_t exponent)
+{
+    const uint32_t low = BELOW == M_BELOW ? code & 127u : code;
+    const uint32_t a = (low + (exponent - BELOW) * 8u) << 20;
+    const float v = __uint_as_float(low ? a : 0u);
+    return BELOW == M_BELOW && (code & 128u) ? -v : v;
+}
+template <int BELOW> __device__ __forceinline__ uint32_t code_of(float x, uint32_t exponent, uint32_t half)
+{
+    const uint32_t bits = __float_as_uint(x), a = bits & 0x7fffffffu;
+    int code = (int)((a + half) >> 20) - (int)(exponent - BELOW) * 8;
+    if (BELOW == V_BELOW) return a ? (uint32_t)max(code, 1) : 0u;
+    return (uint32_t)max(code, 0) | (bits >> 31 << 7);
+}
+__device__ __forceinline__ uint32_t nearest(float x) { return 0x7ffffu + ((__float_as_uint(x) >> 20) & 1u); }
+
+// the exponent that 32 values share, four lanes with eight each
+template <int BELOW> __device__ __forceinline__ uint32_t shared_exponent(const float (&x)[8])
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+    return max((top + 0xfffffu) >> 23, (uint32_t)BELOW);   // one more where rounding may reach the next binade
+}
+
+template <sbn_dtype PT, sbn_dtype GT, bool BITS8, bool STOCHASTIC> __global__ void __launch_bounds__(THREADS) adamw_kernel(const AdamWArgs a)
+{
+    float factor = 1.0f;
+    if (a.clip) {
+        factor = *a.clip;
+        if (!(fabsf(factor) <= 3.4028235e38f)) return;   // gradients that are not finite: no step
+    }
+    int which = 0;
+    while (which + 1 < a.count && (int)blockIdx.x >= a.items[which + 1].first_block) ++which;
+    const AdamWItem it = a.items[which];
+    const int64_t step = *a.step;
+    const double lr = (double)*a.lr;
+    const float rate = (float)(lr / (1.0 - pow(a.beta1, (double)step)));
+    const float keep = (float)(1.0 - lr * (double)it.decay);
+    const float of_v = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)step)));
+    const float b1 = (float)a.beta1, c1 = (float)(1.0 - a.beta1), b2 = (float)a.beta2, c2 = (float)(1.0 - a.beta2);
+    uint32_t key0 = 0, key1 = 0;
+    if (STOCHASTIC) {
+        key0 = mix(a.seed_low, a.seed_high, 0);
+        key0 = mix(key0, (uint32_t)step, (uint32_t)(step >> 32));
+        key0 = mix(key0, (uint32_t)(a.first_item + which), 0);
+        key1 = mix(key0, 0x243F6A88u, 0);
+    }
+    const int64_t begin = (int64_t)((int)blockIdx.x - it.first_block) * CHUNK_VALUES;
+    const int64_t end = min(it.n, begin + CHUNK_VALUES);
+    // a thread has eight values, four threads the 32 that share an exponent: all four go through the loop together
+    for (int64_t at = begin + threadIdx.x * 8; at < (end + 31) / 32 * 32; at += THREADS * 8) {
+        const int64_t unit = at / 8;
+        float p[8], g[8], m[8], v[8];
+        load_unit<PT, 8>(it.p, unit, it.n, p);
+        load_unit<GT, 8>(it.g, unit, it.n, g);
+        if constexpr (BITS8) {
+            const uint2 mc = static_cast<const uint2 *>(it.m)[unit], vc = static_cast<const uint2 *>(it.v)[unit];
+            const uint32_t me = it.m_scales[at / 32], ve = it.v_scales[at / 32];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                m[k] = at + k < it.n ? value_of<M_BELOW>(((k < 4 ? mc.x : mc.y) >> (8 * (k & 3))) & 255u, me) : 0.0f;
+                v[k] = at + k < it.n ? value_of<V_BELOW>(((k < 4 ? vc.x : vc.y) >> (8 * (k & 3))) & 255u, ve) : 0.0f;
+            }
+        } else {
+            load_unit<SBN_F32, 8>(it.m, unit, it.n, m);
+            load_unit<SBN_F32, 8>(it.v, unit, it.n, v);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float s = a.clip ? g[k] * factor : g[k];
+            m[k] = m[k] * b1 + s * c1;
+            v[k] = v[k] * b2 + s * c2 * s;
+            p[k] = p[k] * keep - rate * m[k] / (sqrtf(v[k]) * of_v + a.eps);
+        }
+        uint32_t noise[3][4];   // two values of 16 bits: of p, m and v
+        if constexpr (STOCHASTIC) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t pair = (uint32_t)(at / 2 + k);
+#pragma unroll
+                for (int j = 0; j < 3; ++j) noise[j][k] = mix(3 * pair + j, key0, key1);
+            }
+        }
+        const auto bits16 = [&](int j, int k) { return k & 1 ? noise[j][k / 2] >> 16 : noise[j][k / 2] & 0xffffu; };
+        if constexpr (PT == SBN_BF16 && STOCHASTIC) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) p[k] = __uint_as_float((__float_as_uint(p[k]) + bits16(0, k)) & 0xffff0000u);
+        }
+        store_unit<PT, 8>(it.p, unit, it.n, p);
+        if constexpr (BITS8) {
+            const uint32_t me = shared_exponent<M_BELOW>(m), ve = shared_exponent<V_BELOW>(v);
+            uint32_t mc[2] = {0, 0}, vc[2] = {0, 0};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                mc[k / 4] |= code_of<M_BELOW>(m[k], me, STOCHASTIC ? bits16(1, k) * 16 + 8 : nearest(m[k])) << (8 * (k & 3));
+                vc[k / 4] |= code_of<V_BELOW>(v[k], ve, STOCHASTIC ? bits16(2, k) * 16 + 8 : nearest(v[k])) << (8 * (k & 3));
+            }
+            static_cast<uint2 *>(it.m)[unit] = make_uint2(mc[0], mc[1]);
+            static_cast<uint2 *>(it.v)[unit] = make_uint2(vc[0], vc[1]);
+            if (at % 32 == 0) {
+                it.m_scales[at / 32] = (uint8_t)me;
+                it.v_scales[at / 32] = (uint8_t)ve;
+            }
+        } else {
+            store_unit<SBN_F32, 8>(it.m, unit, it.n, m);
+            store_unit<SBN_F32, 8>(it.v, unit, it.n, v);
+        }
+    }
+}
+
+template <sbn_dtype OUT, int BELOW> __global__ void __launch_bounds__(256) state_values_kernel(const uint2 *codes, const uint8_t *scales, int64_t n, void *out)
+{
+    const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (unit * 8 >= n) return;
+    const uint2 c = codes[unit];
+    const uint32_t e = scales[unit / 4];
+    float f[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f[k] = value_of<BELOW>(((k < 4 ? c.x : c.y) >> (8 * (k & 3))) & 255u, e);
+    store_unit<OUT, 8>(out, unit, n, f);
+}
+
+// ---- the norm of all gradients ----------------------------------------------------------------------------------------------------
+struct NormItem {
+    const void *g;
+    int64_t n;
+    int first_block, pad;
+};
+constexpr int GRAD_NORM_LAUNCH_MAX = 160;
+constexpr int64_t GRAD_NORM_VALUES = 32768;   // values of a block
+
+struct GradNormArgs {
+    NormItem items[GRAD_NORM_LAUNCH_MAX];
+    double *sums;
+    int count;
+};
+static_assert(sizeof(GradNormArgs) <= 4096, "kernel arguments");
+
+__device__ __forceinline__ double block_sum(double s, double *scratch)
+{
+    s = wave_sum(s);
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = 0.0;
+    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) s += scratch[w];
+    return s;
+}
+
+// squares in double: those of fp32 gradients reach past the range of fp32
+template <sbn_dtype GT> __global__ void __launch_bounds__(256) square_sums_kernel(const GradNormArgs a)
+{
+    __shared__ double scratch[4];
+    int which = 0;
+    while (which + 1 < a.count && (int)blockIdx.x >= a.items[which + 1].first_block) ++which;
+    const NormItem it = a.items[which];
+    const int64_t begin = (int64_t)((int)blockIdx.x - it.first_block) * GRAD_NORM_VALUES;
+    const int64_t end = min(it.n, begin + GRAD_NORM_VALUES);
+    double s = 0.0;
+    for (int64_t at = begin + threadIdx.x * 8; at < end; at += 256 * 8) {
+        float g[8];
+        load_unit<GT, 8>(it.g, at / 8, it.n, g);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += (double)g[k] * (double)g[k];
+    }
+    s = block_sum(s, scratch);
+    if (threadIdx.x == 0) a.sums[blockIdx.x] = s;
+}
+
+__global__ void __launch_bounds__(1024) grad_norm_kernel(const double *sums, int64_t blocks, float max_norm, float *out)
+{
+    __shared__ double scratch[16];
+    double s = 0.0;
+    for (int64_t b = threadIdx.x; b < blocks; b += 1024) s += sums[b];
+    s = block_sum(s, scratch);
+    if (threadIdx.x == 0) {
+        const double norm = sqrt(s);
+        out[0] = (float)norm;
+        out[1] = isfinite(norm) ? (float)fmin(1.0, (double)max_norm / norm) : __uint_as_float(0x7fc00000u);
+    }
+}
+
+template <sbn_dtype PT, sbn_dtype GT, bool BITS8> void launch_adamw_as(const AdamWArgs &a, int64_t blocks, bool stochastic, hipStream_t stream)
+{
+    if (stochastic)
+        hipLaunchKernelGGL((adamw_kernel<PT, GT, BITS8, true>), dim3((unsigned)blocks), dim3(THREADS), 0, stream, a);
+    else
+        hipLaunchKernelGGL((adamw_kernel<PT, GT, BITS8, false>), dim3((unsigned)blocks), dim3(THREADS), 0, stream, a);
+}
+template <sbn_dtype PT, sbn_dtype GT> void launch_adamw_bits(const AdamWArgs &a, int64_t blocks, bool bits8, bool stochastic, hipStream_t stream)
+{
+    bits8 ? launch_adamw_as<PT, GT, true>(a, blocks, stochastic, stream) : launch_adamw_as<PT, GT, false>(a, blocks, stochastic, stream);
+}
+
+}  // namespace
+
+size_t grad_norm_workspace_bytes(int count, const int64_t *sizes)
+{
+    int64_t blocks = 0;
+    for (int i = 0; i < count; ++i) blocks += ceil_div(sizes[i], GRAD_NORM_VALUES);
+    return (size_t)blocks * sizeof(double);
+}
+
+sbn_status launch_grad_norm(int count, const void *const *grads, sbn_dtype dtype, const int64_t *sizes, float max_norm, float *out, void *workspace, hipStream_t stream)
+{
+    double *sums = static_cast<double *>(workspace);
+    int64_t all = 0;
+    for (int first = 0; first < count; first += GRAD_NORM_LAUNCH_MAX) {
+        GradNormArgs a{};
+        a.sums = sums + all;
+        a.count = std::min(count - first, GRAD_NORM_LAUNCH_MAX);
+        int64_t blocks = 0;
+        for (int i = 0; i < a.count; ++i) {
+            a.items[i] = NormItem{grads[first + i], sizes[first + i], (int)blocks, 0};
+            blocks += ceil_div(sizes[first + i], GRAD_NORM_VALUES);
+        }
+        if (dtype == SBN_BF16)
+            hipLaunchKernelGGL(square_sums_kernel<SBN_BF16>, dim3((unsigned)blocks), dim3(256), 0, stream, a);
+        else
+            hipLaunchKernelGGL(square_sums_kernel<SBN_F32>, dim3((unsigned)blocks), dim3(256), 0, stream, a);
+        all += blocks;
+    }
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, stream, sums, all, max_norm, out);
+    return check_launch("grad_norm_kernel");
+}
+
+sbn_status launch_adamw(const AdamWCall &c, hipStream_t stream)
+{
+    const bool bits8 = c.m_scales != nullptr;
+    for (int first = 0; first < c.count; first += ADAMW_LAUNCH_MAX) {
+        AdamWArgs a{};
+        a.lr = c.lr;
+        a.clip = c.clip;
+        a.step = c.step;
+        a.beta1 = c.beta1;
+        a.beta2 = c.beta2;
+        a.eps = (float)c.eps;
+        a.seed_low = c.seed ? (uint32_t)*c.seed : 0;
+        a.seed_high = c.seed ? (uint32_t)(*c.seed >> 32) : 0;
+        a.count = std::min(c.count - first, ADAMW_LAUNCH_MAX);
+        a.first_item = first;
+        int64_t blocks = 0;
+        for (int i = 0; i < a.count; ++i) {
+            const int j = first + i;
+            a.items[i] = AdamWItem{c.params[j], c.grads[j], c.m[j], c.v[j], bits8 ? c.m_scales[j] : nullptr, bits8 ? c.v_scales[j] : nullptr, c.sizes[j], (int)blocks,
+                                   c.weight_decay ? c.weight_decay[j] : 0.0f};
+            blocks += ceil_div(c.sizes[j], CHUNK_VALUES);
+        }
+        if (c.param_dtype == SBN_BF16)
+            c.grad_dtype == SBN_BF16 ? launch_adamw_bits<SBN_BF16, SBN_BF16>(a, blocks, bits8, c.seed != nullptr, stream)
+                                     : launch_adamw_bits<SBN_BF16, SBN_F32>(a, blocks, bits8, c.seed != nullptr, stream);
+        else
+            c.grad_dtype == SBN_BF16 ? launch_adamw_bits<SBN_F32, SBN_BF16>(a, blocks, bits8, c.seed != nullptr, stream)
+                                     : launch_adamw_bits<SBN_F32, SBN_F32>(a, blocks, bits8, c.seed != nullptr, stream);
+    }
+    return check_launch("adamw_kernel");
+}
+
+sbn_status launch_adamw_state_values(const void *codes, const uint8_t *scales, int64_t n, bool second, void *out, sbn_dtype dtype, hipStream_t stream)
+{
+    const auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(n, 2048)), dim3(256), 0, stream, static_cast<const uint2 *>(codes), scales, n, out);
+    };
+    if (dtype == SBN_BF16)
+        second ? launch(state_values_kernel<SBN_BF16, V_BELOW>) : launch(state_values_kernel<SBN_BF16, M_BELOW>);
+    else
+        second ? launch(state_values_kernel<SBN_F32, V_BELOW>) : launch(state_values_kernel<SBN_F32, M_BELOW>);
+    return check_launch("state_values_kernel");
+}
+
+}  // namespace sbn
