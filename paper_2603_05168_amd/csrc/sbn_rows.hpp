@@ -31,7 +31,11 @@ template <sbn_dtype DT> struct Row;
 template <> struct Row<SBN_BF16> {
     static constexpr int E = 8;   // values of a vector
     typedef uint16_t value;
-    static __device__ __forceinline__ u32x4 load(const void *row, int64_t vec) { return *(reinterpret_cast<const u32x4_by2 *>(static_cast<const value *>(row) + vec * E)); }
+    template <bool ONCE = false> static __device__ __forceinline__ u32x4 load(const void *row, int64_t vec)
+    {
+        const u32x4_by2 *p = reinterpret_cast<const u32x4_by2 *>(static_cast<const value *>(row) + vec * E);
+        return ONCE ? __builtin_nontemporal_load(p) : *p;
+    }
     static __device__ __forceinline__ void store(void *row, int64_t vec, u32x4 v) { *(reinterpret_cast<u32x4_by2 *>(static_cast<value *>(row) + vec * E)) = v; }
     // the last vector, of which `n` values are the row's; the others come as zeros and are not written
     static __device__ __forceinline__ u32x4 load_part(const void *row, int64_t vec, int n)
@@ -70,7 +74,11 @@ template <> struct Row<SBN_BF16> {
 template <> struct Row<SBN_F32> {
     static constexpr int E = 4;
     typedef float value;
-    static __device__ __forceinline__ u32x4 load(const void *row, int64_t vec) { return *(reinterpret_cast<const u32x4_by4 *>(static_cast<const value *>(row) + vec * E)); }
+    template <bool ONCE = false> static __device__ __forceinline__ u32x4 load(const void *row, int64_t vec)
+    {
+        const u32x4_by4 *p = reinterpret_cast<const u32x4_by4 *>(static_cast<const value *>(row) + vec * E);
+        return ONCE ? __builtin_nontemporal_load(p) : *p;
+    }
     static __device__ __forceinline__ void store(void *row, int64_t vec, u32x4 v) { *(reinterpret_cast<u32x4_by4 *>(static_cast<value *>(row) + vec * E)) = v; }
     static __device__ __forceinline__ u32x4 load_part(const void *row, int64_t vec, int n)
     {
@@ -102,11 +110,11 @@ template <> struct Row<SBN_F32> {
     }
 };
 
-// vector `vec` of a row of d values; zeros behind its end
-template <sbn_dtype DT> __device__ __forceinline__ u32x4 load_vec(const void *row, int64_t vec, int64_t d)
+// vector `vec` of a row of d values; zeros behind its end.  ONCE: nobody will read it again soon (a nontemporal load)
+template <sbn_dtype DT, bool ONCE = false> __device__ __forceinline__ u32x4 load_vec(const void *row, int64_t vec, int64_t d)
 {
     const int64_t left = d - vec * Row<DT>::E;
-    if (left >= Row<DT>::E) return Row<DT>::load(row, vec);
+    if (left >= Row<DT>::E) return Row<DT>::template load<ONCE>(row, vec);
     if (left > 0) return Row<DT>::load_part(row, vec, (int)left);
     return (u32x4){0, 0, 0, 0};
 }
