@@ -465,6 +465,7 @@ sbn_status sbn_mxfp4_linear(const void *X, int64_t tokens, int64_t d_in, int64_t
  *   workspace             device, 256-byte aligned, >= sbn_norm_workspace_bytes(tokens, d_in)
  * Pointers are aligned to their values; d_in is any number up to 16384.  Arithmetic in fp32 (r of the RMS form forward in double, rounded once: where
  * gain is given and bias is not, Y in bf16 is xn_out of sbn_rmsnorm_act_quant), results rounded once.  No atomics: a call repeated gives the same bits.
+ * Where d_in is no multiple of 8, a row's sums go by where it begins in memory, so the last bits of equal rows may differ.
  * A row with a NaN or an infinity is NaN in Y and dX, other rows are not touched by it; dgain and dbias are sums over all rows.
  * Errors: SBN_EINVAL, SBN_EALIGN, SBN_ESIZE, SBN_EUNSUPPORTED (d_in > 16384, tokens > 2^24), SBN_EHIP.
  */

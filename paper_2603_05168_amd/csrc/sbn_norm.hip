@@ -10,6 +10,7 @@
 // The mean of a row is made in two steps, a first sum and the sum of what that leaves over (the differences to a nearby value are exact or
 // nearly so), so that rows far off zero keep their digits; the second sum shares its reduction with the squares.
 #include <algorithm>
+#include <initializer_list>
 #include <type_traits>
 
 #include "sbn_internal.hpp"
@@ -31,10 +32,78 @@ struct NormArgs {
 
 constexpr int MOST_SUMS = 4;   // of a team at once
 
-// How a launch deals rows to threads.  A team shares a row, one vector of it to a thread (VMAX vectors where a row is too long for that): 8, 16 or 32
-// lanes of a wavefront, a wavefront, or the wavefronts of a block.
+// How a launch deals rows to threads.  A team shares a row, VMAX vectors of it to a thread: 8, 16 or 32 lanes of a wavefront, a wavefront, or the
+// wavefronts of a block.
+//
+// Rows whose length is no whole number of vectors begin anywhere in a vector of memory.  Where all rows of a call do so alike, a thread's vectors are
+// those of memory, and a row's first vector begins `shift` values in front of it: accesses off the 16-byte grid took up to twice as long (rows of 500
+// bf16 values: 95 us against 40 for 512).  The rows of a team are a multiple of 8 apart, so that all of them have the same shift and its threads meet the
+// same columns in each.
 struct Deal {
     int team_threads, teams;   // threads of a team; teams of a block (one where a team is more than a wavefront)
+    int shifts;                // whether vectors lie on memory's grid
+    int base;                  // what row 0's shift is
+};
+
+// a thread's place in the row that its team is at
+template <sbn_dtype DT> struct Place {
+    static constexpr int E = Row<DT>::E;
+    typedef typename Row<DT>::value value;
+    int64_t first, total, d;   // of the row, in values of the tensor; values of the tensor, of a row
+    int sub, team_threads, shift;
+
+    // the column of vector i's first value: less than 0 for a vector that begins in front of the row
+    __device__ __forceinline__ int64_t column(int i) const { return (int64_t)(sub + i * team_threads) * E - shift; }
+    __device__ __forceinline__ bool whole(int i) const { return column(i) >= 0 && column(i) + E <= d; }
+    __device__ __forceinline__ bool none(int i) const { return column(i) + E <= 0 || column(i) >= d; }
+    __device__ __forceinline__ bool inside(int i, int k) const { return column(i) + k >= 0 && column(i) + k < d; }
+
+    // vector i, which is read once.  At a row's ends it comes with values of the rows before and behind (which may be written meanwhile) until only()
+    // takes them off: nothing waits for a load before the others are under way
+    __device__ __forceinline__ u32x4 load(const void *rows, int i) const
+    {
+        const int64_t at = first + column(i);
+        const value *p = static_cast<const value *>(rows) + at;
+        u32x4 v = {0, 0, 0, 0};
+        if (none(i)) return v;
+        if (at >= 0 && at + E <= total) return Row<DT>::template load<true>(p, 0);
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+            if (inside(i, k)) Row<DT>::set(v, k, p[k]);
+        return v;
+    }
+    __device__ __forceinline__ void only(u32x4 &v, int i) const
+    {
+        if (whole(i)) return;
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+            if (!inside(i, k)) Row<DT>::clear(v, k);
+    }
+    __device__ __forceinline__ void store(void *rows, int i, u32x4 v) const
+    {
+        value *p = static_cast<value *>(rows) + first + column(i);
+        if (whole(i))
+            Row<DT>::store(p, 0, v);
+        else if (!none(i)) {
+#pragma unroll
+            for (int k = 0; k < E; ++k)
+                if (inside(i, k)) p[k] = Row<DT>::get(v, k);
+        }
+    }
+    // fp32 values that go with the columns of vector i
+    __device__ __forceinline__ void load_columns(const float *p, float other, int i, float (&g)[E]) const
+    {
+#pragma unroll
+        for (int k = 0; k < E; ++k) g[k] = other;
+        if (!p || none(i)) return;
+        if (whole(i))
+            load_floats<E>(p, column(i), d, other, g);
+        else {
+#pragma unroll
+            for (int k = 0; k < E; ++k)
+                if (inside(i, k)) g[k] = p[column(i) + k];
+        }
+    }
 };
 
 // Sums over a team, N of them at once.  A wavefront adds by DPP (the last lane has the sum), the wavefronts of a team by LDS: two pieces of scratch
@@ -85,26 +154,34 @@ template <int L, int N, class F> __device__ __forceinline__ void team_sums(F (&s
     }
 }
 
-// vectors of a row; they are read once
-template <sbn_dtype DT, int VMAX> __device__ __forceinline__ void load_row(u32x4 (&x)[VMAX], const void *rows, int64_t t, const NormArgs &n, const Deal &deal, int sub)
+template <sbn_dtype DT> __device__ __forceinline__ Place<DT> place_of(const NormArgs &n, const Deal &deal)
 {
-#pragma unroll
-    for (int i = 0; i < VMAX; ++i) x[i] = load_vec<DT, true>(static_cast<const typename Row<DT>::value *>(rows) + t * n.d, sub + i * deal.team_threads, n.d);
-}
-template <sbn_dtype DT> __device__ __forceinline__ void store_row(void *rows, int64_t t, const NormArgs &n, const Deal &deal, int sub, int i, u32x4 v)
-{
-    store_vec<DT>(static_cast<typename Row<DT>::value *>(rows) + t * n.d, sub + i * deal.team_threads, n.d, v);
+    const int team = threadIdx.x / deal.team_threads;
+    Place<DT> at;
+    at.sub = threadIdx.x - team * deal.team_threads;
+    at.team_threads = deal.team_threads;
+    at.total = n.tokens * n.d;
+    at.d = n.d;
+    at.first = ((int64_t)blockIdx.x * deal.teams + team) * n.d;
+    at.shift = deal.shifts ? (int)((at.first + deal.base) & (Row<DT>::E - 1)) : 0;
+    return at;
 }
 
-// column factors (or terms) of a thread's vectors
-template <int E, int VMAX> __device__ __forceinline__ void load_columns(float (&g)[VMAX][E], const float *p, float none, const NormArgs &n, const Deal &deal, int sub)
+template <sbn_dtype DT, int VMAX> __device__ __forceinline__ void load_columns(float (&g)[VMAX][Row<DT>::E], const float *p, float other, const Place<DT> &at)
 {
 #pragma unroll
-    for (int i = 0; i < VMAX; ++i) {
+    for (int i = 0; i < VMAX; ++i) at.load_columns(p, other, i, g[i]);
+}
+
+// x less mu, zeros outside the row
+template <sbn_dtype DT> __device__ __forceinline__ void centre(float (&f)[Row<DT>::E], float mu, const Place<DT> &at, int i)
+{
 #pragma unroll
-        for (int k = 0; k < E; ++k) g[i][k] = none;
-        const int64_t c = (int64_t)(sub + i * deal.team_threads) * E;
-        if (p && c < n.d) load_floats<E>(p, c, n.d, none, g[i]);
+    for (int k = 0; k < Row<DT>::E; ++k) f[k] -= mu;
+    if (!at.whole(i)) {
+#pragma unroll
+        for (int k = 0; k < Row<DT>::E; ++k)
+            if (!at.inside(i, k)) f[k] = 0.0f;
     }
 }
 
@@ -135,28 +212,36 @@ template <sbn_dtype DT, bool LAYER, int L, int VMAX> __global__ void __launch_bo
     constexpr int E = Row<DT>::E;
     __shared__ double scratch[2 * 16 * MOST_SUMS];
     float *const fscratch = reinterpret_cast<float *>(scratch);
-    const int team = threadIdx.x / deal.team_threads, sub = threadIdx.x - team * deal.team_threads;
+    constexpr bool KEEP = VMAX * E <= 8;   // gain and bias stay in registers
+    Place<DT> at = place_of<DT>(n, deal);
     int turn = 0;
     float gain[VMAX][E], bias[VMAX][E];
-    if (VMAX == 1) {
-        load_columns<E, VMAX>(gain, n.gain, 1.0f, n, deal, sub);
-        load_columns<E, VMAX>(bias, n.bias, 0.0f, n, deal, sub);
+    if (KEEP) {
+        load_columns<DT>(gain, n.gain, 1.0f, at);
+        load_columns<DT>(bias, n.bias, 0.0f, at);
     }
-    for (int64_t t = (int64_t)blockIdx.x * deal.teams + team; t < n.tokens; t += (int64_t)gridDim.x * deal.teams) {
+    for (; at.first < at.total; at.first += (int64_t)gridDim.x * deal.teams * n.d) {
         u32x4 x[VMAX];
-        load_row<DT>(x, n.X, t, n, deal, sub);
+#pragma unroll
+        for (int i = 0; i < VMAX; ++i) x[i] = at.load(n.X, i);
+        u32x4 res[VMAX];
         if (n.R) {
-            u32x4 r[VMAX];
-            load_row<DT>(r, n.R, t, n, deal, sub);
+#pragma unroll
+            for (int i = 0; i < VMAX; ++i) res[i] = at.load(n.R, i);
+        }
+#pragma unroll
+        for (int i = 0; i < VMAX; ++i) at.only(x[i], i);
+        if (n.R) {
 #pragma unroll
             for (int i = 0; i < VMAX; ++i) {
                 float a[E], b[E];
+                at.only(res[i], i);
                 Row<DT>::unpack(x[i], a);
-                Row<DT>::unpack(r[i], b);
+                Row<DT>::unpack(res[i], b);
 #pragma unroll
                 for (int k = 0; k < E; ++k) a[k] += b[k];
                 x[i] = Row<DT>::pack(a);
-                store_row<DT>(n.S, t, n, deal, sub, i, x[i]);
+                at.store(n.S, i, x[i]);
             }
         }
         float mu = 0.0f, rest = 0.0f, r;
@@ -167,11 +252,11 @@ template <sbn_dtype DT, bool LAYER, int L, int VMAX> __global__ void __launch_bo
             for (int i = 0; i < VMAX; ++i) {
                 float f[E];
                 Row<DT>::unpack(x[i], f);
+                centre<DT>(f, mu, at, i);
 #pragma unroll
                 for (int k = 0; k < E; ++k) {
-                    const float c = (sub + i * deal.team_threads) * E + k < n.d ? f[k] - mu : 0.0f;
-                    q[0] += c;
-                    q[1] += c * c;
+                    q[0] += f[k];
+                    q[1] += f[k] * f[k];
                 }
             }
             team_sums<L>(q, deal, fscratch, turn);
@@ -190,9 +275,9 @@ template <sbn_dtype DT, bool LAYER, int L, int VMAX> __global__ void __launch_bo
             team_sums<L>(s, deal, scratch, turn);
             r = (float)(1.0 / sqrt(s[0] / (double)n.d + (double)n.eps));
         }
-        if (VMAX > 1) {
-            load_columns<E, VMAX>(gain, n.gain, 1.0f, n, deal, sub);
-            load_columns<E, VMAX>(bias, n.bias, 0.0f, n, deal, sub);
+        if (!KEEP) {
+            load_columns<DT>(gain, n.gain, 1.0f, at);
+            load_columns<DT>(bias, n.bias, 0.0f, at);
         }
 #pragma unroll
         for (int i = 0; i < VMAX; ++i) {
@@ -204,34 +289,48 @@ template <sbn_dtype DT, bool LAYER, int L, int VMAX> __global__ void __launch_bo
                 f[k] *= gain[i][k];
                 if (n.bias) f[k] += bias[i][k];
             }
-            store_row<DT>(n.Y, t, n, deal, sub, i, Row<DT>::pack(f));
+            at.store(n.Y, i, Row<DT>::pack(f));
         }
     }
 }
 
 // A thread meets the same columns in every row of its team and adds up their dgain and dbias.  At the end a block adds its teams' sums in LDS and
 // leaves one share of both vectors, which the next kernel adds in the order of the blocks: no atomics, the same bits every time.
-// Bound by memory: 16384 RMS rows of 2560 bf16 values with d_residual move 336 MB in 61 us, 5.5 TB/s.  Three blocks of five wavefronts to each of the 256
-// processors: as many on all of them (819 blocks: 88 us), and no more (four: 72) nor fewer (two: 69).
-template <sbn_dtype DT, bool LAYER, int L, int VMAX> __global__ void __launch_bounds__(most_threads(L)) norm_backward_kernel(const NormArgs n, const Deal deal)
+// Bound by memory: 16384 RMS rows of 2560 bf16 values with d_residual move 336 MB in 60 us, 5.6 TB/s.  Three blocks of five wavefronts to each of the 256
+// processors: as many on all of them (819 blocks: 88 us), and no more (four: 72) nor fewer (two: 69).  At most 96 registers, so that five wavefronts find
+// room on a SIMD: with 106 the layer form took 102 us for 67 (without a residual).
+template <sbn_dtype DT, bool LAYER, int L, int VMAX>
+__global__ void __launch_bounds__(most_threads(L)) __attribute__((amdgpu_waves_per_eu(VMAX * Row<DT>::E <= 8 ? 5 : 4))) norm_backward_kernel(const NormArgs n, const Deal deal)
 {
     constexpr int E = Row<DT>::E;
     __shared__ float scratch[2 * 16 * MOST_SUMS];
     __shared__ float shares[256 * E];   // of the threads of several teams
-    const int team = threadIdx.x / deal.team_threads, sub = threadIdx.x - team * deal.team_threads;
+    constexpr bool KEEP = VMAX * E <= 8;   // gain stays in registers, and d_residual comes with the others
+    Place<DT> at = place_of<DT>(n, deal);
     int turn = 0;
     float dgain[VMAX][E], dbias[VMAX][E], gain[VMAX][E];
 #pragma unroll
     for (int i = 0; i < VMAX; ++i)
 #pragma unroll
         for (int k = 0; k < E; ++k) dgain[i][k] = dbias[i][k] = 0.0f;
-    if (VMAX == 1) load_columns<E, VMAX>(gain, n.gain, 1.0f, n, deal, sub);
-    for (int64_t t = (int64_t)blockIdx.x * deal.teams + team; t < n.tokens; t += (int64_t)gridDim.x * deal.teams) {
+    if (KEEP) load_columns<DT>(gain, n.gain, 1.0f, at);
+    for (; at.first < at.total; at.first += (int64_t)gridDim.x * deal.teams * n.d) {
         u32x4 x[VMAX], y[VMAX], res[VMAX];
-        load_row<DT>(x, n.X, t, n, deal, sub);
-        load_row<DT>(y, n.dY, t, n, deal, sub);
-        if (VMAX == 1 && n.R) load_row<DT>(res, n.R, t, n, deal, sub);   // (with more vectors there are no registers for it)
-        if (VMAX > 1) load_columns<E, VMAX>(gain, n.gain, 1.0f, n, deal, sub);
+#pragma unroll
+        for (int i = 0; i < VMAX; ++i) {
+            x[i] = at.load(n.X, i);
+            y[i] = at.load(n.dY, i);
+        }
+        if (KEEP && n.R) {
+#pragma unroll
+            for (int i = 0; i < VMAX; ++i) res[i] = at.load(n.R, i);
+        }
+        if (!KEEP) load_columns<DT>(gain, n.gain, 1.0f, at);
+#pragma unroll
+        for (int i = 0; i < VMAX; ++i) {
+            at.only(x[i], i);
+            at.only(y[i], i);
+        }
         const float mu = LAYER ? first_mean<DT, L>(x, n, deal, scratch, turn) : 0.0f;
         // sums of c^2 and a c (layer form: of c and a too), with c = x - mu
         float q[LAYER ? 4 : 2] = {};
@@ -240,9 +339,9 @@ template <sbn_dtype DT, bool LAYER, int L, int VMAX> __global__ void __launch_bo
             float f[E], a[E];
             Row<DT>::unpack(x[i], f);
             Row<DT>::unpack(y[i], a);
+            if (LAYER) centre<DT>(f, mu, at, i);
 #pragma unroll
             for (int k = 0; k < E; ++k) {
-                if (LAYER) f[k] = (sub + i * deal.team_threads) * E + k < n.d ? f[k] - mu : 0.0f;
                 a[k] *= gain[i][k];
                 q[0] += f[k] * f[k];
                 q[1] += a[k] * f[k];
@@ -276,26 +375,35 @@ template <sbn_dtype DT, bool LAYER, int L, int VMAX> __global__ void __launch_bo
             }
             if (!n.dX) continue;
             if (n.R) {
-                Row<DT>::unpack(VMAX == 1 ? res[i] : load_vec<DT>(static_cast<const typename Row<DT>::value *>(n.R) + t * n.d, sub + i * deal.team_threads, n.d), f);
+                Row<DT>::unpack(KEEP ? res[i] : at.load(n.R, i), f);
 #pragma unroll
                 for (int k = 0; k < E; ++k) a[k] += f[k];
             }
-            store_row<DT>(n.dX, t, n, deal, sub, i, Row<DT>::pack(a));
+            at.store(n.dX, i, Row<DT>::pack(a));
         }
     }
     const auto leave = [&](const float (&sum)[VMAX][E], float *share) {
         if (deal.teams == 1) {
 #pragma unroll
-            for (int i = 0; i < VMAX; ++i) store_unit<SBN_F32, E>(share, sub + i * deal.team_threads, n.d, sum[i]);
+            for (int i = 0; i < VMAX; ++i) {
+                if (at.whole(i))
+                    store_unit<SBN_F32, E>(share + at.column(i), 0, E, sum[i]);
+                else {
+#pragma unroll
+                    for (int k = 0; k < E; ++k)
+                        if (at.inside(i, k)) share[at.column(i) + k] = sum[i][k];
+                }
+            }
             return;
         }
         // several teams: one vector to a thread, 256 threads
+        const int wide = deal.team_threads * E, team = threadIdx.x / deal.team_threads;
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < E; ++k) shares[threadIdx.x * E + k] = sum[0][k];
+        for (int k = 0; k < E; ++k)
+            if (at.inside(0, k)) shares[team * wide + at.column(0) + k] = sum[0][k];
         __syncthreads();
-        const int wide = deal.team_threads * E;
-        for (int c = threadIdx.x; c < min((int64_t)wide, n.d); c += 256) {
+        for (int c = threadIdx.x; c < n.d; c += 256) {
             float s = 0.0f;
             for (int w = 0; w < deal.teams; ++w) s += shares[w * wide + c];
             share[c] = s;
@@ -329,17 +437,26 @@ __global__ void __launch_bounds__(1024) norm_shares_kernel(const float *partials
     }
 }
 
-constexpr int FORWARD_WAVES = 25, BACKWARD_WAVES = 15;   // of a processor, by the kernels' measurements
 constexpr int PROCESSORS = 256;
+// wavefronts of a processor that stay: as many as its registers hold of the kernel, where that was fastest (see there)
+constexpr int FORWARD_WAVES = 25, FORWARD_WAVES_LONG = 20, BACKWARD_WAVES = 16;
 
 // blocks of `waves` wavefronts each that stay until all rows are done, the same number for every processor
 int64_t staying_blocks(int waves, int most) { return PROCESSORS * std::max(1, most / waves); }
 
+// vectors that a row of d values reaches over: rows that are no whole number of them may begin in the middle of one
+int64_t vectors_of(int64_t d, int values) { return d % values ? ceil_div(d + values - 1, values) : d / values; }
+
+// Vectors of a thread where a team is more than a wavefront: eight values, or sixteen in rows of more than 2560.  Large blocks fill a processor unevenly
+// and wait for each other: rows of 8192 bf16 values 76 us by 16 wavefronts with eight, 67 by eight with sixteen; of 4096 57 by eight, 50 by four; of 2560
+// 36 by five and 38 by three.
+int vectors_of_thread(int64_t vecs, int values) { return vecs <= 320 * 8 / values ? 8 / values : 16 / values; }
+
 // wavefronts of a block: four with a team or several each, or those of one team
 int block_waves(int64_t d, int values)
 {
-    const int64_t vecs = ceil_div(d, values);
-    return vecs <= 64 ? 4 : (int)std::min<int64_t>(16, ceil_div(vecs, 64));
+    const int64_t vecs = vectors_of(d, values);
+    return vecs <= 64 ? 4 : (int)std::min<int64_t>(16, ceil_div(vecs, 64 * vectors_of_thread(vecs, values)));
 }
 
 // blocks of the backward at most, in either type: each leaves its shares
@@ -348,30 +465,39 @@ int64_t most_shares(int64_t d)
     return std::max(staying_blocks(block_waves(d, Row<SBN_BF16>::E), BACKWARD_WAVES), staying_blocks(block_waves(d, Row<SBN_F32>::E), BACKWARD_WAVES));
 }
 
-// calls f with the lanes of a team that is part of a wavefront (64: whole wavefronts), the vectors of a thread, the deal, the wavefronts of a block and
-// the blocks that give every row a team of its own
-template <sbn_dtype DT, class F> sbn_status dealt(int64_t tokens, int64_t d, F &&f)
+// Calls f with the lanes of a team that is part of a wavefront (64: whole wavefronts), the vectors of a thread, the deal, the wavefronts of a block and
+// the blocks that give every row a team of its own.  rows: the tensors of the call (or null).
+template <sbn_dtype DT, class F> sbn_status dealt(const NormArgs &n, std::initializer_list<const void *> rows, F &&f)
 {
     using std::integral_constant;
-    const auto with = [&](auto L, auto VMAX, int team_threads) {
-        const int waves = block_waves(d, Row<DT>::E);
-        const Deal deal{team_threads, 64 * waves / team_threads};
-        return f(L, VMAX, deal, waves, ceil_div(tokens, (int64_t)deal.teams));
+    constexpr int E = Row<DT>::E;
+    const int64_t vecs = vectors_of(n.d, E);
+    const auto base = [](const void *p) { return (int)(reinterpret_cast<uintptr_t>(p) / sizeof(typename Row<DT>::value) % E); };
+    bool alike = vecs <= 1024 * 16 / E;   // (the longest rows have no room for a vector more)
+    for (const void *p : rows) alike = alike && (!p || base(p) == base(n.X));
+    // where row 0 lies off the grid, so do rows of whole vectors: they have no room for a shift
+    alike = alike && (n.d % E != 0 || base(n.X) == 0);
+    const int waves = block_waves(n.d, E);
+    const auto with = [&](auto L, auto VMAX) {
+        // part of a wavefront, or the wavefronts of the block; more than a vector to a thread only in the latter
+        const int team_threads = decltype(L)::value < 64 ? decltype(L)::value : vecs <= 64 ? 64 : 64 * waves;
+        const Deal deal{team_threads, 64 * waves / team_threads, alike, base(n.X)};
+        return f(L, VMAX, deal, waves, ceil_div(n.tokens, (int64_t)deal.teams));
     };
-    const int64_t vecs = ceil_div(d, Row<DT>::E);
     const integral_constant<int, 1> one{};
-    if (vecs <= 8) return with(integral_constant<int, 8>{}, one, 8);
-    if (vecs <= 16) return with(integral_constant<int, 16>{}, one, 16);
-    if (vecs <= 32) return with(integral_constant<int, 32>{}, one, 32);
+    if (vecs <= 8) return with(integral_constant<int, 8>{}, one);
+    if (vecs <= 16) return with(integral_constant<int, 16>{}, one);
+    if (vecs <= 32) return with(integral_constant<int, 32>{}, one);
     const integral_constant<int, 64> wave{};
-    if (vecs <= 1024) return with(wave, one, 64 * (int)ceil_div(vecs, 64));
-    return with(wave, integral_constant<int, 16 / Row<DT>::E>{}, 1024);   // up to NORM_MAX_D values
+    if (vecs <= 64) return with(wave, one);
+    if (vectors_of_thread(vecs, E) == 8 / E) return with(wave, integral_constant<int, 8 / E>{});
+    return with(wave, integral_constant<int, 16 / E>{});   // up to NORM_MAX_D values
 }
 
 template <sbn_dtype DT, bool LAYER> sbn_status forward_as(const NormArgs &n, hipStream_t stream)
 {
-    return dealt<DT>(n.tokens, n.d, [&](auto L, auto VMAX, const Deal &deal, int waves, int64_t all) {
-        const int64_t blocks = std::min(all, staying_blocks(waves, FORWARD_WAVES));
+    return dealt<DT>(n, {n.R, n.S, n.Y}, [&](auto L, auto VMAX, const Deal &deal, int waves, int64_t all) {
+        const int64_t blocks = std::min(all, staying_blocks(waves, decltype(VMAX)::value * Row<DT>::E > 8 ? FORWARD_WAVES_LONG : FORWARD_WAVES));
         hipLaunchKernelGGL((norm_kernel<DT, LAYER, decltype(L)::value, decltype(VMAX)::value>), dim3((unsigned)blocks), dim3(64 * waves), 0, stream, n, deal);
         return check_launch("norm_kernel");
     });
@@ -379,7 +505,7 @@ template <sbn_dtype DT, bool LAYER> sbn_status forward_as(const NormArgs &n, hip
 
 template <sbn_dtype DT, bool LAYER> sbn_status backward_as(const NormArgs &n, float *dgain, float *dbias, hipStream_t stream)
 {
-    return dealt<DT>(n.tokens, n.d, [&](auto L, auto VMAX, const Deal &deal, int waves, int64_t all) {
+    return dealt<DT>(n, {n.dY, n.R, n.dX}, [&](auto L, auto VMAX, const Deal &deal, int waves, int64_t all) {
         const int blocks = (int)std::min(all, staying_blocks(waves, BACKWARD_WAVES));
         hipLaunchKernelGGL((norm_backward_kernel<DT, LAYER, decltype(L)::value, decltype(VMAX)::value>), dim3(blocks), dim3(64 * waves), 0, stream, n, deal);
         if (dgain || dbias) hipLaunchKernelGGL(norm_shares_kernel, dim3((unsigned)ceil_div(n.d, 32), 2), dim3(1024), 0, stream, n.partials, blocks, n.d, dgain, dbias);

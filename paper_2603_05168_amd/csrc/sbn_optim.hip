@@ -9,6 +9,7 @@
 // and codes and values are a shift and a sum apart.  m: a sign and seven bits (15 binades), v: eight bits (31 binades).  Code 0 is 0; a v that is
 // not zero keeps the lowest code, so that what it divides does not blow up.
 #include <algorithm>
+#include <climits>
 #include <cmath>
 
 #include "sbn_internal.hpp"
@@ -18,30 +19,49 @@ namespace sbn {
 
 namespace {
 
-constexpr int64_t CHUNK_VALUES = 8192;   // values of a block
 constexpr int THREADS = 256;
+constexpr int STEP = THREADS * 8;             // values of a block at once
+constexpr int64_t LONG_CHUNK = 16 * STEP;     // values of a block at most
 
 struct AdamWItem {
     void *p;
     const void *g;
     void *m, *v;
     uint8_t *m_scales, *v_scales;
-    int64_t n;
-    int first_block;
+    uint32_t n;
     float decay;
 };
-constexpr int ADAMW_LAUNCH_MAX = 60;   // tensors of a launch: their table is a kernel argument
+constexpr int ADAMW_LAUNCH_MAX = 64;   // tensors of a launch: their table is a kernel argument, and a wavefront looks through it at once
 
 struct AdamWArgs {
+    int first_block[ADAMW_LAUNCH_MAX];   // of a tensor; behind the last one the number of blocks
     AdamWItem items[ADAMW_LAUNCH_MAX];
     const float *lr, *clip;
     const int64_t *step;
     double beta1, beta2;
     float eps;
     uint32_t seed_low, seed_high;
-    int count, first_item;   // first_item: place in the call of items[0]
+    int first_item;   // place in the call of items[0]
+    uint32_t chunk;   // values of a block
 };
 static_assert(sizeof(AdamWArgs) <= 4096, "kernel arguments");
+
+// the tensor of a block: how many begin at or in front of it, less one
+__device__ __forceinline__ int tensor_of(const int *first_block, int block)
+{
+    return __builtin_amdgcn_readfirstlane(__popcll(__ballot(first_block[threadIdx.x & 63] <= block)) - 1);
+}
+
+// x to a whole power: a few products, where pow() takes as long as all the rest of a small tensor
+__device__ __forceinline__ double power(double x, int64_t n)
+{
+    double y = 1.0;
+    for (; n > 0; n >>= 1) {
+        if (n & 1) y *= x;
+        x *= x;
+    }
+    return y;
+}
 
 // 32 random bits of a counter and two keys: two rounds of a multiplication between shifts, the multipliers from the digits of the golden ratio and
 // of pi.  The rounding needs no more than bits that are even on average and not the same for neighbours, moments or steps.
@@ -66,9 +86,9 @@ template <int BELOW> __device__ __forceinline__ float value_of(uint32_t code, ui
 template <int BELOW> __device__ __forceinline__ uint32_t code_of(float x, uint32_t exponent, uint32_t half)
 {
     const uint32_t bits = __float_as_uint(x), a = bits & 0x7fffffffu;
-    int code = (int)((a + half) >> 20) - (int)(exponent - BELOW) * 8;
-    if (BELOW == V_BELOW) return a ? (uint32_t)max(code, 1) : 0u;
-    return (uint32_t)max(code, 0) | (bits >> 31 << 7);
+    const int t = (int)(a + half - ((exponent - BELOW) << 23));   // the code, less its offset, above bit 20
+    if (BELOW == V_BELOW) return a ? (uint32_t)max(t, 1 << 20) >> 20 : 0u;
+    return (uint32_t)max(t, 0) >> 20 | (bits >> 31 << 7);
 }
 __device__ __forceinline__ uint32_t nearest(float x) { return 0x7ffffu + ((__float_as_uint(x) >> 20) & 1u); }
 
@@ -78,10 +98,78 @@ template <int BELOW> __device__ __forceinline__ uint32_t shared_exponent(const f
     uint32_t top = 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+    top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xb1, 0xf, 0xf, true));   // quad_perm: lane ^ 1, lane ^ 2
+    top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4e, 0xf, 0xf, true));
     return max((top + 0xfffffu) >> 23, (uint32_t)BELOW);   // one more where rounding may reach the next binade
 }
+
+// What a thread has of a tensor: eight weights with their gradients and moments.
+template <sbn_dtype PT, sbn_dtype GT, bool BITS8> struct Eight {
+    float p[8], g[8], m[8], v[8];
+
+    template <bool WHOLE> __device__ __forceinline__ void load(const AdamWItem &it, uint32_t at)
+    {
+        const uint32_t unit = at / 8;
+        if (WHOLE) {
+            load_whole<PT>(it.p, at, p);
+            load_whole<GT>(it.g, at, g);
+        } else {
+            load_unit<PT, 8>(it.p, unit, it.n, p);
+            load_unit<GT, 8>(it.g, unit, it.n, g);
+        }
+        if constexpr (BITS8) {
+            uint2 mc = static_cast<const uint2 *>(it.m)[unit], vc = static_cast<const uint2 *>(it.v)[unit];
+            const uint32_t me = it.m_scales[at / 32], ve = it.v_scales[at / 32];
+            if (!WHOLE) {   // what pads the last 32 is zero
+                mc = first_bytes(mc, (int64_t)it.n - at);
+                vc = first_bytes(vc, (int64_t)it.n - at);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                m[k] = value_of<M_BELOW>(((k < 4 ? mc.x : mc.y) >> (8 * (k & 3))) & 255u, me);
+                v[k] = value_of<V_BELOW>(((k < 4 ? vc.x : vc.y) >> (8 * (k & 3))) & 255u, ve);
+            }
+        } else if (WHOLE) {
+            load_whole<SBN_F32>(it.m, at, m);
+            load_whole<SBN_F32>(it.v, at, v);
+        } else {
+            load_unit<SBN_F32, 8>(it.m, unit, it.n, m);
+            load_unit<SBN_F32, 8>(it.v, unit, it.n, v);
+        }
+    }
+    template <bool WHOLE> __device__ __forceinline__ void store(const AdamWItem &it, uint32_t at) const
+    {
+        const uint32_t unit = at / 8;
+        if (WHOLE)
+            store_whole<PT>(it.p, at, p);
+        else
+            store_unit<PT, 8>(it.p, unit, it.n, p);
+        if constexpr (!BITS8) {
+            if (WHOLE) {
+                store_whole<SBN_F32>(it.m, at, m);
+                store_whole<SBN_F32>(it.v, at, v);
+            } else {
+                store_unit<SBN_F32, 8>(it.m, unit, it.n, m);
+                store_unit<SBN_F32, 8>(it.v, unit, it.n, v);
+            }
+        }
+    }
+
+private:
+    template <sbn_dtype DT> static __device__ __forceinline__ void load_whole(const void *p, uint32_t at, float (&f)[8])
+    {
+        load_unit<DT, 8>(static_cast<const typename Row<DT>::value *>(p) + at, 0, 8, f);
+    }
+    template <sbn_dtype DT> static __device__ __forceinline__ void store_whole(void *p, uint32_t at, const float (&f)[8])
+    {
+        store_unit<DT, 8>(static_cast<typename Row<DT>::value *>(p) + at, 0, 8, f);
+    }
+    static __device__ __forceinline__ uint2 first_bytes(uint2 c, int64_t n)
+    {
+        const uint64_t all = (uint64_t)c.y << 32 | c.x, some = n >= 8 ? all : n <= 0 ? 0 : all & (((uint64_t)1 << (8 * n)) - 1);
+        return make_uint2((uint32_t)some, (uint32_t)(some >> 32));
+    }
+};
 
 template <sbn_dtype PT, sbn_dtype GT, bool BITS8, bool STOCHASTIC> __global__ void __launch_bounds__(THREADS) adamw_kernel(const AdamWArgs a)
 {
@@ -90,15 +178,17 @@ template <sbn_dtype PT, sbn_dtype GT, bool BITS8, bool STOCHASTIC> __global__ vo
         factor = *a.clip;
         if (!(fabsf(factor) <= 3.4028235e38f)) return;   // gradients that are not finite: no step
     }
-    int which = 0;
-    while (which + 1 < a.count && (int)blockIdx.x >= a.items[which + 1].first_block) ++which;
+    const int which = tensor_of(a.first_block, blockIdx.x);
     const AdamWItem it = a.items[which];
     const int64_t step = *a.step;
     const double lr = (double)*a.lr;
-    const float rate = (float)(lr / (1.0 - pow(a.beta1, (double)step)));
+    const float rate = (float)(lr / (1.0 - power(a.beta1, step)));
     const float keep = (float)(1.0 - lr * (double)it.decay);
-    const float of_v = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)step)));
+    const float of_v = (float)(1.0 / sqrt(1.0 - power(a.beta2, step)));
     const float b1 = (float)a.beta1, c1 = (float)(1.0 - a.beta1), b2 = (float)a.beta2, c2 = (float)(1.0 - a.beta2);
+    // v_sqrt_f32 and v_rcp_f32 are good to a step of fp32 and take less than half the time of the correctly rounded root and quotient, but make zero of
+    // numbers below 2^-126: with an eps that is nothing beside such a root they must not be met
+    const bool exactly = a.eps < 1e-12f;
     uint32_t key0 = 0, key1 = 0;
     if (STOCHASTIC) {
         key0 = mix(a.seed_low, a.seed_high, 0);
@@ -106,65 +196,57 @@ template <sbn_dtype PT, sbn_dtype GT, bool BITS8, bool STOCHASTIC> __global__ vo
         key0 = mix(key0, (uint32_t)(a.first_item + which), 0);
         key1 = mix(key0, 0x243F6A88u, 0);
     }
-    const int64_t begin = (int64_t)((int)blockIdx.x - it.first_block) * CHUNK_VALUES;
-    const int64_t end = min(it.n, begin + CHUNK_VALUES);
-    // a thread has eight values, four threads the 32 that share an exponent: all four go through the loop together
-    for (int64_t at = begin + threadIdx.x * 8; at < (end + 31) / 32 * 32; at += THREADS * 8) {
-        const int64_t unit = at / 8;
-        float p[8], g[8], m[8], v[8];
-        load_unit<PT, 8>(it.p, unit, it.n, p);
-        load_unit<GT, 8>(it.g, unit, it.n, g);
-        if constexpr (BITS8) {
-            const uint2 mc = static_cast<const uint2 *>(it.m)[unit], vc = static_cast<const uint2 *>(it.v)[unit];
-            const uint32_t me = it.m_scales[at / 32], ve = it.v_scales[at / 32];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                m[k] = at + k < it.n ? value_of<M_BELOW>(((k < 4 ? mc.x : mc.y) >> (8 * (k & 3))) & 255u, me) : 0.0f;
-                v[k] = at + k < it.n ? value_of<V_BELOW>(((k < 4 ? vc.x : vc.y) >> (8 * (k & 3))) & 255u, ve) : 0.0f;
-            }
-        } else {
-            load_unit<SBN_F32, 8>(it.m, unit, it.n, m);
-            load_unit<SBN_F32, 8>(it.v, unit, it.n, v);
-        }
+    const uint32_t begin = (blockIdx.x - a.first_block[which]) * a.chunk;   // at most 2^31 values
+    const uint32_t end = (min(it.n, begin + a.chunk) + 31) / 32 * 32;
+    // four threads have the 32 values that share an exponent, and go through the loop together
+    for (uint32_t at = begin + threadIdx.x * 8; at < end; at += STEP) {
+        Eight<PT, GT, BITS8> e;
+        const bool whole = at + 8 <= it.n;
+        if (whole)
+            e.template load<true>(it, at);
+        else
+            e.template load<false>(it, at);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const float s = a.clip ? g[k] * factor : g[k];
-            m[k] = m[k] * b1 + s * c1;
-            v[k] = v[k] * b2 + s * c2 * s;
-            p[k] = p[k] * keep - rate * m[k] / (sqrtf(v[k]) * of_v + a.eps);
+            const float s = e.g[k] * factor;   // (a factor of one changes nothing)
+            e.m[k] = e.m[k] * b1 + s * c1;
+            e.v[k] = e.v[k] * b2 + s * c2 * s;
         }
-        uint32_t noise[3][4];   // two values of 16 bits: of p, m and v
-        if constexpr (STOCHASTIC) {
+        if (!exactly) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t pair = (uint32_t)(at / 2 + k);
+            for (int k = 0; k < 8; ++k)
+                e.p[k] = fmaf(-rate * e.m[k], __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(e.v[k]), of_v, a.eps)), e.p[k] * keep);
+        } else {
 #pragma unroll
-                for (int j = 0; j < 3; ++j) noise[j][k] = mix(3 * pair + j, key0, key1);
-            }
+            for (int k = 0; k < 8; ++k) e.p[k] = e.p[k] * keep - rate * e.m[k] / (sqrtf(e.v[k]) * of_v + a.eps);
         }
-        const auto bits16 = [&](int j, int k) { return k & 1 ? noise[j][k / 2] >> 16 : noise[j][k / 2] & 0xffffu; };
+        // 16 bits for the rounding of every p, m and v: two values to a hash
+        const auto noise = [&](int j, int k) {
+            const uint32_t bits = mix(3 * (at / 2 + k / 2) + j, key0, key1);
+            return k & 1 ? bits >> 16 : bits & 0xffffu;
+        };
         if constexpr (PT == SBN_BF16 && STOCHASTIC) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) p[k] = __uint_as_float((__float_as_uint(p[k]) + bits16(0, k)) & 0xffff0000u);
+            for (int k = 0; k < 8; ++k) e.p[k] = __uint_as_float((__float_as_uint(e.p[k]) + noise(0, k)) & 0xffff0000u);
         }
-        store_unit<PT, 8>(it.p, unit, it.n, p);
+        if (whole)
+            e.template store<true>(it, at);
+        else
+            e.template store<false>(it, at);
         if constexpr (BITS8) {
-            const uint32_t me = shared_exponent<M_BELOW>(m), ve = shared_exponent<V_BELOW>(v);
+            const uint32_t me = shared_exponent<M_BELOW>(e.m), ve = shared_exponent<V_BELOW>(e.v);
             uint32_t mc[2] = {0, 0}, vc[2] = {0, 0};
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                mc[k / 4] |= code_of<M_BELOW>(m[k], me, STOCHASTIC ? bits16(1, k) * 16 + 8 : nearest(m[k])) << (8 * (k & 3));
-                vc[k / 4] |= code_of<V_BELOW>(v[k], ve, STOCHASTIC ? bits16(2, k) * 16 + 8 : nearest(v[k])) << (8 * (k & 3));
+                mc[k / 4] |= code_of<M_BELOW>(e.m[k], me, STOCHASTIC ? noise(1, k) * 16 + 8 : nearest(e.m[k])) << (8 * (k & 3));
+                vc[k / 4] |= code_of<V_BELOW>(e.v[k], ve, STOCHASTIC ? noise(2, k) * 16 + 8 : nearest(e.v[k])) << (8 * (k & 3));
             }
-            static_cast<uint2 *>(it.m)[unit] = make_uint2(mc[0], mc[1]);
-            static_cast<uint2 *>(it.v)[unit] = make_uint2(vc[0], vc[1]);
+            static_cast<uint2 *>(it.m)[at / 8] = make_uint2(mc[0], mc[1]);
+            static_cast<uint2 *>(it.v)[at / 8] = make_uint2(vc[0], vc[1]);
             if (at % 32 == 0) {
                 it.m_scales[at / 32] = (uint8_t)me;
                 it.v_scales[at / 32] = (uint8_t)ve;
             }
-        } else {
-            store_unit<SBN_F32, 8>(it.m, unit, it.n, m);
-            store_unit<SBN_F32, 8>(it.v, unit, it.n, v);
         }
     }
 }
@@ -182,20 +264,15 @@ template <sbn_dtype OUT, int BELOW> __global__ void __launch_bounds__(256) state
 }
 
 // ---- the norm of all gradients ----------------------------------------------------------------------------------------------------
-struct NormItem {
-    const void *g;
-    int64_t n;
-    int first_block, pad;
-};
-constexpr int GRAD_NORM_LAUNCH_MAX = 160;
-constexpr int64_t GRAD_NORM_VALUES = 32768;   // values of a block
+constexpr int GRAD_NORM_LAUNCH_MAX = 64;
+constexpr int64_t GRAD_NORM_VALUES = 16384;   // values of a block
 
 struct GradNormArgs {
-    NormItem items[GRAD_NORM_LAUNCH_MAX];
+    int first_block[GRAD_NORM_LAUNCH_MAX];
+    const void *g[GRAD_NORM_LAUNCH_MAX];
+    int64_t n[GRAD_NORM_LAUNCH_MAX];
     double *sums;
-    int count;
 };
-static_assert(sizeof(GradNormArgs) <= 4096, "kernel arguments");
 
 __device__ __forceinline__ double block_sum(double s, double *scratch)
 {
@@ -211,17 +288,23 @@ __device__ __forceinline__ double block_sum(double s, double *scratch)
 template <sbn_dtype GT> __global__ void __launch_bounds__(256) square_sums_kernel(const GradNormArgs a)
 {
     __shared__ double scratch[4];
-    int which = 0;
-    while (which + 1 < a.count && (int)blockIdx.x >= a.items[which + 1].first_block) ++which;
-    const NormItem it = a.items[which];
-    const int64_t begin = (int64_t)((int)blockIdx.x - it.first_block) * GRAD_NORM_VALUES;
-    const int64_t end = min(it.n, begin + GRAD_NORM_VALUES);
+    const int which = tensor_of(a.first_block, blockIdx.x);
+    const void *g = a.g[which];
+    const int64_t n = a.n[which], begin = (int64_t)((int)blockIdx.x - a.first_block[which]) * GRAD_NORM_VALUES;
+    const int64_t end = min(n, begin + GRAD_NORM_VALUES);
     double s = 0.0;
-    for (int64_t at = begin + threadIdx.x * 8; at < end; at += 256 * 8) {
-        float g[8];
-        load_unit<GT, 8>(it.g, at / 8, it.n, g);
+    constexpr int E = Row<GT>::E, AT_ONCE = 4;
+    for (int64_t at = begin + threadIdx.x * E; at < end; at += 256 * E * AT_ONCE) {
+        u32x4 x[AT_ONCE];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) s += (double)g[k] * (double)g[k];
+        for (int j = 0; j < AT_ONCE; ++j) x[j] = load_vec<GT>(g, at / E + 256 * j, end);
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            float f[E];
+            Row<GT>::unpack(x[j], f);
+#pragma unroll
+            for (int k = 0; k < E; ++k) s = fma((double)f[k], (double)f[k], s);
+        }
     }
     s = block_sum(s, scratch);
     if (threadIdx.x == 0) a.sums[blockIdx.x] = s;
@@ -231,6 +314,7 @@ __global__ void __launch_bounds__(1024) grad_norm_kernel(const double *sums, int
 {
     __shared__ double scratch[16];
     double s = 0.0;
+#pragma unroll 8
     for (int64_t b = threadIdx.x; b < blocks; b += 1024) s += sums[b];
     s = block_sum(s, scratch);
     if (threadIdx.x == 0) {
@@ -266,13 +350,15 @@ sbn_status launch_grad_norm(int count, const void *const *grads, sbn_dtype dtype
     double *sums = static_cast<double *>(workspace);
     int64_t all = 0;
     for (int first = 0; first < count; first += GRAD_NORM_LAUNCH_MAX) {
-        GradNormArgs a{};
+        GradNormArgs a;
         a.sums = sums + all;
-        a.count = std::min(count - first, GRAD_NORM_LAUNCH_MAX);
+        const int here = std::min(count - first, GRAD_NORM_LAUNCH_MAX);
         int64_t blocks = 0;
-        for (int i = 0; i < a.count; ++i) {
-            a.items[i] = NormItem{grads[first + i], sizes[first + i], (int)blocks, 0};
-            blocks += ceil_div(sizes[first + i], GRAD_NORM_VALUES);
+        for (int i = 0; i < GRAD_NORM_LAUNCH_MAX; ++i) {
+            a.g[i] = i < here ? grads[first + i] : nullptr;
+            a.n[i] = i < here ? sizes[first + i] : 0;
+            a.first_block[i] = i < here ? (int)blocks : INT_MAX;
+            blocks += ceil_div(a.n[i], GRAD_NORM_VALUES);
         }
         if (dtype == SBN_BF16)
             hipLaunchKernelGGL(square_sums_kernel<SBN_BF16>, dim3((unsigned)blocks), dim3(256), 0, stream, a);
@@ -288,7 +374,7 @@ sbn_status launch_adamw(const AdamWCall &c, hipStream_t stream)
 {
     const bool bits8 = c.m_scales != nullptr;
     for (int first = 0; first < c.count; first += ADAMW_LAUNCH_MAX) {
-        AdamWArgs a{};
+        AdamWArgs a;
         a.lr = c.lr;
         a.clip = c.clip;
         a.step = c.step;
@@ -297,14 +383,23 @@ sbn_status launch_adamw(const AdamWCall &c, hipStream_t stream)
         a.eps = (float)c.eps;
         a.seed_low = c.seed ? (uint32_t)*c.seed : 0;
         a.seed_high = c.seed ? (uint32_t)(*c.seed >> 32) : 0;
-        a.count = std::min(c.count - first, ADAMW_LAUNCH_MAX);
+        const int here = std::min(c.count - first, ADAMW_LAUNCH_MAX);
         a.first_item = first;
+        int64_t values = 0;
+        for (int i = 0; i < here; ++i) values += c.sizes[first + i];
+        // some 16 blocks to a processor where there are values for them, which share out evenly; what a block does once is then a few hundredths
+        a.chunk = (uint32_t)std::max<int64_t>(STEP, std::min(LONG_CHUNK, values / (256 * 16) / STEP * STEP));
         int64_t blocks = 0;
-        for (int i = 0; i < a.count; ++i) {
+        for (int i = 0; i < ADAMW_LAUNCH_MAX; ++i) {
             const int j = first + i;
-            a.items[i] = AdamWItem{c.params[j], c.grads[j], c.m[j], c.v[j], bits8 ? c.m_scales[j] : nullptr, bits8 ? c.v_scales[j] : nullptr, c.sizes[j], (int)blocks,
+            a.first_block[i] = i < here ? (int)blocks : INT_MAX;
+            if (i >= here) {
+                a.items[i] = AdamWItem{};
+                continue;
+            }
+            a.items[i] = AdamWItem{c.params[j], c.grads[j], c.m[j], c.v[j], bits8 ? c.m_scales[j] : nullptr, bits8 ? c.v_scales[j] : nullptr, (uint32_t)c.sizes[j],
                                    c.weight_decay ? c.weight_decay[j] : 0.0f};
-            blocks += ceil_div(c.sizes[j], CHUNK_VALUES);
+            blocks += ceil_div(c.sizes[j], (int64_t)a.chunk);
         }
         if (c.param_dtype == SBN_BF16)
             c.grad_dtype == SBN_BF16 ? launch_adamw_bits<SBN_BF16, SBN_BF16>(a, blocks, bits8, c.seed != nullptr, stream)

@@ -31,6 +31,9 @@ template <sbn_dtype DT> struct Row;
 template <> struct Row<SBN_BF16> {
     static constexpr int E = 8;   // values of a vector
     typedef uint16_t value;
+    static __device__ __forceinline__ value get(u32x4 v, int k) { return (value)(v[k / 2] >> (16 * (k % 2))); }
+    static __device__ __forceinline__ void set(u32x4 &v, int k, value x) { v[k / 2] |= (uint32_t)x << (16 * (k % 2)); }   // of a value that is zero
+    static __device__ __forceinline__ void clear(u32x4 &v, int k) { v[k / 2] &= k % 2 ? 0xffffu : 0xffff0000u; }
     template <bool ONCE = false> static __device__ __forceinline__ u32x4 load(const void *row, int64_t vec)
     {
         const u32x4_by2 *p = reinterpret_cast<const u32x4_by2 *>(static_cast<const value *>(row) + vec * E);
@@ -44,7 +47,7 @@ template <> struct Row<SBN_BF16> {
         const value *p = static_cast<const value *>(row) + vec * E;
 #pragma unroll
         for (int k = 0; k < E; ++k)
-            if (k < n) v[k / 2] |= (uint32_t)p[k] << (16 * (k % 2));
+            if (k < n) set(v, k, p[k]);
         return v;
     }
     static __device__ __forceinline__ void store_part(void *row, int64_t vec, int n, u32x4 v)
@@ -52,7 +55,7 @@ template <> struct Row<SBN_BF16> {
         value *p = static_cast<value *>(row) + vec * E;
 #pragma unroll
         for (int k = 0; k < E; ++k)
-            if (k < n) p[k] = (value)(v[k / 2] >> (16 * (k % 2)));
+            if (k < n) p[k] = get(v, k);
     }
     static __device__ __forceinline__ void unpack(u32x4 v, float (&f)[E])
     {
@@ -74,6 +77,9 @@ template <> struct Row<SBN_BF16> {
 template <> struct Row<SBN_F32> {
     static constexpr int E = 4;
     typedef float value;
+    static __device__ __forceinline__ value get(u32x4 v, int k) { return __uint_as_float(v[k]); }
+    static __device__ __forceinline__ void set(u32x4 &v, int k, value x) { v[k] = __float_as_uint(x); }
+    static __device__ __forceinline__ void clear(u32x4 &v, int k) { v[k] = 0; }
     template <bool ONCE = false> static __device__ __forceinline__ u32x4 load(const void *row, int64_t vec)
     {
         const u32x4_by4 *p = reinterpret_cast<const u32x4_by4 *>(static_cast<const value *>(row) + vec * E);
@@ -86,7 +92,7 @@ template <> struct Row<SBN_F32> {
         const value *p = static_cast<const value *>(row) + vec * E;
 #pragma unroll
         for (int k = 0; k < E; ++k)
-            if (k < n) v[k] = __float_as_uint(p[k]);
+            if (k < n) set(v, k, p[k]);
         return v;
     }
     static __device__ __forceinline__ void store_part(void *row, int64_t vec, int n, u32x4 v)
@@ -94,7 +100,7 @@ template <> struct Row<SBN_F32> {
         value *p = static_cast<value *>(row) + vec * E;
 #pragma unroll
         for (int k = 0; k < E; ++k)
-            if (k < n) p[k] = __uint_as_float(v[k]);
+            if (k < n) p[k] = get(v, k);
     }
     static __device__ __forceinline__ void unpack(u32x4 v, float (&f)[E])
     {

@@ -37,13 +37,16 @@ def near(got, ref, tol, what):
     assert worst <= 0, f"{what}: {worst} beyond the tolerance, {(got - ref).abs().max()} off"
 
 
-def check_forward(X, layer, gain=None, bias=None, residual=None, eps=1e-6):
+def check_forward(X, layer, gain=None, bias=None, residual=None, eps=1e-6, Y=None):
+    """Y: where the result is already, else the call is made."""
     s = sbn()
     half = torch.finfo(X.dtype).eps / 2
     dev = lambda t: None if t is None else t.to(DEV)   # noqa: E731
-    Y = torch.full(X.shape, float("nan"), dtype=X.dtype, device=DEV)
+    made = Y is None
+    Y = torch.full(X.shape, float("nan"), dtype=X.dtype, device=DEV) if made else Y
     S = torch.full_like(Y, float("nan")) if residual is not None else None
-    s.sbn_norm(X.to(DEV), Y, gain=dev(gain), bias=dev(bias), eps=eps, layer=layer, residual=dev(residual), sum_out=S)
+    if made:
+        s.sbn_norm(X.to(DEV), Y, gain=dev(gain), bias=dev(bias), eps=eps, layer=layer, residual=dev(residual), sum_out=S)
     if residual is not None:
         X = (X.float() + residual.float()).to(X.dtype)
         assert torch.equal(S.cpu(), X)
@@ -214,7 +217,10 @@ def test_rows_at_odd_addresses_and_what_lies_around_them():
             dy.copy_(dY)
             s.sbn_norm(x, Y, layer=True)
             s.sbn_norm_backward(x, dy, s.new_workspace(s.sbn_norm_workspace_bytes(5, 1003)), dX=dX, layer=True)
-            assert torch.equal(Y, check_forward(X, True)) and torch.equal(dX, check_backward(X, dY, True)["dX"])
+            # against 64 bits and not bit for bit: a row that begins elsewhere in a vector is added up in another order, which the tolerances allow for any
+            check_forward(X, True, Y=Y)
+            want, tol, *_ = backward_reference(X, dY, True, None, 1e-6, None)
+            near(dX, want, torch.finfo(dtype).eps / 2 * want.abs() + tol, "dX")
             for b in bufs:
                 assert (b[:at] == 77.0).all() and (b[at + n:] == 77.0).all()
 
