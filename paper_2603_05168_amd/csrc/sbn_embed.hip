@@ -88,6 +88,16 @@ __device__ __forceinline__ int block_scan(int x, int *scratch, int &total)
     return before + s - x;
 }
 
+// the ids of eight tokens; -1 for those outside the table and behind the last token
+__device__ __forceinline__ void load_ids(const SortArgs &s, int64_t t0, int (&id)[SORT_IDS])
+{
+    int64_t v[SORT_IDS];
+#pragma unroll
+    for (int j = 0; j < SORT_IDS; ++j) v[j] = t0 + j < s.tokens ? s.ids[t0 + j] : -1;
+#pragma unroll
+    for (int j = 0; j < SORT_IDS; ++j) id[j] = v[j] >= 0 && v[j] < s.vocab ? (int)v[j] : -1;
+}
+
 __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
 {
     extern __shared__ int next[];                // [own]: counts, then where the next token of an id goes
@@ -97,12 +107,15 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
     for (int k = threadIdx.x; k < s.own; k += SORT_THREADS) next[k] = 0;
     __syncthreads();
     int lower = 0;
-    for (int64_t t = threadIdx.x; t < s.tokens; t += SORT_THREADS) {
-        const int64_t id = s.ids[t];
-        if (id < 0 || id >= s.vocab) continue;
-        const int b = (int)id & ((1 << s.shift) - 1);
-        lower += b < block;
-        if (b == block) atomicAdd(&next[id >> s.shift], 1);   // whole numbers: in any order
+    for (int64_t tile = 0; tile < s.tokens; tile += SORT_TILE) {
+        int id[SORT_IDS];
+        load_ids(s, tile + threadIdx.x * SORT_IDS, id);
+#pragma unroll
+        for (int j = 0; j < SORT_IDS; ++j) {
+            const int b = id[j] & ((1 << s.shift) - 1);
+            lower += id[j] >= 0 && b < block;
+            if (id[j] >= 0 && b == block) atomicAdd(&next[id[j] >> s.shift], 1);   // whole numbers: in any order
+        }
     }
     int at;
     block_scan(lower, scratch, at);
@@ -125,13 +138,10 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
         const int64_t t0 = tile + (int64_t)threadIdx.x * SORT_IDS;
         int count = 0, total;
         int id[SORT_IDS];
+        load_ids(s, t0, id);
 #pragma unroll
         for (int j = 0; j < SORT_IDS; ++j) {
-            id[j] = -1;
-            if (t0 + j < s.tokens) {
-                const int64_t v = s.ids[t0 + j];
-                if (v >= 0 && v < s.vocab && ((int)v & ((1 << s.shift) - 1)) == block) id[j] = (int)(v >> s.shift);
-            }
+            id[j] = id[j] >= 0 && (id[j] & ((1 << s.shift) - 1)) == block ? id[j] >> s.shift : -1;
             count += id[j] >= 0;
         }
         int to = block_scan(count, scratch, total);
@@ -170,76 +180,114 @@ struct SumArgs {
     void *dE;
     const int *begin, *order, *order_ids;
     float *partials;     // [pieces][2][d]: of the id that the piece begins with, of the one that it ends with
-    int64_t vocab, d;
-    int own, shift, accumulate, pieces;
+    int64_t vocab, d, items;   // items: pieces times tiles
+    int own, shift, accumulate, pieces, tiles;   // tiles: of 64 units of a row
     float scale;
     __device__ __forceinline__ const int *begin_of(int64_t id) const { return begin + (id & ((1 << shift) - 1)) * own + (id >> shift); }
     __device__ __forceinline__ int total() const { return begin[(int64_t)own << shift]; }   // tokens whose id is in the table
 };
 
-template <sbn_dtype TABLE, int U> __device__ __forceinline__ void write_gradient(const SumArgs &s, int id, int64_t unit, const float (&sum)[U])
+template <sbn_dtype TABLE, int U> __device__ __forceinline__ void *row_of(const SumArgs &s, int id)
 {
-    void *row = static_cast<typename Row<TABLE>::value *>(s.dE) + (int64_t)id * s.d;
-    float f[U];
-#pragma unroll
-    for (int k = 0; k < U; ++k) f[k] = sum[k] * s.scale;
-    if (s.accumulate) {
-        float old[U];
-        load_unit<TABLE, U>(row, unit, s.d, old);
-#pragma unroll
-        for (int k = 0; k < U; ++k) f[k] += old[k];
-    }
-    store_unit<TABLE, U>(row, unit, s.d, f);
+    return static_cast<typename Row<TABLE>::value *>(s.dE) + (int64_t)id * s.d;
 }
 
-// blocks below `pieces`: one piece each; those behind: 64 rows of the table each, of which they clear those that no token names
-template <sbn_dtype TABLE, sbn_dtype OUT> __global__ void __launch_bounds__(256) sum_kernel(const SumArgs s)
+// a unit of a row as it is in memory
+template <sbn_dtype DT, int U> struct Raw {
+    static constexpr int E = Row<DT>::E, N = U / E;
+    u32x4 v[N];
+    __device__ __forceinline__ void load(const void *row, int64_t unit, int64_t d)
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = load_vec<DT>(row, unit * N + j, d);
+    }
+    __device__ __forceinline__ void add_to(float (&sum)[U]) const
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            float f[E];
+            Row<DT>::unpack(v[j], f);
+#pragma unroll
+            for (int k = 0; k < E; ++k) sum[j * E + k] += f[k];
+        }
+    }
+};
+
+// Items below `items`: a wavefront has a piece and 64 units of its columns, and asks for the rows of all its tokens before it adds the first (for those of
+// half the piece and the rows that they are added to, where there are such).  Blocks behind: 64 rows of the table each, of which they clear those that no
+// token names.
+template <sbn_dtype TABLE, sbn_dtype OUT, bool ACCUMULATE> __global__ void __launch_bounds__(256) sum_kernel(const SumArgs s)
 {
-    constexpr int U = unit_of(TABLE, OUT);
-    if ((int)blockIdx.x >= s.pieces) {
-        const int64_t v0 = (int64_t)(blockIdx.x - s.pieces) * 64;
+    constexpr int U = unit_of(TABLE, OUT), AT_ONCE = ACCUMULATE ? PIECE / 2 : PIECE;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t item_blocks = (s.items + 3) / 4;
+    if (blockIdx.x >= item_blocks) {
+        const int64_t v0 = (blockIdx.x - item_blocks) * 64;
+        const int *b = s.begin_of(min(v0 + lane, s.vocab - 1));
+        uint64_t nobody = __ballot(v0 + lane < s.vocab && b[0] == b[1]);
         const u32x4 zero = {0, 0, 0, 0};
-        for (int64_t v = v0 + (threadIdx.x >> 6); v < min(v0 + 64, s.vocab); v += 4) {
-            const int *b = s.begin_of(v);
-            if (b[0] != b[1]) continue;
-            void *row = static_cast<typename Row<TABLE>::value *>(s.dE) + v * s.d;
-            for (int64_t vec = threadIdx.x & 63; vec * Row<TABLE>::E < s.d; vec += 64) store_vec<TABLE>(row, vec, s.d, zero);
+        for (int k = 0; nobody; ++k, nobody &= nobody - 1) {
+            if ((k & 3) != wave) continue;
+            void *row = row_of<TABLE, U>(s, (int)v0 + __builtin_ctzll(nobody));
+            for (int64_t vec = lane; vec * Row<TABLE>::E < s.d; vec += 64) store_vec<TABLE>(row, vec, s.d, zero);
         }
         return;
     }
+    const int64_t item = (int64_t)blockIdx.x * 4 + wave;
+    if (item >= s.items) return;
     const int total = s.total();
-    const int piece = blockIdx.x, p0 = piece * PIECE, p1 = min(total, p0 + PIECE);
+    const int piece = (int)(item / s.tiles), p0 = piece * PIECE, p1 = min(total, p0 + PIECE);
+    const int64_t u = (item - (int64_t)piece * s.tiles) * 64 + lane;
     if (p0 >= p1) return;
-    const bool begun = p0 > 0 && s.order_ids[p0 - 1] == s.order_ids[p0];          // the first id's tokens begin in an earlier piece
-    const bool goes_on = p1 < total && s.order_ids[p1 - 1] == s.order_ids[p1];    // the last id's go on in the next
-    for (int64_t u = threadIdx.x; u * U < s.d; u += 256) {
-        float sum[U] = {};
-        int first = p0;   // of the present id in this piece
-        for (int p = p0; p < p1; ++p) {
-            float f[U];
-            load_unit<OUT, U>(static_cast<const typename Row<OUT>::value *>(s.dY) + (int64_t)s.order[p] * s.d, u, s.d, f);
+    // the piece's tokens and ids, and the ids next to it
+    const int p = min(p0 + lane, total - 1);
+    const int token = lane < PIECE ? s.order[p] : 0, id = lane <= PIECE ? s.order_ids[p] : 0;
+    const auto id_at = [&](int k) { return __builtin_amdgcn_readlane(id, k); };
+    const bool begun = p0 > 0 && s.order_ids[max(p0 - 1, 0)] == id_at(0);       // the first id's tokens begin in an earlier piece
+    const bool goes_on = p1 < total && id_at(PIECE - 1) == id_at(PIECE);        // the last id's go on in the next
+    const int count = p1 - p0;
+    const auto last_of_id = [&](int k) { return k + 1 == count || id_at(k) != id_at(k + 1); };
+    float sum[U] = {};
+    bool first = true;   // the present id is the piece's first
 #pragma unroll
-            for (int k = 0; k < U; ++k) sum[k] += f[k];
-            const int id = s.order_ids[p];
-            const bool last = p + 1 == p1;
-            if (!last && s.order_ids[p + 1] == id) continue;
-            if (first == p0 && begun)
-                store_unit<SBN_F32, U>(s.partials + (int64_t)piece * 2 * s.d, u, s.d, sum);
-            else if (last && goes_on)
-                store_unit<SBN_F32, U>(s.partials + ((int64_t)piece * 2 + 1) * s.d, u, s.d, sum);
-            else
-                write_gradient<TABLE, U>(s, id, u, sum);
+    for (int k0 = 0; k0 < PIECE; k0 += AT_ONCE) {
+        Raw<OUT, U> rows[AT_ONCE];
+        Raw<TABLE, U> old[ACCUMULATE ? AT_ONCE : 1];
 #pragma unroll
-            for (int k = 0; k < U; ++k) sum[k] = 0.0f;
-            first = p + 1;
-        }
+        for (int k = 0; k < AT_ONCE; ++k)
+            if (k0 + k < count) {
+                rows[k].load(static_cast<const typename Row<OUT>::value *>(s.dY) + (int64_t)__builtin_amdgcn_readlane(token, k0 + k) * s.d, u, s.d);
+                if (ACCUMULATE && last_of_id(k0 + k)) old[k].load(row_of<TABLE, U>(s, id_at(k0 + k)), u, s.d);
+            }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k)
+            if (k0 + k < count) {
+                rows[k].add_to(sum);
+                if (last_of_id(k0 + k)) {
+                    if (first && begun)
+                        store_unit<SBN_F32, U>(s.partials + (int64_t)piece * 2 * s.d, u, s.d, sum);
+                    else if (k0 + k + 1 == count && goes_on)
+                        store_unit<SBN_F32, U>(s.partials + ((int64_t)piece * 2 + 1) * s.d, u, s.d, sum);
+                    else {
+#pragma unroll
+                        for (int i = 0; i < U; ++i) sum[i] *= s.scale;
+                        if (ACCUMULATE) old[k].add_to(sum);
+                        store_unit<TABLE, U>(row_of<TABLE, U>(s, id_at(k0 + k)), u, s.d, sum);
+                    }
+#pragma unroll
+                    for (int i = 0; i < U; ++i) sum[i] = 0.0f;
+                    first = false;
+                }
+            }
     }
 }
 
-// one block to a piece in which an id begins that goes on behind it
-template <sbn_dtype TABLE> __global__ void __launch_bounds__(256) join_kernel(const SumArgs s)
+// A block to a piece in which an id begins that goes on behind it, and 64 units of its columns: sixteen wavefronts add the partial sums in turn, eight asked
+// for at a time, and their sums are added in order.
+template <sbn_dtype TABLE> __global__ void __launch_bounds__(1024) join_kernel(const SumArgs s)
 {
-    constexpr int U = Row<TABLE>::E;
+    constexpr int U = Row<TABLE>::E, WAVES = 16, AT_ONCE = 4;
+    __shared__ float sums[WAVES][64 * U];
     const int total = s.total();
     const int piece = blockIdx.x, p0 = piece * PIECE, p1 = p0 + PIECE;
     if (p1 >= total) return;
@@ -247,17 +295,38 @@ template <sbn_dtype TABLE> __global__ void __launch_bounds__(256) join_kernel(co
     if (s.order_ids[p1 - 1] != id) return;
     if (p0 > 0 && s.order_ids[p0 - 1] == id) return;   // begins earlier
     const int end = s.begin_of(id)[1];
-    const int64_t u = (int64_t)blockIdx.y * 256 + threadIdx.x;
-    if (u * U >= s.d) return;
-    float sum[U];
-    load_unit<SBN_F32, U>(s.partials + ((int64_t)piece * 2 + 1) * s.d, u, s.d, sum);
-    for (int64_t q = piece + 1; q * PIECE < end; ++q) {
-        float f[U];
-        load_unit<SBN_F32, U>(s.partials + q * 2 * s.d, u, s.d, f);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t u = (int64_t)blockIdx.y * 64 + lane;
+    const int count = (end - 1) / PIECE - piece + 1;   // pieces that the id has a share of: the last of the first one, the first of the others
+    float sum[U] = {};
+    for (int q0 = wave; q0 < count; q0 += WAVES * AT_ONCE) {
+        float f[AT_ONCE][U];
 #pragma unroll
-        for (int k = 0; k < U; ++k) sum[k] += f[k];
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int q = q0 + WAVES * j;
+#pragma unroll
+            for (int k = 0; k < U; ++k) f[j][k] = 0.0f;
+            if (q < count) load_unit<SBN_F32, U>(s.partials + ((int64_t)(piece + q) * 2 + (q == 0)) * s.d, u, s.d, f[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j)
+#pragma unroll
+            for (int k = 0; k < U; ++k) sum[k] += f[j][k];
     }
-    write_gradient<TABLE, U>(s, id, u, sum);
+#pragma unroll
+    for (int k = 0; k < U; ++k) sums[wave][k * 64 + lane] = sum[k];
+    __syncthreads();
+    if (wave > 0 || u * U >= s.d) return;
+    for (int w = 1; w < min(WAVES, count); ++w) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) sum[k] += sums[w][k * 64 + lane];
+    }
+    void *row = row_of<TABLE, U>(s, id);
+    float old[U] = {};
+    if (s.accumulate) load_unit<TABLE, U>(row, u, s.d, old);
+#pragma unroll
+    for (int k = 0; k < U; ++k) sum[k] = s.accumulate ? sum[k] * s.scale + old[k] : sum[k] * s.scale;
+    store_unit<TABLE, U>(row, u, s.d, sum);
 }
 
 struct Carved {
@@ -281,12 +350,15 @@ Carved carve(int64_t tokens, int64_t d, int64_t vocab)
     return c;
 }
 
-template <sbn_dtype TABLE, sbn_dtype OUT> sbn_status sum_as(const SumArgs &s, hipStream_t stream)
+template <sbn_dtype TABLE, sbn_dtype OUT> sbn_status sum_as(SumArgs s, hipStream_t stream)
 {
+    s.tiles = (int)ceil_div(s.d, 64 * unit_of(TABLE, OUT));
+    s.items = (int64_t)s.pieces * s.tiles;
     const int64_t clearing = s.accumulate ? 0 : ceil_div(s.vocab, 64);
-    hipLaunchKernelGGL((sum_kernel<TABLE, OUT>), dim3((unsigned)(s.pieces + clearing)), dim3(256), 0, stream, s);
+    const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(s.items, 4) + clearing)), dim3(256), 0, stream, s); };
+    s.accumulate ? launch(sum_kernel<TABLE, OUT, true>) : launch(sum_kernel<TABLE, OUT, false>);
     if (s.pieces > 1)
-        hipLaunchKernelGGL(join_kernel<TABLE>, dim3((unsigned)s.pieces - 1, (unsigned)ceil_div(ceil_div(s.d, Row<TABLE>::E), 256)), dim3(256), 0, stream, s);
+        hipLaunchKernelGGL(join_kernel<TABLE>, dim3((unsigned)s.pieces - 1, (unsigned)ceil_div(s.d, 64 * Row<TABLE>::E)), dim3(1024), 0, stream, s);
     return check_launch("sum_kernel");
 }
 

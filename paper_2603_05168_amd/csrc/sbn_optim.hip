@@ -103,7 +103,12 @@ template <int BELOW> __device__ __forceinline__ uint32_t shared_exponent(const f
     return max((top + 0xfffffu) >> 23, (uint32_t)BELOW);   // one more where rounding may reach the next binade
 }
 
-// What a thread has of a tensor: eight weights with their gradients and moments.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// What a thread has of a tensor: eight weights with their gradients and moments.  All of it is read and written once a step, and weights, gradients and fp32
+// moments go past the caches (nontemporal): what a step leaves in the memory side's cache has to leave it while the next kernel reads.  The norm of 79M
+// gradients and a step with fp32 moments took 30 + 347 us, with stores through the caches 52 + 330; with 8-bit moments for 317M weights 94 + 602, through
+// the caches 94 + 643.  (Codes go through the caches, eight bytes to a thread: past them 623.)
 template <sbn_dtype PT, sbn_dtype GT, bool BITS8> struct Eight {
     float p[8], g[8], m[8], v[8];
 
@@ -118,7 +123,7 @@ template <sbn_dtype PT, sbn_dtype GT, bool BITS8> struct Eight {
             load_unit<GT, 8>(it.g, unit, it.n, g);
         }
         if constexpr (BITS8) {
-            uint2 mc = static_cast<const uint2 *>(it.m)[unit], vc = static_cast<const uint2 *>(it.v)[unit];
+            u32x2 mc = static_cast<const u32x2 *>(it.m)[unit], vc = static_cast<const u32x2 *>(it.v)[unit];
             const uint32_t me = it.m_scales[at / 32], ve = it.v_scales[at / 32];
             if (!WHOLE) {   // what pads the last 32 is zero
                 mc = first_bytes(mc, (int64_t)it.n - at);
@@ -126,8 +131,8 @@ template <sbn_dtype PT, sbn_dtype GT, bool BITS8> struct Eight {
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                m[k] = value_of<M_BELOW>(((k < 4 ? mc.x : mc.y) >> (8 * (k & 3))) & 255u, me);
-                v[k] = value_of<V_BELOW>(((k < 4 ? vc.x : vc.y) >> (8 * (k & 3))) & 255u, ve);
+                m[k] = value_of<M_BELOW>((mc[k / 4] >> (8 * (k & 3))) & 255u, me);
+                v[k] = value_of<V_BELOW>((vc[k / 4] >> (8 * (k & 3))) & 255u, ve);
             }
         } else if (WHOLE) {
             load_whole<SBN_F32>(it.m, at, m);
@@ -158,16 +163,32 @@ template <sbn_dtype PT, sbn_dtype GT, bool BITS8> struct Eight {
 private:
     template <sbn_dtype DT> static __device__ __forceinline__ void load_whole(const void *p, uint32_t at, float (&f)[8])
     {
-        load_unit<DT, 8>(static_cast<const typename Row<DT>::value *>(p) + at, 0, 8, f);
+        constexpr int E = Row<DT>::E;
+        const void *here = static_cast<const typename Row<DT>::value *>(p) + at;
+#pragma unroll
+        for (int j = 0; j < 8 / E; ++j) {
+            float part[E];
+            Row<DT>::unpack(Row<DT>::template load<true>(here, j), part);
+#pragma unroll
+            for (int k = 0; k < E; ++k) f[j * E + k] = part[k];
+        }
     }
     template <sbn_dtype DT> static __device__ __forceinline__ void store_whole(void *p, uint32_t at, const float (&f)[8])
     {
-        store_unit<DT, 8>(static_cast<typename Row<DT>::value *>(p) + at, 0, 8, f);
+        constexpr int E = Row<DT>::E;
+        void *here = static_cast<typename Row<DT>::value *>(p) + at;
+#pragma unroll
+        for (int j = 0; j < 8 / E; ++j) {
+            float part[E];
+#pragma unroll
+            for (int k = 0; k < E; ++k) part[k] = f[j * E + k];
+            Row<DT>::template store<true>(here, j, Row<DT>::pack(part));
+        }
     }
-    static __device__ __forceinline__ uint2 first_bytes(uint2 c, int64_t n)
+    static __device__ __forceinline__ u32x2 first_bytes(u32x2 c, int64_t n)
     {
-        const uint64_t all = (uint64_t)c.y << 32 | c.x, some = n >= 8 ? all : n <= 0 ? 0 : all & (((uint64_t)1 << (8 * n)) - 1);
-        return make_uint2((uint32_t)some, (uint32_t)(some >> 32));
+        const uint64_t all = (uint64_t)c[1] << 32 | c[0], some = n >= 8 ? all : n <= 0 ? 0 : all & (((uint64_t)1 << (8 * n)) - 1);
+        return (u32x2){(uint32_t)some, (uint32_t)(some >> 32)};
     }
 };
 
@@ -235,14 +256,14 @@ template <sbn_dtype PT, sbn_dtype GT, bool BITS8, bool STOCHASTIC> __global__ vo
             e.template store<false>(it, at);
         if constexpr (BITS8) {
             const uint32_t me = shared_exponent<M_BELOW>(e.m), ve = shared_exponent<V_BELOW>(e.v);
-            uint32_t mc[2] = {0, 0}, vc[2] = {0, 0};
+            u32x2 mc = {0, 0}, vc = {0, 0};
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 mc[k / 4] |= code_of<M_BELOW>(e.m[k], me, STOCHASTIC ? noise(1, k) * 16 + 8 : nearest(e.m[k])) << (8 * (k & 3));
                 vc[k / 4] |= code_of<V_BELOW>(e.v[k], ve, STOCHASTIC ? noise(2, k) * 16 + 8 : nearest(e.v[k])) << (8 * (k & 3));
             }
-            static_cast<uint2 *>(it.m)[at / 8] = make_uint2(mc[0], mc[1]);
-            static_cast<uint2 *>(it.v)[at / 8] = make_uint2(vc[0], vc[1]);
+            static_cast<u32x2 *>(it.m)[at / 8] = mc;
+            static_cast<u32x2 *>(it.v)[at / 8] = vc;
             if (at % 32 == 0) {
                 it.m_scales[at / 32] = (uint8_t)me;
                 it.v_scales[at / 32] = (uint8_t)ve;
@@ -265,7 +286,8 @@ template <sbn_dtype OUT, int BELOW> __global__ void __launch_bounds__(256) state
 
 // ---- the norm of all gradients ----------------------------------------------------------------------------------------------------
 constexpr int GRAD_NORM_LAUNCH_MAX = 64;
-constexpr int64_t GRAD_NORM_VALUES = 16384;   // values of a block
+constexpr int64_t MEMORY_CACHE = 256 << 20;   // bytes of the memory side's cache
+constexpr int64_t GRAD_NORM_VALUES = 32768;   // values of a block
 
 struct GradNormArgs {
     int first_block[GRAD_NORM_LAUNCH_MAX];
@@ -284,8 +306,9 @@ __device__ __forceinline__ double block_sum(double s, double *scratch)
     return s;
 }
 
-// squares in double: those of fp32 gradients reach past the range of fp32
-template <sbn_dtype GT> __global__ void __launch_bounds__(256) square_sums_kernel(const GradNormArgs a)
+// Squares in double: those of fp32 gradients reach past the range of fp32.  ONCE: the gradients are more than the memory side's cache holds, and go past it
+// (317M in bf16: 94 us against 143); else they are left there for the step (79M: 30 + 347 us against 27 + 369).
+template <sbn_dtype GT, bool ONCE> __global__ void __launch_bounds__(256) square_sums_kernel(const GradNormArgs a)
 {
     __shared__ double scratch[4];
     const int which = tensor_of(a.first_block, blockIdx.x);
@@ -293,11 +316,11 @@ template <sbn_dtype GT> __global__ void __launch_bounds__(256) square_sums_kerne
     const int64_t n = a.n[which], begin = (int64_t)((int)blockIdx.x - a.first_block[which]) * GRAD_NORM_VALUES;
     const int64_t end = min(n, begin + GRAD_NORM_VALUES);
     double s = 0.0;
-    constexpr int E = Row<GT>::E, AT_ONCE = 4;
+    constexpr int E = Row<GT>::E, AT_ONCE = 8;
     for (int64_t at = begin + threadIdx.x * E; at < end; at += 256 * E * AT_ONCE) {
         u32x4 x[AT_ONCE];
 #pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) x[j] = load_vec<GT>(g, at / E + 256 * j, end);
+        for (int j = 0; j < AT_ONCE; ++j) x[j] = load_vec<GT, ONCE>(g, at / E + 256 * j, end);
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) {
             float f[E];
@@ -348,7 +371,9 @@ size_t grad_norm_workspace_bytes(int count, const int64_t *sizes)
 sbn_status launch_grad_norm(int count, const void *const *grads, sbn_dtype dtype, const int64_t *sizes, float max_norm, float *out, void *workspace, hipStream_t stream)
 {
     double *sums = static_cast<double *>(workspace);
-    int64_t all = 0;
+    int64_t all = 0, values = 0;
+    for (int i = 0; i < count; ++i) values += sizes[i];
+    const bool once = values * (dtype == SBN_BF16 ? 2 : 4) > MEMORY_CACHE;
     for (int first = 0; first < count; first += GRAD_NORM_LAUNCH_MAX) {
         GradNormArgs a;
         a.sums = sums + all;
@@ -360,10 +385,11 @@ sbn_status launch_grad_norm(int count, const void *const *grads, sbn_dtype dtype
             a.first_block[i] = i < here ? (int)blocks : INT_MAX;
             blocks += ceil_div(a.n[i], GRAD_NORM_VALUES);
         }
+        const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a); };
         if (dtype == SBN_BF16)
-            hipLaunchKernelGGL(square_sums_kernel<SBN_BF16>, dim3((unsigned)blocks), dim3(256), 0, stream, a);
+            once ? launch(square_sums_kernel<SBN_BF16, true>) : launch(square_sums_kernel<SBN_BF16, false>);
         else
-            hipLaunchKernelGGL(square_sums_kernel<SBN_F32>, dim3((unsigned)blocks), dim3(256), 0, stream, a);
+            once ? launch(square_sums_kernel<SBN_F32, true>) : launch(square_sums_kernel<SBN_F32, false>);
         all += blocks;
     }
     hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, stream, sums, all, max_norm, out);

@@ -39,7 +39,14 @@ template <> struct Row<SBN_BF16> {
         const u32x4_by2 *p = reinterpret_cast<const u32x4_by2 *>(static_cast<const value *>(row) + vec * E);
         return ONCE ? __builtin_nontemporal_load(p) : *p;
     }
-    static __device__ __forceinline__ void store(void *row, int64_t vec, u32x4 v) { *(reinterpret_cast<u32x4_by2 *>(static_cast<value *>(row) + vec * E)) = v; }
+    template <bool ONCE = false> static __device__ __forceinline__ void store(void *row, int64_t vec, u32x4 v)
+    {
+        u32x4_by2 *p = reinterpret_cast<u32x4_by2 *>(static_cast<value *>(row) + vec * E);
+        if (ONCE)
+            __builtin_nontemporal_store(v, p);
+        else
+            *p = v;
+    }
     // the last vector, of which `n` values are the row's; the others come as zeros and are not written
     static __device__ __forceinline__ u32x4 load_part(const void *row, int64_t vec, int n)
     {
@@ -85,7 +92,14 @@ template <> struct Row<SBN_F32> {
         const u32x4_by4 *p = reinterpret_cast<const u32x4_by4 *>(static_cast<const value *>(row) + vec * E);
         return ONCE ? __builtin_nontemporal_load(p) : *p;
     }
-    static __device__ __forceinline__ void store(void *row, int64_t vec, u32x4 v) { *(reinterpret_cast<u32x4_by4 *>(static_cast<value *>(row) + vec * E)) = v; }
+    template <bool ONCE = false> static __device__ __forceinline__ void store(void *row, int64_t vec, u32x4 v)
+    {
+        u32x4_by4 *p = reinterpret_cast<u32x4_by4 *>(static_cast<value *>(row) + vec * E);
+        if (ONCE)
+            __builtin_nontemporal_store(v, p);
+        else
+            *p = v;
+    }
     static __device__ __forceinline__ u32x4 load_part(const void *row, int64_t vec, int n)
     {
         u32x4 v = {0, 0, 0, 0};
