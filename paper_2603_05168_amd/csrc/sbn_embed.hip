@@ -9,8 +9,8 @@
 //   sort_kernel   puts the tokens in order of their ids, tokens of one id in their own order.  Ids go to blocks round-robin, which spreads the
 //                 frequent ones; a block looks through all ids, counts those of lower blocks (where its share of the order begins) and its own,
 //                 and places these.
-//   sum_kernel    walks the order in pieces of PIECE tokens, which balances the work however often an id occurs.  An id whose tokens all lie in
-//                 a piece is written there; of one that crosses pieces each leaves a partial sum in fp32.
+//   sum_kernel    walks the order in pieces of PIECE tokens, which balances the work however often an id occurs.  An id whose tokens end in the
+//                 piece that they begin in, or in the next, is written there; of one that goes on each piece leaves a partial sum in fp32.
 //   join_kernel   adds the partial sums of such an id in the order of the pieces.
 #include <algorithm>
 
@@ -22,8 +22,9 @@ namespace sbn {
 namespace {
 
 constexpr int SORT_THREADS = 1024;
-constexpr int SORT_IDS = 8;                              // consecutive ids of a thread
-constexpr int SORT_TILE = SORT_THREADS * SORT_IDS;
+constexpr int SORT_LOADS = 4;                            // of a thread, two ids each
+constexpr int SORT_TILE = SORT_THREADS * SORT_LOADS * 2;
+constexpr int SORT_BITS = 15;                            // of a number up to SORT_OWN
 constexpr int SORT_OWN = 16384;                          // ids of the table that one sorting block has at most: their counts lie in LDS
 constexpr int PIECE = 16;                                // tokens of a piece
 
@@ -66,7 +67,7 @@ struct SortArgs {
     int own, shift;      // ids of a block; log2 of the blocks
 };
 
-// exclusive sum over the block's threads; total: of all of them
+// sum over the threads in front; total: over all of the block's
 __device__ __forceinline__ int block_scan(int x, int *scratch, int &total)
 {
     int s = x;
@@ -80,6 +81,7 @@ __device__ __forceinline__ int block_scan(int x, int *scratch, int &total)
     __syncthreads();
     int before = 0;
     total = 0;
+#pragma unroll
     for (int w = 0; w < SORT_THREADS / 64; ++w) {
         const int o = scratch[w];
         before += w < (int)(threadIdx.x >> 6) ? o : 0;
@@ -88,43 +90,58 @@ __device__ __forceinline__ int block_scan(int x, int *scratch, int &total)
     return before + s - x;
 }
 
-// the ids of eight tokens; -1 for those outside the table and behind the last token
-__device__ __forceinline__ void load_ids(const SortArgs &s, int64_t t0, int (&id)[SORT_IDS])
+// A thread has tokens 2 thread and 2 thread + 1 of each of the SORT_LOADS runs of a tile: whole lines to a wavefront's load (eight tokens in a row to a
+// thread are a line to each lane: 27 us for 16384 tokens in place of 13).  Ids outside the table, and those behind the last token, as -1.
+__device__ __forceinline__ void load_ids(const SortArgs &s, int64_t tile, int (&id)[SORT_LOADS][2])
 {
-    int64_t v[SORT_IDS];
+    typedef int64_t i64x2 __attribute__((ext_vector_type(2), aligned(8)));
+    i64x2 v[SORT_LOADS];
 #pragma unroll
-    for (int j = 0; j < SORT_IDS; ++j) v[j] = t0 + j < s.tokens ? s.ids[t0 + j] : -1;
+    for (int j = 0; j < SORT_LOADS; ++j) {
+        const int64_t t = tile + (int64_t)j * 2 * SORT_THREADS + threadIdx.x * 2;
+        v[j] = (i64x2){-1, -1};
+        if (t + 1 < s.tokens)
+            v[j] = *reinterpret_cast<const i64x2 *>(s.ids + t);
+        else if (t < s.tokens)
+            v[j][0] = s.ids[t];
+    }
 #pragma unroll
-    for (int j = 0; j < SORT_IDS; ++j) id[j] = v[j] >= 0 && v[j] < s.vocab ? (int)v[j] : -1;
+    for (int j = 0; j < SORT_LOADS; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) id[j][e] = v[j][e] >= 0 && v[j][e] < s.vocab ? (int)v[j][e] : -1;
 }
 
 __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
 {
+    constexpr int WAVES = SORT_THREADS / 64;
     extern __shared__ int next[];                // [own]: counts, then where the next token of an id goes
-    __shared__ int scratch[SORT_THREADS / 64];
+    __shared__ int scratch[WAVES];
+    __shared__ int counts[SORT_LOADS * WAVES];   // of the block's tokens, in the tile's order
     __shared__ uint2 found[SORT_TILE];           // (which of the block's ids, token), in the order of the tokens
-    const int block = blockIdx.x;
+    const int block = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mask = (1 << s.shift) - 1;
     for (int k = threadIdx.x; k < s.own; k += SORT_THREADS) next[k] = 0;
     __syncthreads();
     int lower = 0;
-    for (int64_t tile = 0; tile < s.tokens; tile += SORT_TILE) {
-        int id[SORT_IDS];
-        load_ids(s, tile + threadIdx.x * SORT_IDS, id);
+    int id[SORT_LOADS][2];
+    for (int64_t tile = (s.tokens - 1) / SORT_TILE * SORT_TILE; tile >= 0; tile -= SORT_TILE) {   // the first tile last: its ids are at hand below
+        load_ids(s, tile, id);
 #pragma unroll
-        for (int j = 0; j < SORT_IDS; ++j) {
-            const int b = id[j] & ((1 << s.shift) - 1);
-            lower += id[j] >= 0 && b < block;
-            if (id[j] >= 0 && b == block) atomicAdd(&next[id[j] >> s.shift], 1);   // whole numbers: in any order
-        }
+        for (int j = 0; j < SORT_LOADS; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int b = id[j][e] & mask;
+                lower += id[j][e] >= 0 && b < block;
+                if (id[j][e] >= 0 && b == block) atomicAdd(&next[id[j][e] >> s.shift], 1);   // whole numbers: in any order
+            }
     }
     int at;
     block_scan(lower, scratch, at);
     // from counts to beginnings: each thread a run of ids
     const int run = (s.own + SORT_THREADS - 1) / SORT_THREADS;
     const int k0 = min(s.own, (int)threadIdx.x * run), k1 = min(s.own, k0 + run);
-    int mine = 0, all;
-    for (int k = k0; k < k1; ++k) mine += next[k];
-    int begin = at + block_scan(mine, scratch, all);
+    int count_here = 0, all;
+    for (int k = k0; k < k1; ++k) count_here += next[k];
+    int begin = at + block_scan(count_here, scratch, all);
     for (int k = k0; k < k1; ++k) {
         const int count = next[k];
         next[k] = begin;
@@ -133,42 +150,67 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
     }
     if (block == (int)gridDim.x - 1 && threadIdx.x == 0) s.begin[(int64_t)gridDim.x * s.own] = at + all;
     if (!all) return;
+    const uint64_t in_front = (1ull << lane) - 1;
+    const int bits = 32 - __builtin_clz(s.own);   // at most SORT_BITS
     for (int64_t tile = 0; tile < s.tokens; tile += SORT_TILE) {
         // the tile's tokens of this block, side by side and in their order
-        const int64_t t0 = tile + (int64_t)threadIdx.x * SORT_IDS;
-        int count = 0, total;
-        int id[SORT_IDS];
-        load_ids(s, t0, id);
+        if (tile > 0) load_ids(s, tile, id);
+        int place[SORT_LOADS][2];
 #pragma unroll
-        for (int j = 0; j < SORT_IDS; ++j) {
-            id[j] = id[j] >= 0 && (id[j] & ((1 << s.shift) - 1)) == block ? id[j] >> s.shift : -1;
-            count += id[j] >= 0;
+        for (int j = 0; j < SORT_LOADS; ++j) {
+            uint64_t has[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                id[j][e] = id[j][e] >= 0 && (id[j][e] & mask) == block ? id[j][e] >> s.shift : -1;
+                has[e] = __ballot(id[j][e] >= 0);
+            }
+            place[j][0] = __popcll(has[0] & in_front) + __popcll(has[1] & in_front);
+            place[j][1] = place[j][0] + (int)(has[0] >> lane & 1);
+            if (lane == 0) counts[j * WAVES + wave] = __popcll(has[0]) + __popcll(has[1]);
         }
-        int to = block_scan(count, scratch, total);
-#pragma unroll
-        for (int j = 0; j < SORT_IDS; ++j)
-            if (id[j] >= 0) found[to++] = make_uint2(id[j], (unsigned)(t0 + j));
         __syncthreads();
-        // one wavefront places them, 64 at a time: a token goes behind those of its id among the lanes in front
-        if (threadIdx.x < 64) {
-            int bits = 32 - __builtin_clz(s.own);
-            for (int i = threadIdx.x; i - (int)threadIdx.x < total; i += 64) {
-                const bool live = i < total;
-                const uint2 f = live ? found[i] : make_uint2(0, 0);
-                unsigned long long same = __ballot(live);
-                for (int b = 0; b < bits; ++b) {
-                    const unsigned long long set = __ballot(f.x >> b & 1);
+        static_assert(SORT_LOADS * WAVES == 64, "one count to a lane");
+        const int mine = counts[lane];
+        int upto = mine;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int o = __shfl_up(upto, off, 64);
+            if (lane >= off) upto += o;
+        }
+        const int total = __shfl(upto, 63, 64);
+        int before[SORT_LOADS];
+#pragma unroll
+        for (int j = 0; j < SORT_LOADS; ++j) before[j] = __shfl(upto - mine, j * WAVES + wave, 64);
+#pragma unroll
+        for (int j = 0; j < SORT_LOADS; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (id[j][e] >= 0)
+                    found[before[j] + place[j][e]] = make_uint2(id[j][e], (unsigned)(tile + j * 2 * SORT_THREADS + threadIdx.x * 2 + e));
+        __syncthreads();
+        // Each wavefront has 64 of them and counts, of every token, those of its id among the lanes in front (lanes whose ids agree in every bit).  Then
+        // the wavefronts take their places in turn.
+        for (int first = 0; first < total; first += SORT_THREADS) {
+            const int i = first + threadIdx.x;
+            const bool live = i < total;
+            const uint2 f = live ? found[i] : make_uint2(0, 0);
+            uint64_t same = __ballot(live);
+#pragma unroll
+            for (int b = 0; b < SORT_BITS; ++b)
+                if (b < bits) {
+                    const uint64_t set = __ballot(f.x >> b & 1);
                     same &= f.x >> b & 1 ? set : ~set;
                 }
-                const int before = __popcll(same & ((1ull << threadIdx.x) - 1));
-                const int place = live ? next[f.x] + before : 0;
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                if (live) {
-                    s.order[place] = (int)f.y;
-                    s.order_ids[place] = (int)(f.x << s.shift) + block;
-                    if (before == __popcll(same) - 1) next[f.x] = place + 1;
+            const int ahead = __popcll(same & in_front);
+            const bool last = ahead == __popcll(same) - 1;
+            for (int w = 0; first + w * 64 < total && w < WAVES; ++w) {
+                if (w == wave && live) {
+                    const int to = next[f.x] + ahead;
+                    s.order[to] = (int)f.y;
+                    s.order_ids[to] = (int)(f.x << s.shift) + block;
+                    if (last) next[f.x] = to + 1;   // (behind the reads of all lanes: a wavefront's accesses to LDS are done in their order)
                 }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __syncthreads();
             }
         }
         __syncthreads();
@@ -192,14 +234,17 @@ template <sbn_dtype TABLE, int U> __device__ __forceinline__ void *row_of(const 
     return static_cast<typename Row<TABLE>::value *>(s.dE) + (int64_t)id * s.d;
 }
 
+// whether an id's tokens, from place `begin` of the order on, all go with the piece that they begin in: they end in it or in the next
+__device__ __forceinline__ bool of_one_piece(int begin, int end) { return end <= (begin / PIECE + 2) * PIECE; }
+
 // a unit of a row as it is in memory
 template <sbn_dtype DT, int U> struct Raw {
     static constexpr int E = Row<DT>::E, N = U / E;
     u32x4 v[N];
-    __device__ __forceinline__ void load(const void *row, int64_t unit, int64_t d)
+    template <bool ONCE> __device__ __forceinline__ void load(const void *row, int64_t unit, int64_t d)
     {
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = load_vec<DT>(row, unit * N + j, d);
+        for (int j = 0; j < N; ++j) v[j] = load_vec<DT, ONCE>(row, unit * N + j, d);
     }
     __device__ __forceinline__ void add_to(float (&sum)[U]) const
     {
@@ -213,12 +258,12 @@ template <sbn_dtype DT, int U> struct Raw {
     }
 };
 
-// Items below `items`: a wavefront has a piece and 64 units of its columns, and asks for the rows of all its tokens before it adds the first (for those of
-// half the piece and the rows that they are added to, where there are such).  Blocks behind: 64 rows of the table each, of which they clear those that no
+// Items below `items`: a wavefront has a piece and 64 units of its columns, and asks for the rows of all its tokens (and for those that they are added
+// to) before it adds the first.  Blocks behind: 64 rows of the table each, of which they clear those that no
 // token names.
 template <sbn_dtype TABLE, sbn_dtype OUT, bool ACCUMULATE> __global__ void __launch_bounds__(256) sum_kernel(const SumArgs s)
 {
-    constexpr int U = unit_of(TABLE, OUT), AT_ONCE = ACCUMULATE ? PIECE / 2 : PIECE;
+    constexpr int U = unit_of(TABLE, OUT), AT_ONCE = PIECE;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t item_blocks = (s.items + 3) / 4;
     if (blockIdx.x >= item_blocks) {
@@ -239,34 +284,50 @@ template <sbn_dtype TABLE, sbn_dtype OUT, bool ACCUMULATE> __global__ void __lau
     const int piece = (int)(item / s.tiles), p0 = piece * PIECE, p1 = min(total, p0 + PIECE);
     const int64_t u = (item - (int64_t)piece * s.tiles) * 64 + lane;
     if (p0 >= p1) return;
-    // the piece's tokens and ids, and the ids next to it
+    // the tokens and ids of the piece and of the next
     const int p = min(p0 + lane, total - 1);
-    const int token = lane < PIECE ? s.order[p] : 0, id = lane <= PIECE ? s.order_ids[p] : 0;
+    const int token = lane < 2 * PIECE ? s.order[p] : 0, id = lane < 2 * PIECE ? s.order_ids[p] : 0;
     const auto id_at = [&](int k) { return __builtin_amdgcn_readlane(id, k); };
-    const bool begun = p0 > 0 && s.order_ids[max(p0 - 1, 0)] == id_at(0);       // the first id's tokens begin in an earlier piece
-    const bool goes_on = p1 < total && id_at(PIECE - 1) == id_at(PIECE);        // the last id's go on in the next
-    const int count = p1 - p0;
-    const auto last_of_id = [&](int k) { return k + 1 == count || id_at(k) != id_at(k + 1); };
+    // An id that begins in a piece and ends in the next is the former's: no partial sums of ids of few tokens.
+    int first_k = 0, end_k = p1 - p0;
+    bool begun = p0 > 0 && s.order_ids[max(p0 - 1, 0)] == id_at(0);              // the first id's tokens begin in an earlier piece
+    if (begun) {
+        const int *b = s.begin_of(id_at(0));
+        if (of_one_piece(b[0], b[1])) {
+            first_k = b[1] - p0;
+            begun = false;
+        }
+    }
+    bool goes_on = p1 < total && id_at(PIECE - 1) == id_at(PIECE);               // the last id's go on in the next
+    if (goes_on) {
+        const int *b = s.begin_of(id_at(PIECE));
+        if (b[0] >= p0 && of_one_piece(b[0], b[1])) {
+            end_k = b[1] - p0;
+            goes_on = false;
+        }
+    }
+    const auto last_of_id = [&](int k) { return k + 1 == end_k || id_at(k) != id_at(k + 1); };
     float sum[U] = {};
     bool first = true;   // the present id is the piece's first
 #pragma unroll
-    for (int k0 = 0; k0 < PIECE; k0 += AT_ONCE) {
+    for (int k0 = 0; k0 < 2 * PIECE; k0 += AT_ONCE) {
+        if (k0 >= end_k) break;
         Raw<OUT, U> rows[AT_ONCE];
         Raw<TABLE, U> old[ACCUMULATE ? AT_ONCE : 1];
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k)
-            if (k0 + k < count) {
-                rows[k].load(static_cast<const typename Row<OUT>::value *>(s.dY) + (int64_t)__builtin_amdgcn_readlane(token, k0 + k) * s.d, u, s.d);
-                if (ACCUMULATE && last_of_id(k0 + k)) old[k].load(row_of<TABLE, U>(s, id_at(k0 + k)), u, s.d);
+            if (k0 + k >= first_k && k0 + k < end_k) {
+                rows[k].template load<true>(static_cast<const typename Row<OUT>::value *>(s.dY) + (int64_t)__builtin_amdgcn_readlane(token, k0 + k) * s.d, u, s.d);
+                if (ACCUMULATE && last_of_id(k0 + k)) old[k].template load<false>(row_of<TABLE, U>(s, id_at(k0 + k)), u, s.d);
             }
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k)
-            if (k0 + k < count) {
+            if (k0 + k >= first_k && k0 + k < end_k) {
                 rows[k].add_to(sum);
                 if (last_of_id(k0 + k)) {
                     if (first && begun)
                         store_unit<SBN_F32, U>(s.partials + (int64_t)piece * 2 * s.d, u, s.d, sum);
-                    else if (k0 + k + 1 == count && goes_on)
+                    else if (k0 + k + 1 == end_k && goes_on)
                         store_unit<SBN_F32, U>(s.partials + ((int64_t)piece * 2 + 1) * s.d, u, s.d, sum);
                     else {
 #pragma unroll
@@ -282,11 +343,11 @@ template <sbn_dtype TABLE, sbn_dtype OUT, bool ACCUMULATE> __global__ void __lau
     }
 }
 
-// A block to a piece in which an id begins that goes on behind it, and 64 units of its columns: sixteen wavefronts add the partial sums in turn, eight asked
-// for at a time, and their sums are added in order.
-template <sbn_dtype TABLE> __global__ void __launch_bounds__(1024) join_kernel(const SumArgs s)
+// A block to a piece in which an id begins that goes on behind the next, and 64 units of its columns: four wavefronts add the partial sums in turn, eight asked for
+// at a time, and their sums are added in order.
+template <sbn_dtype TABLE> __global__ void __launch_bounds__(256) join_kernel(const SumArgs s)
 {
-    constexpr int U = Row<TABLE>::E, WAVES = 16, AT_ONCE = 4;
+    constexpr int U = Row<TABLE>::E, WAVES = 4, AT_ONCE = 8;
     __shared__ float sums[WAVES][64 * U];
     const int total = s.total();
     const int piece = blockIdx.x, p0 = piece * PIECE, p1 = p0 + PIECE;
@@ -295,24 +356,31 @@ template <sbn_dtype TABLE> __global__ void __launch_bounds__(1024) join_kernel(c
     if (s.order_ids[p1 - 1] != id) return;
     if (p0 > 0 && s.order_ids[p0 - 1] == id) return;   // begins earlier
     const int end = s.begin_of(id)[1];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (of_one_piece(p0, end)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t u = (int64_t)blockIdx.y * 64 + lane;
     const int count = (end - 1) / PIECE - piece + 1;   // pieces that the id has a share of: the last of the first one, the first of the others
     float sum[U] = {};
-    for (int q0 = wave; q0 < count; q0 += WAVES * AT_ONCE) {
-        float f[AT_ONCE][U];
+    const auto add = [&](auto load) {
+        for (int q0 = wave; q0 < count; q0 += WAVES * AT_ONCE) {
+            float f[AT_ONCE][U];
 #pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) {
-            const int q = q0 + WAVES * j;
+            for (int j = 0; j < AT_ONCE; ++j) {
+                const int q = min(q0 + WAVES * j, count - 1);
+                load(s.partials + ((int64_t)(piece + q) * 2 + (q == 0)) * s.d, f[j]);
+            }
 #pragma unroll
-            for (int k = 0; k < U; ++k) f[j][k] = 0.0f;
-            if (q < count) load_unit<SBN_F32, U>(s.partials + ((int64_t)(piece + q) * 2 + (q == 0)) * s.d, u, s.d, f[j]);
+            for (int j = 0; j < AT_ONCE; ++j)
+                if (q0 + WAVES * j < count) {
+#pragma unroll
+                    for (int k = 0; k < U; ++k) sum[k] += f[j][k];
+                }
         }
-#pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j)
-#pragma unroll
-            for (int k = 0; k < U; ++k) sum[k] += f[j][k];
-    }
+    };
+    if ((u + 1) * U <= s.d)
+        add([&](const float *share, float (&f)[U]) { load_floats<U>(share, u * U, u * U + U, 0.0f, f); });
+    else
+        add([&](const float *share, float (&f)[U]) { load_floats<U>(share, u * U, s.d, 0.0f, f); });
 #pragma unroll
     for (int k = 0; k < U; ++k) sums[wave][k * 64 + lane] = sum[k];
     __syncthreads();
@@ -357,8 +425,8 @@ template <sbn_dtype TABLE, sbn_dtype OUT> sbn_status sum_as(SumArgs s, hipStream
     const int64_t clearing = s.accumulate ? 0 : ceil_div(s.vocab, 64);
     const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(s.items, 4) + clearing)), dim3(256), 0, stream, s); };
     s.accumulate ? launch(sum_kernel<TABLE, OUT, true>) : launch(sum_kernel<TABLE, OUT, false>);
-    if (s.pieces > 1)
-        hipLaunchKernelGGL(join_kernel<TABLE>, dim3((unsigned)s.pieces - 1, (unsigned)ceil_div(s.d, 64 * Row<TABLE>::E)), dim3(1024), 0, stream, s);
+    if (s.pieces > 2)   // (an id of two pieces is one piece's)
+        hipLaunchKernelGGL(join_kernel<TABLE>, dim3((unsigned)s.pieces - 2, (unsigned)ceil_div(s.d, 64 * Row<TABLE>::E)), dim3(256), 0, stream, s);
     return check_launch("sum_kernel");
 }
 

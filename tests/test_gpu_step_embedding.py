@@ -92,7 +92,8 @@ def test_one_id_for_all_and_none(T):
 def test_runs_that_end_where_pieces_do():
     """Ids whose tokens fill pieces of the order exactly, reach over one border, or over several."""
     g = torch.Generator().manual_seed(2)
-    for lengths in ([16, 16, 16], [8, 8, 17, 15, 16], [1, 47, 1, 32, 31, 1], [15, 2, 15, 16, 33], [64, 1, 1, 14, 160]):
+    for lengths in ([16, 16, 16], [8, 8, 17, 15, 16], [1, 47, 1, 32, 31, 1], [15, 2, 15, 16, 33], [64, 1, 1, 14, 160], [15, 17, 16, 1, 31, 2], [15, 18, 15], [1, 31, 1, 32, 1, 30, 17],
+                    [16, 32, 33, 32, 31], [15, 33, 5, 300, 3]):
         # ids that lie in one block's share of the vocabulary are neighbours in the order
         ids = torch.cat([torch.full((n,), 256 * k) for k, n in enumerate(lengths)])
         ids = ids[torch.randperm(len(ids), generator=g)]
