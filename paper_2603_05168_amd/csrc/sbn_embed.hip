@@ -22,9 +22,9 @@ namespace sbn {
 namespace {
 
 constexpr int SORT_THREADS = 1024;
-constexpr int SORT_LOADS = 4;                            // of a thread, two ids each
+constexpr int SORT_LOADS = 8;                            // of a thread, two ids each
 constexpr int SORT_TILE = SORT_THREADS * SORT_LOADS * 2;
-constexpr int SORT_BITS = 15;                            // of a number up to SORT_OWN
+constexpr int SORT_BITS = 15;                            // of a number up to SORT_OWN, or of a token in a tile
 constexpr int SORT_OWN = 16384;                          // ids of the table that one sorting block has at most: their counts lie in LDS
 constexpr int PIECE = 16;                                // tokens of a piece
 
@@ -67,49 +67,56 @@ struct SortArgs {
     int own, shift;      // ids of a block; log2 of the blocks
 };
 
+// sum over the lanes up to this one, by DPP (row_shr 1, 2, 4, 8, row_bcast 15, 31)
+__device__ __forceinline__ int wave_scan(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+
 // sum over the threads in front; total: over all of the block's
 __device__ __forceinline__ int block_scan(int x, int *scratch, int &total)
 {
-    int s = x;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int o = __shfl_up(s, off, 64);
-        if ((int)(threadIdx.x & 63) >= off) s += o;
-    }
+    const int s = wave_scan(x);
     __syncthreads();   // the scratch may still be read
     if ((threadIdx.x & 63) == 63) scratch[threadIdx.x >> 6] = s;
     __syncthreads();
-    int before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < SORT_THREADS / 64; ++w) {
-        const int o = scratch[w];
-        before += w < (int)(threadIdx.x >> 6) ? o : 0;
-        total += o;
-    }
-    return before + s - x;
+    // a wavefront's sum to each of 16 lanes
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sums = wave_scan(lane < SORT_THREADS / 64 ? scratch[lane] : 0);
+    total = __builtin_amdgcn_readlane(sums, 63);
+    return (wave > 0 ? __shfl(sums, wave - 1, 64) : 0) + s - x;
 }
 
 // A thread has tokens 2 thread and 2 thread + 1 of each of the SORT_LOADS runs of a tile: whole lines to a wavefront's load (eight tokens in a row to a
 // thread are a line to each lane: 27 us for 16384 tokens in place of 13).  Ids outside the table, and those behind the last token, as -1.
-__device__ __forceinline__ void load_ids(const SortArgs &s, int64_t tile, int (&id)[SORT_LOADS][2])
-{
+struct Ids {
     typedef int64_t i64x2 __attribute__((ext_vector_type(2), aligned(8)));
     i64x2 v[SORT_LOADS];
+    __device__ __forceinline__ void load(const SortArgs &s, int64_t tile)
+    {
 #pragma unroll
-    for (int j = 0; j < SORT_LOADS; ++j) {
-        const int64_t t = tile + (int64_t)j * 2 * SORT_THREADS + threadIdx.x * 2;
-        v[j] = (i64x2){-1, -1};
-        if (t + 1 < s.tokens)
-            v[j] = *reinterpret_cast<const i64x2 *>(s.ids + t);
-        else if (t < s.tokens)
-            v[j][0] = s.ids[t];
+        for (int j = 0; j < SORT_LOADS; ++j) {
+            const int64_t t = tile + (int64_t)j * 2 * SORT_THREADS + threadIdx.x * 2;
+            v[j] = (i64x2){-1, -1};
+            if (t + 1 < s.tokens)
+                v[j] = *reinterpret_cast<const i64x2 *>(s.ids + t);
+            else if (t < s.tokens)
+                v[j][0] = s.ids[t];
+        }
     }
+    __device__ __forceinline__ void in_table(const SortArgs &s, int (&id)[SORT_LOADS][2]) const
+    {
 #pragma unroll
-    for (int j = 0; j < SORT_LOADS; ++j)
+        for (int j = 0; j < SORT_LOADS; ++j)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) id[j][e] = v[j][e] >= 0 && v[j][e] < s.vocab ? (int)v[j][e] : -1;
-}
+            for (int e = 0; e < 2; ++e) id[j][e] = v[j][e] >= 0 && v[j][e] < s.vocab ? (int)v[j][e] : -1;
+    }
+};
 
 __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
 {
@@ -117,14 +124,18 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
     extern __shared__ int next[];                // [own]: counts, then where the next token of an id goes
     __shared__ int scratch[WAVES];
     __shared__ int counts[SORT_LOADS * WAVES];   // of the block's tokens, in the tile's order
-    __shared__ uint2 found[SORT_TILE];           // (which of the block's ids, token), in the order of the tokens
+    __shared__ uint32_t found[SORT_TILE];        // which of the block's ids << SORT_BITS | token of the tile, in the order of the tokens
     const int block = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mask = (1 << s.shift) - 1;
     for (int k = threadIdx.x; k < s.own; k += SORT_THREADS) next[k] = 0;
     __syncthreads();
     int lower = 0;
     int id[SORT_LOADS][2];
-    for (int64_t tile = (s.tokens - 1) / SORT_TILE * SORT_TILE; tile >= 0; tile -= SORT_TILE) {   // the first tile last: its ids are at hand below
-        load_ids(s, tile, id);
+    Ids ahead;   // of the tile that comes next
+    const int64_t last_tile = (s.tokens - 1) / SORT_TILE * SORT_TILE;
+    ahead.load(s, last_tile);
+    for (int64_t tile = last_tile; tile >= 0; tile -= SORT_TILE) {   // the first tile last: its ids are at hand below
+        ahead.in_table(s, id);
+        if (tile > 0) ahead.load(s, tile - SORT_TILE);
 #pragma unroll
         for (int j = 0; j < SORT_LOADS; ++j)
 #pragma unroll
@@ -154,7 +165,8 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
     const int bits = 32 - __builtin_clz(s.own);   // at most SORT_BITS
     for (int64_t tile = 0; tile < s.tokens; tile += SORT_TILE) {
         // the tile's tokens of this block, side by side and in their order
-        if (tile > 0) load_ids(s, tile, id);
+        if (tile > 0) ahead.in_table(s, id);
+        if (tile + SORT_TILE < s.tokens) ahead.load(s, tile + SORT_TILE);
         int place[SORT_LOADS][2];
 #pragma unroll
         for (int j = 0; j < SORT_LOADS; ++j) {
@@ -169,48 +181,44 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
             if (lane == 0) counts[j * WAVES + wave] = __popcll(has[0]) + __popcll(has[1]);
         }
         __syncthreads();
-        static_assert(SORT_LOADS * WAVES == 64, "one count to a lane");
-        const int mine = counts[lane];
-        int upto = mine;
+        static_assert(SORT_LOADS * WAVES == 128, "two counts to a lane");
+        const int c0 = counts[2 * lane], c1 = counts[2 * lane + 1], upto = wave_scan(c0 + c1);
+        const int total = __builtin_amdgcn_readlane(upto, 63);
 #pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int o = __shfl_up(upto, off, 64);
-            if (lane >= off) upto += o;
-        }
-        const int total = __shfl(upto, 63, 64);
-        int before[SORT_LOADS];
-#pragma unroll
-        for (int j = 0; j < SORT_LOADS; ++j) before[j] = __shfl(upto - mine, j * WAVES + wave, 64);
-#pragma unroll
-        for (int j = 0; j < SORT_LOADS; ++j)
+        for (int j = 0; j < SORT_LOADS; ++j) {
+            const int k = j * WAVES + wave;
+            const int before = __shfl(upto - c1 - (k & 1 ? 0 : c0), k / 2, 64);
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                if (id[j][e] >= 0)
-                    found[before[j] + place[j][e]] = make_uint2(id[j][e], (unsigned)(tile + j * 2 * SORT_THREADS + threadIdx.x * 2 + e));
+                if (id[j][e] >= 0) found[before + place[j][e]] = (uint32_t)id[j][e] << SORT_BITS | (j * 2 * SORT_THREADS + threadIdx.x * 2 + e);
+        }
         __syncthreads();
         // Each wavefront has 64 of them and counts, of every token, those of its id among the lanes in front (lanes whose ids agree in every bit).  Then
         // the wavefronts take their places in turn.
         for (int first = 0; first < total; first += SORT_THREADS) {
             const int i = first + threadIdx.x;
             const bool live = i < total;
-            const uint2 f = live ? found[i] : make_uint2(0, 0);
+            const uint32_t f = live ? found[i] : 0, of = f >> SORT_BITS;
             uint64_t same = __ballot(live);
 #pragma unroll
             for (int b = 0; b < SORT_BITS; ++b)
                 if (b < bits) {
-                    const uint64_t set = __ballot(f.x >> b & 1);
-                    same &= f.x >> b & 1 ? set : ~set;
+                    const uint64_t set = __ballot(of >> b & 1);
+                    same &= of >> b & 1 ? set : ~set;
                 }
-            const int ahead = __popcll(same & in_front);
-            const bool last = ahead == __popcll(same) - 1;
+            const int nearer = __popcll(same & in_front);
+            const bool last = nearer == __popcll(same) - 1;
+            int to = 0;
             for (int w = 0; first + w * 64 < total && w < WAVES; ++w) {
                 if (w == wave && live) {
-                    const int to = next[f.x] + ahead;
-                    s.order[to] = (int)f.y;
-                    s.order_ids[to] = (int)(f.x << s.shift) + block;
-                    if (last) next[f.x] = to + 1;   // (behind the reads of all lanes: a wavefront's accesses to LDS are done in their order)
+                    to = next[of] + nearer;
+                    if (last) next[of] = to + 1;   // (behind the reads of all lanes: a wavefront's accesses to LDS are done in their order)
                 }
                 __syncthreads();
+            }
+            if (live) {
+                s.order[to] = (int)(tile + (f & ((1 << SORT_BITS) - 1)));
+                s.order_ids[to] = (int)(of << s.shift) + block;
             }
         }
         __syncthreads();
@@ -343,21 +351,9 @@ template <sbn_dtype TABLE, sbn_dtype OUT, bool ACCUMULATE> __global__ void __lau
     }
 }
 
-// A block to a piece in which an id begins that goes on behind the next, and 64 units of its columns: four wavefronts add the partial sums in turn, eight asked for
-// at a time, and their sums are added in order.
-template <sbn_dtype TABLE> __global__ void __launch_bounds__(256) join_kernel(const SumArgs s)
+template <sbn_dtype TABLE, int U, int WAVES, int AT_ONCE>
+__device__ __forceinline__ void join(const SumArgs &s, int piece, int id, int end, int lane, int wave, float (*sums)[64 * U])
 {
-    constexpr int U = Row<TABLE>::E, WAVES = 4, AT_ONCE = 8;
-    __shared__ float sums[WAVES][64 * U];
-    const int total = s.total();
-    const int piece = blockIdx.x, p0 = piece * PIECE, p1 = p0 + PIECE;
-    if (p1 >= total) return;
-    const int id = s.order_ids[p1];
-    if (s.order_ids[p1 - 1] != id) return;
-    if (p0 > 0 && s.order_ids[p0 - 1] == id) return;   // begins earlier
-    const int end = s.begin_of(id)[1];
-    if (of_one_piece(p0, end)) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t u = (int64_t)blockIdx.y * 64 + lane;
     const int count = (end - 1) / PIECE - piece + 1;   // pieces that the id has a share of: the last of the first one, the first of the others
     float sum[U] = {};
@@ -381,6 +377,7 @@ template <sbn_dtype TABLE> __global__ void __launch_bounds__(256) join_kernel(co
         add([&](const float *share, float (&f)[U]) { load_floats<U>(share, u * U, u * U + U, 0.0f, f); });
     else
         add([&](const float *share, float (&f)[U]) { load_floats<U>(share, u * U, s.d, 0.0f, f); });
+    __syncthreads();   // the sums may still be read
 #pragma unroll
     for (int k = 0; k < U; ++k) sums[wave][k * 64 + lane] = sum[k];
     __syncthreads();
@@ -395,6 +392,31 @@ template <sbn_dtype TABLE> __global__ void __launch_bounds__(256) join_kernel(co
 #pragma unroll
     for (int k = 0; k < U; ++k) sum[k] = s.accumulate ? sum[k] * s.scale + old[k] : sum[k] * s.scale;
     store_unit<TABLE, U>(row, u, s.d, sum);
+}
+
+// A block to JOIN_PIECES pieces and 64 units of the columns.  For every one of them in which an id begins that goes on behind the next (there are few: a
+// block each spent 15 us on looking, at 16384 tokens), sixteen wavefronts add the partial sums in turn, eight asked for at a time, and their sums are added
+// in order.
+constexpr int JOIN_PIECES = 8;
+template <sbn_dtype TABLE> __global__ void __launch_bounds__(1024) join_kernel(const SumArgs s)
+{
+    constexpr int U = Row<TABLE>::E, WAVES = 16, AT_ONCE = 8;
+    __shared__ float sums[WAVES][64 * U];
+    const int total = s.total();
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // a piece to a lane
+    const int64_t p0 = ((int64_t)blockIdx.x * JOIN_PIECES + lane) * PIECE, p1 = p0 + PIECE;
+    int id = -1, end = 0;
+    if (lane < JOIN_PIECES && p1 < total) {
+        id = s.order_ids[p1];
+        const bool begins = s.order_ids[p1 - 1] == id && (p0 == 0 || s.order_ids[p0 - 1] != id);
+        if (begins) end = s.begin_of(id)[1];
+        if (!begins || of_one_piece((int)p0, end)) id = -1;
+    }
+    for (uint64_t todo = __ballot(id >= 0); todo; todo &= todo - 1) {
+        const int k = __builtin_ctzll(todo);
+        join<TABLE, U, WAVES, AT_ONCE>(s, blockIdx.x * JOIN_PIECES + k, __builtin_amdgcn_readlane(id, k), __builtin_amdgcn_readlane(end, k), lane, wave, sums);
+    }
 }
 
 struct Carved {
@@ -426,7 +448,7 @@ template <sbn_dtype TABLE, sbn_dtype OUT> sbn_status sum_as(SumArgs s, hipStream
     const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(s.items, 4) + clearing)), dim3(256), 0, stream, s); };
     s.accumulate ? launch(sum_kernel<TABLE, OUT, true>) : launch(sum_kernel<TABLE, OUT, false>);
     if (s.pieces > 2)   // (an id of two pieces is one piece's)
-        hipLaunchKernelGGL(join_kernel<TABLE>, dim3((unsigned)s.pieces - 2, (unsigned)ceil_div(s.d, 64 * Row<TABLE>::E)), dim3(256), 0, stream, s);
+        hipLaunchKernelGGL(join_kernel<TABLE>, dim3((unsigned)ceil_div(s.pieces - 2, JOIN_PIECES), (unsigned)ceil_div(s.d, 64 * Row<TABLE>::E)), dim3(1024), 0, stream, s);
     return check_launch("sum_kernel");
 }
 

@@ -80,7 +80,7 @@ def test_gradient(T, V, d, table, out):
     check_gradient(dY, ids, V, table, old=torch.randn(V, d, generator=g).to(table))
 
 
-@pytest.mark.parametrize("T", [1, 15, 16, 17, 31, 32, 33, 48, 1000, 8191, 8193])
+@pytest.mark.parametrize("T", [1, 15, 16, 17, 31, 32, 33, 48, 1000, 8191, 8193, 16384, 16385, 40000])
 def test_one_id_for_all_and_none(T):
     g = torch.Generator().manual_seed(T)
     dY = torch.randn(T, 24, generator=g)
