@@ -65,6 +65,8 @@ struct SortArgs {
     int *order;          // [tokens]: the tokens
     int *order_ids;      // [tokens]: their ids
     int own, shift;      // ids of a block; log2 of the blocks
+    char *clear;         // the table's gradient, to be cleared by the blocks behind (null: not)
+    int64_t clear_bytes;
 };
 
 // sum over the lanes up to this one, by DPP (row_shr 1, 2, 4, 8, row_bcast 15, 31)
@@ -118,14 +120,39 @@ struct Ids {
     }
 };
 
+// Clears the table's gradient: 256 threads of each of CLEARING blocks, from one end to the other, so that all stores of a moment lie near each other (a
+// plain fill of 671 MB: 106 us so, by 1024 threads of each 119, by pieces of 64 KB to a block 128).  The first block clears what lies off 16 bytes at
+// either end too (whole values: two bytes at least).
+constexpr int CLEARING = 256, CLEARING_THREADS = 256;
+__device__ __forceinline__ void clear(const SortArgs &s)
+{
+    if (threadIdx.x >= CLEARING_THREADS) return;
+    char *const end = s.clear + s.clear_bytes;
+    char *const first = min(end, s.clear + (-reinterpret_cast<uintptr_t>(s.clear) & 15)), *const last = first + (end - first) / 16 * 16;
+    const u32x4 zero = {0, 0, 0, 0};
+    for (char *p = first + ((int64_t)blockIdx.x * CLEARING_THREADS + threadIdx.x) * 16; p < last; p += (int64_t)CLEARING * CLEARING_THREADS * 16)
+        *reinterpret_cast<u32x4 *>(p) = zero;
+    if (blockIdx.x == 0 && threadIdx.x < 16) {
+        uint16_t *const front = reinterpret_cast<uint16_t *>(s.clear) + threadIdx.x, *const back = reinterpret_cast<uint16_t *>(last) + threadIdx.x;
+        if (reinterpret_cast<char *>(front) < first) *front = 0;
+        if (reinterpret_cast<char *>(back) < end) *back = 0;
+    }
+}
+
+// The last 2^shift blocks sort; CLEARING in front of them (where there is something to clear) clear the table's gradient meanwhile, all of it: the rows that
+// have one are written again by the next kernel.
 __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
 {
+    if (s.clear && blockIdx.x < CLEARING) {
+        clear(s);
+        return;
+    }
     constexpr int WAVES = SORT_THREADS / 64;
     extern __shared__ int next[];                // [own]: counts, then where the next token of an id goes
     __shared__ int scratch[WAVES];
     __shared__ int counts[SORT_LOADS * WAVES];   // of the block's tokens, in the tile's order
     __shared__ uint32_t found[SORT_TILE];        // which of the block's ids << SORT_BITS | token of the tile, in the order of the tokens
-    const int block = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mask = (1 << s.shift) - 1;
+    const int block = blockIdx.x - (s.clear ? CLEARING : 0), lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mask = (1 << s.shift) - 1;
     for (int k = threadIdx.x; k < s.own; k += SORT_THREADS) next[k] = 0;
     __syncthreads();
     int lower = 0;
@@ -159,7 +186,7 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
         s.begin[(int64_t)block * s.own + k] = begin;
         begin += count;
     }
-    if (block == (int)gridDim.x - 1 && threadIdx.x == 0) s.begin[(int64_t)gridDim.x * s.own] = at + all;
+    if (block == mask && threadIdx.x == 0) s.begin[(int64_t)s.own << s.shift] = at + all;
     if (!all) return;
     const uint64_t in_front = (1ull << lane) - 1;
     const int bits = 32 - __builtin_clz(s.own);   // at most SORT_BITS
@@ -266,26 +293,12 @@ template <sbn_dtype DT, int U> struct Raw {
     }
 };
 
-// Items below `items`: a wavefront has a piece and 64 units of its columns, and asks for the rows of all its tokens (and for those that they are added
-// to) before it adds the first.  Blocks behind: 64 rows of the table each, of which they clear those that no
-// token names.
+// A wavefront has a piece and 64 units of its columns, and asks for the rows of all its tokens (and for those that they are added
+// to) before it adds the first.
 template <sbn_dtype TABLE, sbn_dtype OUT, bool ACCUMULATE> __global__ void __launch_bounds__(256) sum_kernel(const SumArgs s)
 {
     constexpr int U = unit_of(TABLE, OUT), AT_ONCE = PIECE;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t item_blocks = (s.items + 3) / 4;
-    if (blockIdx.x >= item_blocks) {
-        const int64_t v0 = (blockIdx.x - item_blocks) * 64;
-        const int *b = s.begin_of(min(v0 + lane, s.vocab - 1));
-        uint64_t nobody = __ballot(v0 + lane < s.vocab && b[0] == b[1]);
-        const u32x4 zero = {0, 0, 0, 0};
-        for (int k = 0; nobody; ++k, nobody &= nobody - 1) {
-            if ((k & 3) != wave) continue;
-            void *row = row_of<TABLE, U>(s, (int)v0 + __builtin_ctzll(nobody));
-            for (int64_t vec = lane; vec * Row<TABLE>::E < s.d; vec += 64) store_vec<TABLE>(row, vec, s.d, zero);
-        }
-        return;
-    }
     const int64_t item = (int64_t)blockIdx.x * 4 + wave;
     if (item >= s.items) return;
     const int total = s.total();
@@ -444,8 +457,7 @@ template <sbn_dtype TABLE, sbn_dtype OUT> sbn_status sum_as(SumArgs s, hipStream
 {
     s.tiles = (int)ceil_div(s.d, 64 * unit_of(TABLE, OUT));
     s.items = (int64_t)s.pieces * s.tiles;
-    const int64_t clearing = s.accumulate ? 0 : ceil_div(s.vocab, 64);
-    const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(s.items, 4) + clearing)), dim3(256), 0, stream, s); };
+    const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(s.items, 4)), dim3(256), 0, stream, s); };
     s.accumulate ? launch(sum_kernel<TABLE, OUT, true>) : launch(sum_kernel<TABLE, OUT, false>);
     if (s.pieces > 2)   // (an id of two pieces is one piece's)
         hipLaunchKernelGGL(join_kernel<TABLE>, dim3((unsigned)ceil_div(s.pieces - 2, JOIN_PIECES), (unsigned)ceil_div(s.d, 64 * Row<TABLE>::E)), dim3(1024), 0, stream, s);
@@ -487,7 +499,11 @@ sbn_status launch_embedding_backward(const void *dY, sbn_dtype out, const int64_
         set_hip_error(e, "hipFuncSetAttribute(sort_kernel)");
         return SBN_EHIP;
     }
-    hipLaunchKernelGGL(sort_kernel, dim3(1u << o.shift), dim3(SORT_THREADS), lds, stream, o);
+    if (!accumulate) {
+        o.clear = static_cast<char *>(dE);
+        o.clear_bytes = vocab * d * (table == SBN_BF16 ? 2 : 4);
+    }
+    hipLaunchKernelGGL(sort_kernel, dim3((unsigned)((1 << o.shift) + (o.clear ? CLEARING : 0))), dim3(SORT_THREADS), lds, stream, o);
     SumArgs s{};
     s.dY = dY;
     s.dE = dE;

@@ -21,7 +21,9 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int STEP = THREADS * 8;             // values of a block at once
-constexpr int64_t LONG_CHUNK = 16 * STEP;     // values of a block at most
+// Values of a block at most.  Short pieces keep the stores of all blocks near each other in memory (79M weights with fp32 moments: 305 us, by 8 steps 336, by
+// 16 347); with moments in 8 bits what a block does once has to be spread (317M weights: 660 by one step, 612 by two, 592 by eight, 602 by 16).
+constexpr int64_t CHUNK_32BIT = STEP, CHUNK_8BIT = 8 * STEP;
 
 struct AdamWItem {
     void *p;
@@ -38,7 +40,8 @@ struct AdamWArgs {
     AdamWItem items[ADAMW_LAUNCH_MAX];
     const float *lr, *clip;
     const int64_t *step;
-    double beta1, beta2;
+    double log_beta1, log_beta2;
+    float beta1, less_beta1, beta2, less_beta2;   // less_beta: 1 - beta
     float eps;
     uint32_t seed_low, seed_high;
     int first_item;   // place in the call of items[0]
@@ -52,16 +55,8 @@ __device__ __forceinline__ int tensor_of(const int *first_block, int block)
     return __builtin_amdgcn_readfirstlane(__popcll(__ballot(first_block[threadIdx.x & 63] <= block)) - 1);
 }
 
-// x to a whole power: a few products, where pow() takes as long as all the rest of a small tensor
-__device__ __forceinline__ double power(double x, int64_t n)
-{
-    double y = 1.0;
-    for (; n > 0; n >>= 1) {
-        if (n & 1) y *= x;
-        x *= x;
-    }
-    return y;
-}
+// 1 - beta^t from the logarithm of beta: to a few steps of fp32, where powers in double took as long as a thousand values
+__device__ __forceinline__ float less_power(double log_beta, double t) { return -expm1f((float)(t * log_beta)); }
 
 // 32 random bits of a counter and two keys: two rounds of a multiplication between shifts, the multipliers from the digits of the golden ratio and
 // of pi.  The rounding needs no more than bits that are even on average and not the same for neighbours, moments or steps.
@@ -202,11 +197,10 @@ template <sbn_dtype PT, sbn_dtype GT, bool BITS8, bool STOCHASTIC> __global__ vo
     const int which = tensor_of(a.first_block, blockIdx.x);
     const AdamWItem it = a.items[which];
     const int64_t step = *a.step;
-    const double lr = (double)*a.lr;
-    const float rate = (float)(lr / (1.0 - power(a.beta1, step)));
-    const float keep = (float)(1.0 - lr * (double)it.decay);
-    const float of_v = (float)(1.0 / sqrt(1.0 - power(a.beta2, step)));
-    const float b1 = (float)a.beta1, c1 = (float)(1.0 - a.beta1), b2 = (float)a.beta2, c2 = (float)(1.0 - a.beta2);
+    const float lr = *a.lr, keep = (float)(1.0 - (double)lr * (double)it.decay);
+    const float rate = lr / less_power(a.log_beta1, (double)step);
+    const float of_v = 1.0f / sqrtf(less_power(a.log_beta2, (double)step));
+    const float b1 = a.beta1, c1 = a.less_beta1, b2 = a.beta2, c2 = a.less_beta2;
     // v_sqrt_f32 and v_rcp_f32 are good to a step of fp32 and take less than half the time of the correctly rounded root and quotient, but make zero of
     // numbers below 2^-126: with an eps that is nothing beside such a root they must not be met
     const bool exactly = a.eps < 1e-12f;
@@ -404,8 +398,12 @@ sbn_status launch_adamw(const AdamWCall &c, hipStream_t stream)
         a.lr = c.lr;
         a.clip = c.clip;
         a.step = c.step;
-        a.beta1 = c.beta1;
-        a.beta2 = c.beta2;
+        a.log_beta1 = std::log(c.beta1);
+        a.log_beta2 = std::log(c.beta2);
+        a.beta1 = (float)c.beta1;
+        a.less_beta1 = (float)(1.0 - c.beta1);
+        a.beta2 = (float)c.beta2;
+        a.less_beta2 = (float)(1.0 - c.beta2);
         a.eps = (float)c.eps;
         a.seed_low = c.seed ? (uint32_t)*c.seed : 0;
         a.seed_high = c.seed ? (uint32_t)(*c.seed >> 32) : 0;
@@ -413,8 +411,8 @@ sbn_status launch_adamw(const AdamWCall &c, hipStream_t stream)
         a.first_item = first;
         int64_t values = 0;
         for (int i = 0; i < here; ++i) values += c.sizes[first + i];
-        // some 16 blocks to a processor where there are values for them, which share out evenly; what a block does once is then a few hundredths
-        a.chunk = (uint32_t)std::max<int64_t>(STEP, std::min(LONG_CHUNK, values / (256 * 16) / STEP * STEP));
+        // four blocks to a processor at least where there are values for them
+        a.chunk = (uint32_t)std::max<int64_t>(STEP, std::min(bits8 ? CHUNK_8BIT : CHUNK_32BIT, values / (256 * 4) / STEP * STEP));
         int64_t blocks = 0;
         for (int i = 0; i < ADAMW_LAUNCH_MAX; ++i) {
             const int j = first + i;
