@@ -36,25 +36,99 @@ inline int sort_shift(int64_t vocab)
     return shift;
 }
 
-// a wavefront copies a row
+// A thread's U columns of a row of U values or more.  The last of a row whose length is no multiple of U begin where they still are all in the row:
+// neither loads nor stores have ends to look after, and what two threads write twice is the same.
+template <int U> __device__ __forceinline__ int64_t columns(int64_t unit, int64_t d) { return min(unit * U, d - U); }
+
+// U columns of a row as they are in memory
+template <sbn_dtype DT, int U> struct Raw {
+    static constexpr int E = Row<DT>::E, N = U / E;
+    typedef typename Row<DT>::value value;
+    u32x4 v[N];
+    template <bool ONCE> __device__ __forceinline__ void load(const void *row, int64_t column)
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = Row<DT>::template load<ONCE>(static_cast<const value *>(row) + column, j);
+    }
+    __device__ __forceinline__ void store(void *row, int64_t column) const
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) Row<DT>::store(static_cast<value *>(row) + column, j, v[j]);
+    }
+    // those from column `own` on
+    __device__ __forceinline__ void store_own(void *row, int64_t column, int64_t own) const
+    {
+        if (column == own) return store(row, column);
+        value *p = static_cast<value *>(row) + column;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int k = 0; k < E; ++k)
+                if (column + j * E + k >= own) p[j * E + k] = Row<DT>::get(v[j], k);
+    }
+    __device__ __forceinline__ void add_to(float (&sum)[U]) const
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            float f[E];
+            Row<DT>::unpack(v[j], f);
+#pragma unroll
+            for (int k = 0; k < E; ++k) sum[j * E + k] += f[k];
+        }
+    }
+    static __device__ __forceinline__ Raw of(const float (&sum)[U])
+    {
+        Raw raw;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            float f[E];
+#pragma unroll
+            for (int k = 0; k < E; ++k) f[k] = sum[j * E + k];
+            raw.v[j] = Row<DT>::pack(f);
+        }
+        return raw;
+    }
+};
+
+template <sbn_dtype DT> __device__ __forceinline__ float value_at(const void *row, int64_t column) { return Row<DT>::number(static_cast<const typename Row<DT>::value *>(row)[column]); }
+template <sbn_dtype DT> __device__ __forceinline__ void set_value(void *row, int64_t column, float f)
+{
+    static_cast<typename Row<DT>::value *>(row)[column] = Row<DT>::rounded(f);
+}
+
+// A wavefront copies a row, four units of it at a time: 168 MB (16384 rows of 2560 bf16 values) in 27 us, where a copy of as much takes 24.
 template <sbn_dtype TABLE, sbn_dtype OUT> __global__ void __launch_bounds__(256) embedding_kernel(const void *E, const int64_t *ids, int64_t tokens, int64_t vocab,
                                                                                                   int64_t d, float scale, void *Y)
 {
-    constexpr int U = unit_of(TABLE, OUT);
-    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    constexpr int U = unit_of(TABLE, OUT), AT_ONCE = 4;
+    const int lane = threadIdx.x & 63;
+    const int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (t >= tokens) return;
     const int64_t id = ids[t];
     const bool inside = id >= 0 && id < vocab;
     const void *from = static_cast<const typename Row<TABLE>::value *>(E) + (inside ? id : 0) * d;
     void *to = static_cast<typename Row<OUT>::value *>(Y) + t * d;
-    for (int64_t u = threadIdx.x & 63; u * U < d; u += 64) {
-        float f[U] = {};
+    if (d < U) {
+        if (lane < d) set_value<OUT>(to, lane, inside ? value_at<TABLE>(from, lane) * scale : 0.0f);
+        return;
+    }
+    for (int64_t u0 = lane; u0 * U < d; u0 += 64 * AT_ONCE) {
+        Raw<TABLE, U> rows[AT_ONCE];
         if (inside) {
-            load_unit<TABLE, U>(from, u, d, f);
 #pragma unroll
-            for (int k = 0; k < U; ++k) f[k] *= scale;
+            for (int j = 0; j < AT_ONCE; ++j) rows[j].template load<false>(from, columns<U>(u0 + 64 * j, d));
         }
-        store_unit<OUT, U>(to, u, d, f);
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            if ((u0 + 64 * j) * U >= d) break;
+            float f[U] = {};
+            if (inside) {
+                rows[j].add_to(f);
+#pragma unroll
+                for (int k = 0; k < U; ++k) f[k] *= scale;
+            }
+            Raw<OUT, U>::of(f).store(to, columns<U>(u0 + 64 * j, d));
+        }
     }
 }
 
@@ -89,9 +163,9 @@ __device__ __forceinline__ int block_scan(int x, int *scratch, int &total)
     if ((threadIdx.x & 63) == 63) scratch[threadIdx.x >> 6] = s;
     __syncthreads();
     // a wavefront's sum to each of 16 lanes
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sums = wave_scan(lane < SORT_THREADS / 64 ? scratch[lane] : 0);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, sums = wave_scan(lane < SORT_THREADS / 64 ? scratch[lane] : 0);
     total = __builtin_amdgcn_readlane(sums, 63);
-    return (wave > 0 ? __shfl(sums, wave - 1, 64) : 0) + s - x;
+    return (wave > 0 ? __builtin_amdgcn_readlane(sums, wave - 1) : 0) + s - x;
 }
 
 // A thread has tokens 2 thread and 2 thread + 1 of each of the SORT_LOADS runs of a tile: whole lines to a wavefront's load (eight tokens in a row to a
@@ -152,7 +226,8 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
     __shared__ int scratch[WAVES];
     __shared__ int counts[SORT_LOADS * WAVES];   // of the block's tokens, in the tile's order
     __shared__ uint32_t found[SORT_TILE];        // which of the block's ids << SORT_BITS | token of the tile, in the order of the tokens
-    const int block = blockIdx.x - (s.clear ? CLEARING : 0), lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mask = (1 << s.shift) - 1;
+    const int block = blockIdx.x - (s.clear ? CLEARING : 0), lane = threadIdx.x & 63, mask = (1 << s.shift) - 1;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (int k = threadIdx.x; k < s.own; k += SORT_THREADS) next[k] = 0;
     __syncthreads();
     int lower = 0;
@@ -189,7 +264,7 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
     if (block == mask && threadIdx.x == 0) s.begin[(int64_t)s.own << s.shift] = at + all;
     if (!all) return;
     const uint64_t in_front = (1ull << lane) - 1;
-    const int bits = 32 - __builtin_clz(s.own);   // at most SORT_BITS
+    const int bits = 32 - __builtin_clz(s.own);
     for (int64_t tile = 0; tile < s.tokens; tile += SORT_TILE) {
         // the tile's tokens of this block, side by side and in their order
         if (tile > 0) ahead.in_table(s, id);
@@ -214,7 +289,7 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
 #pragma unroll
         for (int j = 0; j < SORT_LOADS; ++j) {
             const int k = j * WAVES + wave;
-            const int before = __shfl(upto - c1 - (k & 1 ? 0 : c0), k / 2, 64);
+            const int before = __builtin_amdgcn_readlane(upto, k / 2) - __builtin_amdgcn_readlane(k & 1 ? c1 : c0 + c1, k / 2);
 #pragma unroll
             for (int e = 0; e < 2; ++e)
                 if (id[j][e] >= 0) found[before + place[j][e]] = (uint32_t)id[j][e] << SORT_BITS | (j * 2 * SORT_THREADS + threadIdx.x * 2 + e);
@@ -227,12 +302,10 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
             const bool live = i < total;
             const uint32_t f = live ? found[i] : 0, of = f >> SORT_BITS;
             uint64_t same = __ballot(live);
-#pragma unroll
-            for (int b = 0; b < SORT_BITS; ++b)
-                if (b < bits) {
-                    const uint64_t set = __ballot(of >> b & 1);
-                    same &= of >> b & 1 ? set : ~set;
-                }
+            for (int b = 0; b < bits; ++b) {
+                const uint64_t set = __ballot(of >> b & 1);
+                same &= of >> b & 1 ? set : ~set;
+            }
             const int nearer = __popcll(same & in_front);
             const bool last = nearer == __popcll(same) - 1;
             int to = 0;
@@ -272,55 +345,6 @@ template <sbn_dtype TABLE, int U> __device__ __forceinline__ void *row_of(const 
 // whether an id's tokens, from place `begin` of the order on, all go with the piece that they begin in: they end in it or in the next
 __device__ __forceinline__ bool of_one_piece(int begin, int end) { return end <= (begin / PIECE + 2) * PIECE; }
 
-// A thread's U columns of a row.  The last of a row whose length is no multiple of U begin where they still are all in the row, and of what the thread in
-// front has too it writes nothing: loads have no ends to look after.  (FEW: rows of less than U values, value by value.)
-template <int U, bool FEW> struct Columns {
-    int64_t first, own;   // the first that it has, and the first that it writes
-    int64_t d;
-    __device__ __forceinline__ Columns(int64_t unit, int64_t d) : first(FEW ? unit * U : min(unit * U, d - U)), own(unit * U), d(d) {}
-};
-
-// those of a row as they are in memory
-template <sbn_dtype DT, int U, bool FEW> struct Raw {
-    static constexpr int E = Row<DT>::E, N = U / E;
-    u32x4 v[N];
-    template <bool ONCE> __device__ __forceinline__ void load(const void *row, const Columns<U, FEW> &c)
-    {
-        const typename Row<DT>::value *p = static_cast<const typename Row<DT>::value *>(row) + c.first;
-#pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = FEW ? load_vec<DT, ONCE>(p, j, c.d - c.first) : Row<DT>::template load<ONCE>(p, j);
-    }
-    __device__ __forceinline__ void add_to(float (&sum)[U]) const
-    {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            float f[E];
-            Row<DT>::unpack(v[j], f);
-#pragma unroll
-            for (int k = 0; k < E; ++k) sum[j * E + k] += f[k];
-        }
-    }
-};
-template <sbn_dtype DT, int U, bool FEW> __device__ __forceinline__ void store_sum(void *row, const Columns<U, FEW> &c, const float (&sum)[U])
-{
-    constexpr int E = Row<DT>::E, N = U / E;
-    typename Row<DT>::value *p = static_cast<typename Row<DT>::value *>(row) + c.first;
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        float part[E];
-#pragma unroll
-        for (int k = 0; k < E; ++k) part[k] = sum[j * E + k];
-        const u32x4 v = Row<DT>::pack(part);
-        if (!FEW && c.first == c.own)
-            Row<DT>::store(p, j, v);
-        else {
-#pragma unroll
-            for (int k = 0; k < E; ++k)
-                if (c.first + j * E + k >= c.own && c.first + j * E + k < c.d) p[j * E + k] = Row<DT>::get(v, k);
-        }
-    }
-}
-
 // what a piece has to do; the same for a whole wavefront
 struct Piece {
     int token, id;          // of its places and those of the next piece, one to a lane
@@ -331,18 +355,17 @@ struct Piece {
 };
 
 // All rows are asked for before the first is added, those of places that are not the piece's too: nothing branches between the loads (in which case each
-// waited for the one before: 22 us in place of 13 for 2125 tokens of 2120 values).
-template <sbn_dtype TABLE, sbn_dtype OUT, bool ACCUMULATE, bool FEW> __device__ __forceinline__ void sum_piece(const SumArgs &s, const Piece &piece, int number, int64_t u)
+// waited for the one before: 22 us in place of 14 for 2125 tokens of 2120 values).
+template <sbn_dtype TABLE, sbn_dtype OUT, bool ACCUMULATE> __device__ __forceinline__ void sum_piece(const SumArgs &s, const Piece &piece, int number, int64_t u)
 {
     constexpr int U = unit_of(TABLE, OUT);
-    const Columns<U, FEW> c(u, s.d);
-    float sum[U] = {};
-    bool first = true;   // the present id is the piece's first
-#pragma unroll
-    for (int k0 = 0; k0 < 2 * PIECE; k0 += PIECE) {
-        if (k0 >= piece.end_k) break;
-        Raw<OUT, U, FEW> rows[PIECE];
-        Raw<TABLE, U, FEW> old[ACCUMULATE ? PIECE : 1];
+    const int64_t c = columns<U>(u, s.d);
+    float sum[U] = {}, sum_begun[U] = {};
+    bool first = piece.begun;   // the present id is the piece's first, and begins in an earlier one
+#pragma unroll 1
+    for (int k0 = 0; k0 < piece.end_k; k0 += PIECE) {
+        Raw<OUT, U> rows[PIECE];
+        Raw<TABLE, U> old[ACCUMULATE ? PIECE : 1];
 #pragma unroll
         for (int k = 0; k < PIECE; ++k) {
             rows[k].template load<true>(static_cast<const typename Row<OUT>::value *>(s.dY) + (int64_t)__builtin_amdgcn_readlane(piece.token, k0 + k) * s.d, c);
@@ -352,22 +375,55 @@ template <sbn_dtype TABLE, sbn_dtype OUT, bool ACCUMULATE, bool FEW> __device__ 
         for (int k = 0; k < PIECE; ++k)
             if (k0 + k >= piece.first_k && k0 + k < piece.end_k) {
                 rows[k].add_to(sum);
-                if (piece.last_of_id(k0 + k)) {
-                    if (first && piece.begun)
-                        store_sum<SBN_F32>(s.partials + (int64_t)number * 2 * s.d, c, sum);
-                    else if (k0 + k + 1 == piece.end_k && piece.goes_on)
-                        store_sum<SBN_F32>(s.partials + ((int64_t)number * 2 + 1) * s.d, c, sum);
-                    else {
+                if (!piece.last_of_id(k0 + k) || (k0 + k + 1 == piece.end_k && (first || piece.goes_on))) continue;
+                if (first) {
 #pragma unroll
-                        for (int i = 0; i < U; ++i) sum[i] *= s.scale;
-                        if (ACCUMULATE) old[k].add_to(sum);
-                        store_sum<TABLE>(row_of<TABLE, U>(s, piece.id_at(k0 + k)), c, sum);
-                    }
+                    for (int i = 0; i < U; ++i) sum_begun[i] = sum[i];
+                } else {
 #pragma unroll
-                    for (int i = 0; i < U; ++i) sum[i] = 0.0f;
-                    first = false;
+                    for (int i = 0; i < U; ++i) sum[i] *= s.scale;
+                    if (ACCUMULATE) old[k].add_to(sum);
+                    const Raw<TABLE, U> done = Raw<TABLE, U>::of(sum);
+                    void *row = row_of<TABLE, U>(s, piece.id_at(k0 + k));
+                    ACCUMULATE ? done.store_own(row, c, u * U) : done.store(row, c);   // (what is added to must not be written twice)
                 }
+                first = false;
+#pragma unroll
+                for (int i = 0; i < U; ++i) sum[i] = 0.0f;
             }
+    }
+    // partial sums: of the first id where it is not the last too, and of the last
+    float *share = s.partials + (int64_t)number * 2 * s.d;
+    if (piece.begun && !first) Raw<SBN_F32, U>::of(sum_begun).store(share, c);
+    if (first)
+        Raw<SBN_F32, U>::of(sum).store(share, c);
+    else if (piece.goes_on)
+        Raw<SBN_F32, U>::of(sum).store(share + s.d, c);
+}
+
+// the same for rows of less than U values, one to a lane
+template <sbn_dtype TABLE, sbn_dtype OUT> __device__ __forceinline__ void sum_piece_few(const SumArgs &s, const Piece &piece, int number, int lane)
+{
+    constexpr int U = unit_of(TABLE, OUT);
+    float *share = s.partials + (int64_t)number * 2 * s.d;
+    const int c = min(lane, (int)s.d - 1);
+    float sum = 0.0f;
+    bool first = piece.begun;
+#pragma unroll 1
+    for (int k = piece.first_k; k < piece.end_k; ++k) {
+        sum += value_at<OUT>(static_cast<const typename Row<OUT>::value *>(s.dY) + (int64_t)__builtin_amdgcn_readlane(piece.token, k) * s.d, c);
+        if (!piece.last_of_id(k)) continue;
+        void *row = row_of<TABLE, U>(s, piece.id_at(k));
+        if (lane < s.d) {
+            if (first)
+                share[c] = sum;
+            else if (k + 1 == piece.end_k && piece.goes_on)
+                share[s.d + c] = sum;
+            else
+                set_value<TABLE>(row, c, s.accumulate ? sum * s.scale + value_at<TABLE>(row, c) : sum * s.scale);
+        }
+        first = false;
+        sum = 0.0f;
     }
 }
 
@@ -405,11 +461,10 @@ template <sbn_dtype TABLE, sbn_dtype OUT, bool ACCUMULATE> __global__ void __lau
             piece.goes_on = false;
         }
     }
-    if (u * U >= s.d) return;
-    if (s.d >= U)
-        sum_piece<TABLE, OUT, ACCUMULATE, false>(s, piece, number, u);
-    else
-        sum_piece<TABLE, OUT, ACCUMULATE, true>(s, piece, number, u);
+    if (s.d < U)
+        sum_piece_few<TABLE, OUT>(s, piece, number, lane);
+    else if (u * U < s.d)
+        sum_piece<TABLE, OUT, ACCUMULATE>(s, piece, number, u);
 }
 
 template <sbn_dtype TABLE, int U, int WAVES, int AT_ONCE>

@@ -31,6 +31,8 @@ template <sbn_dtype DT> struct Row;
 template <> struct Row<SBN_BF16> {
     static constexpr int E = 8;   // values of a vector
     typedef uint16_t value;
+    static __device__ __forceinline__ float number(value x) { return __uint_as_float((uint32_t)x << 16); }
+    static __device__ __forceinline__ value rounded(float f) { return (value)bf16_pair(f, 0.0f); }
     static __device__ __forceinline__ value get(u32x4 v, int k) { return (value)(v[k / 2] >> (16 * (k % 2))); }
     static __device__ __forceinline__ void set(u32x4 &v, int k, value x) { v[k / 2] |= (uint32_t)x << (16 * (k % 2)); }   // of a value that is zero
     static __device__ __forceinline__ void clear(u32x4 &v, int k) { v[k / 2] &= k % 2 ? 0xffffu : 0xffff0000u; }
@@ -84,6 +86,8 @@ template <> struct Row<SBN_BF16> {
 template <> struct Row<SBN_F32> {
     static constexpr int E = 4;
     typedef float value;
+    static __device__ __forceinline__ float number(value x) { return x; }
+    static __device__ __forceinline__ value rounded(float f) { return f; }
     static __device__ __forceinline__ value get(u32x4 v, int k) { return __uint_as_float(v[k]); }
     static __device__ __forceinline__ void set(u32x4 &v, int k, value x) { v[k] = __float_as_uint(x); }
     static __device__ __forceinline__ void clear(u32x4 &v, int k) { v[k] = 0; }
