@@ -331,7 +331,7 @@ struct SumArgs {
     const int *begin, *order, *order_ids;
     float *partials;     // [pieces][2][d]: of the id that the piece begins with, of the one that it ends with
     int64_t vocab, d, items;   // items: pieces times tiles
-    int own, shift, accumulate, pieces, tiles;   // tiles: of 64 units of a row
+    int tokens, own, shift, accumulate, pieces, tiles;   // tiles: of 64 units of a row
     float scale;
     __device__ __forceinline__ const int *begin_of(int64_t id) const { return begin + (id & ((1 << shift) - 1)) * own + (id >> shift); }
     __device__ __forceinline__ int total() const { return begin[(int64_t)own << shift]; }   // tokens whose id is in the table
@@ -347,11 +347,17 @@ __device__ __forceinline__ bool of_one_piece(int begin, int end) { return end <=
 
 // what a piece has to do; the same for a whole wavefront
 struct Piece {
-    int token, id;          // of its places and those of the next piece, one to a lane
+    int token, id;          // of its places, and of those around it, one to a lane: place k at lane PIECE + 1 + k
     int first_k, end_k;     // its places
     bool begun, goes_on;    // the first id's tokens begin in an earlier piece; the last id's go on in a later one
-    __device__ __forceinline__ int id_at(int k) const { return __builtin_amdgcn_readlane(id, k); }
+    __device__ __forceinline__ int token_at(int k) const { return __builtin_amdgcn_readlane(token, PIECE + 1 + k); }
+    __device__ __forceinline__ int id_at(int k) const { return __builtin_amdgcn_readlane(id, PIECE + 1 + k); }
     __device__ __forceinline__ bool last_of_id(int k) const { return k + 1 == end_k || id_at(k) != id_at(k + 1); }
+    // how many places an id has that has place k, and no more than PIECE from there on
+    __device__ __forceinline__ int places_of(int which, int k) const
+    {
+        return __popcll(__ballot(id == which) >> (PIECE + 1 + k) & ((1ull << PIECE) - 1));
+    }
 };
 
 // All rows are asked for before the first is added, those of places that are not the piece's too: nothing branches between the loads (in which case each
@@ -368,8 +374,8 @@ template <sbn_dtype TABLE, sbn_dtype OUT, bool ACCUMULATE> __device__ __forceinl
         Raw<TABLE, U> old[ACCUMULATE ? PIECE : 1];
 #pragma unroll
         for (int k = 0; k < PIECE; ++k) {
-            rows[k].template load<true>(static_cast<const typename Row<OUT>::value *>(s.dY) + (int64_t)__builtin_amdgcn_readlane(piece.token, k0 + k) * s.d, c);
-            if (ACCUMULATE) old[k].template load<false>(row_of<TABLE, U>(s, piece.id_at(k0 + k)), c);
+            rows[k].template load<true>(static_cast<const typename Row<OUT>::value *>(s.dY) + (int64_t)piece.token_at(k0 + k) * s.d, c);
+            if (ACCUMULATE) old[k].template load<false>(row_of<TABLE, U>(s, max(piece.id_at(k0 + k), 0)), c);
         }
 #pragma unroll
         for (int k = 0; k < PIECE; ++k)
@@ -411,7 +417,7 @@ template <sbn_dtype TABLE, sbn_dtype OUT> __device__ __forceinline__ void sum_pi
     bool first = piece.begun;
 #pragma unroll 1
     for (int k = piece.first_k; k < piece.end_k; ++k) {
-        sum += value_at<OUT>(static_cast<const typename Row<OUT>::value *>(s.dY) + (int64_t)__builtin_amdgcn_readlane(piece.token, k) * s.d, c);
+        sum += value_at<OUT>(static_cast<const typename Row<OUT>::value *>(s.dY) + (int64_t)piece.token_at(k) * s.d, c);
         if (!piece.last_of_id(k)) continue;
         void *row = row_of<TABLE, U>(s, piece.id_at(k));
         if (lane < s.d) {
@@ -434,32 +440,30 @@ template <sbn_dtype TABLE, sbn_dtype OUT, bool ACCUMULATE> __global__ void __lau
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t item = (int64_t)blockIdx.x * 4 + wave;
     if (item >= s.items) return;
-    const int total = s.total();
-    const int number = (int)(item / s.tiles), p0 = number * PIECE, p1 = min(total, p0 + PIECE);
+    const int number = (int)(item / s.tiles), p0 = number * PIECE;
     const int64_t u = (item - (int64_t)number * s.tiles) * 64 + lane;
-    if (p0 >= p1) return;
+    // the places from the one in front of the piece before on, to the first behind the piece after: one to a lane
+    constexpr int HERE = PIECE + 1;
+    const int place = p0 + lane - HERE, at = min(max(place, 0), s.tokens - 1);
+    const int total = s.total(), token = s.order[at], id = s.order_ids[at];
+    if (p0 >= total) return;
+    const bool there = place >= 0 && place < total;   // (behind the last there is anything)
     Piece piece;
-    const int p = min(p0 + (lane & (2 * PIECE - 1)), total - 1);
-    piece.token = s.order[p];
-    piece.id = s.order_ids[p];
+    piece.token = there ? token : __builtin_amdgcn_readlane(token, HERE);
+    piece.id = there ? id : -1;
+    const int p1 = min(total, p0 + PIECE), front = piece.id_at(-1), behind = piece.id_at(PIECE);
     piece.first_k = 0;
     piece.end_k = p1 - p0;
     // an id that begins in a piece and ends in the next is the former's: no partial sums of ids of few tokens
-    piece.begun = p0 > 0 && s.order_ids[max(p0 - 1, 0)] == piece.id_at(0);
-    if (piece.begun) {
-        const int *b = s.begin_of(piece.id_at(0));
-        if (of_one_piece(b[0], b[1])) {
-            piece.first_k = b[1] - p0;
-            piece.begun = false;
-        }
+    piece.begun = piece.id_at(0) == front;
+    if (piece.begun && front != piece.id_at(-HERE) && front != behind) {
+        piece.first_k = piece.places_of(front, 0);
+        piece.begun = false;
     }
-    piece.goes_on = p1 < total && piece.id_at(PIECE - 1) == piece.id_at(PIECE);
-    if (piece.goes_on) {
-        const int *b = s.begin_of(piece.id_at(PIECE));
-        if (b[0] >= p0 && of_one_piece(b[0], b[1])) {
-            piece.end_k = b[1] - p0;
-            piece.goes_on = false;
-        }
+    piece.goes_on = behind >= 0 && piece.id_at(PIECE - 1) == behind;
+    if (piece.goes_on && behind != front && behind != piece.id_at(2 * PIECE)) {
+        piece.end_k = PIECE + piece.places_of(behind, PIECE);
+        piece.goes_on = false;
     }
     if (s.d < U)
         sum_piece_few<TABLE, OUT>(s, piece, number, lane);
@@ -616,6 +620,7 @@ sbn_status launch_embedding_backward(const void *dY, sbn_dtype out, const int64_
     s.partials = reinterpret_cast<float *>(ws + c.partials);
     s.vocab = vocab;
     s.d = d;
+    s.tokens = (int)tokens;
     s.own = o.own;
     s.shift = o.shift;
     s.accumulate = accumulate;
