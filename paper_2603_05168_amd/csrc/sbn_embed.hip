@@ -22,11 +22,10 @@ namespace sbn {
 namespace {
 
 constexpr int SORT_THREADS = 1024;
-constexpr int SORT_LOADS = 8;                            // of a thread, two ids each
-constexpr int SORT_TILE = SORT_THREADS * SORT_LOADS * 2;
+constexpr int SORT_LOADS = 8;                            // of a thread in a tile, two ids each; one where all tokens fit a tile of so few (less code to fetch)
 constexpr int SORT_BITS = 15;                            // of a number up to SORT_OWN, or of a token in a tile
 constexpr int SORT_OWN = 16384;                          // ids of the table that one sorting block has at most: their counts lie in LDS
-constexpr int PIECE = 16;                                // tokens of a piece
+constexpr int PIECE = 8;                                 // tokens of a piece: with 16 the code that a wavefront goes through once, and fetches, costs more than the rows (7 us against 11 at 1024 tokens)
 
 // the sorting blocks are 2^sort_shift() and share out the ids of the table
 inline int sort_shift(int64_t vocab)
@@ -170,13 +169,13 @@ __device__ __forceinline__ int block_scan(int x, int *scratch, int &total)
 
 // A thread has tokens 2 thread and 2 thread + 1 of each of the SORT_LOADS runs of a tile: whole lines to a wavefront's load (eight tokens in a row to a
 // thread are a line to each lane: 27 us for 16384 tokens in place of 13).  Ids outside the table, and those behind the last token, as -1.
-struct Ids {
+template <int LOADS> struct Ids {
     typedef int64_t i64x2 __attribute__((ext_vector_type(2), aligned(8)));
-    i64x2 v[SORT_LOADS];
+    i64x2 v[LOADS];
     __device__ __forceinline__ void load(const SortArgs &s, int64_t tile)
     {
 #pragma unroll
-        for (int j = 0; j < SORT_LOADS; ++j) {
+        for (int j = 0; j < LOADS; ++j) {
             const int64_t t = tile + (int64_t)j * 2 * SORT_THREADS + threadIdx.x * 2;
             v[j] = (i64x2){-1, -1};
             if (t + 1 < s.tokens)
@@ -185,10 +184,10 @@ struct Ids {
                 v[j][0] = s.ids[t];
         }
     }
-    __device__ __forceinline__ void in_table(const SortArgs &s, int (&id)[SORT_LOADS][2]) const
+    __device__ __forceinline__ void in_table(const SortArgs &s, int (&id)[LOADS][2]) const
     {
 #pragma unroll
-        for (int j = 0; j < SORT_LOADS; ++j)
+        for (int j = 0; j < LOADS; ++j)
 #pragma unroll
             for (int e = 0; e < 2; ++e) id[j][e] = v[j][e] >= 0 && v[j][e] < s.vocab ? (int)v[j][e] : -1;
     }
@@ -215,31 +214,31 @@ __device__ __forceinline__ void clear(const SortArgs &s)
 
 // The last 2^shift blocks sort; CLEARING in front of them (where there is something to clear) clear the table's gradient meanwhile, all of it: the rows that
 // have one are written again by the next kernel.
-__global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
+template <int LOADS> __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
 {
     if (s.clear && blockIdx.x < CLEARING) {
         clear(s);
         return;
     }
-    constexpr int WAVES = SORT_THREADS / 64;
+    constexpr int WAVES = SORT_THREADS / 64, TILE = SORT_THREADS * LOADS * 2;
     extern __shared__ int next[];                // [own]: counts, then where the next token of an id goes
     __shared__ int scratch[WAVES];
-    __shared__ int counts[SORT_LOADS * WAVES];   // of the block's tokens, in the tile's order
-    __shared__ uint32_t found[SORT_TILE];        // which of the block's ids << SORT_BITS | token of the tile, in the order of the tokens
+    __shared__ int counts[LOADS * WAVES];   // of the block's tokens, in the tile's order
+    __shared__ uint32_t found[TILE];        // which of the block's ids << SORT_BITS | token of the tile, in the order of the tokens
     const int block = blockIdx.x - (s.clear ? CLEARING : 0), lane = threadIdx.x & 63, mask = (1 << s.shift) - 1;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (int k = threadIdx.x; k < s.own; k += SORT_THREADS) next[k] = 0;
     __syncthreads();
     int lower = 0;
-    int id[SORT_LOADS][2];
-    Ids ahead;   // of the tile that comes next
-    const int64_t last_tile = (s.tokens - 1) / SORT_TILE * SORT_TILE;
+    int id[LOADS][2];
+    Ids<LOADS> ahead;   // of the tile that comes next
+    const int64_t last_tile = (s.tokens - 1) / TILE * TILE;
     ahead.load(s, last_tile);
-    for (int64_t tile = last_tile; tile >= 0; tile -= SORT_TILE) {   // the first tile last: its ids are at hand below
+    for (int64_t tile = last_tile; tile >= 0; tile -= TILE) {   // the first tile last: its ids are at hand below
         ahead.in_table(s, id);
-        if (tile > 0) ahead.load(s, tile - SORT_TILE);
+        if (tile > 0) ahead.load(s, tile - TILE);
 #pragma unroll
-        for (int j = 0; j < SORT_LOADS; ++j)
+        for (int j = 0; j < LOADS; ++j)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int b = id[j][e] & mask;
@@ -265,13 +264,13 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
     if (!all) return;
     const uint64_t in_front = (1ull << lane) - 1;
     const int bits = 32 - __builtin_clz(s.own);
-    for (int64_t tile = 0; tile < s.tokens; tile += SORT_TILE) {
+    for (int64_t tile = 0; tile < s.tokens; tile += TILE) {
         // the tile's tokens of this block, side by side and in their order
         if (tile > 0) ahead.in_table(s, id);
-        if (tile + SORT_TILE < s.tokens) ahead.load(s, tile + SORT_TILE);
-        int place[SORT_LOADS][2];
+        if (tile + TILE < s.tokens) ahead.load(s, tile + TILE);
+        int place[LOADS][2];
 #pragma unroll
-        for (int j = 0; j < SORT_LOADS; ++j) {
+        for (int j = 0; j < LOADS; ++j) {
             uint64_t has[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -283,11 +282,12 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_kernel(const SortArgs s)
             if (lane == 0) counts[j * WAVES + wave] = __popcll(has[0]) + __popcll(has[1]);
         }
         __syncthreads();
-        static_assert(SORT_LOADS * WAVES == 128, "two counts to a lane");
-        const int c0 = counts[2 * lane], c1 = counts[2 * lane + 1], upto = wave_scan(c0 + c1);
+        static_assert(LOADS * WAVES <= 128, "two counts to a lane");
+        const bool counted = 2 * lane < LOADS * WAVES;
+        const int c0 = counted ? counts[2 * lane] : 0, c1 = counted ? counts[2 * lane + 1] : 0, upto = wave_scan(c0 + c1);
         const int total = __builtin_amdgcn_readlane(upto, 63);
 #pragma unroll
-        for (int j = 0; j < SORT_LOADS; ++j) {
+        for (int j = 0; j < LOADS; ++j) {
             const int k = j * WAVES + wave;
             const int before = __builtin_amdgcn_readlane(upto, k / 2) - __builtin_amdgcn_readlane(k & 1 ? c1 : c0 + c1, k / 2);
 #pragma unroll
@@ -514,9 +514,9 @@ __device__ __forceinline__ void join(const SumArgs &s, int piece, int id, int en
     store_unit<TABLE, U>(row, u, s.d, sum);
 }
 
-// A block to JOIN_PIECES pieces and 64 units of the columns.  For every one of them in which an id begins that goes on behind the next (there are few: a
-// block each spent 15 us on looking, at 16384 tokens), sixteen wavefronts add the partial sums in turn, eight asked for at a time, and their sums are added
-// in order.
+// A block to JOIN_PIECES pieces and 64 units of the columns (fewer pieces: more blocks that only look; more: ids that wait for each other).  For every
+// piece in which an id begins that goes on behind the next, sixteen wavefronts add the partial sums in turn, eight asked for at a time, and their sums are
+// added in order.
 constexpr int JOIN_PIECES = 8;
 template <sbn_dtype TABLE> __global__ void __launch_bounds__(1024) join_kernel(const SumArgs s)
 {
@@ -560,6 +560,17 @@ Carved carve(int64_t tokens, int64_t d, int64_t vocab)
     return c;
 }
 
+template <int LOADS> sbn_status launch_sort(const SortArgs &s, hipStream_t stream)
+{
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(sort_kernel<LOADS>), hipFuncAttributeMaxDynamicSharedMemorySize, SORT_OWN * sizeof(int));
+    if (e != hipSuccess) {
+        set_hip_error(e, "hipFuncSetAttribute(sort_kernel)");
+        return SBN_EHIP;
+    }
+    hipLaunchKernelGGL(sort_kernel<LOADS>, dim3((unsigned)((1 << s.shift) + (s.clear ? CLEARING : 0))), dim3(SORT_THREADS), (size_t)s.own * sizeof(int), stream, s);
+    return check_launch("sort_kernel");
+}
+
 template <sbn_dtype TABLE, sbn_dtype OUT> sbn_status sum_as(SumArgs s, hipStream_t stream)
 {
     s.tiles = (int)ceil_div(s.d, 64 * unit_of(TABLE, OUT));
@@ -600,17 +611,12 @@ sbn_status launch_embedding_backward(const void *dY, sbn_dtype out, const int64_
     o.order_ids = reinterpret_cast<int *>(ws + c.order_ids);
     o.shift = sort_shift(vocab);
     o.own = (int)ceil_div(vocab, (int64_t)1 << o.shift);
-    const size_t lds = (size_t)o.own * sizeof(int);
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(sort_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, SORT_OWN * sizeof(int));
-    if (e != hipSuccess) {
-        set_hip_error(e, "hipFuncSetAttribute(sort_kernel)");
-        return SBN_EHIP;
-    }
     if (!accumulate) {
         o.clear = static_cast<char *>(dE);
         o.clear_bytes = vocab * d * (table == SBN_BF16 ? 2 : 4);
     }
-    hipLaunchKernelGGL(sort_kernel, dim3((unsigned)((1 << o.shift) + (o.clear ? CLEARING : 0))), dim3(SORT_THREADS), lds, stream, o);
+    const sbn_status st = tokens <= SORT_THREADS * 2 ? launch_sort<1>(o, stream) : launch_sort<SORT_LOADS>(o, stream);
+    if (st != SBN_OK) return st;
     SumArgs s{};
     s.dY = dY;
     s.dE = dE;

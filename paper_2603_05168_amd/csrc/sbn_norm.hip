@@ -506,7 +506,8 @@ template <sbn_dtype DT, bool LAYER> sbn_status forward_as(const NormArgs &n, hip
 template <sbn_dtype DT, bool LAYER> sbn_status backward_as(const NormArgs &n, float *dgain, float *dbias, hipStream_t stream)
 {
     return dealt<DT>(n, {n.dY, n.R, n.dX}, [&](auto L, auto VMAX, const Deal &deal, int waves, int64_t all) {
-        const int blocks = (int)std::min(all, staying_blocks(waves, BACKWARD_WAVES));
+        // where there are few rows, two blocks to a processor, or four rows to a team: shares cost as well (1531 rows of 1001: 13 + 8 us by 766 blocks, 12 + 4 by 512)
+        const int blocks = (int)std::min({all, staying_blocks(waves, BACKWARD_WAVES), std::max<int64_t>(2 * PROCESSORS, ceil_div(all, 4))});
         hipLaunchKernelGGL((norm_backward_kernel<DT, LAYER, decltype(L)::value, decltype(VMAX)::value>), dim3(blocks), dim3(64 * waves), 0, stream, n, deal);
         if (dgain || dbias) hipLaunchKernelGGL(norm_shares_kernel, dim3((unsigned)ceil_div(n.d, 32), 2), dim3(1024), 0, stream, n.partials, blocks, n.d, dgain, dbias);
         return check_launch("norm_backward_kernel");
