@@ -146,6 +146,9 @@ def _load_fastcall(path=os.path.join(_HERE, "_fastcall.so")):
     module.bind_head(*(address(f) for f in (
         _lib.sbn_head_cross_entropy, _lib.sbn_head_cross_entropy_backward, _lib.sbn_head_distill, _lib.sbn_head_distill_backward, _lib.sbn_mxfp4_quantize,
         _lib.sbn_mxfp4_dequantize, _lib.sbn_mxfp4_linear, _lib.sbn_head_workspace_bytes, _lib.sbn_mxfp4_bytes, _lib.sbn_mxfp4_workspace_bytes)))
+    module.bind_step(*(address(f) for f in (
+        _lib.sbn_norm, _lib.sbn_norm_backward, _lib.sbn_embedding, _lib.sbn_embedding_backward, _lib.sbn_grad_norm, _lib.sbn_adamw_step, _lib.sbn_adamw_state_values,
+        _lib.sbn_norm_workspace_bytes, _lib.sbn_embedding_workspace_bytes)))
     return module
 
 
@@ -155,13 +158,16 @@ _fast_grouped = _fastcall.grouped if _fastcall else lambda *args: None
 
 
 def _fast(name):
-    """A call of the output head in C++: its status, or None where the Python code beside it is to do it."""
+    """A call in C++: its status, or None where the Python code beside it is to do it."""
     return getattr(_fastcall, name) if _fastcall else lambda *args: None
 
 
 _fast_head_ce, _fast_head_ce_backward = _fast("head_ce"), _fast("head_ce_backward")
 _fast_head_distill, _fast_head_distill_backward = _fast("head_distill"), _fast("head_distill_backward")
 _fast_mxfp4_quantize, _fast_mxfp4_dequantize, _fast_mxfp4_linear = _fast("mxfp4_quantize"), _fast("mxfp4_dequantize"), _fast("mxfp4_linear")
+_fast_norm, _fast_norm_backward, _fast_embedding, _fast_embedding_backward = _fast("norm"), _fast("norm_backward"), _fast("embedding"), _fast("embedding_backward")
+_fast_grad_norm, _fast_adamw, _fast_state_values = _fast("grad_norm"), _fast("adamw"), _fast("state_values")
+_fast_norm_bytes, _fast_embedding_bytes = _fast("norm_bytes"), _fast("embedding_bytes")
 _fast_head_bytes, _fast_mxfp4_bytes, _fast_mxfp4_workspace_bytes = _fast("head_bytes"), _fast("mxfp4_bytes"), _fast("mxfp4_workspace_bytes")
 
 
@@ -700,6 +706,11 @@ def _row_type(name, t):
 
 def sbn_norm(X, Y, gain=None, bias=None, eps: float = 1e-6, layer: bool = False, residual=None, sum_out=None):
     """Y = the RMS norm (layer: layer norm) of the rows of X, or of X + residual, which is then given back in sum_out; gain, bias fp32."""
+    status = _fast_norm(X, Y, gain, bias, eps, layer, residual, sum_out)
+    if status is not None:
+        if status:
+            _check(status, "sbn_norm")
+        return
     dtype, shape = _row_type("X", X), X.shape
     for name, t in (("X", X), ("Y", Y), ("residual", residual), ("sum_out", sum_out)):
         _expect(name, t, shape, X.dtype)
@@ -710,11 +721,17 @@ def sbn_norm(X, Y, gain=None, bias=None, eps: float = 1e-6, layer: bool = False,
 
 
 def sbn_norm_workspace_bytes(tokens: int, d_in: int) -> int:
-    return _size_query(_lib.sbn_norm_workspace_bytes, "sbn_norm_workspace_bytes", tokens, d_in)
+    nbytes = _fast_norm_bytes(tokens, d_in)
+    return nbytes if nbytes is not None else _size_query(_lib.sbn_norm_workspace_bytes, "sbn_norm_workspace_bytes", tokens, d_in)
 
 
 def sbn_norm_backward(X, dY, workspace, dX=None, dgain=None, dbias=None, gain=None, eps: float = 1e-6, layer: bool = False, d_residual=None):
     """dX (+ d_residual), dgain and dbias (fp32) of sbn_norm for the gradient dY of its Y; X is what was normalised.  None: not wanted."""
+    status = _fast_norm_backward(X, dY, workspace, dX, dgain, dbias, gain, eps, layer, d_residual)
+    if status is not None:
+        if status:
+            _check(status, "sbn_norm_backward")
+        return
     dtype, shape = _row_type("X", X), X.shape
     for name, t in (("X", X), ("dY", dY), ("dX", dX), ("d_residual", d_residual)):
         _expect(name, t, shape, X.dtype)
@@ -737,17 +754,28 @@ def _embedding(table_name, table, rows_name, rows, ids):
 
 def sbn_embedding(E, ids, Y, scale: float = 1.0):
     """Y[t,:] = scale E[ids[t],:] (fp32 or bf16 each); zeros where the id (int64) is outside the table."""
+    status = _fast_embedding(E, ids, Y, scale)
+    if status is not None:
+        if status:
+            _check(status, "sbn_embedding")
+        return
     table, rows, vocab, d, tokens = _embedding("E", E, "Y", Y, ids)
     _here(E, ids, Y)
     _check(_lib.sbn_embedding(_ptr(E), table, vocab, d, _ptr(ids), tokens, scale, _ptr(Y), rows, _stream()), "sbn_embedding")
 
 
 def sbn_embedding_workspace_bytes(tokens: int, d_in: int, vocab: int) -> int:
-    return _size_query(_lib.sbn_embedding_workspace_bytes, "sbn_embedding_workspace_bytes", tokens, d_in, vocab)
+    nbytes = _fast_embedding_bytes(tokens, d_in, vocab)
+    return nbytes if nbytes is not None else _size_query(_lib.sbn_embedding_workspace_bytes, "sbn_embedding_workspace_bytes", tokens, d_in, vocab)
 
 
 def sbn_embedding_backward(dY, ids, dE, workspace, scale: float = 1.0, accumulate: bool = False):
     """dE[v,:] = scale sum of dY[t,:] over the tokens of id v: every row written, or (accumulate) the sums added to what dE holds."""
+    status = _fast_embedding_backward(dY, ids, dE, workspace, scale, accumulate)
+    if status is not None:
+        if status:
+            _check(status, "sbn_embedding_backward")
+        return
     table, rows, vocab, d, tokens = _embedding("dE", dE, "dY", dY, ids)
     _here(dY, ids, dE, workspace)
     _check(_lib.sbn_embedding_backward(_ptr(dY), rows, _ptr(ids), tokens, vocab, d, scale, int(accumulate), _ptr(dE), table, _ptr(workspace), _bytes_of(workspace),
@@ -759,12 +787,15 @@ def _tensors(name, tensors, *dtypes, like=None):
     tensors = list(tensors)
     if not tensors or (like is not None and len(tensors) != len(like)):
         raise ValueError(f"{name} must be a list of {len(like) if like is not None else 'one or more'} tensors")
+    dtype, device = tensors[0].dtype, -1
     for i, t in enumerate(tensors):
-        if t.dtype not in dtypes or t.dtype != tensors[0].dtype:
+        if t.dtype is not dtype or dtype not in dtypes:
             raise TypeError(f"{name} must all be {' or all '.join(str(d).removeprefix('torch.') for d in dtypes)}")
         if not t.is_contiguous() or (like is not None and t.numel() != like[i]):
             raise ValueError(f"{name}[{i}] must be contiguous" + (f" and have {like[i]} values, not {t.numel()}" if like is not None else ""))
-    _here(*tensors)
+        if t.get_device() != device or device < 0:   # look once where they lie, and that the others lie there too
+            _here(t)
+            device = t.get_device()
     return tensors
 
 
@@ -783,8 +814,13 @@ class GradNormGroup:
         self.grads, self.sizes, self.workspace = _ptr_array(self.keep), _i64_array([g.numel() for g in self.keep]), workspace
 
     def run(self, max_norm: float, out):
-        _expect("out", out, (2,), torch.float32)
         ws = self.workspace
+        status = _fast_grad_norm(self.count, self.grads, self.dtype, self.sizes, max_norm, out, ws)
+        if status is not None:
+            if status:
+                _check(status, "sbn_grad_norm")
+            return
+        _expect("out", out, (2,), torch.float32)
         _here(out, ws)
         _check(_lib.sbn_grad_norm(self.count, self.grads, self.dtype, self.sizes, max_norm, _ptr(out), _ptr(ws), _bytes_of(ws), _stream()), "sbn_grad_norm")
 
@@ -803,6 +839,11 @@ def sbn_adamw_state_bytes(n: int):
 
 def sbn_adamw_state_values(codes, scales, out, second: bool = False):
     """The values that moments in 8 bits stand for, exactly, into out (fp32 or bf16, any shape); second: of v, else of m."""
+    status = _fast_state_values(codes, scales, out, second)
+    if status is not None:
+        if status:
+            _check(status, "sbn_adamw_state_values")
+        return
     _expect("out", out, out.shape, torch.float32, torch.bfloat16)
     for name, t, nbytes in zip(("codes", "scales"), (codes, scales), sbn_adamw_state_bytes(out.numel())):
         _expect(name, t, (nbytes,), torch.uint8)
@@ -835,13 +876,22 @@ class AdamWGroup:
         self.decay = (ctypes.c_float * len(decay))(*decay)
         self.betas, self.eps = betas, eps
         self.keep = (params, grads, m, v, m_scales, v_scales)
+        self.device = params[0].get_device()
 
     def run(self, lr, step, clip=None, seed: int | None = None):
         """One step: lr (fp32 [1]), step (int64 [1], counted from 1) and clip (fp32 [1], or None) on the device; seed: round stochastically."""
+        if self.device != (_current_device or torch.cuda.current_device)():
+            raise ValueError(f"the group's tensors lie on cuda:{self.device}, which is not the current device")
+        status = _fast_adamw(self.count, self.params, self.types[0], self.grads, self.types[1], self.m, self.v, self.m_scales, self.v_scales, self.sizes, self.decay, lr,
+                             step, *self.betas, self.eps, clip, seed)
+        if status is not None:
+            if status:
+                _check(status, "sbn_adamw_step")
+            return
         _expect("lr", lr, (1,), torch.float32)
         _expect("step", step, (1,), torch.int64)
         _expect("clip", clip, (1,), torch.float32)
-        _here(lr, step, clip, self.keep[0][0])
+        _here(lr, step, clip)
         _check(_lib.sbn_adamw_step(self.count, self.params, self.types[0], self.grads, self.types[1], self.m, self.v, self.m_scales, self.v_scales, self.sizes,
                                    self.decay, _ptr(lr), _ptr(step), *self.betas, self.eps, _ptr(clip),
                                    None if seed is None else ctypes.byref(ctypes.c_uint64(seed)), _stream()), "sbn_adamw_step")

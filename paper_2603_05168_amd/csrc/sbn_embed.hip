@@ -562,11 +562,16 @@ Carved carve(int64_t tokens, int64_t d, int64_t vocab)
 
 template <int LOADS> sbn_status launch_sort(const SortArgs &s, hipStream_t stream)
 {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(sort_kernel<LOADS>), hipFuncAttributeMaxDynamicSharedMemorySize, SORT_OWN * sizeof(int));
+    static thread_local int raised_on = -1;   // the device on which this thread has raised the kernel's LDS
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e == hipSuccess && device != raised_on)
+        e = hipFuncSetAttribute(reinterpret_cast<const void *>(sort_kernel<LOADS>), hipFuncAttributeMaxDynamicSharedMemorySize, SORT_OWN * sizeof(int));
     if (e != hipSuccess) {
         set_hip_error(e, "hipFuncSetAttribute(sort_kernel)");
         return SBN_EHIP;
     }
+    raised_on = device;
     hipLaunchKernelGGL(sort_kernel<LOADS>, dim3((unsigned)((1 << s.shift) + (s.clear ? CLEARING : 0))), dim3(SORT_THREADS), (size_t)s.own * sizeof(int), stream, s);
     return check_launch("sort_kernel");
 }

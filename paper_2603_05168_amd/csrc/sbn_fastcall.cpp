@@ -102,11 +102,11 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n)
     }
 }
 
-// A ctypes array of at least `count` pointers or 64-bit integers, held while its address is in use; anything else is not held.
+// A ctypes array of at least `count` pointers, 64-bit integers or floats, held while its address is in use; anything else is not held.
 struct Array {
     Py_buffer view{};
     bool held;
-    enum Kind { POINTERS, INTEGERS };
+    enum Kind { POINTERS, INTEGERS, FLOATS };
     Array(PyObject *o, int count, Kind kind)
     {
         held = PyObject_GetBuffer(o, &view, PyBUF_ND | PyBUF_FORMAT) == 0;
@@ -116,7 +116,8 @@ struct Array {
         }
         // the formats of ctypes, which names the byte order; a ctypes pointer has no dimension
         const auto is = [&](const char *format) { return !strcmp(view.format, format); };
-        if (view.ndim != 1 || view.itemsize != 8 || view.shape[0] < count || !(kind == POINTERS ? is("<P") : is("<q") || is("<l"))) release();
+        if (view.ndim != 1 || view.itemsize != (kind == FLOATS ? 4 : 8) || view.shape[0] < count || !(kind == POINTERS ? is("<P") : kind == FLOATS ? is("<f") : is("<q") || is("<l")))
+            release();
     }
     ~Array() { release(); }
     Array(const Array &) = delete;
@@ -419,6 +420,210 @@ PyObject *bind_head(PyObject *, PyObject *args)
     Py_RETURN_NONE;
 }
 
+// ---- norms, embedding and optimizer: the checks of the Python code, on tensors of the current device -----------------------------------------
+using norm_fn = int (*)(const void *, const void *, int, int64_t, int64_t, const void *, const void *, float, int, void *, void *, void *);
+using norm_backward_fn = int (*)(const void *, const void *, const void *, int, int64_t, int64_t, const void *, float, int, void *, void *, void *, void *, size_t, void *);
+using embedding_fn = int (*)(const void *, int, int64_t, int64_t, const void *, int64_t, float, void *, int, void *);
+using embedding_backward_fn = int (*)(const void *, int, const void *, int64_t, int64_t, int64_t, float, int, void *, int, void *, size_t, void *);
+using grad_norm_fn = int (*)(int, const void *const *, int, const int64_t *, float, void *, void *, size_t, void *);
+using adamw_fn = int (*)(int, void *const *, int, const void *const *, int, void *const *, void *const *, uint8_t *const *, uint8_t *const *, const int64_t *, const float *,
+                         const void *, const void *, double, double, double, const void *, const uint64_t *, void *);
+using state_values_fn = int (*)(const void *, const void *, int64_t, int, void *, int, void *);
+using norm_bytes_fn = int (*)(int64_t, int64_t, size_t *);
+using embedding_bytes_fn = int (*)(int64_t, int64_t, int64_t, size_t *);
+struct StepCalls {
+    norm_fn norm;
+    norm_backward_fn norm_backward;
+    embedding_fn embedding;
+    embedding_backward_fn embedding_backward;
+    grad_norm_fn grad_norm;
+    adamw_fn adamw;
+    state_values_fn state_values;
+    norm_bytes_fn norm_bytes;
+    embedding_bytes_fn embedding_bytes;
+};
+StepCalls g_step{};
+
+// whether every tensor there is lies on the current device
+template <class... Tensors> bool here(const Tensors *...tensors)
+{
+    const auto device = c10::hip::current_device();
+    return ((!tensors || (tensors->is_cuda() && tensors->device().index() == device)) && ...);
+}
+bool flag(PyObject *o, bool &v)
+{
+    v = o == Py_True;
+    return v || o == Py_False;
+}
+bool number(PyObject *o, double &v)
+{
+    if (!PyFloat_CheckExact(o)) return false;
+    v = PyFloat_AS_DOUBLE(o);
+    return true;
+}
+const at::Tensor *rows_like(PyObject *o, const at::Tensor *X) { return matrix(o, X->scalar_type(), X->size(0), X->size(1)); }
+
+// (X, Y, gain, bias, eps, layer, residual, sum_out) -> status, or None
+PyObject *norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n == 8 && g_step.norm, [&]() -> PyObject * {
+        int type;
+        const at::Tensor *X = floats(a[0], type);
+        if (!X) Py_RETURN_NONE;
+        const at::Tensor *Y = rows_like(a[1], X), *gain = vector(a[2], at::kFloat, X->size(1)), *bias = vector(a[3], at::kFloat, X->size(1)), *R = rows_like(a[6], X),
+                         *S = rows_like(a[7], X);
+        double eps;
+        bool layer;
+        if (!Y || !maybe(a[2], gain) || !maybe(a[3], bias) || !maybe(a[6], R) || !maybe(a[7], S) || !number(a[4], eps) || !flag(a[5], layer) || !here(X, Y, gain, bias, R, S))
+            Py_RETURN_NONE;
+        void *const stream = current_stream();
+        return released([&] { return g_step.norm(data(X), data(R), type, X->size(0), X->size(1), data(gain), data(bias), (float)eps, layer, data(Y), data(S), stream); });
+    });
+}
+
+// (X, dY, workspace, dX, dgain, dbias, gain, eps, layer, d_residual)
+PyObject *norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n == 10 && g_step.norm_backward, [&]() -> PyObject * {
+        int type;
+        const at::Tensor *X = floats(a[0], type), *ws = plain(a[2]);
+        if (!X || !ws) Py_RETURN_NONE;
+        const int64_t d = X->size(1);
+        const at::Tensor *dY = rows_like(a[1], X), *dX = rows_like(a[3], X), *dgain = vector(a[4], at::kFloat, d), *dbias = vector(a[5], at::kFloat, d),
+                         *gain = vector(a[6], at::kFloat, d), *R = rows_like(a[9], X);
+        double eps;
+        bool layer;
+        if (!dY || !maybe(a[3], dX) || !maybe(a[4], dgain) || !maybe(a[5], dbias) || !maybe(a[6], gain) || !maybe(a[9], R) || !number(a[7], eps) || !flag(a[8], layer) ||
+            !here(X, dY, ws, dX, dgain, dbias, gain, R))
+            Py_RETURN_NONE;
+        void *const stream = current_stream();
+        return released([&] {
+            return g_step.norm_backward(data(X), data(dY), data(R), type, X->size(0), d, data(gain), (float)eps, layer, data(dX), data(dgain), data(dbias), data(ws), ws->nbytes(),
+                                        stream);
+        });
+    });
+}
+
+// (E, ids, Y, scale)
+PyObject *embedding(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n == 4 && g_step.embedding, [&]() -> PyObject * {
+        int table, rows;
+        const at::Tensor *E = floats(a[0], table), *Y = floats(a[2], rows), *ids = Y ? vector(a[1], at::kLong, Y->size(0)) : nullptr;
+        double scale;
+        if (!E || !Y || !ids || Y->size(1) != E->size(1) || !number(a[3], scale) || !here(E, Y, ids)) Py_RETURN_NONE;
+        void *const stream = current_stream();
+        return released([&] { return g_step.embedding(data(E), table, E->size(0), E->size(1), data(ids), Y->size(0), (float)scale, data(Y), rows, stream); });
+    });
+}
+
+// (dY, ids, dE, workspace, scale, accumulate)
+PyObject *embedding_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n == 6 && g_step.embedding_backward, [&]() -> PyObject * {
+        int table, rows;
+        const at::Tensor *dY = floats(a[0], rows), *dE = floats(a[2], table), *ids = dY ? vector(a[1], at::kLong, dY->size(0)) : nullptr, *ws = plain(a[3]);
+        double scale;
+        bool accumulate;
+        if (!dY || !dE || !ids || !ws || dY->size(1) != dE->size(1) || !number(a[4], scale) || !flag(a[5], accumulate) || !here(dY, dE, ids, ws)) Py_RETURN_NONE;
+        void *const stream = current_stream();
+        return released([&] {
+            return g_step.embedding_backward(data(dY), rows, data(ids), dY->size(0), dE->size(0), dE->size(1), (float)scale, accumulate, data(dE), table, data(ws), ws->nbytes(),
+                                             stream);
+        });
+    });
+}
+
+// (count, grads, dtype, sizes, max_norm, out, workspace): the arrays as they are at this call
+PyObject *grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n == 7 && g_step.grad_norm, [&]() -> PyObject * {
+        int count, type;
+        double most;
+        const at::Tensor *out = vector(a[5], at::kFloat, 2), *ws = plain(a[6]);
+        if (!small_int(a[0], count) || count < 0 || !small_int(a[2], type) || !number(a[4], most) || !out || !ws || !here(out, ws)) Py_RETURN_NONE;
+        const Array grads(a[1], count, Array::POINTERS), sizes(a[3], count, Array::INTEGERS);
+        if (!grads.held || !sizes.held) Py_RETURN_NONE;
+        void *const stream = current_stream();
+        return released(
+            [&] { return g_step.grad_norm(count, grads.as<const void *const *>(), type, sizes.as<const int64_t *>(), (float)most, data(out), data(ws), ws->nbytes(), stream); });
+    });
+}
+
+// (count, params, type, grads, type, m, v, m_scales, v_scales, sizes, weight_decay, lr, step, beta1, beta2, eps, clip, seed): as above
+PyObject *adamw(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n == 18 && g_step.adamw, [&]() -> PyObject * {
+        int count, pt, gt;
+        double b1, b2, eps;
+        const at::Tensor *lr = vector(a[11], at::kFloat, 1), *step = vector(a[12], at::kLong, 1), *clip = vector(a[16], at::kFloat, 1);
+        const bool bits8 = a[7] != Py_None;
+        if (!small_int(a[0], count) || count < 0 || !small_int(a[2], pt) || !small_int(a[4], gt) || !number(a[13], b1) || !number(a[14], b2) || !number(a[15], eps) || !lr || !step ||
+            !maybe(a[16], clip) || !here(lr, step, clip) || bits8 != (a[8] != Py_None) || !(a[17] == Py_None || PyLong_CheckExact(a[17])))
+            Py_RETURN_NONE;
+        uint64_t seed = 0;
+        if (a[17] != Py_None) {
+            seed = PyLong_AsUnsignedLongLongMask(a[17]);
+            if (PyErr_Occurred()) {
+                PyErr_Clear();
+                Py_RETURN_NONE;
+            }
+        }
+        const Array p(a[1], count, Array::POINTERS), g(a[3], count, Array::POINTERS), m(a[5], count, Array::POINTERS), v(a[6], count, Array::POINTERS),
+            sizes(a[9], count, Array::INTEGERS), decay(a[10], count, Array::FLOATS);
+        if (!p.held || !g.held || !m.held || !v.held || !sizes.held || !decay.held) Py_RETURN_NONE;
+        const Array ms(bits8 ? a[7] : a[5], count, Array::POINTERS), vs(bits8 ? a[8] : a[6], count, Array::POINTERS);
+        if (!ms.held || !vs.held) Py_RETURN_NONE;
+        void *const stream = current_stream();
+        return released([&] {
+            return g_step.adamw(count, p.as<void *const *>(), pt, g.as<const void *const *>(), gt, m.as<void *const *>(), v.as<void *const *>(),
+                                bits8 ? ms.as<uint8_t *const *>() : nullptr, bits8 ? vs.as<uint8_t *const *>() : nullptr, sizes.as<const int64_t *>(), decay.as<const float *>(),
+                                data(lr), data(step), b1, b2, eps, data(clip), a[17] == Py_None ? nullptr : &seed, stream);
+        });
+    });
+}
+
+// (codes, scales, out, second)
+PyObject *state_values(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n == 4 && g_step.state_values, [&]() -> PyObject * {
+        const at::Tensor *out = plain(a[2]);
+        bool second;
+        if (!out || !out->is_contiguous() || (out->scalar_type() != at::kFloat && out->scalar_type() != at::kBFloat16) || !flag(a[3], second)) Py_RETURN_NONE;
+        const int64_t values = out->numel(), blocks = (values + 31) / 32;
+        const at::Tensor *codes = vector(a[0], at::kByte, blocks * 32), *scales = vector(a[1], at::kByte, blocks);
+        if (!codes || !scales || !here(codes, scales, out)) Py_RETURN_NONE;
+        void *const stream = current_stream();
+        return released([&] { return g_step.state_values(data(codes), data(scales), values, second, data(out), out->scalar_type() == at::kBFloat16, stream); });
+    });
+}
+
+PyObject *norm_bytes(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    int64_t v[2];
+    size_t bytes;
+    if (n != 2 || !g_step.norm_bytes || !whole(a, 2, v) || g_step.norm_bytes(v[0], v[1], &bytes) != 0) Py_RETURN_NONE;
+    return PyLong_FromSize_t(bytes);
+}
+PyObject *embedding_bytes(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    int64_t v[3];
+    size_t bytes;
+    if (n != 3 || !g_step.embedding_bytes || !whole(a, 3, v) || g_step.embedding_bytes(v[0], v[1], v[2], &bytes) != 0) Py_RETURN_NONE;
+    return PyLong_FromSize_t(bytes);
+}
+
+// addresses of the C ABI's functions of this part, in the order of StepCalls
+PyObject *bind_step(PyObject *, PyObject *args)
+{
+    unsigned long long f[9];
+    if (!PyArg_ParseTuple(args, "KKKKKKKKK", f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7, f + 8)) return nullptr;
+    g_step = StepCalls{reinterpret_cast<norm_fn>(f[0]),  reinterpret_cast<norm_backward_fn>(f[1]), reinterpret_cast<embedding_fn>(f[2]), reinterpret_cast<embedding_backward_fn>(f[3]),
+                       reinterpret_cast<grad_norm_fn>(f[4]), reinterpret_cast<adamw_fn>(f[5]), reinterpret_cast<state_values_fn>(f[6]), reinterpret_cast<norm_bytes_fn>(f[7]),
+                       reinterpret_cast<embedding_bytes_fn>(f[8])};
+    Py_RETURN_NONE;
+}
+
 // (object, count): whether the grouped call takes the object as an array
 template <Array::Kind KIND> PyObject *takes_array(PyObject *, PyObject *args)
 {
@@ -462,6 +667,16 @@ PyMethodDef methods[] = {
     {"mxfp4_bytes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mxfp4_bytes)), METH_FASTCALL, nullptr},
     {"mxfp4_workspace_bytes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mxfp4_workspace_bytes)), METH_FASTCALL, nullptr},
     {"bind_head", bind_head, METH_VARARGS, nullptr},
+    {"norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm)), METH_FASTCALL, nullptr},
+    {"norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm_backward)), METH_FASTCALL, nullptr},
+    {"embedding", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(embedding)), METH_FASTCALL, nullptr},
+    {"embedding_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(embedding_backward)), METH_FASTCALL, nullptr},
+    {"grad_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(grad_norm)), METH_FASTCALL, nullptr},
+    {"adamw", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(adamw)), METH_FASTCALL, nullptr},
+    {"state_values", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(state_values)), METH_FASTCALL, nullptr},
+    {"norm_bytes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm_bytes)), METH_FASTCALL, nullptr},
+    {"embedding_bytes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(embedding_bytes)), METH_FASTCALL, nullptr},
+    {"bind_step", bind_step, METH_VARARGS, nullptr},
     {"array_of_pointers", takes_array<Array::POINTERS>, METH_VARARGS, nullptr},
     {"array_of_integers", takes_array<Array::INTEGERS>, METH_VARARGS, nullptr},
     {"call", call, METH_VARARGS, nullptr},
