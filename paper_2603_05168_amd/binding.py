@@ -167,7 +167,7 @@ _fast_head_distill, _fast_head_distill_backward = _fast("head_distill"), _fast("
 _fast_mxfp4_quantize, _fast_mxfp4_dequantize, _fast_mxfp4_linear = _fast("mxfp4_quantize"), _fast("mxfp4_dequantize"), _fast("mxfp4_linear")
 _fast_norm, _fast_norm_backward, _fast_embedding, _fast_embedding_backward = _fast("norm"), _fast("norm_backward"), _fast("embedding"), _fast("embedding_backward")
 _fast_grad_norm, _fast_adamw, _fast_state_values = _fast("grad_norm"), _fast("adamw"), _fast("state_values")
-_fast_norm_bytes, _fast_embedding_bytes = _fast("norm_bytes"), _fast("embedding_bytes")
+_fast_norm_bytes, _fast_embedding_bytes, _fast_gather = _fast("norm_bytes"), _fast("embedding_bytes"), _fast("gather")
 _fast_head_bytes, _fast_mxfp4_bytes, _fast_mxfp4_workspace_bytes = _fast("head_bytes"), _fast("mxfp4_bytes"), _fast("mxfp4_workspace_bytes")
 
 
@@ -782,21 +782,25 @@ def sbn_embedding_backward(dY, ids, dE, workspace, scale: float = 1.0, accumulat
                                        _stream()), "sbn_embedding_backward")
 
 
-def _tensors(name, tensors, *dtypes, like=None):
-    """A non-empty list of contiguous tensors of one of these types, as many values each as those of `like`."""
-    tensors = list(tensors)
-    if not tensors or (like is not None and len(tensors) != len(like)):
-        raise ValueError(f"{name} must be a list of {len(like) if like is not None else 'one or more'} tensors")
-    dtype, device = tensors[0].dtype, -1
-    for i, t in enumerate(tensors):
-        if t.dtype is not dtype or dtype not in dtypes:
-            raise TypeError(f"{name} must all be {' or all '.join(str(d).removeprefix('torch.') for d in dtypes)}")
-        if not t.is_contiguous() or (like is not None and t.numel() != like[i]):
-            raise ValueError(f"{name}[{i}] must be contiguous" + (f" and have {like[i]} values, not {t.numel()}" if like is not None else ""))
-        if t.get_device() != device or device < 0:   # look once where they lie, and that the others lie there too
-            _here(t)
-            device = t.get_device()
-    return tensors
+class _Tensors:
+    """A non-empty list of contiguous tensors of one of these types, as many values each as `like` says: with their addresses and sizes as ctypes arrays."""
+
+    def __init__(self, name, tensors, *dtypes, like=None):
+        self.list = tensors = list(tensors)
+        if not tensors or (like is not None and len(tensors) != len(like)):
+            raise ValueError(f"{name} must be a list of {len(like) if like is not None else 'one or more'} tensors")
+        self.pointers, self.sizes = (ctypes.c_void_p * len(tensors))(), (ctypes.c_int64 * len(tensors))()
+        code = _fast_gather(tensors, self.pointers, self.sizes)
+        if code is not None and (torch.float32, torch.bfloat16, torch.uint8)[code] in dtypes and (like is None or self.sizes[:] == like):
+            return
+        dtype = tensors[0].dtype
+        for i, t in enumerate(tensors):
+            if t.dtype is not dtype or dtype not in dtypes:
+                raise TypeError(f"{name} must all be {' or all '.join(str(d).removeprefix('torch.') for d in dtypes)}")
+            if not t.is_contiguous() or (like is not None and t.numel() != like[i]):
+                raise ValueError(f"{name}[{i}] must be contiguous" + (f" and have {like[i]} values, not {t.numel()}" if like is not None else ""))
+        _here(*tensors)
+        self.pointers, self.sizes = _ptr_array(tensors), _i64_array([t.numel() for t in tensors])
 
 
 def sbn_grad_norm_workspace_bytes(sizes) -> int:
@@ -808,10 +812,10 @@ class GradNormGroup:
     """Host-side argument arrays of sbn_grad_norm, marshalled once and reusable."""
 
     def __init__(self, grads, workspace):
-        self.keep = _tensors("grads", grads, torch.float32, torch.bfloat16)
+        grads = _Tensors("grads", grads, torch.float32, torch.bfloat16)
         _here(workspace)
-        self.count, self.dtype = len(self.keep), _dtype_code(self.keep[0])
-        self.grads, self.sizes, self.workspace = _ptr_array(self.keep), _i64_array([g.numel() for g in self.keep]), workspace
+        self.count, self.dtype, self.keep = len(grads.list), _dtype_code(grads.list[0]), grads.list
+        self.grads, self.sizes, self.workspace = grads.pointers, grads.sizes, workspace
 
     def run(self, max_norm: float, out):
         ws = self.workspace
@@ -856,27 +860,27 @@ class AdamWGroup:
     fp32, or (with m_scales and v_scales) the bytes of moments in 8 bits; weight_decay is a number, or one per weight."""
 
     def __init__(self, params, grads, m, v, m_scales=None, v_scales=None, weight_decay=0.0, betas=(0.9, 0.95), eps: float = 1e-8):
-        params = _tensors("params", params, torch.float32, torch.bfloat16)
-        sizes = [p.numel() for p in params]
-        grads = _tensors("grads", grads, torch.float32, torch.bfloat16, like=sizes)
+        params = _Tensors("params", params, torch.float32, torch.bfloat16)
+        sizes = params.sizes[:]
+        grads = _Tensors("grads", grads, torch.float32, torch.bfloat16, like=sizes)
         if (m_scales is None) != (v_scales is None):
             raise ValueError("m_scales and v_scales are both given or neither")
         bits8 = m_scales is not None
-        codes, scales = zip(*(sbn_adamw_state_bytes(n) for n in sizes)) if bits8 else (sizes, None)
-        m, v = (_tensors(name, t, torch.uint8 if bits8 else torch.float32, like=codes) for name, t in (("m", m), ("v", v)))
+        scales = [(n + 31) // 32 for n in sizes]
+        m, v = (_Tensors(name, t, torch.uint8 if bits8 else torch.float32, like=[32 * n for n in scales] if bits8 else sizes) for name, t in (("m", m), ("v", v)))
         if bits8:
-            m_scales, v_scales = (_tensors(name, t, torch.uint8, like=scales) for name, t in (("m_scales", m_scales), ("v_scales", v_scales)))
-        decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * len(params)
-        if len(decay) != len(params):
-            raise ValueError(f"weight_decay must be a number or {len(params)} of them")
-        self.count, self.sizes = len(params), _i64_array(sizes)
-        self.types = _dtype_code(params[0]), _dtype_code(grads[0])
-        self.params, self.grads, self.m, self.v = (_ptr_array(t) for t in (params, grads, m, v))
-        self.m_scales, self.v_scales = (_ptr_array(t) if bits8 else None for t in (m_scales, v_scales))
+            m_scales, v_scales = (_Tensors(name, t, torch.uint8, like=scales) for name, t in (("m_scales", m_scales), ("v_scales", v_scales)))
+        decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * len(sizes)
+        if len(decay) != len(sizes):
+            raise ValueError(f"weight_decay must be a number or {len(sizes)} of them")
+        self.count, self.sizes = len(sizes), params.sizes
+        self.types = _dtype_code(params.list[0]), _dtype_code(grads.list[0])
+        self.params, self.grads, self.m, self.v = params.pointers, grads.pointers, m.pointers, v.pointers
+        self.m_scales, self.v_scales = (t.pointers if bits8 else None for t in (m_scales, v_scales))
         self.decay = (ctypes.c_float * len(decay))(*decay)
         self.betas, self.eps = betas, eps
         self.keep = (params, grads, m, v, m_scales, v_scales)
-        self.device = params[0].get_device()
+        self.device = params.list[0].get_device()
 
     def run(self, lr, step, clip=None, seed: int | None = None):
         """One step: lr (fp32 [1]), step (int64 [1], counted from 1) and clip (fp32 [1], or None) on the device; seed: round stochastically."""

@@ -613,6 +613,28 @@ PyObject *embedding_bytes(PyObject *, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromSize_t(bytes);
 }
 
+// (tensors, pointers, integers) -> the type of contiguous tensors of the current device, whose addresses and numbers of values are then in the two ctypes
+// arrays: 0 fp32, 1 bf16, 2 uint8; None where they are not that
+PyObject *gather(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n == 3 && PyList_CheckExact(a[0]) && PyList_GET_SIZE(a[0]) <= INT32_MAX, [&]() -> PyObject * {
+        const int count = (int)PyList_GET_SIZE(a[0]);
+        const Array pointers(a[1], count, Array::POINTERS), sizes(a[2], count, Array::INTEGERS);
+        if (!pointers.held || !sizes.held || pointers.view.readonly || sizes.view.readonly) Py_RETURN_NONE;
+        at::ScalarType type = at::kFloat;
+        for (int i = 0; i < count; ++i) {
+            const at::Tensor *t = plain(PyList_GET_ITEM(a[0], i));
+            if (!t || !t->is_contiguous() || !here(t) || (i > 0 && t->scalar_type() != type)) Py_RETURN_NONE;
+            type = t->scalar_type();
+            pointers.as<void **>()[i] = t->data_ptr();
+            sizes.as<int64_t *>()[i] = t->numel();
+        }
+        const int code = type == at::kFloat ? 0 : type == at::kBFloat16 ? 1 : type == at::kByte ? 2 : -1;
+        if (code < 0) Py_RETURN_NONE;
+        return PyLong_FromLong(code);
+    });
+}
+
 // addresses of the C ABI's functions of this part, in the order of StepCalls
 PyObject *bind_step(PyObject *, PyObject *args)
 {
@@ -676,6 +698,7 @@ PyMethodDef methods[] = {
     {"state_values", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(state_values)), METH_FASTCALL, nullptr},
     {"norm_bytes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm_bytes)), METH_FASTCALL, nullptr},
     {"embedding_bytes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(embedding_bytes)), METH_FASTCALL, nullptr},
+    {"gather", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(gather)), METH_FASTCALL, nullptr},
     {"bind_step", bind_step, METH_VARARGS, nullptr},
     {"array_of_pointers", takes_array<Array::POINTERS>, METH_VARARGS, nullptr},
     {"array_of_integers", takes_array<Array::INTEGERS>, METH_VARARGS, nullptr},

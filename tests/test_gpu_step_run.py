@@ -233,7 +233,7 @@ def test_calls_on_streams_of_their_own():
 
 
 FAST = ["_fast_norm", "_fast_norm_backward", "_fast_embedding", "_fast_embedding_backward", "_fast_grad_norm", "_fast_adamw", "_fast_state_values", "_fast_norm_bytes",
-        "_fast_embedding_bytes"]
+        "_fast_embedding_bytes", "_fast_gather"]
 
 
 def test_marshalled_in_cpp_and_in_python_alike(monkeypatch):
@@ -256,6 +256,10 @@ def test_marshalled_in_cpp_and_in_python_alike(monkeypatch):
                      lambda: b.sbn_embedding(m.E, m.ids, Y, scale=float("nan")), lambda: b.sbn_embedding_backward(X, m.ids, m.dE, m.ws[:256]),
                      lambda: b.sbn_embedding_backward(X.cpu(), m.ids, m.dE, m.ws), lambda: m.norms.run(-1.0, m.norm), lambda: m.norms.run(1.0, m.norm[:1]),
                      lambda: m.optim.run(m.lr, m.step.int()), lambda: m.optim.run(m.lr.cpu(), m.step), lambda: b.sbn_adamw_state_values(m.codes[1][0], m.codes[3][0], values[:3]),
+                     lambda: b.AdamWGroup([m.g1, m.g2], [m.dg1], [m.g1] * 2, [m.g1] * 2), lambda: b.AdamWGroup([m.g1, m.E], [m.dg1] * 2, [m.g1] * 2, [m.g1] * 2),
+                     lambda: b.AdamWGroup([m.g1], [m.dg1[:-1]], [m.g1], [m.g1]), lambda: b.AdamWGroup([m.g1], [m.dg1], [m.g1], [m.g1.cpu()]),
+                     lambda: b.AdamWGroup([m.g1], [m.dg1], m.codes[0], m.codes[1], m.codes[2], m.codes[3]), lambda: b.GradNormGroup([m.E.t()], m.ws),
+                     lambda: b.AdamWGroup([m.g1, m.g2], [m.dg1, m.dg2], [m.g1, m.g1], [m.g1, m.g2]).run(m.lr, m.step),
                      lambda: b.sbn_norm_workspace_bytes(0, 1), lambda: b.sbn_embedding_workspace_bytes(1, 1, 1 << 30)):
             with pytest.raises(Exception) as e:
                 call()
