@@ -185,6 +185,9 @@ template <sbn_dtype DT> __device__ __forceinline__ void centre(float (&f)[Row<DT
     }
 }
 
+// 1 / sqrt(variance + eps); a variance that rounding took below 0 is 0, and one that is no number stays that
+__device__ __forceinline__ float factor_of(float variance, float eps) { return 1.0f / sqrtf((variance < 0.0f ? 0.0f : variance) + eps); }
+
 // the mean of a row by its first sum
 template <sbn_dtype DT, int L, int VMAX> __device__ __forceinline__ float first_mean(const u32x4 (&x)[VMAX], const NormArgs &n, const Deal &deal, float *scratch, int &turn)
 {
@@ -261,7 +264,7 @@ template <sbn_dtype DT, bool LAYER, int L, int VMAX> __global__ void __launch_bo
             }
             team_sums<L>(q, deal, fscratch, turn);
             rest = q[0] * n.inverse_d;
-            r = 1.0f / sqrtf(fmaxf(q[1] * n.inverse_d - rest * rest, 0.0f) + n.eps);
+            r = factor_of(q[1] * n.inverse_d - rest * rest, n.eps);
         } else {
             // in double, rounded once: the row's factor is then the one of the fused norm and quantizer, bit for bit
             double s[1] = {0.0};
@@ -358,7 +361,7 @@ __global__ void __launch_bounds__(most_threads(L)) __attribute__((amdgpu_waves_p
             of_a = q[3] * n.inverse_d;
             q[1] -= rest * q[3];
         }
-        const float r = 1.0f / sqrtf(fmaxf(q[0] * n.inverse_d - rest * rest, 0.0f) + n.eps);
+        const float r = factor_of(q[0] * n.inverse_d - rest * rest, n.eps);
         const float of_h = q[1] * r * n.inverse_d;
 #pragma unroll
         for (int i = 0; i < VMAX; ++i) {

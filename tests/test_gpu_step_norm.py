@@ -106,6 +106,23 @@ def test_one_bad_row_leaves_the_others():
                 assert torch.isnan(Y.cpu()[4]).all() and torch.equal(Y.cpu()[keep], want.cpu()[keep])
 
 
+@pytest.mark.parametrize("layer", [False, True])
+@pytest.mark.parametrize("d", [60, 2560, 8192])
+def test_a_nan_in_a_row_is_a_nan_in_every_gradient(d, layer):
+    """r of such a row is NaN, and so is its share of every dgain."""
+    s = sbn()
+    X, g = rows(9, d, F32, d)
+    dY = torch.randn(9, d, generator=g)
+    X[4, 7] = float("nan")
+    dX, dgain, dbias = torch.empty(9, d, device=DEV), torch.empty(d, device=DEV), torch.empty(d, device=DEV)
+    s.sbn_norm_backward(X.to(DEV), dY.to(DEV), s.new_workspace(s.sbn_norm_workspace_bytes(9, d)), dX=dX, dgain=dgain, dbias=dbias, layer=layer)
+    assert torch.isnan(dgain).all() and torch.isfinite(dbias).all()
+    assert torch.isnan(dX[4]).all() and torch.isfinite(dX[:4]).all() and torch.isfinite(dX[5:]).all()
+    Y = torch.empty(9, d, device=DEV)
+    s.sbn_norm(torch.full((9, d), 1e30).index_fill_(1, torch.arange(0, d, 2), -1e30).to(DEV), Y, layer=True)   # squares past the range: no number, or r = 0
+    assert (torch.isnan(Y) | (Y == 0)).all()
+
+
 def test_rms_is_the_fused_norm_of_the_quantizer():
     """Y of the RMS form is what sbn_rmsnorm_act_quant normalises to, bit for bit."""
     s = sbn()
