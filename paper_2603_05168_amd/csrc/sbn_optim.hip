@@ -95,7 +95,7 @@ template <int BELOW> __device__ __forceinline__ uint32_t shared_exponent(const f
     for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
     top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xb1, 0xf, 0xf, true));   // quad_perm: lane ^ 1, lane ^ 2
     top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4e, 0xf, 0xf, true));
-    return max((top + 0xfffffu) >> 23, (uint32_t)BELOW);   // one more where rounding may reach the next binade
+    return min(max((top + 0xfffffu) >> 23, (uint32_t)BELOW), 255u);   // one more where rounding may reach the next binade
 }
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -242,7 +242,10 @@ template <sbn_dtype PT, sbn_dtype GT, bool BITS8, bool STOCHASTIC> __global__ vo
         };
         if constexpr (PT == SBN_BF16 && STOCHASTIC) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) e.p[k] = __uint_as_float((__float_as_uint(e.p[k]) + noise(0, k)) & 0xffff0000u);
+            for (int k = 0; k < 8; ++k) {
+                const float rounded = __uint_as_float((__float_as_uint(e.p[k]) + noise(0, k)) & 0xffff0000u);
+                e.p[k] = e.p[k] == e.p[k] ? rounded : e.p[k];   // the pattern of a NaN could run over to that of a zero
+            }
         }
         if (whole)
             e.template store<true>(it, at);

@@ -233,6 +233,17 @@ def test_no_step_where_the_factor_is_not_finite(bits, bad):
         assert all(torch.equal(a, b) for a, b in zip(before[name], after[name])), name
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("seed", [None, 5])
+@pytest.mark.parametrize("pt", [F32, BF16])
+def test_gradients_of_every_nan_leave_none_but_nan(pt, seed, bits):
+    """A NaN of all ones (memory filled with 0xff) is one too: what is added to its pattern must not make a number of it."""
+    t = Tensors([100], pt=pt, bits=bits)
+    t.g[0].view(torch.int32)[:64] = torch.tensor([-1, 0x7fffffff]).int().repeat(32)
+    d = run(t, seed=seed)
+    assert torch.isnan(d["params"][0][:64]).all() and torch.isfinite(d["params"][0][64:]).all()
+
+
 def test_tensors_of_a_buffer():
     """Weights and moments that lie in one buffer at odd places; what lies between them is not touched."""
     s = sbn()
