@@ -187,7 +187,7 @@ def test_two_graphs_share_a_workspace():
     g = torch.Generator(device=DEV).manual_seed(3)
     T, d, V = 900, 72, 300
     ws = s.new_workspace(max(s.sbn_embedding_workspace_bytes(T, d, V), s.sbn_norm_workspace_bytes(T, d)))
-    calls = []
+    calls, held = [], []
     for k in range(2):
         ids, dY = torch.randint(0, V, (T,), generator=g, device=DEV), torch.randn(T, d, generator=g, device=DEV)
         dE, dX, dg = torch.empty(V, d, device=DEV), torch.empty(T, d, device=DEV), torch.empty(d, device=DEV)
@@ -201,6 +201,7 @@ def test_two_graphs_share_a_workspace():
         with torch.cuda.graph(graph):
             call()
         calls.append((graph, dE, dE.clone(), dg, dg.clone()))
+        held.append(call)   # and with it the buffers whose addresses the graph has
     for _ in range(3):
         for graph, dE, *_, dg, _ in calls:
             dE.fill_(float("nan"))
