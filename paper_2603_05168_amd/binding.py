@@ -129,7 +129,7 @@ _lib = _load()
 
 
 def _load_fastcall(path=os.path.join(_HERE, "_fastcall.so")):
-    """The marshalling of the two forward calls in C++ (csrc/sbn_fastcall.cpp), or None where it was not built, or was built for
+    """The marshalling of the forward calls, the head's and the training step's in C++ (csrc/sbn_fastcall.cpp), or None where it was not built, or was built for
     another torch: the Python code here does the same."""
     if not os.path.exists(path):
         return None
