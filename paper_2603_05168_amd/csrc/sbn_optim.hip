@@ -62,8 +62,7 @@ __device__ __forceinline__ float less_power(double log_beta, double t) { return 
 // of pi.  The rounding needs no more than bits that are even on average and not the same for neighbours, moments or steps.
 __device__ __forceinline__ uint32_t mix(uint32_t x, uint32_t key0, uint32_t key1)
 {
-    x ^= key0;
-    x = (x ^ (x >> 16)) * 0x9E3779B1u;
+    x = (x ^ (x >> 16) ^ (key0 ^ (key0 >> 16))) * 0x9E3779B1u;   // x ^ key0, shifted and added to itself
     x = (x ^ (x >> 15)) + key1;
     x *= 0x85A308D3u;
     return x ^ (x >> 16);
@@ -71,19 +70,60 @@ __device__ __forceinline__ uint32_t mix(uint32_t x, uint32_t key0, uint32_t key1
 
 constexpr int M_BELOW = 15, V_BELOW = 31;
 
-template <int BELOW> __device__ __forceinline__ float value_of(uint32_t code, uint32_t exponent)
+// A value's pattern lies in its upper 16 bits, so two values are decoded, and their codes made, at once.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+
+// the upper halves of two patterns, the first one's in the low half
+__device__ __forceinline__ uint32_t upper_halves(uint32_t first, uint32_t second) { return __builtin_amdgcn_perm(second, first, 0x07060302u); }
+
+// the values of four codes
+template <int BELOW> __device__ __forceinline__ void values_of(uint32_t codes, uint32_t exponent, float *f)
 {
-    const uint32_t low = BELOW == M_BELOW ? code & 127u : code;
-    const uint32_t a = (low + (exponent - BELOW) * 8u) << 20;
-    const float v = __uint_as_float(low ? a : 0u);
-    return BELOW == M_BELOW && (code & 128u) ? -v : v;
+    const u16x2 offset = (u16x2)(uint16_t)((exponent - BELOW) << 7);   // 8 codes to a binade, a code at bit 4
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const uint32_t x = __builtin_amdgcn_perm(0, codes, j ? 0x030c020cu : 0x010c000cu);   // two codes, in the upper byte of each half
+        const u16x2 low = __builtin_bit_cast(u16x2, (BELOW == M_BELOW ? x & 0x7f007f00u : x) >> 4);
+        // the offset where the code is not 0: less than any 2^16 - low
+        uint32_t both = __builtin_bit_cast(uint32_t, (u16x2)(low + __builtin_elementwise_min((u16x2)(-low), offset)));
+        if (BELOW == M_BELOW) both |= x & 0x80008000u;
+        f[2 * j] = __uint_as_float(both << 16);
+        f[2 * j + 1] = __uint_as_float(both & 0xffff0000u);
+    }
 }
-template <int BELOW> __device__ __forceinline__ uint32_t code_of(float x, uint32_t exponent, uint32_t half)
+
+// 0 for 0, else 1, in one instruction (the compiler makes two of a minimum)
+__device__ __forceinline__ uint32_t not_zero(uint32_t x)
 {
-    const uint32_t bits = __float_as_uint(x), a = bits & 0x7fffffffu;
-    const int t = (int)(a + half - ((exponent - BELOW) << 23));   // the code, less its offset, above bit 20
-    if (BELOW == V_BELOW) return a ? (uint32_t)max(t, 1 << 20) >> 20 : 0u;
-    return (uint32_t)max(t, 0) >> 20 | (bits >> 31 << 7);
+    uint32_t y;
+    asm("v_min_u32 %0, 1, %1" : "=v"(y) : "v"(x));
+    return y;
+}
+
+// the codes of four values; half: what rounding adds to their patterns
+template <int BELOW> __device__ __forceinline__ uint32_t codes_of(const float *x, uint32_t exponent, const uint32_t (&half)[4])
+{
+    const uint32_t offset = (exponent - BELOW) << 23;
+    i16x2 q[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        uint32_t t[2], sign[2], some[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t bits = __float_as_uint(x[2 * j + k]), a = BELOW == V_BELOW ? bits : bits & 0x7fffffffu;   // (v has no sign)
+            t[k] = a + (half[2 * j + k] - offset);   // the code, less its offset, above bit 20
+            sign[k] = bits;
+            some[k] = BELOW == V_BELOW ? not_zero(a) : 0;
+        }
+        const i16x2 code = __builtin_bit_cast(i16x2, upper_halves(t[0], t[1])) >> (int16_t)4;
+        if constexpr (BELOW == V_BELOW)
+            q[j] = __builtin_elementwise_max(code, __builtin_bit_cast(i16x2, some[0] | some[1] << 16));
+        else
+            q[j] = __builtin_bit_cast(i16x2, __builtin_bit_cast(uint32_t, __builtin_elementwise_max(code, (i16x2)(int16_t)0)) |
+                                                 ((upper_halves(sign[0], sign[1]) >> 8) & 0x00800080u));
+    }
+    return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, q[1]), __builtin_bit_cast(uint32_t, q[0]), 0x06040200u);
 }
 __device__ __forceinline__ uint32_t nearest(float x) { return 0x7ffffu + ((__float_as_uint(x) >> 20) & 1u); }
 
@@ -92,7 +132,7 @@ template <int BELOW> __device__ __forceinline__ uint32_t shared_exponent(const f
 {
     uint32_t top = 0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
+    for (int k = 0; k < 8; ++k) top = max(top, BELOW == V_BELOW ? __float_as_uint(x[k]) : __float_as_uint(x[k]) & 0x7fffffffu);
     top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xb1, 0xf, 0xf, true));   // quad_perm: lane ^ 1, lane ^ 2
     top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4e, 0xf, 0xf, true));
     return min(max((top + 0xfffffu) >> 23, (uint32_t)BELOW), 255u);   // one more where rounding may reach the next binade
@@ -125,9 +165,9 @@ template <sbn_dtype PT, sbn_dtype GT, bool BITS8> struct Eight {
                 vc = first_bytes(vc, (int64_t)it.n - at);
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                m[k] = value_of<M_BELOW>((mc[k / 4] >> (8 * (k & 3))) & 255u, me);
-                v[k] = value_of<V_BELOW>((vc[k / 4] >> (8 * (k & 3))) & 255u, ve);
+            for (int k = 0; k < 8; k += 4) {
+                values_of<M_BELOW>(mc[k / 4], me, m + k);
+                values_of<V_BELOW>(vc[k / 4], ve, v + k);
             }
         } else if (WHOLE) {
             load_whole<SBN_F32>(it.m, at, m);
@@ -137,10 +177,19 @@ template <sbn_dtype PT, sbn_dtype GT, bool BITS8> struct Eight {
             load_unit<SBN_F32, 8>(it.v, unit, it.n, v);
         }
     }
-    template <bool WHOLE> __device__ __forceinline__ void store(const AdamWItem &it, uint32_t at) const
+    // CUT: bf16 weights are the upper halves of what p holds
+    template <bool WHOLE, bool CUT> __device__ __forceinline__ void store(const AdamWItem &it, uint32_t at) const
     {
         const uint32_t unit = at / 8;
-        if (WHOLE)
+        if constexpr (CUT) {
+            u32x4 w;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = upper_halves(__float_as_uint(p[2 * k]), __float_as_uint(p[2 * k + 1]));
+            if (WHOLE)
+                Row<PT>::template store<true>(it.p, unit, w);
+            else
+                store_vec<PT>(it.p, unit, it.n, w);
+        } else if (WHOLE)
             store_whole<PT>(it.p, at, p);
         else
             store_unit<PT, 8>(it.p, unit, it.n, p);
@@ -197,7 +246,8 @@ template <sbn_dtype PT, sbn_dtype GT, bool BITS8, bool STOCHASTIC> __global__ vo
     const int which = tensor_of(a.first_block, blockIdx.x);
     const AdamWItem it = a.items[which];
     const int64_t step = *a.step;
-    const float lr = *a.lr, keep = (float)(1.0 - (double)lr * (double)it.decay);
+    const float given = *a.lr, lr = given == given ? given : __uint_as_float(0x7fc00000u);   // (a NaN whose pattern rounding does not run over)
+    const float keep = (float)(1.0 - (double)lr * (double)it.decay);
     const float rate = lr / less_power(a.log_beta1, (double)step);
     const float of_v = 1.0f / sqrtf(less_power(a.log_beta2, (double)step));
     const float b1 = a.beta1, c1 = a.less_beta1, b2 = a.beta2, c2 = a.less_beta2;
@@ -240,24 +290,32 @@ template <sbn_dtype PT, sbn_dtype GT, bool BITS8, bool STOCHASTIC> __global__ vo
             const uint32_t bits = mix(3 * (at / 2 + k / 2) + j, key0, key1);
             return k & 1 ? bits >> 16 : bits & 0xffffu;
         };
-        if constexpr (PT == SBN_BF16 && STOCHASTIC) {
+        constexpr bool CUT = PT == SBN_BF16 && STOCHASTIC;
+        if constexpr (CUT) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float rounded = __uint_as_float((__float_as_uint(e.p[k]) + noise(0, k)) & 0xffff0000u);
-                e.p[k] = e.p[k] == e.p[k] ? rounded : e.p[k];   // the pattern of a NaN could run over to that of a zero
+                const float rounded = __uint_as_float(__float_as_uint(e.p[k]) + noise(0, k));
+                // the pattern of a NaN in fp32 could run over to that of a zero; those that come of bf16 and 8 bits, or of infinities, do not reach so far
+                e.p[k] = (GT == SBN_BF16 && BITS8) || e.p[k] == e.p[k] ? rounded : e.p[k];
             }
         }
         if (whole)
-            e.template store<true>(it, at);
+            e.template store<true, CUT>(it, at);
         else
-            e.template store<false>(it, at);
+            e.template store<false, CUT>(it, at);
         if constexpr (BITS8) {
             const uint32_t me = shared_exponent<M_BELOW>(e.m), ve = shared_exponent<V_BELOW>(e.v);
-            u32x2 mc = {0, 0}, vc = {0, 0};
+            u32x2 mc, vc;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                mc[k / 4] |= code_of<M_BELOW>(e.m[k], me, STOCHASTIC ? noise(1, k) * 16 + 8 : nearest(e.m[k])) << (8 * (k & 3));
-                vc[k / 4] |= code_of<V_BELOW>(e.v[k], ve, STOCHASTIC ? noise(2, k) * 16 + 8 : nearest(e.v[k])) << (8 * (k & 3));
+            for (int k = 0; k < 8; k += 4) {
+                uint32_t m_half[4], v_half[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    m_half[i] = STOCHASTIC ? noise(1, k + i) * 16 + 8 : nearest(e.m[k + i]);
+                    v_half[i] = STOCHASTIC ? noise(2, k + i) * 16 + 8 : nearest(e.v[k + i]);
+                }
+                mc[k / 4] = codes_of<M_BELOW>(e.m + k, me, m_half);
+                vc[k / 4] = codes_of<V_BELOW>(e.v + k, ve, v_half);
             }
             static_cast<u32x2 *>(it.m)[at / 8] = mc;
             static_cast<u32x2 *>(it.v)[at / 8] = vc;
@@ -276,8 +334,8 @@ template <sbn_dtype OUT, int BELOW> __global__ void __launch_bounds__(256) state
     const uint2 c = codes[unit];
     const uint32_t e = scales[unit / 4];
     float f[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) f[k] = value_of<BELOW>(((k < 4 ? c.x : c.y) >> (8 * (k & 3))) & 255u, e);
+    values_of<BELOW>(c.x, e, f);
+    values_of<BELOW>(c.y, e, f + 4);
     store_unit<OUT, 8>(out, unit, n, f);
 }
 
