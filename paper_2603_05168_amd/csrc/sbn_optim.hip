@@ -22,8 +22,8 @@ namespace {
 constexpr int THREADS = 256;
 constexpr int STEP = THREADS * 8;             // values of a block at once
 // Values of a block at most.  Short pieces keep the stores of all blocks near each other in memory (79M weights with fp32 moments: 305 us, by 8 steps 336, by
-// 16 347); with moments in 8 bits what a block does once has to be spread (317M weights: 660 by one step, 612 by two, 592 by eight, 602 by 16).
-constexpr int64_t CHUNK_32BIT = STEP, CHUNK_8BIT = 8 * STEP;
+// 16 347); with moments in 8 bits what a block does once weighs too (317M weights: 608 by one step, 574 by two, 576 by four, 581 by eight, 607 by 16).
+constexpr int64_t CHUNK_32BIT = STEP, CHUNK_8BIT = 4 * STEP;
 
 struct AdamWItem {
     void *p;
@@ -54,6 +54,8 @@ __device__ __forceinline__ int tensor_of(const int *first_block, int block)
 {
     return __builtin_amdgcn_readfirstlane(__popcll(__ballot(first_block[threadIdx.x & 63] <= block)) - 1);
 }
+
+__device__ __forceinline__ float lane_value(float x, int lane) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), lane)); }
 
 // 1 - beta^t from the logarithm of beta: to a few steps of fp32, where powers in double took as long as a thousand values
 __device__ __forceinline__ float less_power(double log_beta, double t) { return -expm1f((float)(t * log_beta)); }
@@ -142,8 +144,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // What a thread has of a tensor: eight weights with their gradients and moments.  All of it is read and written once a step, and weights, gradients and fp32
 // moments go past the caches (nontemporal): what a step leaves in the memory side's cache has to leave it while the next kernel reads.  The norm of 79M
-// gradients and a step with fp32 moments took 30 + 347 us, with stores through the caches 52 + 330; with 8-bit moments for 317M weights 94 + 602, through
-// the caches 94 + 643.  (Codes go through the caches, eight bytes to a thread: past them 623.)
+// gradients and a step with fp32 moments took 30 + 347 us (30 + 305 now), with stores through the caches 52 + 330; with 8-bit moments for 317M weights 94 + 602
+// (94 + 576 now), through the caches 94 + 643.  (Codes go through the caches, eight bytes to a thread: past them 623, their loads alone 598 for 583.)
 template <sbn_dtype PT, sbn_dtype GT, bool BITS8> struct Eight {
     float p[8], g[8], m[8], v[8];
 
@@ -248,8 +250,10 @@ template <sbn_dtype PT, sbn_dtype GT, bool BITS8, bool STOCHASTIC> __global__ vo
     const int64_t step = *a.step;
     const float given = *a.lr, lr = given == given ? given : __uint_as_float(0x7fc00000u);   // (a NaN whose pattern rounding does not run over)
     const float keep = (float)(1.0 - (double)lr * (double)it.decay);
-    const float rate = lr / less_power(a.log_beta1, (double)step);
-    const float of_v = 1.0f / sqrtf(less_power(a.log_beta2, (double)step));
+    // both powers at once, in lanes of their own: rate = lr / (1 - beta1^t), of_v = 1 / sqrt(1 - beta2^t)
+    const bool second = threadIdx.x & 1;
+    const float power = less_power(second ? a.log_beta2 : a.log_beta1, (double)step), of = (second ? 1.0f : lr) / (second ? sqrtf(power) : power);
+    const float rate = lane_value(of, 0), of_v = lane_value(of, 1);
     const float b1 = a.beta1, c1 = a.less_beta1, b2 = a.beta2, c2 = a.less_beta2;
     // v_sqrt_f32 and v_rcp_f32 are good to a step of fp32 and take less than half the time of the correctly rounded root and quotient, but make zero of
     // numbers below 2^-126: with an eps that is nothing beside such a root they must not be met
