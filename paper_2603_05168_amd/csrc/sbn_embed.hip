@@ -331,7 +331,7 @@ struct SumArgs {
     const int *begin, *order, *order_ids;
     float *partials;     // [pieces][2][d]: of the id that the piece begins with, of the one that it ends with
     int64_t vocab, d, items;   // items: pieces times tiles
-    int tokens, own, shift, accumulate, pieces, tiles;   // tiles: of 64 units of a row
+    int tokens, own, shift, accumulate, pieces, tiles, join_pieces;   // tiles: of 64 units of a row
     float scale;
     __device__ __forceinline__ const int *begin_of(int64_t id) const { return begin + (id & ((1 << shift) - 1)) * own + (id >> shift); }
     __device__ __forceinline__ int total() const { return begin[(int64_t)own << shift]; }   // tokens whose id is in the table
@@ -514,20 +514,20 @@ __device__ __forceinline__ void join(const SumArgs &s, int piece, int id, int en
     store_unit<TABLE, U>(row, u, s.d, sum);
 }
 
-// A block to JOIN_PIECES pieces and 64 units of the columns (fewer pieces: more blocks that only look; more: ids that wait for each other).  For every
-// piece in which an id begins that goes on behind the next, sixteen wavefronts add the partial sums in turn, eight asked for at a time, and their sums are
-// added in order.
-constexpr int JOIN_PIECES = 8;
-template <sbn_dtype TABLE> __global__ void __launch_bounds__(1024) join_kernel(const SumArgs s)
+// A block to join_pieces pieces and 64 units of the columns.  For every piece in which an id begins that goes on behind the next, eight wavefronts add the
+// partial sums in turn, eight asked for at a time, and their sums are added in order (sixteen wavefronts: 9.5 us in place of 8.3 for 16384 tokens of 2560
+// values, four 9.4; one id of 65536 tokens: 187, 175 and 289).
+constexpr int JOIN_THREADS = 512;
+template <sbn_dtype TABLE> __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const SumArgs s)
 {
-    constexpr int U = Row<TABLE>::E, WAVES = 16, AT_ONCE = 8;
+    constexpr int U = Row<TABLE>::E, WAVES = JOIN_THREADS / 64, AT_ONCE = 8;
     __shared__ float sums[WAVES][64 * U];
     const int total = s.total();
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // a piece to a lane
-    const int64_t p0 = ((int64_t)blockIdx.x * JOIN_PIECES + lane) * PIECE, p1 = p0 + PIECE;
+    const int64_t p0 = ((int64_t)blockIdx.x * s.join_pieces + lane) * PIECE, p1 = p0 + PIECE;
     int id = -1, end = 0;
-    if (lane < JOIN_PIECES && p1 < total) {
+    if (lane < s.join_pieces && p1 < total) {
         id = s.order_ids[p1];
         const bool begins = s.order_ids[p1 - 1] == id && (p0 == 0 || s.order_ids[p0 - 1] != id);
         if (begins) end = s.begin_of(id)[1];
@@ -535,7 +535,7 @@ template <sbn_dtype TABLE> __global__ void __launch_bounds__(1024) join_kernel(c
     }
     for (uint64_t todo = __ballot(id >= 0); todo; todo &= todo - 1) {
         const int k = __builtin_ctzll(todo);
-        join<TABLE, U, WAVES, AT_ONCE>(s, blockIdx.x * JOIN_PIECES + k, __builtin_amdgcn_readlane(id, k), __builtin_amdgcn_readlane(end, k), lane, wave, sums);
+        join<TABLE, U, WAVES, AT_ONCE>(s, blockIdx.x * s.join_pieces + k, __builtin_amdgcn_readlane(id, k), __builtin_amdgcn_readlane(end, k), lane, wave, sums);
     }
 }
 
@@ -582,8 +582,13 @@ template <sbn_dtype TABLE, sbn_dtype OUT> sbn_status sum_as(SumArgs s, hipStream
     s.items = (int64_t)s.pieces * s.tiles;
     const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(s.items, 4)), dim3(256), 0, stream, s); };
     s.accumulate ? launch(sum_kernel<TABLE, OUT, true>) : launch(sum_kernel<TABLE, OUT, false>);
-    if (s.pieces > 2)   // (an id of two pieces is one piece's)
-        hipLaunchKernelGGL(join_kernel<TABLE>, dim3((unsigned)ceil_div(s.pieces - 2, JOIN_PIECES), (unsigned)ceil_div(s.d, 64 * Row<TABLE>::E)), dim3(1024), 0, stream, s);
+    if (s.pieces > 2) {   // (an id of two pieces is one piece's)
+        // up to four pieces to a block: most only look, but ids of one block wait for each other (16384 tokens of 2560 values by one 14.9 us, two 11.4, four 8.3,
+        // eight 8.2; 65536 of 50000 ids, the frequent ones more often: four 39, eight 45; 1531 tokens of 1001: one and two 4.8, four 6.2)
+        const int64_t tiles = ceil_div(s.d, 64 * Row<TABLE>::E);
+        s.join_pieces = (int)std::min<int64_t>(4, ceil_div((s.pieces - 2) * tiles, 1024));
+        hipLaunchKernelGGL(join_kernel<TABLE>, dim3((unsigned)ceil_div(s.pieces - 2, s.join_pieces), (unsigned)tiles), dim3(JOIN_THREADS), 0, stream, s);
+    }
     return check_launch("sum_kernel");
 }
 
