@@ -43,8 +43,10 @@ def test_a_left_out_token_is_zeros_whatever_the_table_holds():
     assert (Y[0] == 0).all() and (Y[1] == 2).all() and (Y[2] == 0).all()
 
 
-def check_gradient(dY, ids, V, table, scale=1.3, old=None):
+def check_gradient(dY, ids, V, table, scale=1.3, old=None, more=0):
+    """more: tokens besides that have no share; many tokens go another way than few."""
     s = sbn()
+    dY, ids = torch.cat([dY, dY.new_full((more, dY.shape[1]), float("nan"))]), torch.cat([ids, torch.full((more,), -1)])
     T, d = dY.shape
     dE = torch.full((V, d), float("nan"), dtype=table, device=DEV) if old is None else old.to(DEV)
     ws = s.new_workspace(s.sbn_embedding_workspace_bytes(T, d, V)).fill_(0xff)
@@ -72,20 +74,23 @@ def check_gradient(dY, ids, V, table, scale=1.3, old=None):
 
 
 @pytest.mark.parametrize("table,out", TYPES)
-@pytest.mark.parametrize("T,V,d", [(1, 1, 1), (2, 3, 5), (16, 4, 64), (17, 300, 40), (100, 50, 1001), (500, 2000, 264), (9000, 700, 72), (20000, 30, 33), (300, 70000, 8)])
+@pytest.mark.parametrize("T,V,d", [(1, 1, 1), (2, 3, 5), (16, 4, 64), (17, 300, 40), (100, 50, 1001), (500, 2000, 264), (9000, 700, 72), (20000, 30, 33), (300, 70000, 8),
+                                   (1536, 300, 1001), (1537, 300, 1001), (2100, 3000, 264), (1500, 9, 2563), (1000, 40, 12), (64, 2, 8), (400, 390, 9000)])
 def test_gradient(T, V, d, table, out):
     g = torch.Generator().manual_seed(T + V)
     dY, ids = torch.randn(T, d, generator=g).to(out), some_ids(T, V, g)
-    check_gradient(dY, ids, V, table)
-    check_gradient(dY, ids, V, table, old=torch.randn(V, d, generator=g).to(table))
+    for more in (0, 1600) if T <= 1536 else (0,):
+        check_gradient(dY, ids, V, table, more=more)
+        check_gradient(dY, ids, V, table, old=torch.randn(V, d, generator=g).to(table), more=more)
 
 
-@pytest.mark.parametrize("T", [1, 15, 16, 17, 31, 32, 33, 48, 1000, 8191, 8193, 16384, 16385, 40000])
+@pytest.mark.parametrize("T", [1, 15, 16, 17, 31, 32, 33, 48, 1000, 1535, 1536, 1537, 8191, 8193, 16384, 16385, 40000])
 def test_one_id_for_all_and_none(T):
     g = torch.Generator().manual_seed(T)
     dY = torch.randn(T, 24, generator=g)
-    check_gradient(dY, torch.full((T,), 5), 9, F32)
-    check_gradient(dY, torch.full((T,), -1), 9, F32)
+    for more in (0, 1600):
+        check_gradient(dY, torch.full((T,), 5), 9, F32, more=more)
+        check_gradient(dY, torch.full((T,), -1), 9, F32, more=more)
     check_gradient(dY, torch.full((T,), 9), 9, F32, old=torch.randn(9, 24, generator=g))
 
 
@@ -97,7 +102,9 @@ def test_runs_that_end_where_pieces_do():
         # ids that lie in one block's share of the vocabulary are neighbours in the order
         ids = torch.cat([torch.full((n,), 256 * k) for k, n in enumerate(lengths)])
         ids = ids[torch.randperm(len(ids), generator=g)]
-        check_gradient(torch.randn(len(ids), 40, generator=g), ids, 256 * len(lengths), F32)
+        dY = torch.randn(len(ids), 40, generator=g)
+        for more in (0, 1600):
+            check_gradient(dY, ids, 256 * len(lengths), F32, more=more)
 
 
 def test_left_out_tokens_may_hold_anything():
