@@ -509,7 +509,7 @@ sbn_status sbn_embedding_backward(const void *dY, sbn_dtype y_dtype, const int64
  *   seed        HOST, NULL: bf16 weights and 8-bit moments are rounded to nearest, ties to even; else they are rounded stochastically, by 16 bits
  *               for each from a hash of *seed, *step, the tensor's place in the call and the value's place in the tensor.  An update below half a step of
  *               bf16, or a v that falls by less than half a step of its code, is lost by the one and kept on average by the other.
- *   workspace   device, 256-byte aligned, >= sbn_grad_norm_workspace_bytes(count, sizes)
+ *   workspace   device, 256-byte aligned, >= sbn_grad_norm_workspace_bytes(count, sizes), which never falls as tensors or values are added
  * Moments in 8 bits.  32 consecutive values of a tensor share a byte e, the exponent field (as of fp32) of their largest magnitude (one more where its
  * mantissa is above 1.875), at least 15 (m) or 31 (v).  With c the low seven bits of m's code, or v's code, a value is 0 for c = 0, else the fp32 number
  * of pattern (c + 8 (e - 15 or 31)) << 20: three bits of mantissa, 15 or 31 binades; m's top bit is the sign.  Values below are 0 for m, and the
