@@ -462,7 +462,7 @@ sbn_status sbn_mxfp4_linear(const void *X, int64_t tokens, int64_t d_in, int64_t
  *   residual, sum_out     both given or both NULL; sum_out may be X or residual, Y may be X or residual unless that is sum_out
  *   gain, bias            device, fp32 [d_in]; NULL: 1 and 0
  *   dX, dgain, dbias      device, overwritten; NULL: not wanted (not all three); dX may be dY or d_residual; d_residual NULL: none.  dgain, dbias fp32 [d_in]
- *   workspace             device, 256-byte aligned, >= sbn_norm_workspace_bytes(tokens, d_in)
+ *   workspace             device, 256-byte aligned, >= sbn_norm_workspace_bytes(tokens, d_in), which never falls as either grows
  * Pointers are aligned to their values; d_in is any number up to 16384.  Arithmetic in fp32 (r of the RMS form forward in double, rounded once: where
  * gain is given and bias is not, Y in bf16 is xn_out of sbn_rmsnorm_act_quant), results rounded once.  No atomics: a call repeated gives the same bits.
  * Where d_in is no multiple of 8, a row's sums go by where it begins in memory, so the last bits of equal rows may differ.
@@ -483,7 +483,7 @@ sbn_status sbn_norm_backward(const void *X, const void *dY, const void *d_residu
  *   ids        device, int64 [tokens]; a token whose id is outside [0, vocab) gets zeros and has no share in the gradient
  *   accumulate 0: every row of dE is written, those that no token names with zeros; else the sums are added to what dE holds (a table that is the
  *              head's matrix as well: after sbn_head_*_backward), and rows that no token names are not touched
- *   workspace  device, 256-byte aligned, >= sbn_embedding_workspace_bytes(tokens, d_in, vocab)
+ *   workspace  device, 256-byte aligned, >= sbn_embedding_workspace_bytes(tokens, d_in, vocab), which never falls as any of them grows
  * Pointers are aligned to their values; d_in is any number.  Sums are fp32, multiplied by scale, then rounded once (accumulate: after the addition).
  * The tokens of an id are added in their own order, in runs whose sums are added in turn; no atomics on values: a call repeated gives the same bits.
  * Errors: SBN_EINVAL, SBN_EALIGN, SBN_ESIZE, SBN_EUNSUPPORTED (tokens or vocab > 2^24, d_in > 2^16, tokens or vocab times d_in > 2^34), SBN_EHIP.

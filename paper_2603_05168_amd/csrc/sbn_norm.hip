@@ -465,10 +465,13 @@ int block_waves(int64_t d, int values)
     return vecs <= 64 ? 4 : (int)std::min<int64_t>(16, ceil_div(vecs, 64 * vectors_of_thread(vecs, values)));
 }
 
-// blocks of the backward at most, in either type: each leaves its shares
-int64_t most_shares(int64_t d)
+// The most that a call's shares of one vector hold, in values of either type: staying_blocks() leaves BACKWARD_WAVES wavefronts to a processor (or one block of as
+// many), 64 lanes of 8 values each, or of 16 in rows whose vectors reach past 2560 values.  No more blocks than wavefronts, nor than rows.  Never falls as rows or
+// values are added, as blocks times values do (1024 blocks of 512 values, 512 of 1001, 768 of 2560): what was made for a program's longest rows serves shorter ones.
+int64_t share_values(int64_t tokens, int64_t d)
 {
-    return std::max(staying_blocks(block_waves(d, Row<SBN_BF16>::E), BACKWARD_WAVES), staying_blocks(block_waves(d, Row<SBN_F32>::E), BACKWARD_WAVES));
+    const int64_t waves = PROCESSORS * BACKWARD_WAVES, of_waves = waves * 64 * (d + Row<SBN_BF16>::E - 1 > 2560 ? 16 : 8);
+    return std::min(std::min(waves, tokens) * d, of_waves);
 }
 
 // Calls f with the lanes of a team that is part of a wavefront (64: whole wavefronts), the vectors of a thread, the deal, the wavefronts of a block and
@@ -526,7 +529,7 @@ template <sbn_dtype DT, bool LAYER> sbn_status backward_as(NormArgs &n, float *d
 
 }  // namespace
 
-size_t norm_workspace_bytes(int64_t, int64_t d) { return (size_t)2 * most_shares(d) * d * sizeof(float); }
+size_t norm_workspace_bytes(int64_t tokens, int64_t d) { return (size_t)2 * share_values(tokens, d) * sizeof(float); }
 
 sbn_status launch_norm(const void *X, const void *residual, sbn_dtype dtype, int64_t tokens, int64_t d, const float *gain, const float *bias, float eps, bool layer,
                        void *Y, void *sum_out, hipStream_t stream)

@@ -24,3 +24,28 @@ def test_grad_norm_takes_no_less_for_more():
     for _ in range(50):
         part = rng.sample(sizes, rng.randint(1, len(sizes) - 1))
         assert need(part) <= need(sizes), part
+
+
+def test_norm_takes_no_less_for_more():
+    """Longer rows and more of them never need less: rows of 512 values go by more blocks than those of 2560, whose shares are longer."""
+    need = sbn.sbn_norm_workspace_bytes
+    for tokens in (1, 2, 7, 600, 3000, 1 << 20):
+        sizes = [need(tokens, d) for d in range(1, 16385)]
+        assert sizes == sorted(sizes), tokens
+    for d in (1, 64, 512, 1001, 2560, 8192, 16384):
+        sizes = [need(tokens, d) for tokens in list(range(1, 5000)) + [1 << k for k in range(13, 25)]]
+        assert sizes == sorted(sizes), d
+    assert need(1, 1024) <= 3 * 1024 * 4   # one row's shares at most
+
+
+def test_embedding_takes_no_less_for_more():
+    need = sbn.sbn_embedding_workspace_bytes
+    rng = random.Random(2)
+    for _ in range(20000):
+        size = [int(2 ** rng.uniform(0, 20)), int(2 ** rng.uniform(0, 9)), int(2 ** rng.uniform(0, 23))]   # tokens, d_in, vocab
+        more = list(size)
+        more[rng.randrange(3)] += rng.choice([1, 1, 255, 256, 4096])
+        if more[1] * max(more[0], more[2]) <= 1 << 34:   # the most that a call takes
+            assert need(*size) <= need(*more), (size, more)
+    for vocab in (1 << 14, 1 << 22, 1 << 23):   # where the ids are dealt to more blocks
+        assert need(100, 64, vocab) <= need(100, 64, vocab + 1)
