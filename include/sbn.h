@@ -465,7 +465,8 @@ sbn_status sbn_mxfp4_linear(const void *X, int64_t tokens, int64_t d_in, int64_t
  *   workspace             device, 256-byte aligned, >= sbn_norm_workspace_bytes(tokens, d_in), which never falls as either grows
  * Pointers are aligned to their values; d_in is any number up to 16384.  Arithmetic in fp32 (r of the RMS form forward in double, rounded once: where
  * gain is given and bias is not, Y in bf16 is xn_out of sbn_rmsnorm_act_quant), results rounded once.  No atomics: a call repeated gives the same bits.
- * Where d_in is no multiple of 8, a row's sums go by where it begins in memory, so the last bits of equal rows may differ.
+ * Where d_in is no multiple of 8, a row's sums go by where it begins in a vector of 16 bytes (of the backward's fewest rows: where the first one does), so the
+ * last bits of equal rows may differ.
  * A row with a NaN is NaN in Y and dX, and one with an infinity too, but for Y of the RMS form: there h is 0 beside it (r is 0).  Other rows are not
  * touched by it; dgain and dbias are sums over all rows.  Squares are fp32 numbers (forward RMS form: double): rows of values beyond 1e18 are out of range.
  * Errors: SBN_EINVAL, SBN_EALIGN, SBN_ESIZE, SBN_EUNSUPPORTED (d_in > 16384, tokens > 2^24), SBN_EHIP.

@@ -36,8 +36,9 @@ constexpr int MOST_SUMS = 4;   // of a team at once
 //
 // Rows whose length is no whole number of vectors begin anywhere in a vector of memory.  Where all rows of a call do so alike, a thread's vectors are
 // those of memory, and a row's first vector begins `shift` values in front of it: accesses off the 16-byte grid took up to twice as long (rows of 500
-// bf16 values: 95 us against 40 for 512).  The rows of a team are a multiple of 8 apart, so that all of them have the same shift and its threads meet the
-// same columns in each.
+// bf16 values: 95 us against 40 for 512).  A thread meets the same columns in every row of its team, so a team has one shift, that of its first row.  Launches
+// in which a team has several rows have a multiple of 8 blocks: its rows lie a multiple of 8 values apart, and all have that shift.  (But for one block with two
+// rows to a team, too few to matter: the second goes by the first one's.)
 struct Deal {
     int team_threads, teams;   // threads of a team; teams of a block (one where a team is more than a wavefront)
     int shifts;                // whether vectors lie on memory's grid
@@ -515,8 +516,11 @@ template <sbn_dtype DT, bool LAYER> sbn_status forward_as(const NormArgs &n, hip
 template <sbn_dtype DT, bool LAYER> sbn_status backward_as(NormArgs &n, float *dgain, float *dbias, float *workspace, hipStream_t stream)
 {
     return dealt<DT>(n, {n.dY, n.R, n.dX}, [&](auto L, auto VMAX, const Deal &deal, int waves, int64_t all) {
-        // where there are few rows, two blocks to a processor, or four rows to a team: shares cost as well (1531 rows of 1001: 13 + 8 us by 766 blocks, 12 + 4 by 512)
-        const int blocks = all <= ONE_BLOCK_ROWS ? 1 : (int)std::min({all, staying_blocks(waves, BACKWARD_WAVES), std::max<int64_t>(2 * PROCESSORS, ceil_div(all, 4))});
+        // where there are few rows, two blocks to a processor, or four rows to a team: shares cost as well (1531 rows of 1001: 13 + 8 us by 766 blocks, 12 + 4 by 512);
+        // a multiple of 8 unless every team has one row, so that a team's rows begin alike (5000 rows of 777 bf16 values: 17.6 us by 1256 blocks, 18.2 by 1250; 2500 of 1001,
+        // by 632 and 625: 13.6 and 13.9)
+        const int64_t few = std::max<int64_t>(2 * PROCESSORS, ceil_div(ceil_div(all, 4), 8) * 8);
+        const int blocks = all <= ONE_BLOCK_ROWS ? 1 : (int)std::min({all, staying_blocks(waves, BACKWARD_WAVES), few});
         // one block's shares are the sums
         n.gain_shares = !dgain ? nullptr : blocks == 1 ? dgain : workspace;
         n.bias_shares = !dbias ? nullptr : blocks == 1 ? dbias : workspace + blocks * n.d;
