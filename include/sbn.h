@@ -516,8 +516,12 @@ sbn_status sbn_embedding_backward(const void *dY, sbn_dtype y_dtype, const int64
  * of pattern (c + 8 (e - 15 or 31)) << 20: three bits of mantissa, 15 or 31 binades; m's top bit is the sign.  Values below are 0 for m, and the
  * lowest code for a v that is not 0.  Every value is exact in bf16.
  * Pointers are aligned to their values, codes to 8 bytes.  No params, m, v or scales may share memory with another of its own list (SBN_EINVAL), nor
- * with another list.  Arithmetic in fp32, each operation rounded (the norm in double).  No atomics: a call repeated gives the same bits.  A gradient
- * that is not finite and no clip: its weight and moments in fp32 are not finite after; moments in 8 bits of its 32 values stand for nothing in particular.
+ * with another list.  No atomics: a call repeated gives the same bits.  Arithmetic in fp32 (the norm in double).
+ * Moments: each operation is rounded.  Weights: with an eps of 1e-12 or more root and reciprocal are the hardware's, good to a step of fp32, products are
+ * fused with the sums that take them, and the root of a v' below 2^-126 counts as 0; with a smaller eps each operation is correctly rounded.  In both p' is, before
+ * its own rounding, within 3 2^-24 |p| + 24 2^-24 lr / (1 - beta1^t) (beta1 |m| + (1 - beta1) |g|) / (sqrt(v' / (1 - beta2^t)) + eps) of the formula, with that root.
+ * A gradient that is not finite and no clip: its weight and moments in fp32 are not finite after; moments in 8 bits of its 32 values stand for nothing in
+ * particular.
  * Errors: SBN_EINVAL (null, sizes not positive, beta outside [0, 1), eps or weight_decay not finite, max_norm not positive), SBN_EALIGN, SBN_ESIZE,
  * SBN_EUNSUPPORTED (count > 4096, a tensor of more than 2^31 values), SBN_EHIP.
  */
