@@ -333,14 +333,14 @@ struct SumArgs {
     void *dE;
     const int *begin, *order, *order_ids;
     float *partials;     // [pieces][2][d]: of the id that the piece begins with, of the one that it ends with
-    int64_t vocab, d, items;   // items: pieces times tiles
+    int64_t d, items;    // items: pieces times tiles
     int tokens, own, shift, accumulate, pieces, tiles, join_pieces;   // tiles: of 64 units of a row
     float scale;
     __device__ __forceinline__ const int *begin_of(int64_t id) const { return begin + (id & ((1 << shift) - 1)) * own + (id >> shift); }
     __device__ __forceinline__ int total() const { return begin[(int64_t)own << shift]; }   // tokens whose id is in the table
 };
 
-template <sbn_dtype TABLE, int U> __device__ __forceinline__ void *row_of(const SumArgs &s, int id)
+template <sbn_dtype TABLE> __device__ __forceinline__ void *row_of(const SumArgs &s, int id)
 {
     return static_cast<typename Row<TABLE>::value *>(s.dE) + (int64_t)id * s.d;
 }
@@ -378,7 +378,7 @@ template <sbn_dtype TABLE, sbn_dtype OUT, bool ACCUMULATE> __device__ __forceinl
 #pragma unroll
         for (int k = 0; k < PIECE; ++k) {
             rows[k].template load<true>(static_cast<const typename Row<OUT>::value *>(s.dY) + (int64_t)piece.token_at(k0 + k) * s.d, c);
-            if (ACCUMULATE) old[k].template load<false>(row_of<TABLE, U>(s, max(piece.id_at(k0 + k), 0)), c);
+            if (ACCUMULATE) old[k].template load<false>(row_of<TABLE>(s, max(piece.id_at(k0 + k), 0)), c);
         }
 #pragma unroll
         for (int k = 0; k < PIECE; ++k)
@@ -393,7 +393,7 @@ template <sbn_dtype TABLE, sbn_dtype OUT, bool ACCUMULATE> __device__ __forceinl
                     for (int i = 0; i < U; ++i) sum[i] *= s.scale;
                     if (ACCUMULATE) old[k].add_to(sum);
                     const Raw<TABLE, U> done = Raw<TABLE, U>::of(sum);
-                    void *row = row_of<TABLE, U>(s, piece.id_at(k0 + k));
+                    void *row = row_of<TABLE>(s, piece.id_at(k0 + k));
                     ACCUMULATE ? done.store_own(row, c, u * U) : done.store(row, c);   // (what is added to must not be written twice)
                 }
                 first = false;
@@ -413,7 +413,6 @@ template <sbn_dtype TABLE, sbn_dtype OUT, bool ACCUMULATE> __device__ __forceinl
 // the same for rows of less than U values, one to a lane
 template <sbn_dtype TABLE, sbn_dtype OUT> __device__ __forceinline__ void sum_piece_few(const SumArgs &s, const Piece &piece, int number, int lane)
 {
-    constexpr int U = unit_of(TABLE, OUT);
     float *share = s.partials + (int64_t)number * 2 * s.d;
     const int c = min(lane, (int)s.d - 1);
     float sum = 0.0f;
@@ -422,7 +421,7 @@ template <sbn_dtype TABLE, sbn_dtype OUT> __device__ __forceinline__ void sum_pi
     for (int k = piece.first_k; k < piece.end_k; ++k) {
         sum += value_at<OUT>(static_cast<const typename Row<OUT>::value *>(s.dY) + (int64_t)piece.token_at(k) * s.d, c);
         if (!piece.last_of_id(k)) continue;
-        void *row = row_of<TABLE, U>(s, piece.id_at(k));
+        void *row = row_of<TABLE>(s, piece.id_at(k));
         if (lane < s.d) {
             if (first)
                 share[c] = sum;
@@ -509,7 +508,7 @@ __device__ __forceinline__ void join(const SumArgs &s, int piece, int id, int en
 #pragma unroll
         for (int k = 0; k < U; ++k) sum[k] += sums[w][k * 64 + lane];
     }
-    void *row = row_of<TABLE, U>(s, id);
+    void *row = row_of<TABLE>(s, id);
     float old[U] = {};
     if (s.accumulate) load_unit<TABLE, U>(row, u, s.d, old);
 #pragma unroll
@@ -798,7 +797,6 @@ sbn_status launch_embedding_backward(const void *dY, sbn_dtype out, const int64_
     s.order = o.order;
     s.order_ids = o.order_ids;
     s.partials = reinterpret_cast<float *>(ws + c.partials);
-    s.vocab = vocab;
     s.d = d;
     s.tokens = (int)tokens;
     s.own = o.own;

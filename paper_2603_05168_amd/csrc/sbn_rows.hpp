@@ -192,12 +192,6 @@ template <int E> __device__ __forceinline__ void load_floats(const float *p, int
     }
 }
 
-__device__ __forceinline__ float wave_sum(float x)
-{
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
-    return x;
-}
 __device__ __forceinline__ double wave_sum(double x)
 {
 #pragma unroll
