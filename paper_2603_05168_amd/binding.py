@@ -809,7 +809,7 @@ def sbn_grad_norm_workspace_bytes(sizes) -> int:
 
 
 class GradNormGroup:
-    """Host-side argument arrays of sbn_grad_norm, marshalled once and reusable."""
+    """Host-side argument arrays of sbn_grad_norm, marshalled once and reusable: with the addresses that the gradients had when it was made, as in AdamWGroup."""
 
     def __init__(self, grads, workspace):
         grads = _Tensors("grads", grads, torch.float32, torch.bfloat16)
@@ -857,7 +857,10 @@ def sbn_adamw_state_values(codes, scales, out, second: bool = False):
 
 class AdamWGroup:
     """Host-side argument arrays of sbn_adamw_step, marshalled once and reusable.  Lists hold one tensor per weight: params and grads fp32 or bf16, m and v
-    fp32, or (with m_scales and v_scales) the bytes of moments in 8 bits; weight_decay is a number, or one per weight."""
+    fp32, or (with m_scales and v_scales) the bytes of moments in 8 bits; weight_decay is a number, or one per weight.
+
+    The group holds the tensors and the addresses that they had when it was made: gradients are written into the same tensors (zero_grad(set_to_none=False)).
+    Where a tensor is another one at each step, or its storage is exchanged (p.data = ...), make a new group, or call sbn_adamw_step, which makes one."""
 
     def __init__(self, params, grads, m, v, m_scales=None, v_scales=None, weight_decay=0.0, betas=(0.9, 0.95), eps: float = 1e-8):
         params = _Tensors("params", params, torch.float32, torch.bfloat16)
@@ -902,6 +905,7 @@ class AdamWGroup:
 
 
 def sbn_adamw_step(params, grads, m, v, lr, step, m_scales=None, v_scales=None, weight_decay=0.0, betas=(0.9, 0.95), eps: float = 1e-8, clip=None, seed=None):
+    """One step over lists of tensors that may be others at the next: an AdamWGroup of them, run once."""
     AdamWGroup(params, grads, m, v, m_scales, v_scales, weight_decay, betas, eps).run(lr, step, clip, seed)
 
 

@@ -518,7 +518,8 @@ __device__ __forceinline__ void join(const SumArgs &s, int piece, int id, int en
 
 // A block to join_pieces pieces and 64 units of the columns.  For every piece in which an id begins that goes on behind the next, eight wavefronts add the
 // partial sums in turn, eight asked for at a time, and their sums are added in order (sixteen wavefronts: 9.5 us in place of 8.3 for 16384 tokens of 2560
-// values, four 9.4; one id of 65536 tokens: 187, 175 and 289).
+// values, four 9.4; one id of 65536 tokens: 187, 175 and 289, beside 255 of the sort, in which
+// one block places all of them, and 74 of the sums).
 constexpr int JOIN_THREADS = 512;
 template <sbn_dtype TABLE> __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const SumArgs s)
 {

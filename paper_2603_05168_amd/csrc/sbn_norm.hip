@@ -299,9 +299,11 @@ template <sbn_dtype DT, bool LAYER, int L, int VMAX> __global__ void __launch_bo
 
 // A thread meets the same columns in every row of its team and adds up their dgain and dbias.  At the end a block adds its teams' sums in LDS and
 // leaves one share of both vectors, which the next kernel adds in the order of the blocks: no atomics, the same bits every time.
-// Bound by memory: 16384 RMS rows of 2560 bf16 values with d_residual move 336 MB in 60 us, 5.6 TB/s.  Three blocks of five wavefronts to each of the 256
-// processors: as many on all of them (819 blocks: 88 us), and no more (four: 72) nor fewer (two: 69).  At most 96 registers, so that five wavefronts find
-// room on a SIMD: with 106 the layer form took 102 us for 67 (without a residual).
+// Bound by memory: 16384 RMS rows of 2560 bf16 values with d_residual move 336 MB in 57 to 64 us, 5.3 to 5.9 TB/s (a call, with the shares, 62; of the layer form,
+// with both shares, 73, and 72 without d_residual).  Three blocks of five wavefronts to each of the 256 processors: as many on all of them (819 blocks: 88 us), and
+// no more (four: 72) nor fewer (two: 69).  At most 96 registers, so that five wavefronts find room on a SIMD: with 106 the layer form took 102 us for 67 (without a
+// residual, the kernel alone).  For that the layer form of bf16 rows keeps two to four registers in memory, and two instances of the RMS form and of longer rows one
+// or two; fp32 rows of more than 2560 values in the layer form ten.
 template <sbn_dtype DT, bool LAYER, int L, int VMAX>
 __global__ void __launch_bounds__(most_threads(L)) __attribute__((amdgpu_waves_per_eu(VMAX * Row<DT>::E <= 8 ? 5 : 4))) norm_backward_kernel(const NormArgs n, const Deal deal)
 {

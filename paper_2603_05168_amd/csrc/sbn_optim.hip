@@ -346,8 +346,8 @@ template <sbn_dtype OUT, int BELOW> __global__ void __launch_bounds__(256) state
 // ---- the norm of all gradients ----------------------------------------------------------------------------------------------------
 constexpr int GRAD_NORM_LAUNCH_MAX = 64;
 constexpr int64_t MEMORY_CACHE = 256 << 20;   // bytes of the memory side's cache
-// Values of a block: 64 KB, or 32 where that is not four blocks to a processor (4M values: 7.0 us for 12.4 in fp32, with the sum of the sums; 2M in bf16 6.3
-// for 6.9).
+// Values of a block: 64 KB, or 32 where that is not four blocks to a processor (a call on 4M values in fp32 12.4 -> 6.2 us, on 2M in bf16 6.9 -> 6.3; the
+// kernels alone now take 4.4 and 2.2, 4.1 and 2.0, and calls up to 8.8 where the host is slower than they).
 int64_t grad_norm_chunk(int count, const int64_t *sizes, sbn_dtype dtype)
 {
     const int64_t size = dtype == SBN_BF16 ? 2 : 4;
